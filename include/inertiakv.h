@@ -67,10 +67,16 @@ typedef enum { KV_F32 = 0, KV_BF16 = 1 } kv_dtype;
 /* Bits of the workspace's fault word.  KV_FAULT_EXCHANGE_TIMEOUT: a chunk of a long-slab scorer (path
  * KV_PATH_EXCHANGE) did not receive its peers' softmax statistics within the wait limit; its scores, and
  * everything computed from them by that call (utilities, retention decision, compaction), are invalid. */
-typedef enum { KV_FAULT_EXCHANGE_TIMEOUT = 1 } kv_fault;
+typedef enum {
+    KV_FAULT_EXCHANGE_TIMEOUT = 1,
+    /* paged 4-bit cache (kv_q4_*): see each call for what it leaves undone */
+    KV_FAULT_CACHE = 2,      /* a length, table entry, reference count, slot or row out of its range           */
+    KV_FAULT_NO_PAGES = 4,   /* too few free pages: some sequences were not extended, or not compacted         */
+    KV_FAULT_SHARED_PAGE = 8 /* a row was not stored: its page belongs to other sequences too                  */
+} kv_fault;
 
 /* Prior utility of the token appended on a NON-refresh step (appendix "New token insertion": MEAN). */
-typedef enum { KV_INIT_MEAN = 0, KV_INIT_MIN = 1 } kv_init;
+typedef enum { KV_INIT_MEAN = 0, KV_INIT_MIN = 1, KV_INIT_ZERO = 2 /* kv_q4_reserve only */ } kv_init;
 
 /* Aggregation rule (Eq. 2-4), applied layer by layer: EMA u <- alpha u + (1-alpha) s_l; single-step u <- s_l;
  * cumulative u <- u + s_l. */
@@ -305,6 +311,122 @@ kv_status kv_attend_score(const kv_shape* shape, int32_t layer0, int32_t layer_c
 kv_status kv_evict_finish(const kv_shape* shape, const kv_params* params, int32_t t, int32_t n, void* k, void* v,
                           float* u, int32_t* pos, float* v_norms, int32_t* n_out, uint8_t* keep_out, float* s_out,
                           const kv_rank_trace* rank_trace, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Paged 4-bit cache ----
+ * The same method on a cache that is held in 4 bits and in pages: sequences of different lengths share one pool of pages,
+ * a prompt's samples share the prompt's pages, and what an eviction drops goes back to the pool.
+ *
+ * Elements: blocks of 32 consecutive elements of a row hold one scale byte E and 32 codes of 4 bits (sign, two exponent
+ * bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6; the OCP microscaling format MXFP4); an element is code * 2^(E - 127).
+ * Storing takes the smallest e = E - 127 in [-100, 125] with max |x| < 7 * 2^e and rounds x / 2^e to the nearest code, ties
+ * to the even code, saturating at 6: the error is at most half the distance of two neighbouring codes, at most 2^e.  A block
+ * with an infinite or NaN element gets E = 255 and reads back as NaN.  A row of d = 128 takes 68 bytes (bf16: 256).
+ *
+ * Pool: [layers][n_pages][n_kv_heads][record], kv_q4_pool_bytes() bytes, no initialisation needed.  A record holds page_rows
+ * rows of one KV head: keys' codes [page_rows][d / 2] (element 2 i in the low half of byte i), keys' scales
+ * [page_rows][d / 32], values' codes, values' scales.
+ *
+ * Sequences: slot b holds len[b] rows; row i lies in page table[b][i / page_rows] (in every layer and KV head).  A page is
+ * free when refs is 0; else refs counts the table entries that name it.  Entries from ceil(len / page_rows) on are -1.  At
+ * the start: table all -1, len and refs all 0.  Only the calls below change these three; the calls that take pages take the
+ * lowest free ones, for the slots in order, from the counts before the call.
+ *
+ * As above, every call is queued on `stream` and validated on the host; what only the device can see (lengths, table
+ * entries, slots) is checked there before it is used as an index, and what fails raises KV_FAULT_CACHE in the workspace's
+ * fault word (kv_fault_status) and is left out.  Calls on one cache must be in stream order, and calls that share a
+ * workspace must not overlap; nothing in the workspace but the fault word outlives a call.  Arrays of the batch (add,
+ * budget, ...) are device memory, so a captured graph can be replayed with other lengths, slots and budgets. */
+typedef struct {
+    int32_t batch;      /* slots                                                             >= 1              */
+    int32_t layers;     /* 1..256                                                                              */
+    int32_t n_q_heads;  /* multiple of n_kv_heads, at most 16 times as many                                    */
+    int32_t n_kv_heads;
+    int32_t head_dim;   /* 64 or 128                                                                           */
+    int32_t dtype;      /* kv_dtype of queries, outputs and the rows stored and loaded                         */
+    int32_t page_rows;  /* 16, 32, 64, 128 or 256                                                              */
+    int32_t n_pages;    /* pages of the pool                                                                   */
+    int32_t max_pages;  /* table entries of a slot; capacity = max_pages * page_rows <= 2^27 rows              */
+} kv_q4_shape;
+
+typedef struct {
+    uint8_t* pool;  /* 16-byte aligned                                                                         */
+    int32_t* table; /* [batch][max_pages]                                                                      */
+    int32_t* len;   /* [batch]                                                                                 */
+    int32_t* refs;  /* [n_pages]                                                                               */
+    float* u;       /* [batch][capacity] utilities, nullable: not kept (kv_q4_evict needs them)                */
+    int32_t* pos;   /* [batch][capacity] positions, nullable likewise                                          */
+} kv_q4_cache;
+
+/* Strides in elements of rows [layer][batch][head][row][d], the d elements of a row consecutive; multiples of 16 bytes. */
+typedef struct {
+    int64_t layer, batch, head, row;
+} kv_q4_strides;
+
+/* Bytes of the pool (host only). */
+kv_status kv_q4_pool_bytes(const kv_q4_shape* shape, size_t* bytes);
+
+/* Bytes of workspace for every kv_q4 call on sequences of at most n_max rows and on at most layer_count layers at once
+ * (host only).  kv_q4_store, kv_q4_load, kv_q4_fork and kv_q4_free use its fault word alone (256 bytes). */
+kv_status kv_q4_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t layer_count, size_t* bytes);
+
+/* Extends every slot by add[b] >= 0 rows: pages for them, and, where the last page ends inside and other slots share it, a
+ * copy of it of the slot's own.  The new rows hold nothing yet (kv_q4_store); their utility is the mean or minimum of the
+ * slot's cached utilities, or zero (init, a kv_init; 0 for an empty slot), and their positions new_pos[b], new_pos[b] + 1,
+ * ... (new_pos nullable: positions are left as they are).  granted[b] (nullable; may be add itself) receives the rows added:
+ * add[b], or 0 where the slot was left alone: it would pass its capacity, add[b] is negative (KV_FAULT_CACHE), or free
+ * pages ran out (KV_FAULT_NO_PAGES: the slots are served in order, and from the first one that does not fit on, none that
+ * needs a page). */
+kv_status kv_q4_reserve(const kv_q4_shape* shape, const kv_q4_cache* cache, const int32_t* add, const int32_t* new_pos,
+                        int32_t init, int32_t* granted, void* ws, size_t ws_bytes, void* stream);
+
+/* Stores rows of layers [layer0, layer0 + layer_count): row r < count[b] of k and v becomes row first[b] + r of slot b.
+ * count nullable: `rows` of every slot; first nullable: len[b] - count[b], the newest rows (after kv_q4_reserve, with its
+ * granted as count).  Rows r >= count[b] are not read.  Rows outside the slot, and rows in pages that other slots share
+ * (KV_FAULT_SHARED_PAGE), are not stored. */
+kv_status kv_q4_store(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t rows,
+                      const int32_t* first, const int32_t* count, const void* k, const kv_q4_strides* k_strides, const void* v,
+                      const kv_q4_strides* v_strides, void* ws, size_t ws_bytes, void* stream);
+
+/* The reverse: row r < count[b] of k and v receives row first[b] + r of slot b, exactly (zeros where the slot has no such
+ * row: KV_FAULT_CACHE).  Rows r >= count[b] are left as they were.  No stride may be 0 where its extent is above 1. */
+kv_status kv_q4_load(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t rows,
+                     const int32_t* first, const int32_t* count, void* k, const kv_q4_strides* k_strides, void* v,
+                     const kv_q4_strides* v_strides, void* ws, size_t ws_bytes, void* stream);
+
+/* Decode attention of layers [layer0, layer0 + layer_count) over the len[b] <= n_max rows of every slot, as
+ * kv_attend_score: q and o are [layer_count][batch][n_q_heads][d]; recency_bias is added to the logits of rows with
+ * pos >= cur_pos[b] - (recency_window - 1) (cur_pos and cache->pos are needed for a bias other than 0 in a window other than
+ * 0 only).  A slot without rows, or longer than n_max (KV_FAULT_CACHE), gets zeros; rows in pages that do not exist
+ * (KV_FAULT_CACHE) take no part.  s_out (nullable, [layer_count][batch][n_max]) receives the pooled scores of Eq. 1, 0
+ * behind the slot's rows; u_out (nullable, [batch][capacity], may be u_prior) the fold of Eq. 4 over the call's layers
+ * in order, u_out = alpha u + (1 - alpha) s from u_prior, for the slot's rows (others are left as they were). */
+kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t n_max,
+                       const void* q, const int32_t* cur_pos, float recency_bias, int32_t recency_window, void* o,
+                       float* s_out, float alpha, const float* u_prior, float* u_out, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* Slot dst[i] becomes a copy of slot src[i] (rows, utilities, positions) that shares its pages, for i < count <= batch.  A
+ * destination has to be empty and named once, and no source may be a destination of the call; what is not so is left out
+ * (KV_FAULT_CACHE), of a destination named twice all but the first. */
+kv_status kv_q4_fork(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t count, const int32_t* src, const int32_t* dst,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/* Slots slots[0 .. count), count <= batch, give their pages back and are empty.  A slot named twice is freed once. */
+kv_status kv_q4_free(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t count, const int32_t* slots, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* Compaction by a retention decision keep [batch][capacity] (entries behind a slot's rows are not read), as kv_compact:
+ * with k the rows that a slot keeps, the kept rows from k on move, ascending, into the dropped ones before k, ascending, in
+ * every layer, with their utilities and positions (those from k on are left as they were).  Then len = k, and the pages
+ * behind go back to the pool.  A shared page in which a row is written is replaced by a page of the slot's own; where there
+ * are too few (KV_FAULT_NO_PAGES, as kv_q4_reserve), the slot is left as it was, and so is one longer than n_max. */
+kv_status kv_q4_compact(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t n_max, const uint8_t* keep, void* ws,
+                        size_t ws_bytes, void* stream);
+
+/* Top-B selection and compaction: every slot keeps the budget[b] >= 0 rows first under (u descending, position ascending),
+ * all of them when it has no more.  keep_out (nullable, [batch][capacity]) receives the decision over the slot's rows. */
+kv_status kv_q4_evict(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t n_max, const int32_t* budget,
+                      uint8_t* keep_out, void* ws, size_t ws_bytes, void* stream);
 
 /* Static description of a status code. */
 const char* kv_status_string(kv_status status);

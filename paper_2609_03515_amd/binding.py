@@ -16,11 +16,11 @@ LIB_PATH = os.path.join(_HERE, "libinertiakv.so")
 
 KV_OK, KV_ERR_INVALID_ARG, KV_ERR_UNSUPPORTED, KV_ERR_WORKSPACE, KV_ERR_HIP = 0, -1, -2, -3, -4
 KV_F32, KV_BF16 = 0, 1
-KV_INIT_MEAN, KV_INIT_MIN = 0, 1
+KV_INIT_MEAN, KV_INIT_MIN, KV_INIT_ZERO = 0, 1, 2
 KV_RULE_EMA, KV_RULE_SINGLE_STEP, KV_RULE_CUMULATIVE = 0, 1, 2
 KV_SCORE_ATTENTION, KV_SCORE_VNORM, KV_SCORE_ENTROPY, KV_SCORE_NORMS_EMITTED = 0, 1, 2, 4
 KV_EMIT_SCORES, KV_EMIT_VNORMS = 1, 2
-KV_FAULT_EXCHANGE_TIMEOUT = 1
+KV_FAULT_EXCHANGE_TIMEOUT, KV_FAULT_CACHE, KV_FAULT_NO_PAGES, KV_FAULT_SHARED_PAGE = 1, 2, 4, 8
 KV_PATH_LDS, KV_PATH_EXCHANGE, KV_PATH_LOGITS = 0, 1, 2
 KV_PHASES = 5
 PHASES = ("append", "score", "fold", "select", "compact")
@@ -28,7 +28,8 @@ PHASES = ("append", "score", "fold", "select", "compact")
 EXPORTED = ("kv_workspace_bytes", "kv_score_ema", "kv_topk_select", "kv_compact", "kv_evict_step",
             "kv_append", "kv_attend_score", "kv_evict_finish", "kv_rank_trace_state_bytes", "kv_score_merge",
             "kv_score_plan", "kv_fault_status", "kv_set_exchange_wait_limit", "kv_evict_step_static",
-            "kv_value_norms", "kv_status_string")
+            "kv_value_norms", "kv_q4_pool_bytes", "kv_q4_workspace_bytes", "kv_q4_reserve", "kv_q4_store", "kv_q4_load",
+            "kv_q4_attend", "kv_q4_fork", "kv_q4_free", "kv_q4_compact", "kv_q4_evict", "kv_status_string")
 KV_STATIC_SCRATCH_BYTES = 64 << 20
 KV_TRACE_COUNTS = 10
 
@@ -65,6 +66,19 @@ class KvRankTrace(ctypes.Structure):
                 ("counts", ctypes.c_void_p), ("raw_keep", ctypes.c_void_p), ("ema_keep", ctypes.c_void_p)]
 
 
+class KvQ4Shape(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "layers", "n_q_heads", "n_kv_heads", "head_dim", "dtype",
+                                                    "page_rows", "n_pages", "max_pages")]
+
+
+class KvQ4Buffers(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("pool", "table", "len", "refs", "u", "pos")]
+
+
+class KvQ4Strides(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("layer", "batch", "head", "row")]
+
+
 _lib = None
 
 
@@ -97,6 +111,17 @@ def load_library(path: str = LIB_PATH):
     lib.kv_set_exchange_wait_limit.argtypes = [i32]
     lib.kv_evict_step_static.argtypes = [shp, prm, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp,
                                          ctypes.POINTER(i32), vp, vp, trc, rtr, vp]
+    qsh, buf, std = ctypes.POINTER(KvQ4Shape), ctypes.POINTER(KvQ4Buffers), ctypes.POINTER(KvQ4Strides)
+    lib.kv_q4_pool_bytes.argtypes = [qsh, ctypes.POINTER(sz)]
+    lib.kv_q4_workspace_bytes.argtypes = [qsh, i32, i32, ctypes.POINTER(sz)]
+    lib.kv_q4_reserve.argtypes = [qsh, buf, vp, vp, i32, vp, vp, sz, vp]
+    lib.kv_q4_store.argtypes = [qsh, buf, i32, i32, i32, vp, vp, vp, std, vp, std, vp, sz, vp]
+    lib.kv_q4_load.argtypes = lib.kv_q4_store.argtypes
+    lib.kv_q4_attend.argtypes = [qsh, buf, i32, i32, i32, vp, vp, f32, i32, vp, vp, f32, vp, vp, vp, sz, vp]
+    lib.kv_q4_fork.argtypes = [qsh, buf, i32, vp, vp, vp, sz, vp]
+    lib.kv_q4_free.argtypes = [qsh, buf, i32, vp, vp, sz, vp]
+    lib.kv_q4_compact.argtypes = [qsh, buf, i32, vp, vp, sz, vp]
+    lib.kv_q4_evict.argtypes = [qsh, buf, i32, vp, vp, vp, sz, vp]
     for fn in EXPORTED[:-1]:
         getattr(lib, fn).restype = i32
     lib.kv_status_string.argtypes = [i32]
@@ -337,6 +362,167 @@ def faults(ws, clear=False) -> int:
     out = torch.zeros(1, dtype=torch.int32, device=ws.device)
     kv_fault_status(ws, out, clear=clear)
     return int(out.item()) & 0xffffffff
+
+
+# --- Paged 4-bit cache ----------------------------------------------------------------------------------------
+def make_q4_shape(batch, layers, n_q_heads, n_kv_heads, head_dim, page_rows, n_pages, max_pages, dtype) -> KvQ4Shape:
+    if isinstance(dtype, str):
+        dtype = {"f32": KV_F32, "bf16": KV_BF16}[dtype]
+    elif dtype in (torch.float32, torch.bfloat16):
+        dtype = KV_F32 if dtype == torch.float32 else KV_BF16
+    return KvQ4Shape(batch, layers, n_q_heads, n_kv_heads, head_dim, dtype, page_rows, n_pages, max_pages)
+
+
+def kv_q4_pool_bytes(shape: KvQ4Shape) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kv_q4_pool_bytes", load_library().kv_q4_pool_bytes(ctypes.byref(shape), ctypes.byref(out)))
+    return out.value
+
+
+def kv_q4_workspace_bytes(shape: KvQ4Shape, n_max: int, layer_count: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kv_q4_workspace_bytes", load_library().kv_q4_workspace_bytes(ctypes.byref(shape), int(n_max),
+                                                                          int(layer_count), ctypes.byref(out)))
+    return out.value
+
+
+def q4_workspace(shape: KvQ4Shape, n_max: int, layer_count: int, device="cuda") -> torch.Tensor:
+    """A caller-owned workspace tensor of kv_q4_workspace_bytes() bytes, its fault word cleared on the current stream."""
+    ws = torch.empty(kv_q4_workspace_bytes(shape, n_max, layer_count), dtype=torch.uint8, device=device)
+    kv_fault_status(ws, None, clear=True)
+    return ws
+
+
+class KvQ4Cache:
+    """One paged 4-bit cache's device buffers (caller-owned, contiguous torch tensors) for the kv_q4 calls.
+
+    pool: uint8, kv_q4_pool_bytes(shape); table: [batch][max_pages] int32; len: [batch] int32; refs: [n_pages] int32;
+    u: [batch][capacity] f32 and pos: [batch][capacity] int32 (nullable: not kept), capacity = max_pages * page_rows."""
+
+    def __init__(self, shape: KvQ4Shape, pool, table, len, refs, u=None, pos=None):
+        cap = shape.max_pages * shape.page_rows
+        _q4_buffer("KvQ4Cache", pool, torch.uint8, kv_q4_pool_bytes(shape), pool.device)
+        for t, dtype, n in ((table, torch.int32, shape.batch * shape.max_pages), (len, torch.int32, shape.batch),
+                            (refs, torch.int32, shape.n_pages), (u, torch.float32, shape.batch * cap),
+                            (pos, torch.int32, shape.batch * cap)):
+            _q4_buffer("KvQ4Cache", t, dtype, n, pool.device)
+        self.shape, self.pool, self.table, self.len, self.refs, self.u, self.pos = shape, pool, table, len, refs, u, pos
+        self.buffers = KvQ4Buffers(*(_ptr(t) for t in (pool, table, len, refs, u, pos)))
+        self.element = torch.float32 if shape.dtype == KV_F32 else torch.bfloat16
+
+    @classmethod
+    def allocate(cls, shape: KvQ4Shape, device="cuda") -> "KvQ4Cache":
+        """Buffers of an empty cache."""
+        cap = shape.max_pages * shape.page_rows
+        return cls(shape, torch.empty(kv_q4_pool_bytes(shape), dtype=torch.uint8, device=device),
+                   torch.full((shape.batch, shape.max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(shape.batch, dtype=torch.int32, device=device),
+                   torch.zeros(shape.n_pages, dtype=torch.int32, device=device),
+                   torch.zeros(shape.batch, cap, dtype=torch.float32, device=device),
+                   torch.zeros(shape.batch, cap, dtype=torch.int32, device=device))
+
+
+def _q4_buffer(fn, t, dtype, numel, device):
+    """A buffer that a kernel indexes without knowing its size: type, place, layout and size are checked here."""
+    if t is not None and (t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < numel):
+        raise KVError(fn, KV_ERR_INVALID_ARG)
+
+
+def _q4_call(fn, cache, ws, stream):
+    """The library, the shared arguments, and the stream of a call: the cache's device has to be the current one."""
+    _q4_buffer(fn, ws, torch.uint8, 0, cache.pool.device)
+    if cache.pool.is_cuda and cache.pool.device.index != torch.cuda.current_device():
+        raise KVError(fn, KV_ERR_INVALID_ARG)
+    return (getattr(load_library(), fn), ctypes.byref(cache.shape), ctypes.byref(cache.buffers), _ptr(ws), _ws_bytes(ws),
+            _stream(stream))
+
+
+def _q4_rows(fn, cache, layer_count, rows, t):
+    """Strides of a tensor [layer_count][batch][n_kv_heads][rows][head_dim] whose rows are contiguous."""
+    s = cache.shape
+    if (t.dtype != cache.element or t.device != cache.pool.device or t.stride(-1) != 1
+            or t.shape != (layer_count, s.batch, s.n_kv_heads, rows, s.head_dim)):
+        raise KVError(fn, KV_ERR_INVALID_ARG)
+    return ctypes.byref(KvQ4Strides(*(st if n > 1 else 0 for st, n in zip(t.stride()[:4], t.shape))))
+
+
+def kv_q4_reserve(cache: KvQ4Cache, add, new_pos, ws, granted=None, init="mean", stream=None):
+    """add, new_pos, granted: [batch] int32 (new_pos and granted nullable); init: "mean", "min" or "zero"."""
+    for t in (add, new_pos, granted):
+        _q4_buffer("kv_q4_reserve", t, torch.int32, cache.shape.batch, cache.pool.device)
+    mode = {"mean": KV_INIT_MEAN, "min": KV_INIT_MIN, "zero": KV_INIT_ZERO}[init] if isinstance(init, str) else int(init)
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_reserve", cache, ws, stream)
+    _check("kv_q4_reserve", call(shape, buffers, _ptr(add), _ptr(new_pos), mode, _ptr(granted), w, nbytes, st))
+
+
+def kv_q4_store(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None, count=None, stream=None):
+    """k, v: [layer_count][batch][n_kv_heads][rows][head_dim] in any strides with contiguous rows; first, count: [batch]."""
+    for t in (first, count):
+        _q4_buffer("kv_q4_store", t, torch.int32, cache.shape.batch, cache.pool.device)
+    ks, vs = (_q4_rows("kv_q4_store", cache, layer_count, rows, t) for t in (k, v))
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_store", cache, ws, stream)
+    _check("kv_q4_store", call(shape, buffers, int(layer0), int(layer_count), int(rows), _ptr(first), _ptr(count), _ptr(k), ks,
+                               _ptr(v), vs, w, nbytes, st))
+
+
+def kv_q4_load(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None, count=None, stream=None):
+    """As kv_q4_store, into k and v."""
+    for t in (first, count):
+        _q4_buffer("kv_q4_load", t, torch.int32, cache.shape.batch, cache.pool.device)
+    ks, vs = (_q4_rows("kv_q4_load", cache, layer_count, rows, t) for t in (k, v))
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_load", cache, ws, stream)
+    _check("kv_q4_load", call(shape, buffers, int(layer0), int(layer_count), int(rows), _ptr(first), _ptr(count), _ptr(k), ks,
+                              _ptr(v), vs, w, nbytes, st))
+
+
+def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos=None, recency_bias=0.0, recency_window=0,
+                 s_out=None, alpha=0.0, u_prior=None, u_out=None, stream=None):
+    """q, o: [layer_count][batch][n_q_heads][head_dim]; cur_pos: [batch] int32; s_out: [layer_count][batch][n_max] f32;
+    u_prior, u_out: [batch][capacity] f32."""
+    s, dev = cache.shape, cache.pool.device
+    heads, cap = layer_count * s.batch * s.n_q_heads * s.head_dim, s.batch * s.max_pages * s.page_rows
+    for t, dtype, n in ((q, cache.element, heads), (o, cache.element, heads), (cur_pos, torch.int32, s.batch),
+                        (s_out, torch.float32, layer_count * s.batch * n_max), (u_prior, torch.float32, cap),
+                        (u_out, torch.float32, cap)):
+        _q4_buffer("kv_q4_attend", t, dtype, n, dev)
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_attend", cache, ws, stream)
+    _check("kv_q4_attend", call(shape, buffers, int(layer0), int(layer_count), int(n_max), _ptr(q), _ptr(cur_pos),
+                                float(recency_bias), int(recency_window), _ptr(o), _ptr(s_out), float(alpha), _ptr(u_prior),
+                                _ptr(u_out), w, nbytes, st))
+
+
+def kv_q4_fork(cache: KvQ4Cache, src, dst, ws, stream=None):
+    """src, dst: int32 tensors of the same size (at most batch)."""
+    if src.numel() != dst.numel():
+        raise KVError("kv_q4_fork", KV_ERR_INVALID_ARG)
+    for t in (src, dst):
+        _q4_buffer("kv_q4_fork", t, torch.int32, 0, cache.pool.device)
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_fork", cache, ws, stream)
+    _check("kv_q4_fork", call(shape, buffers, src.numel(), _ptr(src), _ptr(dst), w, nbytes, st))
+
+
+def kv_q4_free(cache: KvQ4Cache, slots, ws, stream=None):
+    """slots: int32 tensor of at most batch entries."""
+    _q4_buffer("kv_q4_free", slots, torch.int32, 0, cache.pool.device)
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_free", cache, ws, stream)
+    _check("kv_q4_free", call(shape, buffers, slots.numel(), _ptr(slots), w, nbytes, st))
+
+
+def kv_q4_compact(cache: KvQ4Cache, n_max, keep, ws, stream=None):
+    """keep: [batch][capacity] uint8."""
+    s = cache.shape
+    _q4_buffer("kv_q4_compact", keep, torch.uint8, s.batch * s.max_pages * s.page_rows, cache.pool.device)
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_compact", cache, ws, stream)
+    _check("kv_q4_compact", call(shape, buffers, int(n_max), _ptr(keep), w, nbytes, st))
+
+
+def kv_q4_evict(cache: KvQ4Cache, n_max, budget, ws, keep_out=None, stream=None):
+    """budget: [batch] int32; keep_out: [batch][capacity] uint8."""
+    s = cache.shape
+    _q4_buffer("kv_q4_evict", budget, torch.int32, s.batch, cache.pool.device)
+    _q4_buffer("kv_q4_evict", keep_out, torch.uint8, s.batch * s.max_pages * s.page_rows, cache.pool.device)
+    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_evict", cache, ws, stream)
+    _check("kv_q4_evict", call(shape, buffers, int(n_max), _ptr(budget), _ptr(keep_out), w, nbytes, st))
 
 
 # --- HIP events for the timing hooks (runtime plumbing, no computation) -------------------------------------
