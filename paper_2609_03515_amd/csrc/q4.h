@@ -67,16 +67,19 @@ struct Q4AttendArgs {
     float scale2;            // log2(e) / sqrt(d)
     float bias2;             // log2(e) * bias
     int nchunk, chunk_rows;
-    float* z;                // [slab][group][n_stride]: base-2 logits (scores only), slab = (layer * batch + b) * hkv + head
-    float2* part;            // [slab][nchunk][group]: (max, sum of 2^(z - max))
+    float* z;                // scores wanted: [slab][group][n_stride] base-2 logits, slab = (layer * batch + b) * hkv + head
+    float2* part;            // [slab][nchunk][group]: (max, sum of 2^(z - max)); the head's own in its first chunk's place
     float* opart;            // [slab][nchunk][group][d]: unnormalised partial outputs
     float* s_out;            // nullable [layer_count][batch][n_max]
+    float* s_scratch;        // [layer_count][batch][n_stride]: the scores of several layers that are folded but not asked for
     const float* u_prior;    // nullable [batch][cap]
     float* u_out;            // nullable [batch][cap]
     float alpha;
     uint32_t* faults;
 };
-// Row chunks per slab, and rows of a chunk, of a call on `slabs` slabs of at most n rows.
+// Row chunks per slab, and rows of a chunk, of a call on `slabs` slabs of at most n rows; and a bound on the chunks that does
+// not fall when n grows.
+int q4_attend_chunks(int slabs, int n);
 void q4_attend_plan(int slabs, int n, int* nchunk, int* chunk_rows);
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);
 

@@ -101,24 +101,29 @@ size_t page_layout(const Q4Dims& d, int n_max, void* ws, Q4PageScratch* out) {
     return off;
 }
 
-// The attention's scratch after the fault word.
+// The attention's scratch after the fault word, sized for every n up to n_max.
 struct AttendLayout {
     int n_stride, nchunk, chunk_rows;
-    size_t z_off, part_off, opart_off, total;
+    size_t z_off, part_off, opart_off, s_off, total;
 };
-AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count) {
+AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool scores) {
     AttendLayout L{};
     const int slabs = layer_count * d.batch * d.hkv;
     q4_attend_plan(slabs, n_max, &L.nchunk, &L.chunk_rows);
+    const size_t chunks = q4_attend_chunks(slabs, n_max);
     L.n_stride = (n_max + 63) / 64 * 64;
     const size_t heads = (size_t)slabs * d.group;
     size_t off = kFaultBytes;
-    L.z_off = off;
-    off = align256(off + heads * L.n_stride * sizeof(float));
     L.part_off = off;
-    off = align256(off + heads * L.nchunk * sizeof(float2));
+    off = align256(off + heads * chunks * sizeof(float2));
     L.opart_off = off;
-    if (L.nchunk > 1) off = align256(off + heads * L.nchunk * d.d * sizeof(float));
+    if (chunks > 1) off = align256(off + heads * chunks * d.d * sizeof(float));
+    if (scores) {
+        L.z_off = off;
+        off = align256(off + heads * L.n_stride * sizeof(float));
+        L.s_off = off;
+        off = align256(off + (size_t)layer_count * d.batch * L.n_stride * sizeof(float));
+    }
     L.total = off;
     return L;
 }
@@ -193,7 +198,7 @@ kv_status kv_q4_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t
     if (!bytes || n_max < 1 || n_max > d.cap || layer_count < 1 || layer_count > shape->layers) return KV_ERR_INVALID_ARG;
     size_t need = page_layout(d, n_max, nullptr, nullptr);
     for (int l = 1; l <= layer_count; ++l) {  // (calls on fewer layers may cut their slabs into more chunks)
-        const size_t t = attend_layout(d, n_max, l).total;
+        const size_t t = attend_layout(d, n_max, l, true).total;
         if (t > need) need = t;
     }
     *bytes = need;
@@ -260,7 +265,8 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     if (u_out && (!u_prior || !(alpha >= 0.0f && alpha < 1.0f))) return KV_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(o, 16) || !aligned(cur_pos, 4) || !aligned(s_out, 4) || !aligned(u_prior, 4) || !aligned(u_out, 4))
         return KV_ERR_UNSUPPORTED;
-    const AttendLayout L = attend_layout(d, n_max, layer_count);
+    const bool scores = s_out || u_out;
+    const AttendLayout L = attend_layout(d, n_max, layer_count, scores);
     if ((double)layer_count * s.batch * s.n_kv_heads * L.nchunk > 2.0e9) return KV_ERR_UNSUPPORTED;
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
     Q4AttendArgs a{};
@@ -281,7 +287,8 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     a.nchunk = L.nchunk;
     a.chunk_rows = L.chunk_rows;
     char* base = static_cast<char*>(ws);
-    a.z = reinterpret_cast<float*>(base + L.z_off);
+    a.z = scores ? reinterpret_cast<float*>(base + L.z_off) : nullptr;
+    a.s_scratch = reinterpret_cast<float*>(base + L.s_off);
     a.part = reinterpret_cast<float2*>(base + L.part_off);
     a.opart = reinterpret_cast<float*>(base + L.opart_off);
     a.s_out = s_out;
