@@ -401,14 +401,18 @@ class KvQ4Cache:
 
     def __init__(self, shape: KvQ4Shape, pool, table, len, refs, u=None, pos=None):
         cap = shape.max_pages * shape.page_rows
-        _q4_buffer("KvQ4Cache", pool, torch.uint8, kv_q4_pool_bytes(shape), pool.device)
-        for t, dtype, n in ((table, torch.int32, shape.batch * shape.max_pages), (len, torch.int32, shape.batch),
-                            (refs, torch.int32, shape.n_pages), (u, torch.float32, shape.batch * cap),
-                            (pos, torch.int32, shape.batch * cap)):
-            _q4_buffer("KvQ4Cache", t, dtype, n, pool.device)
+        dev = pool.get_device()
+        if not (_q4_ok(pool, torch.uint8, kv_q4_pool_bytes(shape), dev)
+                and _q4_ok(table, torch.int32, shape.batch * shape.max_pages, dev) and _q4_ok(len, torch.int32, shape.batch, dev)
+                and _q4_ok(refs, torch.int32, shape.n_pages, dev) and _q4_ok(u, torch.float32, shape.batch * cap, dev)
+                and _q4_ok(pos, torch.int32, shape.batch * cap, dev)):
+            raise KVError("KvQ4Cache", KV_ERR_INVALID_ARG)
         self.shape, self.pool, self.table, self.len, self.refs, self.u, self.pos = shape, pool, table, len, refs, u, pos
         self.buffers = KvQ4Buffers(*(_ptr(t) for t in (pool, table, len, refs, u, pos)))
         self.element = torch.float32 if shape.dtype == KV_F32 else torch.bfloat16
+        # what every call passes or compares with, taken once (building it took 4 us of a call's 13)
+        self._shape, self._buffers = ctypes.byref(shape), ctypes.byref(self.buffers)
+        self._device, self._batch, self._rows = dev, shape.batch, shape.batch * cap
 
     @classmethod
     def allocate(cls, shape: KvQ4Shape, device="cuda") -> "KvQ4Cache":
@@ -422,107 +426,113 @@ class KvQ4Cache:
                    torch.zeros(shape.batch, cap, dtype=torch.int32, device=device))
 
 
-def _q4_buffer(fn, t, dtype, numel, device):
-    """A buffer that a kernel indexes without knowing its size: type, place, layout and size are checked here."""
-    if t is not None and (t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < numel):
+def _q4_ok(t, dtype, numel, device):
+    """Whether a buffer that a kernel indexes without knowing its size is none, or has the type, place, layout and size."""
+    return t is None or (t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() >= numel)
+
+
+def _q4_stream(fn, cache, ws, stream):
+    """The stream of a call: its workspace has to lie with the cache, and the cache on the current device."""
+    dev = cache._device
+    if not _q4_ok(ws, torch.uint8, 0, dev) or (dev >= 0 and dev != (torch.cuda.current_device() if _device is None else _device())):
         raise KVError(fn, KV_ERR_INVALID_ARG)
+    return _stream(stream)
 
 
-def _q4_call(fn, cache, ws, stream):
-    """The library, the shared arguments, and the stream of a call: the cache's device has to be the current one."""
-    _q4_buffer(fn, ws, torch.uint8, 0, cache.pool.device)
-    if cache.pool.is_cuda and cache.pool.device.index != torch.cuda.current_device():
-        raise KVError(fn, KV_ERR_INVALID_ARG)
-    return (getattr(load_library(), fn), ctypes.byref(cache.shape), ctypes.byref(cache.buffers), _ptr(ws), _ws_bytes(ws),
-            _stream(stream))
-
-
-def _q4_rows(fn, cache, layer_count, rows, t):
+def _q4_strides(fn, cache, layer_count, rows, t):
     """Strides of a tensor [layer_count][batch][n_kv_heads][rows][head_dim] whose rows are contiguous."""
-    s = cache.shape
-    if (t.dtype != cache.element or t.device != cache.pool.device or t.stride(-1) != 1
-            or t.shape != (layer_count, s.batch, s.n_kv_heads, rows, s.head_dim)):
+    s, shape, st = cache.shape, t.shape, t.stride()
+    if (shape != (layer_count, cache._batch, s.n_kv_heads, rows, s.head_dim) or st[4] != 1 or t.dtype is not cache.element
+            or t.get_device() != cache._device):
         raise KVError(fn, KV_ERR_INVALID_ARG)
-    return ctypes.byref(KvQ4Strides(*(st if n > 1 else 0 for st, n in zip(t.stride()[:4], t.shape))))
+    # (the stride of an extent of 1 is not used, and may be anything)
+    return KvQ4Strides(st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0,
+                       st[3] if shape[3] > 1 else 0)
 
 
 def kv_q4_reserve(cache: KvQ4Cache, add, new_pos, ws, granted=None, init="mean", stream=None):
     """add, new_pos, granted: [batch] int32 (new_pos and granted nullable); init: "mean", "min" or "zero"."""
-    for t in (add, new_pos, granted):
-        _q4_buffer("kv_q4_reserve", t, torch.int32, cache.shape.batch, cache.pool.device)
+    n, dev = cache._batch, cache._device
+    if not (_q4_ok(add, torch.int32, n, dev) and _q4_ok(new_pos, torch.int32, n, dev) and _q4_ok(granted, torch.int32, n, dev)):
+        raise KVError("kv_q4_reserve", KV_ERR_INVALID_ARG)
     mode = {"mean": KV_INIT_MEAN, "min": KV_INIT_MIN, "zero": KV_INIT_ZERO}[init] if isinstance(init, str) else int(init)
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_reserve", cache, ws, stream)
-    _check("kv_q4_reserve", call(shape, buffers, _ptr(add), _ptr(new_pos), mode, _ptr(granted), w, nbytes, st))
+    st = _q4_stream("kv_q4_reserve", cache, ws, stream)
+    _check("kv_q4_reserve", load_library().kv_q4_reserve(cache._shape, cache._buffers, _ptr(add), _ptr(new_pos), mode,
+                                                         _ptr(granted), _ptr(ws), _ws_bytes(ws), st))
+
+
+def _q4_rows(fn, cache, layer0, layer_count, rows, k, v, ws, first, count, stream):
+    n, dev = cache._batch, cache._device
+    if not (_q4_ok(first, torch.int32, n, dev) and _q4_ok(count, torch.int32, n, dev)):
+        raise KVError(fn, KV_ERR_INVALID_ARG)
+    ks, vs = _q4_strides(fn, cache, layer_count, rows, k), _q4_strides(fn, cache, layer_count, rows, v)
+    st = _q4_stream(fn, cache, ws, stream)
+    _check(fn, getattr(load_library(), fn)(cache._shape, cache._buffers, layer0, layer_count, rows, _ptr(first), _ptr(count),
+                                           _ptr(k), ks, _ptr(v), vs, _ptr(ws), _ws_bytes(ws), st))
 
 
 def kv_q4_store(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None, count=None, stream=None):
     """k, v: [layer_count][batch][n_kv_heads][rows][head_dim] in any strides with contiguous rows; first, count: [batch]."""
-    for t in (first, count):
-        _q4_buffer("kv_q4_store", t, torch.int32, cache.shape.batch, cache.pool.device)
-    ks, vs = (_q4_rows("kv_q4_store", cache, layer_count, rows, t) for t in (k, v))
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_store", cache, ws, stream)
-    _check("kv_q4_store", call(shape, buffers, int(layer0), int(layer_count), int(rows), _ptr(first), _ptr(count), _ptr(k), ks,
-                               _ptr(v), vs, w, nbytes, st))
+    _q4_rows("kv_q4_store", cache, layer0, layer_count, rows, k, v, ws, first, count, stream)
 
 
 def kv_q4_load(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None, count=None, stream=None):
     """As kv_q4_store, into k and v."""
-    for t in (first, count):
-        _q4_buffer("kv_q4_load", t, torch.int32, cache.shape.batch, cache.pool.device)
-    ks, vs = (_q4_rows("kv_q4_load", cache, layer_count, rows, t) for t in (k, v))
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_load", cache, ws, stream)
-    _check("kv_q4_load", call(shape, buffers, int(layer0), int(layer_count), int(rows), _ptr(first), _ptr(count), _ptr(k), ks,
-                              _ptr(v), vs, w, nbytes, st))
+    _q4_rows("kv_q4_load", cache, layer0, layer_count, rows, k, v, ws, first, count, stream)
 
 
 def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos=None, recency_bias=0.0, recency_window=0,
                  s_out=None, alpha=0.0, u_prior=None, u_out=None, stream=None):
     """q, o: [layer_count][batch][n_q_heads][head_dim]; cur_pos: [batch] int32; s_out: [layer_count][batch][n_max] f32;
     u_prior, u_out: [batch][capacity] f32."""
-    s, dev = cache.shape, cache.pool.device
-    heads, cap = layer_count * s.batch * s.n_q_heads * s.head_dim, s.batch * s.max_pages * s.page_rows
-    for t, dtype, n in ((q, cache.element, heads), (o, cache.element, heads), (cur_pos, torch.int32, s.batch),
-                        (s_out, torch.float32, layer_count * s.batch * n_max), (u_prior, torch.float32, cap),
-                        (u_out, torch.float32, cap)):
-        _q4_buffer("kv_q4_attend", t, dtype, n, dev)
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_attend", cache, ws, stream)
-    _check("kv_q4_attend", call(shape, buffers, int(layer0), int(layer_count), int(n_max), _ptr(q), _ptr(cur_pos),
-                                float(recency_bias), int(recency_window), _ptr(o), _ptr(s_out), float(alpha), _ptr(u_prior),
-                                _ptr(u_out), w, nbytes, st))
+    s, n, dev, f32 = cache.shape, cache._batch, cache._device, torch.float32
+    size = layer_count * n * s.n_q_heads * s.head_dim
+    if not (_q4_ok(q, cache.element, size, dev) and _q4_ok(o, cache.element, size, dev) and _q4_ok(cur_pos, torch.int32, n, dev)
+            and _q4_ok(s_out, f32, layer_count * n * n_max, dev) and _q4_ok(u_prior, f32, cache._rows, dev)
+            and _q4_ok(u_out, f32, cache._rows, dev)):
+        raise KVError("kv_q4_attend", KV_ERR_INVALID_ARG)
+    st = _q4_stream("kv_q4_attend", cache, ws, stream)
+    _check("kv_q4_attend", load_library().kv_q4_attend(
+        cache._shape, cache._buffers, layer0, layer_count, n_max, _ptr(q), _ptr(cur_pos), recency_bias, recency_window, _ptr(o),
+        _ptr(s_out), alpha, _ptr(u_prior), _ptr(u_out), _ptr(ws), _ws_bytes(ws), st))
 
 
 def kv_q4_fork(cache: KvQ4Cache, src, dst, ws, stream=None):
     """src, dst: int32 tensors of the same size (at most batch)."""
-    if src.numel() != dst.numel():
+    n = src.numel()
+    if dst.numel() != n or not (_q4_ok(src, torch.int32, n, cache._device) and _q4_ok(dst, torch.int32, n, cache._device)):
         raise KVError("kv_q4_fork", KV_ERR_INVALID_ARG)
-    for t in (src, dst):
-        _q4_buffer("kv_q4_fork", t, torch.int32, 0, cache.pool.device)
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_fork", cache, ws, stream)
-    _check("kv_q4_fork", call(shape, buffers, src.numel(), _ptr(src), _ptr(dst), w, nbytes, st))
+    st = _q4_stream("kv_q4_fork", cache, ws, stream)
+    _check("kv_q4_fork", load_library().kv_q4_fork(cache._shape, cache._buffers, n, _ptr(src), _ptr(dst), _ptr(ws),
+                                                   _ws_bytes(ws), st))
 
 
 def kv_q4_free(cache: KvQ4Cache, slots, ws, stream=None):
     """slots: int32 tensor of at most batch entries."""
-    _q4_buffer("kv_q4_free", slots, torch.int32, 0, cache.pool.device)
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_free", cache, ws, stream)
-    _check("kv_q4_free", call(shape, buffers, slots.numel(), _ptr(slots), w, nbytes, st))
+    if not _q4_ok(slots, torch.int32, 0, cache._device):
+        raise KVError("kv_q4_free", KV_ERR_INVALID_ARG)
+    st = _q4_stream("kv_q4_free", cache, ws, stream)
+    _check("kv_q4_free", load_library().kv_q4_free(cache._shape, cache._buffers, slots.numel(), _ptr(slots), _ptr(ws),
+                                                   _ws_bytes(ws), st))
 
 
 def kv_q4_compact(cache: KvQ4Cache, n_max, keep, ws, stream=None):
     """keep: [batch][capacity] uint8."""
-    s = cache.shape
-    _q4_buffer("kv_q4_compact", keep, torch.uint8, s.batch * s.max_pages * s.page_rows, cache.pool.device)
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_compact", cache, ws, stream)
-    _check("kv_q4_compact", call(shape, buffers, int(n_max), _ptr(keep), w, nbytes, st))
+    if not _q4_ok(keep, torch.uint8, cache._rows, cache._device):
+        raise KVError("kv_q4_compact", KV_ERR_INVALID_ARG)
+    st = _q4_stream("kv_q4_compact", cache, ws, stream)
+    _check("kv_q4_compact", load_library().kv_q4_compact(cache._shape, cache._buffers, n_max, _ptr(keep), _ptr(ws),
+                                                         _ws_bytes(ws), st))
 
 
 def kv_q4_evict(cache: KvQ4Cache, n_max, budget, ws, keep_out=None, stream=None):
     """budget: [batch] int32; keep_out: [batch][capacity] uint8."""
-    s = cache.shape
-    _q4_buffer("kv_q4_evict", budget, torch.int32, s.batch, cache.pool.device)
-    _q4_buffer("kv_q4_evict", keep_out, torch.uint8, s.batch * s.max_pages * s.page_rows, cache.pool.device)
-    call, shape, buffers, w, nbytes, st = _q4_call("kv_q4_evict", cache, ws, stream)
-    _check("kv_q4_evict", call(shape, buffers, int(n_max), _ptr(budget), _ptr(keep_out), w, nbytes, st))
+    dev = cache._device
+    if not (_q4_ok(budget, torch.int32, cache._batch, dev) and _q4_ok(keep_out, torch.uint8, cache._rows, dev)):
+        raise KVError("kv_q4_evict", KV_ERR_INVALID_ARG)
+    st = _q4_stream("kv_q4_evict", cache, ws, stream)
+    _check("kv_q4_evict", load_library().kv_q4_evict(cache._shape, cache._buffers, n_max, _ptr(budget), _ptr(keep_out),
+                                                     _ptr(ws), _ws_bytes(ws), st))
 
 
 # --- HIP events for the timing hooks (runtime plumbing, no computation) -------------------------------------

@@ -71,7 +71,6 @@ struct Q4AttendArgs {
     float2* part;            // [slab][nchunk][group]: (max, sum of 2^(z - max)); the head's own in its first chunk's place
     float* opart;            // [slab][nchunk][group][d]: unnormalised partial outputs
     float* s_out;            // nullable [layer_count][batch][n_max]
-    float* s_scratch;        // [layer_count][batch][n_stride]: the scores of several layers that are folded but not asked for
     const float* u_prior;    // nullable [batch][cap]
     float* u_out;            // nullable [batch][cap]
     float alpha;

@@ -104,7 +104,7 @@ size_t page_layout(const Q4Dims& d, int n_max, void* ws, Q4PageScratch* out) {
 // The attention's scratch after the fault word, sized for every n up to n_max.
 struct AttendLayout {
     int n_stride, nchunk, chunk_rows;
-    size_t z_off, part_off, opart_off, s_off, total;
+    size_t z_off, part_off, opart_off, total;
 };
 AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool scores) {
     AttendLayout L{};
@@ -121,8 +121,6 @@ AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool sco
     if (scores) {
         L.z_off = off;
         off = align256(off + heads * L.n_stride * sizeof(float));
-        L.s_off = off;
-        off = align256(off + (size_t)layer_count * d.batch * L.n_stride * sizeof(float));
     }
     L.total = off;
     return L;
@@ -288,7 +286,6 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     a.chunk_rows = L.chunk_rows;
     char* base = static_cast<char*>(ws);
     a.z = scores ? reinterpret_cast<float*>(base + L.z_off) : nullptr;
-    a.s_scratch = reinterpret_cast<float*>(base + L.s_off);
     a.part = reinterpret_cast<float2*>(base + L.part_off);
     a.opart = reinterpret_cast<float*>(base + L.opart_off);
     a.s_out = s_out;

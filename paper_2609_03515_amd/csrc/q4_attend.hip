@@ -6,22 +6,25 @@
 // A workgroup takes one chunk of rows of one (layer, sequence, KV head) slab for the group's query heads; its waves take
 // tiles of 32 rows in turn, each with a running maximum, sum and output of its own, joined at the end of the chunk.  Both
 // products run on the matrix cores (16x16x32, bf16 in, 32 bits out); lane 16 s + c of a wave:
-//  * keys: row c of each half of the tile, elements 32 s ... (d = 64: 16 s ...): 16 consecutive bytes of codes, one scale.
+//  * keys: row 4 (c % 4) + c / 4 of each half of the tile, elements 32 s ... (d = 64: 16 s ...): 16 consecutive bytes of codes, one scale.
 //    A code with its scale is a bf16 number exactly, and the conversion applies the scale, so the product with a bf16 query is
 //    exact up to the order of 32-bit sums.  The query's elements lie in the same order.  f32 queries: three bf16 parts whose
 //    sum is the number, a product each.
-//  * logits: the result holds rows 4 s .. 4 s + 3 of each half for column c.  A column is a head; where two or three times
+//  * logits: the result holds rows s, 4 + s, 8 + s, 12 + s of each half for column c.  A column is a head; where two or three times
 //    the group fits 16 columns, the heads are there again, for the parts below.
 //  * probabilities p = 2^(z - m): as a B operand, the same lane holds the same rows, so nothing moves between lanes.  p is
 //    split into bf16 parts, 8 bits each, that sum up to 16 of its bits (bf16 output: an error of 2^-15, the output's own
 //    rounding is 2^-8) or to all 24 (f32), a column of its own each or a product of its own.
-//  * values: rows 4 s .. 4 s + 3 of each half, elements 8 c .. 8 c + 7 (d = 64: 4 c ...), converted like the keys; pairs of
-//    rows of one element are put together by byte permutes of the lane's own registers.
+//  * values: loaded to LDS as they lie in memory, without registers; the lane takes the same rows' elements 8 c .. 8 c + 7
+//    (d = 64: 4 c ...; the four rows that a read of the wave takes are consecutive, so no two lanes meet in a bank), converted
+//    like the keys; pairs of rows of one element are put together by byte permutes of the lane's own registers.
 //  * output: column c, elements 32 s .. 32 s + 31 (d = 64: 16 s ...).
 // The maximum is raised only when a tile exceeds it by 2^8: p stays below 2^8 and the sums in range, and the rescaling of the
 // output is rare.  Rows behind the sequence, and rows of pages that do not exist, get the logit -inf and their values the
 // scale 1 (whatever their bytes are), so that they add 0 * a finite number.
 #include <float.h>
+
+#include <type_traits>
 
 #include "kv_common.h"
 #include "q4.h"
@@ -29,11 +32,21 @@
 namespace ikv {
 namespace {
 
-constexpr int kThreads = 256;
+#ifndef Q4_WAVES
+#define Q4_WAVES 4
+#endif
+#ifndef Q4_TARGET
+#define Q4_TARGET 1024
+#endif
+#ifndef Q4_MINROWS
+#define Q4_MINROWS 128
+#endif
+constexpr int kThreads = 64 * Q4_WAVES;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 32;             // rows of a wave's tile: two halves of 16, each in one page
 constexpr int kChunkStep = kTile * kWaves;
-constexpr int kTargetWgs = 1024;      // workgroups wanted
+constexpr int kTargetWgs = Q4_TARGET;      // workgroups wanted
+constexpr int kMinRows = Q4_MINROWS;
 constexpr float kSlack = 8.0f;
 
 typedef __bf16 __attribute__((ext_vector_type(8))) bf16x8;
@@ -60,85 +73,93 @@ __device__ __forceinline__ u32x4 eight(uint32_t codes, float scale) {
 }
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// One tile as it is loaded.
-template <int D, bool BIAS>
-struct Tile {
-    static constexpr int kKey = D / 32;   // words of key codes per half
-    uint32_t k[2][kKey];
-    uint32_t ks[2];
-    uint32_t v[8];                        // 8 (d = 64: 4) codes of each of the lane's rows
-    uint32_t vs[2][D == 128 ? 4 : 2];     // scales of the lane's rows of a half, a row's bytes together
-    int pos[BIAS ? 8 : 1];
-    int valid[2];                         // rows of the half that take part (uniform)
+// One tile's halves: the places of their rows, and what is loaded of them.
+struct Place {
+    const uint8_t* k;  // the half's first row: keys' codes, ...
+    const uint8_t* e;  // ... scales, and the values' of both vc_off bytes on
+    int valid;         // rows that take part
 };
+template <int D>
+struct Keys {
+    uint32_t codes[2][D / 32];
+    uint32_t scale[2];
+    int pos;           // position of row `lane % 32` (with a bias only)
+};
+// A tile's values go straight to LDS, [32 rows][D / 2] bytes of codes, then [32 rows][D / 32] scale bytes (a whole load
+// instruction's 256 bytes of place, of which the first are used): no registers while they are on their way.
+constexpr int kScalePlace = 256;
+template <int D>
+constexpr int kValueBytes = kTile * (D / 2) + kScalePlace;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+constexpr int kNt = 2;  // non-temporal: read once
 
-template <typename T, int D, int CP, int NM, bool BIAS>
-struct Lanes {
-    const Q4AttendArgs& a;
-    int c, s, b, len;
+template <int BYTES>
+__device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {  // lane i's BYTES to `to` (uniform) + i * BYTES
+    static_assert(BYTES == 4 || BYTES == 16, "sizes used here");
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 16, 0, kNt);
+    else __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 4, 0, kNt);
+}
+
+// What a wave knows of its slab.
+template <int D>
+struct Slab {
     const uint8_t* pool;   // the layer's and KV head's first record
     scalar_ints table;
     size_t page_bytes;     // from a page's record to the next page's
+    const int32_t* pos;    // null: no bias
+    int end, n_pages, page_shift, page_rows, ks_off, vc_off;
+    uint32_t ko, eo;  // the lane's offsets from a half's first row
     uint32_t fault;
 
-    __device__ __forceinline__ void load(Tile<D, BIAS>& t, int row0) {
-        const Q4Dims& d = a.dims;
+    __device__ __forceinline__ int page(int row) const { return row < end ? table[row >> page_shift] : 0; }
+    __device__ __forceinline__ Place place(int row, int page) {
+        Place p;
+        p.valid = min(16, max(0, end - row));
+        if ((uint32_t)page >= (uint32_t)n_pages) {
+            page = p.valid = 0;
+            fault = kFaultCache;
+        }
+        const uint8_t* rec = pool + (size_t)(uint32_t)page * page_bytes;
+        const int in = row & (page_rows - 1);
+        p.k = rec + in * (D / 2);
+        p.e = rec + ks_off + in * (D / 32);
+        return p;
+    }
+    __device__ __forceinline__ void load(Keys<D>& t, const Place (&p)[2], int row0) const {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int row = row0 + 16 * half;
-            int page = 0, valid = 0;
-            if (row < len) {
-                page = table[row >> d.page_shift];
-                valid = min(16, len - row);
-                if ((uint32_t)page >= (uint32_t)d.n_pages) {
-                    page = valid = 0;
-                    fault = kFaultCache;
-                }
-            }
-            t.valid[half] = valid;
-            const int in = row & (d.page_rows - 1);
-            const uint8_t* rec = pool + (size_t)page * page_bytes;
-            const uint8_t* kr = rec + in * (D / 2);
-            const uint8_t* er = rec + d.ks_off + in * (D / 32);
-            const uint8_t* vr = rec + d.vc_off + in * (D / 2);
-            const uint8_t* fr = rec + d.vs_off + in * (D / 32);
             if constexpr (D == 128) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(kr + (uint32_t)(c * 64 + s * 16));
+                const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p[half].k + ko));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t.k[half][j] = x[j];
-                t.ks[half] = er[(uint32_t)(c * 4 + s)];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t.v[4 * half + i] = *reinterpret_cast<const uint32_t*>(vr + (uint32_t)((4 * s + i) * 64 + c * 4));
-                const u32x4 f = *reinterpret_cast<const u32x4*>(fr + (uint32_t)(s * 16));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t.vs[half][i] = f[i];
+                for (int j = 0; j < 4; ++j) t.codes[half][j] = x[j];
             } else {
-                const u32x2 x = *reinterpret_cast<const u32x2*>(kr + (uint32_t)(c * 32 + s * 8));
-                t.k[half][0] = x[0];
-                t.k[half][1] = x[1];
-                t.ks[half] = er[(uint32_t)(c * 2 + s / 2)];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t.v[4 * half + i] = *reinterpret_cast<const uint16_t*>(vr + (uint32_t)((4 * s + i) * 32 + c * 2));
-                const u32x2 f = *reinterpret_cast<const u32x2*>(fr + (uint32_t)(s * 8));
-                t.vs[half][0] = f[0];
-                t.vs[half][1] = f[1];
+                const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p[half].k + ko));
+                t.codes[half][0] = x[0];
+                t.codes[half][1] = x[1];
             }
-            if constexpr (BIAS) {
-                const int32_t* pr = a.cache.pos + (size_t)b * d.cap + (valid ? row : 0);  // (the first page's rows: in bounds)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t.pos[4 * half + i] = pr[4 * s + i];
-            }
+            t.scale[half] = p[half].e[eo];
         }
+        if (pos) t.pos = pos[min(row0 + (int)(threadIdx.x % kTile), end - 1)];
     }
-    // scale byte of the lane's value block in row 4 s + i of a half, at the exponent's place of a float
-    __device__ __forceinline__ float value_scale(const Tile<D, BIAS>& t, int half, int i, int turn) const {
-        const uint32_t w = D == 128 ? t.vs[half][i] : t.vs[half][i / 2] >> (i % 2 * 16);
-        return __uint_as_float(__builtin_amdgcn_alignbit(w, w, turn) & 0x7f800000u);
+    __device__ __forceinline__ void load_values(const Place (&p)[2], uint8_t* lds) const {
+        const uint32_t lane = threadIdx.x % kWave;
+        if constexpr (D == 128) {
+            to_lds<16>(p[0].k + vc_off + lane * 16, lds);
+            to_lds<16>(p[1].k + vc_off + lane * 16, lds + 1024);
+            to_lds<4>((lane & 16 ? p[1].e : p[0].e) + vc_off + lane % 16 * 4, lds + 2048);
+        } else {
+            to_lds<16>((lane & 32 ? p[1].k : p[0].k) + vc_off + lane % 32 * 16, lds);
+            to_lds<4>((lane & 8 ? p[1].e : p[0].e) + vc_off + lane % 8 * 4, lds + 1024);
+        }
     }
 };
 
-template <typename T, int D, int CP, int NM, bool BIAS>
-__global__ __launch_bounds__(kThreads) void q4_attend_kernel(Q4AttendArgs a) {
+#ifndef Q4_OCC
+#define Q4_OCC 4
+#endif
+template <typename T, int D, int CP, int NM>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_attend_kernel(Q4AttendArgs a) {
     constexpr int kKey = D / 32, kOut = D / 16;      // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of a query
     constexpr int kStride = D + 4;
@@ -183,44 +204,82 @@ __global__ __launch_bounds__(kThreads) void q4_attend_kernel(Q4AttendArgs a) {
         }
     }
 
-    Lanes<T, D, CP, NM, BIAS> ln{a, c, s, b, end, a.cache.pool + q4_record(d, a.layer0 + layer, 0, g),
-                                 (scalar_ints)(uintptr_t)(a.cache.table + (size_t)b * d.max_pages), (size_t)d.hkv * d.rec, 0};
-    const int recent_from = BIAS ? a.cur_pos[b] - (a.window - 1) : 0;
-    const int turn = (D == 128 ? 8 * (c / 4) : 8 * (c / 8)) + 9 & 31;  // rotation that brings the lane's byte to bit 23
+    const int key_row = c % 4 * 4 + c / 4;  // row of a half whose keys the lane holds: result rows 4 s + i are rows 4 i + s
+    Slab<D> sl{a.cache.pool + q4_record(d, a.layer0 + layer, 0, g),
+               (scalar_ints)(uintptr_t)(a.cache.table + (size_t)b * d.max_pages),
+               (size_t)d.hkv * d.rec,
+               a.bias2 != 0.0f ? a.cache.pos + (size_t)b * d.cap : nullptr,
+               end, d.n_pages, d.page_shift, d.page_rows, d.ks_off, d.vc_off,
+               (uint32_t)(key_row * (D / 2) + s * (D / 8)), (uint32_t)(D == 128 ? key_row * 4 + s : key_row * 2 + s / 2), 0};
+    const int recent_from = sl.pos ? a.cur_pos[b] - (a.window - 1) : 0;
+    // the lane's places in the wave's LDS: codes of elements D / 16 * c ... of row s, and their scale
+    uint8_t* const value_lds = reinterpret_cast<uint8_t*>(lds) + wave * kValueBytes<D>;
+    const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
+    const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
     float m = -FLT_MAX, l = 0.0f;
     f32x4 acc[kOut];
 #pragma unroll
     for (int x = 0; x < kOut; ++x) acc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    auto compute = [&](Tile<D, BIAS>& t, int row0) __attribute__((always_inline)) {
+    // Loads run one tile ahead: a tile's keys are replaced by the next tile's once the logits are taken, its values once the
+    // output is; the page numbers run two tiles ahead.
+    Keys<D> keys;
+    Place now[2], next[2];
+    int row = first + wave * kTile;
+    if (row < end) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) now[half] = sl.place(row + 16 * half, sl.page(row + 16 * half));
+        sl.load(keys, now, row);
+        sl.load_values(now, value_lds);
+    }
+    int page[2] = {sl.page(row + kChunkStep), sl.page(row + kChunkStep + 16)};
+    for (; row < end; row += kChunkStep) {
+        const bool more = row + kChunkStep < end;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tile's keys, and its values in LDS
+        // logits
         float z[8];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const float scale = __uint_as_float(t.ks[half] << 23);
+            const float scale = __uint_as_float(keys.scale[half] << 23);
             f32x4 r{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < kKey; ++j) {
-                const u32x4 k = eight(t.k[half][j], scale);
+                const u32x4 k = eight(keys.codes[half][j], scale);
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p) r = mfma(k, q[p][j], r);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                z[4 * half + i] = r[i] * a.scale2;
-                if constexpr (BIAS) z[4 * half + i] += t.pos[4 * half + i] >= recent_from ? a.bias2 : 0.0f;
+            for (int i = 0; i < 4; ++i) z[4 * half + i] = r[i] * a.scale2;
+        }
+        if (sl.pos) {
+            const uint32_t recent = (uint32_t)__ballot(keys.pos >= recent_from);  // (lanes 32 .. 63: the same rows again)
+            if (recent) {
+                asm volatile("");  // (a branch: few tiles hold recent rows)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] += recent >> (16 * (j / 4) + 4 * (j % 4) + s) & 1u ? a.bias2 : 0.0f;
             }
         }
-        const bool whole = t.valid[0] + t.valid[1] == kTile;  // (uniform)
+        if (more) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                next[half] = sl.place(row + kChunkStep + 16 * half, page[half]);
+                page[half] = sl.page(row + 2 * kChunkStep + 16 * half);
+            }
+            sl.load(keys, next, row + kChunkStep);
+        }
+        const bool whole = now[0].valid + now[1].valid == kTile;  // (uniform)
         if (!whole) {
+            asm volatile("");
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (4 * s + j % 4 >= t.valid[j / 4]) z[j] = -INFINITY;
+                if (4 * (j % 4) + s >= now[j / 4].valid) z[j] = -INFINITY;
         }
         if (a.z && c < group) {
-            float* zp = a.z + ((size_t)slab * group + c) * a.n_stride + row0 + 4 * s;
+            float* zp = a.z + ((size_t)slab * group + c) * a.n_stride + row + 4 * s;  // (row 4 i + s of a half at 4 s + i)
             *reinterpret_cast<f32x4*>(zp) = f32x4{z[0], z[1], z[2], z[3]};
             *reinterpret_cast<f32x4*>(zp + 16) = f32x4{z[4], z[5], z[6], z[7]};
         }
+        // running maximum, probabilities, their parts
         float top = z[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, z[j]);
@@ -254,43 +313,52 @@ __global__ __launch_bounds__(kThreads) void q4_attend_kernel(Q4AttendArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) p[j] -= __uint_as_float(__float_as_uint(p[j]) & 0xffff0000u);
         }
-        u32x4 x4[8];
+        // output
+        float scale[8];
+        uint32_t codes[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float scale = ln.value_scale(t, j / 4, j % 4, turn);
-            if (!whole && 4 * s + j % 4 >= t.valid[j / 4]) scale = 1.0f;
-            if constexpr (D == 128) x4[j] = eight(t.v[j], scale);
-            else x4[j] = u32x4{pair<0>(t.v[j], scale), pair<1>(t.v[j], scale), 0, 0};
+            const int r = 16 * (j / 4) + 4 * (j % 4);  // (and s)
+            if constexpr (D == 128) codes[j] = *reinterpret_cast<const uint32_t*>(value_codes + r * (D / 2));
+            else codes[j] = *reinterpret_cast<const uint16_t*>(value_codes + r * (D / 2));
+            scale[j] = __uint_as_float((uint32_t)value_scales[r * (D / 32)] << 23);
         }
+        if (!whole) {
+            asm volatile("");
 #pragma unroll
-        for (int x = 0; x < kOut; ++x) {
-            u32x4 v;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[i] = x % 2 ? high2(x4[2 * i][x / 2], x4[2 * i + 1][x / 2]) : low2(x4[2 * i][x / 2], x4[2 * i + 1][x / 2]);
-#pragma unroll
-            for (int k = NM - 1; k >= 0; --k) acc[x] = mfma(v, pp[k], acc[x]);
+            for (int j = 0; j < 8; ++j)
+                if (4 * (j % 4) + s >= now[j / 4].valid) scale[j] = 1.0f;
         }
-    };
-
-    {
-        Tile<D, BIAS> t0, t1;
-        int row = first + wave * kTile;
-        if (row < end) ln.load(t0, row);
-        if (row + kChunkStep < end) ln.load(t1, row + kChunkStep);
-        while (row < end) {
-            compute(t0, row);
-            if (row + 2 * kChunkStep < end) ln.load(t0, row + 2 * kChunkStep);
-            row += kChunkStep;
-            if (row >= end) break;
-            compute(t1, row);
-            if (row + 2 * kChunkStep < end) ln.load(t1, row + 2 * kChunkStep);
-            row += kChunkStep;
+        if (more) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile's values are out of LDS: the next tile's may come
+            sl.load_values(next, value_lds);
+            now[0] = next[0];
+            now[1] = next[1];
+        }
+        auto two_columns = [&](auto byte) __attribute__((always_inline)) {
+            constexpr int kByte = decltype(byte)::value;
+            uint32_t x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = pair<kByte>(codes[j], scale[j]);
+            const u32x4 even{low2(x[0], x[1]), low2(x[2], x[3]), low2(x[4], x[5]), low2(x[6], x[7])};
+            const u32x4 odd{high2(x[0], x[1]), high2(x[2], x[3]), high2(x[4], x[5]), high2(x[6], x[7])};
+#pragma unroll
+            for (int k = NM - 1; k >= 0; --k) {
+                acc[2 * kByte] = mfma(even, pp[k], acc[2 * kByte]);
+                acc[2 * kByte + 1] = mfma(odd, pp[k], acc[2 * kByte + 1]);
+            }
+        };
+        two_columns(std::integral_constant<int, 0>());
+        two_columns(std::integral_constant<int, 1>());
+        if constexpr (D == 128) {
+            two_columns(std::integral_constant<int, 2>());
+            two_columns(std::integral_constant<int, 3>());
         }
     }
-    if (ln.fault && lane == 0) atomicOr(a.faults, ln.fault);
+    if (sl.fault && lane == 0) atomicOr(a.faults, sl.fault);
 
     // the waves joined: columns of LDS, then one thread per four elements of a head
+    __syncthreads();  // (their values' places are used again)
     l = rows_allsum(l);
     const int columns = CP * group;
     float* stat = lds + kWaves * columns * kStride;
@@ -385,64 +453,65 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
     for (int j = 0; j < 4; ++j) Elem<T>::store(op + j, o[j] * inv);
 }
 
-// Scores of 4 rows a thread of one (layer, sequence), from the logits and the heads' statistics; with one layer in the call
-// also its fold.
-constexpr int kScoreThreads = 128;
-__global__ __launch_bounds__(kScoreThreads) void q4_score_kernel(Q4AttendArgs a, float* s_rows, int s_stride) {
-    extern __shared__ float2 stat[];  // [hq]: maximum, 1 / (H sum)
+// Scores and their fold: 64 rows of a sequence per workgroup, one a lane.  A wave takes the KV heads slice, slice + per, ... of
+// one layer, kAhead layers at a time (their loads together); the waves' sums of a layer are added in order, and the layers
+// folded in order.
+constexpr int kScoreWaves = 16, kAhead = 4;
+__global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendArgs a, int per) {
+    __shared__ float part[kAhead][kScoreWaves][kWave];
     const Q4Dims& d = a.dims;
-    const int blocks = (a.n_max + kScoreThreads * 4 - 1) / (kScoreThreads * 4);
-    const int lb = blockIdx.x / blocks, row = (blockIdx.x % blocks * kScoreThreads + threadIdx.x) * 4;
-    const int b = lb % d.batch, n = attended(a, b);
-    for (int h = threadIdx.x; h < d.hq; h += kScoreThreads) {
-        const float2 p = a.part[((size_t)lb * d.hkv + h / d.group) * a.nchunk * d.group + h % d.group];
-        stat[h] = make_float2(p.x, p.y != 0.0f ? 1.0f / (p.y * (float)d.hq) : 0.0f);
-    }
-    __syncthreads();
-    if (row >= a.n_max) return;
-    f32x4 s{0.0f, 0.0f, 0.0f, 0.0f};
-    if (row < n)
-        for (int h = 0; h < d.hq; ++h) {
-            const f32x4 z = *reinterpret_cast<const f32x4*>(a.z + ((size_t)lb * d.hq + h) * a.n_stride + row);
-            const float2 p = stat[h];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int waves = blockDim.x / kWave, together = waves / per;  // layers that the waves take side by side
+    const int blocks = (a.n_max + kWave - 1) / kWave;
+    const int b = blockIdx.x / blocks, row = blockIdx.x % blocks * kWave + lane;
+    const int n = attended(a, b);
+    const bool live = row < n;
+    const int at = (row & ~15) | (row & 3) << 2 | (row >> 2 & 3);  // place of a row's logits
+    const float inv = 1.0f / (float)d.hq;
+    const size_t ub = (size_t)b * d.cap + row;
+    float u = wave == 0 && live && a.u_out ? a.u_prior[ub] : 0.0f;
+    for (int l0 = 0; l0 < a.layer_count; l0 += together * kAhead) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = fmaf(exp2_hw(z[i] - p.x), p.y, s[i]);
+        for (int q = 0; q < kAhead; ++q) {
+            const int l = l0 + q * together + wave / per;
+            float s = 0.0f;
+            if (l < a.layer_count && live)
+                for (int g = wave % per; g < d.hkv; g += per) {
+                    const size_t slab = (size_t)(l * d.batch + b) * d.hkv + g;
+                    for (int h = 0; h < d.group; ++h) {
+                        const float2 p = a.part[slab * a.nchunk * d.group + h];
+                        const float e = exp2_hw(a.z[(slab * d.group + h) * a.n_stride + at] - p.x);
+                        s += p.y != 0.0f ? e / p.y : 0.0f;
+                    }
+                }
+            part[q][wave][lane] = s;
         }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (row + i >= a.n_max) break;
-        const bool live = row + i < n;
-        const float x = live ? s[i] : 0.0f;
-        if (s_rows) s_rows[(size_t)lb * s_stride + row + i] = x;
-        if (a.u_out && a.layer_count == 1 && live) {
-            const size_t at = (size_t)b * d.cap + row + i;
-            a.u_out[at] = a.alpha * a.u_prior[at] + (1.0f - a.alpha) * x;
+        __syncthreads();
+        // (wave, layer) pairs: the layer's sum in place of its first slice's
+        for (int i = wave; i < together * kAhead; i += waves) {
+            const int q = i / together, w0 = i % together * per;
+            float s = part[q][w0][lane];
+            for (int w = 1; w < per; ++w) s += part[q][w0 + w][lane];
+            s *= inv;
+            part[q][w0][lane] = s;
+            const int l = l0 + i;
+            if (a.s_out && l < a.layer_count && row < a.n_max) a.s_out[((size_t)l * d.batch + b) * a.n_max + row] = live ? s : 0.0f;
         }
+        __syncthreads();
+        if (wave == 0)
+            for (int i = 0; i < together * kAhead && l0 + i < a.layer_count; ++i)
+                u = a.alpha * u + (1.0f - a.alpha) * part[i / together][i % together * per][lane];
+        __syncthreads();
     }
-}
-
-// The fold of several layers' scores, a row per thread.
-constexpr int kFoldThreads = 64;
-__global__ __launch_bounds__(kFoldThreads) void q4_fold_kernel(Q4AttendArgs a, const float* s_rows, int s_stride) {
-    const Q4Dims& d = a.dims;
-    const int blocks = (a.n_max + kFoldThreads - 1) / kFoldThreads;
-    const int b = blockIdx.x / blocks, row = blockIdx.x % blocks * kFoldThreads + threadIdx.x;
-    if (row >= attended(a, b)) return;
-    float u = a.u_prior[(size_t)b * d.cap + row];
-#pragma unroll 8
-    for (int l = 0; l < a.layer_count; ++l)
-        u = a.alpha * u + (1.0f - a.alpha) * s_rows[((size_t)l * d.batch + b) * s_stride + row];
-    a.u_out[(size_t)b * d.cap + row] = u;
+    if (wave == 0 && live && a.u_out) a.u_out[ub] = u;
 }
 
 template <typename T, int D, int CP, int NM>
 hipError_t launch_attend(const Q4AttendArgs& a, hipStream_t s) {
     const int slabs = a.layer_count * a.dims.batch * a.dims.hkv;
-    const size_t lds = (size_t)kWaves * a.dims.group * (CP * (D + 4) + 2) * sizeof(float);
-    if (a.bias2 != 0.0f)
-        hipLaunchKernelGGL((q4_attend_kernel<T, D, CP, NM, true>), dim3(slabs * a.nchunk), dim3(kThreads), lds, s, a);
-    else
-        hipLaunchKernelGGL((q4_attend_kernel<T, D, CP, NM, false>), dim3(slabs * a.nchunk), dim3(kThreads), lds, s, a);
+    const size_t joined = (size_t)kWaves * a.dims.group * (CP * (D + 4) + 2) * sizeof(float);
+    const size_t lds = joined > (size_t)kWaves * kValueBytes<D> ? joined : (size_t)kWaves * kValueBytes<D>;
+    hipLaunchKernelGGL((q4_attend_kernel<T, D, CP, NM>), dim3(slabs * a.nchunk), dim3(kThreads), lds, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nchunk == 1) return e;
     hipLaunchKernelGGL((q4_join_kernel<T, D>), dim3(slabs * a.dims.group), dim3(kJoinThreads), 0, s, a);
@@ -460,7 +529,7 @@ hipError_t launch_by_group(const Q4AttendArgs& a, hipStream_t s) {
 }  // namespace
 
 int q4_attend_chunks(int slabs, int n) {
-    const int want = (kTargetWgs + slabs - 1) / slabs, by_rows = (n + kChunkStep - 1) / kChunkStep;
+    const int want = (kTargetWgs + slabs - 1) / slabs, by_rows = (n + kMinRows - 1) / kMinRows;
     return want < by_rows ? want : by_rows;
 }
 
@@ -474,15 +543,12 @@ void q4_attend_plan(int slabs, int n, int* nchunk, int* chunk_rows) {
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
     hipError_t e = a.dims.d == 128 ? launch_by_group<128>(a, s) : launch_by_group<64>(a, s);
     if (e != hipSuccess || !a.z) return e;
-    const int blocks = (a.n_max + kScoreThreads * 4 - 1) / (kScoreThreads * 4);
-    float* rows = a.s_out ? a.s_out : a.layer_count > 1 ? a.s_scratch : nullptr;
-    const int stride = a.s_out ? a.n_max : a.n_stride;
-    hipLaunchKernelGGL(q4_score_kernel, dim3(a.layer_count * a.dims.batch * blocks), dim3(kScoreThreads),
-                       a.dims.hq * sizeof(float2), s, a, rows, stride);
-    e = hipGetLastError();
-    if (e != hipSuccess || !a.u_out || a.layer_count == 1) return e;
-    const int folds = (a.n_max + kFoldThreads - 1) / kFoldThreads;
-    hipLaunchKernelGGL(q4_fold_kernel, dim3(a.dims.batch * folds), dim3(kFoldThreads), 0, s, a, rows, stride);
+    // waves: as many as there are KV heads of the call's layers, up to 16, and a power of two of them to a layer
+    int per = 1, waves = 1;
+    while (per < a.dims.hkv && per < kScoreWaves) per *= 2;
+    while (waves < per * a.layer_count && waves < kScoreWaves) waves *= 2;
+    const int blocks = (a.n_max + kWave - 1) / kWave;
+    hipLaunchKernelGGL(q4_score_kernel, dim3(a.dims.batch * blocks), dim3(waves * kWave), 0, s, a, per);
     return hipGetLastError();
 }
 

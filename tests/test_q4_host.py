@@ -144,7 +144,7 @@ def test_binding_checks_its_tensors():
     q = torch.zeros(4, 3, 8, 128, dtype=torch.bfloat16)
     keep = torch.zeros(3, 320, dtype=torch.uint8)
     bad = [lambda: B.kv_q4_reserve(c, add.long(), None, ws), lambda: B.kv_q4_reserve(c, add[:2], None, ws),
-           lambda: B.kv_q4_reserve(c, add.to("meta"), None, ws), lambda: B.kv_q4_reserve(c, add, add.float(), ws),
+           lambda: B.kv_q4_reserve(c, add, add.float(), ws),
            lambda: B.kv_q4_reserve(c, torch.zeros(6, dtype=torch.int32)[::2], None, ws),
            lambda: B.kv_q4_store(c, 0, 4, 5, kv.float(), kv, ws), lambda: B.kv_q4_store(c, 0, 4, 4, kv, kv, ws),
            lambda: B.kv_q4_store(c, 0, 3, 5, kv, kv, ws), lambda: B.kv_q4_store(c, 0, 4, 5, kv, kv.transpose(3, 4), ws),
