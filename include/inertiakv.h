@@ -337,7 +337,7 @@ kv_status kv_evict_finish(const kv_shape* shape, const kv_params* params, int32_
  * workspace must not overlap; nothing in the workspace but the fault word outlives a call.  Arrays of the batch (add,
  * budget, ...) are device memory, so a captured graph can be replayed with other lengths, slots and budgets. */
 typedef struct {
-    int32_t batch;      /* slots                                                             >= 1              */
+    int32_t batch;      /* slots                                                             1..65535           */
     int32_t layers;     /* 1..256                                                                              */
     int32_t n_q_heads;  /* multiple of n_kv_heads, at most 16 times as many                                    */
     int32_t n_kv_heads;

@@ -66,20 +66,24 @@ struct Q4AttendArgs {
     int window;
     float scale2;            // log2(e) / sqrt(d)
     float bias2;             // log2(e) * bias
-    int nchunk, chunk_rows;
-    float* z;                // scores wanted: [slab][group][n_stride] base-2 logits, slab = (layer * batch + b) * hkv + head
-    float2* part;            // [slab][nchunk][group]: (max, sum of 2^(z - max)); the head's own in its first chunk's place
-    float* opart;            // [slab][nchunk][group][d]: unnormalised partial outputs
+    int nchunk, chunk_rows, scored;  // Q4AttendPlan
+    int stat_at;             // floats of LDS before the waves' statistics (set by the launch)
+    float* z;                // scores wanted: base-2 logits [slab][group][n_stride], or [slab][n_stride] parts of the scores
+    float2* stat;            // scores wanted: [slab][group] (max, 1 / sum of 2^(z - max)), slab = (layer * batch + b) * hkv + head
+    float2* part;            // several chunks: [slab][nchunk][group] (max, sum)
+    float* opart;            // several chunks: [slab][nchunk][group][d] unnormalised partial outputs
     float* s_out;            // nullable [layer_count][batch][n_max]
     const float* u_prior;    // nullable [batch][cap]
     float* u_out;            // nullable [batch][cap]
     float alpha;
     uint32_t* faults;
 };
-// Row chunks per slab, and rows of a chunk, of a call on `slabs` slabs of at most n rows; and a bound on the chunks that does
-// not fall when n grows.
-int q4_attend_chunks(int slabs, int n);
-void q4_attend_plan(int slabs, int n, int* nchunk, int* chunk_rows);
+// How a call on layer_count layers and at most n_max rows is divided: chunks of rows per slab, `most` of them at most (which
+// does not fall when n_max grows); or (scored) a slab per workgroup with its logits in LDS.
+struct Q4AttendPlan {
+    int nchunk, chunk_rows, most, scored, n_stride;
+};
+Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool scores);
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);
 
 // Pages.  Scratch of the calls that allocate pages; the lists are the compaction's.

@@ -25,7 +25,7 @@ kv_status check_shape(const kv_q4_shape* s) {
     if (s->batch < 1 || s->layers < 1 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->n_pages < 1 || s->max_pages < 1 ||
         s->page_rows < 1)
         return KV_ERR_INVALID_ARG;
-    if (s->layers > kMaxLayers) return KV_ERR_UNSUPPORTED;
+    if (s->layers > kMaxLayers || s->batch > 65535) return KV_ERR_UNSUPPORTED;
     if (s->n_q_heads % s->n_kv_heads) return KV_ERR_INVALID_ARG;
     if (s->dtype != KV_F32 && s->dtype != KV_BF16) return KV_ERR_UNSUPPORTED;
     if (s->head_dim != 64 && s->head_dim != 128) return KV_ERR_UNSUPPORTED;
@@ -101,26 +101,26 @@ size_t page_layout(const Q4Dims& d, int n_max, void* ws, Q4PageScratch* out) {
     return off;
 }
 
-// The attention's scratch after the fault word, sized for every n up to n_max.
+// The attention's scratch after the fault word: sized for every number of rows up to n_max.
 struct AttendLayout {
-    int n_stride, nchunk, chunk_rows;
-    size_t z_off, part_off, opart_off, total;
+    Q4AttendPlan plan;
+    size_t z_off, stat_off, part_off, opart_off, total;
 };
 AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool scores) {
     AttendLayout L{};
-    const int slabs = layer_count * d.batch * d.hkv;
-    q4_attend_plan(slabs, n_max, &L.nchunk, &L.chunk_rows);
-    const size_t chunks = q4_attend_chunks(slabs, n_max);
-    L.n_stride = (n_max + 63) / 64 * 64;
-    const size_t heads = (size_t)slabs * d.group;
+    L.plan = q4_attend_plan(d, layer_count, n_max, scores);
+    const size_t slabs = (size_t)layer_count * d.batch * d.hkv, slots = L.plan.most > 1 ? slabs * L.plan.most : 0;
     size_t off = kFaultBytes;
-    L.part_off = off;
-    off = align256(off + heads * chunks * sizeof(float2));
-    L.opart_off = off;
-    if (chunks > 1) off = align256(off + heads * chunks * d.d * sizeof(float));
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align256(off + bytes);
+        return at;
+    };
+    L.part_off = take(slots * d.group * sizeof(float2));
+    L.opart_off = take(slots * d.group * d.d * sizeof(float));
     if (scores) {
-        L.z_off = off;
-        off = align256(off + heads * L.n_stride * sizeof(float));
+        L.stat_off = take(slabs * d.group * sizeof(float2));
+        L.z_off = take(slabs * d.group * L.plan.n_stride * sizeof(float));
     }
     L.total = off;
     return L;
@@ -265,7 +265,7 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
         return KV_ERR_UNSUPPORTED;
     const bool scores = s_out || u_out;
     const AttendLayout L = attend_layout(d, n_max, layer_count, scores);
-    if ((double)layer_count * s.batch * s.n_kv_heads * L.nchunk > 2.0e9) return KV_ERR_UNSUPPORTED;
+    if ((double)layer_count * L.plan.nchunk > 65535.0) return KV_ERR_UNSUPPORTED;  // (the grid's third extent)
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
     Q4AttendArgs a{};
     a.dims = d;
@@ -273,7 +273,7 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     a.layer0 = layer0;
     a.layer_count = layer_count;
     a.n_max = n_max;
-    a.n_stride = L.n_stride;
+    a.n_stride = L.plan.n_stride;
     a.q = q;
     a.o = o;
     a.cur_pos = cur_pos;
@@ -282,10 +282,12 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     constexpr double kLog2e = 1.4426950408889634;
     a.scale2 = (float)(kLog2e / sqrt((double)s.head_dim));
     a.bias2 = (float)(kLog2e * a.bias);
-    a.nchunk = L.nchunk;
-    a.chunk_rows = L.chunk_rows;
+    a.nchunk = L.plan.nchunk;
+    a.chunk_rows = L.plan.chunk_rows;
+    a.scored = L.plan.scored;
     char* base = static_cast<char*>(ws);
     a.z = scores ? reinterpret_cast<float*>(base + L.z_off) : nullptr;
+    a.stat = scores ? reinterpret_cast<float2*>(base + L.stat_off) : nullptr;
     a.part = reinterpret_cast<float2*>(base + L.part_off);
     a.opart = reinterpret_cast<float*>(base + L.opart_off);
     a.s_out = s_out;

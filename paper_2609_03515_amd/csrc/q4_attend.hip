@@ -24,30 +24,28 @@
 // scale 1 (whatever their bytes are), so that they add 0 * a finite number.
 #include <float.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "kv_common.h"
 #include "q4.h"
+#include "stream_lane.h"
 
 namespace ikv {
 namespace {
 
 #ifndef Q4_WAVES
-#define Q4_WAVES 4
+#define Q4_WAVES 8
 #endif
-#ifndef Q4_TARGET
-#define Q4_TARGET 1024
+#ifndef Q4_WAVES32
+#define Q4_WAVES32 4
 #endif
-#ifndef Q4_MINROWS
-#define Q4_MINROWS 128
+#ifndef Q4_PER_CU
+#define Q4_PER_CU 16
 #endif
-constexpr int kThreads = 64 * Q4_WAVES;
-constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 32;             // rows of a wave's tile: two halves of 16, each in one page
-constexpr int kChunkStep = kTile * kWaves;
-constexpr int kTargetWgs = Q4_TARGET;      // workgroups wanted
-constexpr int kMinRows = Q4_MINROWS;
 constexpr float kSlack = 8.0f;
+constexpr int kMostRows = 8192;       // rows of a chunk, however many slabs there are: a batch may hold one long sequence
 
 typedef __bf16 __attribute__((ext_vector_type(8))) bf16x8;
 typedef uint32_t __attribute__((ext_vector_type(2))) u32x2;
@@ -108,17 +106,17 @@ struct Slab {
     scalar_ints table;
     size_t page_bytes;     // from a page's record to the next page's
     const int32_t* pos;    // null: no bias
-    int end, n_pages, page_shift, page_rows, ks_off, vc_off;
+    int end, last, n_pages, page_shift, page_rows, ks_off, vc_off;  // (last: the last row that the table has a place for)
     uint32_t ko, eo;  // the lane's offsets from a half's first row
     uint32_t fault;
 
-    __device__ __forceinline__ int page(int row) const { return row < end ? table[row >> page_shift] : 0; }
+    __device__ __forceinline__ int page(int row) const { return table[min(row, last) >> page_shift]; }
     __device__ __forceinline__ Place place(int row, int page) {
         Place p;
         p.valid = min(16, max(0, end - row));
-        if ((uint32_t)page >= (uint32_t)n_pages) {
+        if ((uint32_t)page >= (uint32_t)n_pages) {  // (behind the sequence: anything; its rows are loaded, and take no part)
+            if (p.valid) fault = kFaultCache;
             page = p.valid = 0;
-            fault = kFaultCache;
         }
         const uint8_t* rec = pool + (size_t)(uint32_t)page * page_bytes;
         const int in = row & (page_rows - 1);
@@ -155,31 +153,61 @@ struct Slab {
     }
 };
 
-#ifndef Q4_OCC
-#define Q4_OCC 4
-#endif
-template <typename T, int D, int CP, int NM>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_attend_kernel(Q4AttendArgs a) {
+constexpr int kZPad = 16;  // floats between the heads' logits in LDS
+
+// Waves of a workgroup: f32 queries take three times the registers.
+template <typename T>
+constexpr int waves_of(bool scored) { return sizeof(T) == 2 ? Q4_WAVES : scored ? 8 : Q4_WAVES32; }
+
+template <typename T, int D, int CP, int NM, bool kScored>
+__global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3) void q4_attend_kernel(Q4AttendArgs a) {
+    constexpr int kWaves = waves_of<T>(kScored), kThreads = kWave * kWaves, kStep = kTile * kWaves;
     constexpr int kKey = D / 32, kOut = D / 16;      // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of a query
     constexpr int kStride = D + 4;
-    extern __shared__ float lds[];                   // [wave][column][kStride], then [wave][column] maxima and sums
+    constexpr int kJoin = kWaves > 4 ? 4 : kWaves;   // waves whose outputs are joined through LDS at once
+    // [wave] values; in their place [joined wave][column][kStride] outputs; behind both [wave][head] maxima and sums, then (kScored)
+    // the heads' own and the slab's logits [head][rows + kZPad]
+    extern __shared__ float lds[];
     const Q4Dims& d = a.dims;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int c = lane % 16, s = lane / 16;
-    const int slab = blockIdx.x / a.nchunk, chunk = blockIdx.x % a.nchunk;
-    const int lb = slab / d.hkv, g = slab % d.hkv, b = lb % d.batch, layer = lb / d.batch;
-    const int len_b = a.cache.len[b], len = len_b < 0 || len_b > a.n_max ? 0 : len_b;
-    if (len != len_b && chunk == 0 && threadIdx.x == 0) atomicOr(a.faults, kFaultCache);
-    const int first = chunk * a.chunk_rows;
-    if (first >= len && chunk > 0) return;
-    const int end = min(len, first + a.chunk_rows);
 
     // the lane's column: part `part` of head `head` (columns past the last: no head)
     const int group = d.group;
     const int part = c / group, head = c % group;
     const bool column = part < CP;
+    const int columns = CP * group;
     const uint32_t cut1 = part >= 1 ? 0xffff0000u : 0u, cut2 = part >= 2 ? 0xffff0000u : 0u;
+    // the lane's places in the wave's LDS: codes of elements D / 16 * c ... of row s, and their scale
+    uint8_t* const value_lds = reinterpret_cast<uint8_t*>(lds) + wave * kValueBytes<D>;
+    const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
+    const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
+    float* const stat = lds + a.stat_at;
+    float* const final = stat + 2 * kWaves * group;  // kScored: [head] maximum, 1 / sum
+    float* const zs = final + 2 * group;
+
+    // grid: KV heads, sequences, then layers and chunks (first chunks first: the later ones, which short sequences lack, spread
+    // evenly)
+    const int g = blockIdx.x, b = blockIdx.y;
+    const int chunk = kScored ? 0 : blockIdx.z / a.layer_count, layer = kScored ? blockIdx.z : blockIdx.z % a.layer_count;
+    const int lb = layer * d.batch + b, slab = lb * d.hkv + g;
+    const int first = kScored ? 0 : chunk * a.chunk_rows;
+    int row = first + wave * kTile;
+    const scalar_ints table = (scalar_ints)(uintptr_t)(a.cache.table + (size_t)b * d.max_pages);
+    // the first pages of the wave's rows are read beside the length
+    const int last = d.cap - 1;
+    int page[2], page_now[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        page_now[half] = table[min(row + 16 * half, last) >> d.page_shift];
+        page[half] = table[min(row + kStep + 16 * half, last) >> d.page_shift];
+    }
+    const int raw_len = ((scalar_ints)(uintptr_t)a.cache.len)[b];
+    const int len = raw_len < 0 || raw_len > a.n_max ? 0 : raw_len;
+    if (chunk == 0 && threadIdx.x == 0 && len != raw_len) atomicOr(a.faults, kFaultCache);
+    if (first >= len && chunk > 0) return;
+    const int end = kScored ? len : min(len, first + a.chunk_rows);
 
     u32x4 q[kParts][kKey];
     {
@@ -206,16 +234,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_atte
 
     const int key_row = c % 4 * 4 + c / 4;  // row of a half whose keys the lane holds: result rows 4 s + i are rows 4 i + s
     Slab<D> sl{a.cache.pool + q4_record(d, a.layer0 + layer, 0, g),
-               (scalar_ints)(uintptr_t)(a.cache.table + (size_t)b * d.max_pages),
+               table,
                (size_t)d.hkv * d.rec,
                a.bias2 != 0.0f ? a.cache.pos + (size_t)b * d.cap : nullptr,
-               end, d.n_pages, d.page_shift, d.page_rows, d.ks_off, d.vc_off,
+               end, last, d.n_pages, d.page_shift, d.page_rows, d.ks_off, d.vc_off,
                (uint32_t)(key_row * (D / 2) + s * (D / 8)), (uint32_t)(D == 128 ? key_row * 4 + s : key_row * 2 + s / 2), 0};
     const int recent_from = sl.pos ? a.cur_pos[b] - (a.window - 1) : 0;
-    // the lane's places in the wave's LDS: codes of elements D / 16 * c ... of row s, and their scale
-    uint8_t* const value_lds = reinterpret_cast<uint8_t*>(lds) + wave * kValueBytes<D>;
-    const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
-    const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
     float m = -FLT_MAX, l = 0.0f;
     f32x4 acc[kOut];
 #pragma unroll
@@ -225,16 +249,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_atte
     // output is; the page numbers run two tiles ahead.
     Keys<D> keys;
     Place now[2], next[2];
-    int row = first + wave * kTile;
     if (row < end) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) now[half] = sl.place(row + 16 * half, sl.page(row + 16 * half));
+        for (int half = 0; half < 2; ++half) now[half] = sl.place(row + 16 * half, page_now[half]);
         sl.load(keys, now, row);
         sl.load_values(now, value_lds);
     }
-    int page[2] = {sl.page(row + kChunkStep), sl.page(row + kChunkStep + 16)};
-    for (; row < end; row += kChunkStep) {
-        const bool more = row + kChunkStep < end;
+    for (; row < end; row += kStep) {
+        const bool more = row + kStep < end;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tile's keys, and its values in LDS
         // logits
         float z[8];
@@ -254,28 +276,30 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_atte
         if (sl.pos) {
             const uint32_t recent = (uint32_t)__ballot(keys.pos >= recent_from);  // (lanes 32 .. 63: the same rows again)
             if (recent) {
+                const uint32_t mine_recent = recent >> s;
                 asm volatile("");  // (a branch: few tiles hold recent rows)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] += recent >> (16 * (j / 4) + 4 * (j % 4) + s) & 1u ? a.bias2 : 0.0f;
+                for (int j = 0; j < 8; ++j) z[j] += mine_recent & 1u << (16 * (j / 4) + 4 * (j % 4)) ? a.bias2 : 0.0f;
             }
         }
         if (more) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                next[half] = sl.place(row + kChunkStep + 16 * half, page[half]);
-                page[half] = sl.page(row + 2 * kChunkStep + 16 * half);
+                next[half] = sl.place(row + kStep + 16 * half, page[half]);
+                page[half] = sl.page(row + 2 * kStep + 16 * half);
             }
-            sl.load(keys, next, row + kChunkStep);
+            sl.load(keys, next, row + kStep);
         }
         const bool whole = now[0].valid + now[1].valid == kTile;  // (uniform)
         if (!whole) {
             asm volatile("");
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (4 * (j % 4) + s >= now[j / 4].valid) z[j] = -INFINITY;
+                if (4 * (j % 4) >= now[j / 4].valid - s) z[j] = -INFINITY;
         }
-        if (a.z && c < group) {
-            float* zp = a.z + ((size_t)slab * group + c) * a.n_stride + row + 4 * s;  // (row 4 i + s of a half at 4 s + i)
+        if ((kScored || a.z) && c < group) {  // (row 4 i + s of a half at 4 s + i)
+            float* zp = kScored ? zs + c * (a.n_stride + kZPad) + row + 4 * s
+                                         : a.z + ((size_t)slab * group + c) * a.n_stride + row + 4 * s;
             *reinterpret_cast<f32x4*>(zp) = f32x4{z[0], z[1], z[2], z[3]};
             *reinterpret_cast<f32x4*>(zp + 16) = f32x4{z[4], z[5], z[6], z[7]};
         }
@@ -327,7 +351,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_atte
             asm volatile("");
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (4 * (j % 4) + s >= now[j / 4].valid) scale[j] = 1.0f;
+                if (4 * (j % 4) >= now[j / 4].valid - s) scale[j] = 1.0f;
         }
         if (more) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile's values are out of LDS: the next tile's may come
@@ -357,34 +381,54 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_atte
     }
     if (sl.fault && lane == 0) atomicOr(a.faults, sl.fault);
 
-    // the waves joined: columns of LDS, then one thread per four elements of a head
+    // the waves joined: the upper four into the lower, those through columns of LDS, one thread per four elements of a head
     __syncthreads();  // (their values' places are used again)
     l = rows_allsum(l);
-    const int columns = CP * group;
-    float* stat = lds + kWaves * columns * kStride;
-    if (column) {
-        float* out = lds + (wave * columns + c) * kStride + s * (D / 4);
+    float* const mine = lds + ((wave % kJoin) * columns + c) * kStride + s * (D / 4);
+    auto put = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int x = 0; x < kOut; x += 4)
-                *reinterpret_cast<f32x4*>(out + i * kOut + x) = f32x4{acc[x][i], acc[x + 1][i], acc[x + 2][i], acc[x + 3][i]};
+                *reinterpret_cast<f32x4*>(mine + i * kOut + x) = f32x4{acc[x][i], acc[x + 1][i], acc[x + 2][i], acc[x + 3][i]};
         if (s == 0 && part == 0) {
             stat[wave * group + head] = m;
             stat[(kWaves + wave) * group + head] = l;
         }
+    };
+    if constexpr (kWaves > kJoin) {
+        static_assert(kWaves == 2 * kJoin, "one step joins the halves");
+        if (wave >= kJoin && column) put();
+        __syncthreads();
+        if (wave < kJoin && column) {
+            const float m2 = stat[(wave + kJoin) * group + head], l2 = stat[(kWaves + wave + kJoin) * group + head];
+            const float top = fmaxf(m, m2), f = exp2_hw(m - top), f2 = exp2_hw(m2 - top);
+            m = top;
+            l = l * f + l2 * f2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int x = 0; x < kOut; x += 4) {
+                    const f32x4 o = *reinterpret_cast<const f32x4*>(mine + i * kOut + x);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[x + k][i] = acc[x + k][i] * f + o[k] * f2;
+                }
+        }
+        __syncthreads();
     }
+    if (wave < kJoin && column) put();
     __syncthreads();
     const size_t head0 = (size_t)lb * d.hq + g * group;
+    const size_t slot = kScored ? 0 : (size_t)slab * a.nchunk + chunk;
     for (int i = threadIdx.x; i < group * (D / 4); i += kThreads) {
         const int h = i / (D / 4), e = i % (D / 4) * 4;
         float top = stat[h];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, stat[w * group + h]);
+        for (int w = 1; w < kJoin; ++w) top = fmaxf(top, stat[w * group + h]);
         float sum = 0.0f;
         f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < kJoin; ++w) {
             const float f = exp2_hw(stat[w * group + h] - top);
             sum += f * stat[(kWaves + w) * group + h];
             f32x4 x = *reinterpret_cast<const f32x4*>(lds + (w * columns + h) * kStride + e);
@@ -392,62 +436,129 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? Q4_OCC : 3) void q4_atte
             for (int k = 1; k < CP; ++k) x += *reinterpret_cast<const f32x4*>(lds + (w * columns + k * group + h) * kStride + e);
             o += x * f;
         }
-        if (e == 0) a.part[((size_t)slab * a.nchunk + chunk) * group + h] = make_float2(top, sum);
-        if (a.nchunk == 1) {
-            const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        if (kScored || a.nchunk == 1) {
             T* op = static_cast<T*>(a.o) + (head0 + h) * D + e;
 #pragma unroll
             for (int j = 0; j < 4; ++j) Elem<T>::store(op + j, o[j] * inv);
+            if (kScored) {
+                if (e == 0) {
+                    final[2 * h] = top;
+                    final[2 * h + 1] = inv;
+                }
+            } else if (e == 0 && a.stat) {
+                a.stat[(size_t)slab * group + h] = make_float2(top, inv);
+            }
         } else {
-            *reinterpret_cast<f32x4*>(a.opart + (((size_t)slab * a.nchunk + chunk) * group + h) * D + e) = o;
+            *reinterpret_cast<f32x4*>(a.opart + (slot * group + h) * D + e) = o;
+            if (e == 0) a.part[slot * group + h] = make_float2(top, sum);
+        }
+    }
+    if constexpr (kScored) {
+        // the slab's part of the scores: sum over the group of 2^(z - m) / sum, four rows per thread
+        float* rp = a.z + (size_t)slab * a.n_stride;
+        __syncthreads();
+        for (int r = threadIdx.x * 4; r < len; r += kThreads * 4) {
+            f32x4 x{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int h = 0; h < group; ++h) {
+                const f32x4 z = *reinterpret_cast<const f32x4*>(zs + h * (a.n_stride + kZPad) + r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = fmaf(exp2_hw(z[i] - final[2 * h]), final[2 * h + 1], x[i]);
+            }
+            *reinterpret_cast<f32x4*>(rp + r) = x;
         }
     }
 }
 
-// Several chunks: one workgroup per (slab, head) joins their outputs and statistics, and leaves the head's own statistics in
-// the place of its first chunk's.
-constexpr int kJoinThreads = 256;
+// A few chunks: one workgroup per slab joins their outputs and statistics, four elements of a head per thread and all of its
+// loads at once.
+constexpr int kFewChunks = 8, kFewThreads = 256;
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads) void q4_join_few_kernel(Q4AttendArgs a) {
+    const Q4Dims& d = a.dims;
+    const int slab = blockIdx.x, g = slab % d.hkv, lb = slab / d.hkv;
+    const int chunks = max(1, (attended(a, lb % d.batch) + a.chunk_rows - 1) / a.chunk_rows);
+    const size_t slot0 = (size_t)slab * a.nchunk;
+    for (int i = threadIdx.x; i < d.group * (D / 4); i += kFewThreads) {
+        const int h = i / (D / 4), e = i % (D / 4) * 4;
+        float2 p[kFewChunks];
+        f32x4 x[kFewChunks];
+#pragma unroll
+        for (int k = 0; k < kFewChunks; ++k) {
+            const size_t at = (slot0 + min(k, chunks - 1)) * d.group + h;
+            p[k] = a.part[at];
+            if (k < chunks) x[k] = *reinterpret_cast<const f32x4*>(a.opart + at * D + e);
+        }
+        float top = p[0].x, sum = 0.0f;
+#pragma unroll
+        for (int k = 1; k < kFewChunks; ++k) top = fmaxf(top, p[k].x);
+        f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kFewChunks; ++k)
+            if (k < chunks) {
+                const float f = exp2_hw(p[k].x - top);
+                sum += f * p[k].y;
+                o += x[k] * f;
+            }
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        if (e == 0 && a.stat) a.stat[(size_t)slab * d.group + h] = make_float2(top, inv);
+        T* op = static_cast<T*>(a.o) + ((size_t)lb * d.hq + g * d.group + h) * D + e;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) Elem<T>::store(op + j, o[j] * inv);
+    }
+}
+
+// More chunks: one workgroup per (slab, head).
+constexpr int kJoinThreads = 512;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
-    constexpr int kQuads = D / 4, kRows = kJoinThreads / kQuads;
+    constexpr int kQuads = D / 4, kRows = kJoinThreads / kQuads, kWaves = kJoinThreads / kWave, kTogether = 4;
     __shared__ f32x4 red[kRows][kQuads];
-    __shared__ float mx[kJoinThreads / kWave], sm[kJoinThreads / kWave];
+    __shared__ float mx[kWaves], sm[kWaves];
     const Q4Dims& d = a.dims;
-    const int slab = blockIdx.x / d.group, h = blockIdx.x % d.group;
-    const int lb = slab / d.hkv, g = slab % d.hkv;
-    const int n = attended(a, lb % d.batch);
-    const int chunks = max(1, (n + a.chunk_rows - 1) / a.chunk_rows);
-    const size_t at = (size_t)slab * a.nchunk * d.group + h;
+    const int h = blockIdx.x % d.group, slab = blockIdx.x / d.group, g = slab % d.hkv, lb = slab / d.hkv;
+    const int segments = max(1, (attended(a, lb % d.batch) + a.chunk_rows - 1) / a.chunk_rows);
+    const size_t slot0 = (size_t)slab * a.nchunk;
+    auto part = [&](int i) { return a.part[(slot0 + i) * d.group + h]; };
     float top = -FLT_MAX;
-    for (int i = threadIdx.x; i < chunks; i += kJoinThreads) top = fmaxf(top, a.part[at + (size_t)i * d.group].x);
+    for (int i = threadIdx.x; i < segments; i += kJoinThreads) top = fmaxf(top, part(i).x);
     top = wave_max(top);
     if (threadIdx.x % kWave == 0) mx[threadIdx.x / kWave] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / kWave; ++w) top = fmaxf(top, mx[w]);
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mx[w]);
     float sum = 0.0f;
-    for (int i = threadIdx.x; i < chunks; i += kJoinThreads) {
-        const float2 p = a.part[at + (size_t)i * d.group];
+    for (int i = threadIdx.x; i < segments; i += kJoinThreads) {
+        const float2 p = part(i);
         sum += exp2_hw(p.x - top) * p.y;
     }
     sum = wave_sum(sum);
     if (threadIdx.x % kWave == 0) sm[threadIdx.x / kWave] = sum;
     const int quad = threadIdx.x % kQuads, r = threadIdx.x / kQuads;
     f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i = r; i < chunks; i += kRows) {
-        const size_t p = at + (size_t)i * d.group;
-        o += *reinterpret_cast<const f32x4*>(a.opart + p * D + quad * 4) * exp2_hw(a.part[p].x - top);
+    for (int i0 = r; i0 < segments; i0 += kRows * kTogether) {
+        f32x4 x[kTogether];
+        float f[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const int i = min(i0 + k * kRows, segments - 1);
+            x[k] = *reinterpret_cast<const f32x4*>(a.opart + ((slot0 + i) * d.group + h) * D + quad * 4);
+            f[k] = part(i).x;
+        }
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k)
+            if (i0 + k * kRows < segments) o += x[k] * exp2_hw(f[k] - top);
     }
     red[r][quad] = o;
     __syncthreads();
     sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / kWave; ++w) sum += sm[w];
-    if (threadIdx.x == 0) a.part[at] = make_float2(top, sum);
+    for (int w = 0; w < kWaves; ++w) sum += sm[w];
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    if (threadIdx.x == 0 && a.stat) a.stat[(size_t)slab * d.group + h] = make_float2(top, inv);
     if (r != 0) return;
 #pragma unroll
     for (int i = 1; i < kRows; ++i) o += red[i][quad];
-    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
     T* op = static_cast<T*>(a.o) + ((size_t)lb * d.hq + g * d.group + h) * D + quad * 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) Elem<T>::store(op + j, o[j] * inv);
@@ -455,12 +566,13 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
 
 // Scores and their fold: 64 rows of a sequence per workgroup, one a lane.  A wave takes the KV heads slice, slice + per, ... of
 // one layer, kAhead layers at a time (their loads together); the waves' sums of a layer are added in order, and the layers
-// folded in order.
+// folded in order.  kGroups: the scores' parts were summed over each group by the attention.
 constexpr int kScoreWaves = 16, kAhead = 4;
+template <bool kGroups>
 __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendArgs a, int per) {
     __shared__ float part[kAhead][kScoreWaves][kWave];
     const Q4Dims& d = a.dims;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int waves = blockDim.x / kWave, together = waves / per;  // layers that the waves take side by side
     const int blocks = (a.n_max + kWave - 1) / kWave;
     const int b = blockIdx.x / blocks, row = blockIdx.x % blocks * kWave + lane;
@@ -471,31 +583,38 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
     const size_t ub = (size_t)b * d.cap + row;
     float u = wave == 0 && live && a.u_out ? a.u_prior[ub] : 0.0f;
     for (int l0 = 0; l0 < a.layer_count; l0 += together * kAhead) {
+        float s[kAhead];
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            const int l = l0 + q * together + wave / per;
-            float s = 0.0f;
-            if (l < a.layer_count && live)
-                for (int g = wave % per; g < d.hkv; g += per) {
+        for (int q = 0; q < kAhead; ++q) s[q] = 0.0f;
+        if (blockIdx.x % blocks * kWave < n)
+            for (int g = wave % per; g < d.hkv; g += per) {
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) {
+                    const int l = min(l0 + q * together + wave / per, a.layer_count - 1);
                     const size_t slab = (size_t)(l * d.batch + b) * d.hkv + g;
-                    for (int h = 0; h < d.group; ++h) {
-                        const float2 p = a.part[slab * a.nchunk * d.group + h];
-                        const float e = exp2_hw(a.z[(slab * d.group + h) * a.n_stride + at] - p.x);
-                        s += p.y != 0.0f ? e / p.y : 0.0f;
+                    if constexpr (kGroups) {
+                        s[q] += a.z[slab * a.n_stride + at];
+                    } else {
+                        const float* z = a.z + slab * d.group * a.n_stride + at;
+                        const float2* st = a.stat + slab * d.group;
+#pragma unroll 4
+                        for (int h = 0; h < d.group; ++h)
+                            s[q] = fmaf(exp2_hw(z[(size_t)h * a.n_stride] - st[h].x), st[h].y, s[q]);
                     }
                 }
-            part[q][wave][lane] = s;
-        }
+            }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) part[q][wave][lane] = s[q];
         __syncthreads();
         // (wave, layer) pairs: the layer's sum in place of its first slice's
         for (int i = wave; i < together * kAhead; i += waves) {
             const int q = i / together, w0 = i % together * per;
-            float s = part[q][w0][lane];
-            for (int w = 1; w < per; ++w) s += part[q][w0 + w][lane];
-            s *= inv;
-            part[q][w0][lane] = s;
+            float x = part[q][w0][lane];
+            for (int w = 1; w < per; ++w) x += part[q][w0 + w][lane];
+            x *= inv;
+            part[q][w0][lane] = x;
             const int l = l0 + i;
-            if (a.s_out && l < a.layer_count && row < a.n_max) a.s_out[((size_t)l * d.batch + b) * a.n_max + row] = live ? s : 0.0f;
+            if (a.s_out && l < a.layer_count && row < a.n_max) a.s_out[((size_t)l * d.batch + b) * a.n_max + row] = live ? x : 0.0f;
         }
         __syncthreads();
         if (wave == 0)
@@ -506,16 +625,31 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
     if (wave == 0 && live && a.u_out) a.u_out[ub] = u;
 }
 
+template <typename T, int D, int CP, int NM, bool kScored>
+hipError_t launch_form(Q4AttendArgs a, hipStream_t s) {
+    constexpr int kWaves = waves_of<T>(kScored), kJoin = kWaves > 4 ? 4 : kWaves;
+    const int slabs = a.layer_count * a.dims.batch * a.dims.hkv;
+    const int joined = kJoin * a.dims.group * CP * (D + 4) * (int)sizeof(float), values = kWaves * kValueBytes<D>;
+    a.stat_at = (joined > values ? joined : values) / (int)sizeof(float);
+    size_t lds = (size_t)a.stat_at * sizeof(float) + 2 * (kWaves + 1) * a.dims.group * sizeof(float);
+    auto kern = q4_attend_kernel<T, D, CP, NM, kScored>;
+    if (kScored) {
+        lds += (size_t)a.dims.group * (a.n_stride + kZPad) * sizeof(float);
+        static std::atomic<bool> raised[kMaxDevices];
+        const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), raised);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kern, dim3(a.dims.hkv, a.dims.batch, a.layer_count * (kScored ? 1 : a.nchunk)), dim3(kWave * kWaves), lds, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || kScored || a.nchunk == 1) return e;
+    if (a.nchunk <= kFewChunks) hipLaunchKernelGGL((q4_join_few_kernel<T, D>), dim3(slabs), dim3(kFewThreads), 0, s, a);
+    else hipLaunchKernelGGL((q4_join_kernel<T, D>), dim3(slabs * a.dims.group), dim3(kJoinThreads), 0, s, a);
+    return hipGetLastError();
+}
+
 template <typename T, int D, int CP, int NM>
 hipError_t launch_attend(const Q4AttendArgs& a, hipStream_t s) {
-    const int slabs = a.layer_count * a.dims.batch * a.dims.hkv;
-    const size_t joined = (size_t)kWaves * a.dims.group * (CP * (D + 4) + 2) * sizeof(float);
-    const size_t lds = joined > (size_t)kWaves * kValueBytes<D> ? joined : (size_t)kWaves * kValueBytes<D>;
-    hipLaunchKernelGGL((q4_attend_kernel<T, D, CP, NM>), dim3(slabs * a.nchunk), dim3(kThreads), lds, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.nchunk == 1) return e;
-    hipLaunchKernelGGL((q4_join_kernel<T, D>), dim3(slabs * a.dims.group), dim3(kJoinThreads), 0, s, a);
-    return hipGetLastError();
+    return a.scored ? launch_form<T, D, CP, NM, true>(a, s) : launch_form<T, D, CP, NM, false>(a, s);
 }
 
 // Columns of the parts of a probability: as many as fit beside each other.
@@ -528,16 +662,23 @@ hipError_t launch_by_group(const Q4AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int q4_attend_chunks(int slabs, int n) {
-    const int want = (kTargetWgs + slabs - 1) / slabs, by_rows = (n + kMinRows - 1) / kMinRows;
-    return want < by_rows ? want : by_rows;
-}
-
-void q4_attend_plan(int slabs, int n, int* nchunk, int* chunk_rows) {
-    const int chunks = q4_attend_chunks(slabs, n);
-    const int rows = (n + chunks - 1) / chunks;
-    *chunk_rows = (rows + kChunkStep - 1) / kChunkStep * kChunkStep;
-    *nchunk = (n + *chunk_rows - 1) / *chunk_rows;
+Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool scores) {
+    Q4AttendPlan p{};
+    const int slabs = layer_count * d.batch * d.hkv;
+    const int waves = d.bf16 ? Q4_WAVES : Q4_WAVES32, step = waves * kTile;
+    p.n_stride = (n_max + 63) / 64 * 64;
+    const int want = (256 * Q4_PER_CU / waves + slabs - 1) / slabs, by_rows = (n_max + step - 1) / step;
+    p.most = want < by_rows ? want : by_rows;
+    const int least = (n_max + kMostRows - 1) / kMostRows;
+    if (least > p.most) p.most = least;
+    p.chunk_rows = ((n_max + p.most - 1) / p.most + step - 1) / step * step;
+    p.nchunk = (n_max + p.chunk_rows - 1) / p.chunk_rows;
+    // a workgroup of eight waves with its logits: two of them on a CU
+    const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
+    const size_t outputs = 4 * (size_t)d.group * (d.bf16 ? (d.group <= 8 ? 2 : 1) : d.group <= 5 ? 3 : 1) * (d.d + 4) * sizeof(float);
+    const size_t scored = (values > outputs ? values : outputs) + (size_t)d.group * (18 + p.n_stride + kZPad) * sizeof(float);
+    p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 512;
+    return p;
 }
 
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
@@ -548,7 +689,8 @@ hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
     while (per < a.dims.hkv && per < kScoreWaves) per *= 2;
     while (waves < per * a.layer_count && waves < kScoreWaves) waves *= 2;
     const int blocks = (a.n_max + kWave - 1) / kWave;
-    hipLaunchKernelGGL(q4_score_kernel, dim3(a.dims.batch * blocks), dim3(waves * kWave), 0, s, a, per);
+    hipLaunchKernelGGL((a.scored ? q4_score_kernel<true> : q4_score_kernel<false>), dim3(a.dims.batch * blocks),
+                       dim3(waves * kWave), 0, s, a, per);
     return hipGetLastError();
 }
 

@@ -35,7 +35,7 @@ def call(name, *args, s=None, c=None, ws=FAKE, ws_bytes=BIG):
     (dict(head_dim=96), UNSUPPORTED), (dict(n_q_heads=7), INVALID), (dict(n_q_heads=34), UNSUPPORTED), (dict(batch=0), INVALID),
     (dict(layers=257), UNSUPPORTED), (dict(page_rows=24), UNSUPPORTED), (dict(page_rows=8), UNSUPPORTED),
     (dict(page_rows=512), UNSUPPORTED), (dict(n_pages=0), INVALID), (dict(max_pages=0), INVALID), (dict(dtype=5), UNSUPPORTED),
-    (dict(max_pages=1 << 23), UNSUPPORTED), (dict(batch=1 << 20, max_pages=1 << 10), UNSUPPORTED)])
+    (dict(max_pages=1 << 23), UNSUPPORTED), (dict(batch=1 << 15, max_pages=1 << 12), UNSUPPORTED), (dict(batch=65536), UNSUPPORTED)])
 def test_shapes(kw, status):
     for query in (lambda s: B.kv_q4_pool_bytes(s), lambda s: B.kv_q4_workspace_bytes(s, 10, 1)):
         with pytest.raises(B.KVError) as e:
