@@ -24,43 +24,45 @@ __device__ __forceinline__ uint32_t dpp_u(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
 }
 
-// One row of the cache, for the lanes that hold it: where it lies, or page < 0 (none).
-struct RowAt {
-    int page, row;
-};
-
-// Cached row first + r of sequence b: `wanted` where r < count; a page only where the row exists.
-__device__ __forceinline__ RowAt locate(const Q4RowArgs& a, int b, int r, bool* wanted, uint32_t* fault) {
-    const Q4Dims& d = a.dims;
-    const int count = a.count ? a.count[b] : a.rows;
-    *wanted = r < count;
-    RowAt at{-1, 0};
-    if (!*wanted) return at;
-    const int len = a.cache.len[b];
-    const int64_t row = (int64_t)(a.first ? a.first[b] : (int64_t)len - count) + r;
-    if (row < 0 || row >= len || row >= d.cap) {
-        *fault |= kFaultCache;
-        return at;
-    }
-    const int page = a.cache.table[(size_t)b * d.max_pages + (int)(row >> d.page_shift)];
-    if ((uint32_t)page >= (uint32_t)d.n_pages) {
-        *fault |= kFaultCache;
-        return at;
-    }
-    at.page = page;
-    at.row = (int)row & (d.page_rows - 1);
-    return at;
-}
-
-// Work item `i` of a call: row r of (layer l, sequence b, KV head g), rows fastest.
+// A work item: row r of (layer l, sequence b, KV head g), rows fastest, and where it lies in the cache.
 struct Item {
     int l, b, g, r;
+    bool wanted;     // r < count
+    int page, row;   // page < 0: the cache has no such row
 };
-__device__ __forceinline__ Item item_of(const Q4RowArgs& a, uint32_t i) {
-    const uint32_t slab = i / (uint32_t)a.rows;
-    const uint32_t lb = slab / (uint32_t)a.dims.hkv;
-    return {(int)(lb / (uint32_t)a.dims.batch), (int)(lb % (uint32_t)a.dims.batch), (int)(slab % (uint32_t)a.dims.hkv),
-            (int)(i % (uint32_t)a.rows)};
+
+// Items first, first + step, ... of a thread, located together: their loads in flight at once (items past the last one repeat
+// it, and are not wanted).
+template <int N>
+__device__ __forceinline__ uint32_t locate(const Q4RowArgs& a, uint32_t first, uint32_t step, uint32_t items, Item (&it)[N]) {
+    const Q4Dims& d = a.dims;
+    uint32_t fault = 0;
+    int count[N], len[N], from[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint32_t i = min(first + k * step, items - 1);
+        const uint32_t slab = i / (uint32_t)a.rows, lb = slab / (uint32_t)d.hkv;
+        it[k].r = (int)(i - slab * (uint32_t)a.rows);
+        it[k].g = (int)(slab - lb * (uint32_t)d.hkv);
+        it[k].l = (int)(lb / (uint32_t)d.batch);
+        it[k].b = (int)(lb - (uint32_t)it[k].l * (uint32_t)d.batch);
+        count[k] = a.count ? a.count[it[k].b] : a.rows;
+        len[k] = a.cache.len[it[k].b];
+        from[k] = a.first ? a.first[it[k].b] : 0;
+        it[k].wanted = first + k * step < items;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        it[k].wanted = it[k].wanted && it[k].r < count[k];
+        const int64_t row = (a.first ? (int64_t)from[k] : (int64_t)len[k] - count[k]) + it[k].r;
+        const bool in = row >= 0 && row < len[k] && row < d.cap;
+        const int page = a.cache.table[(size_t)it[k].b * d.max_pages + (in ? (int)(row >> d.page_shift) : 0)];
+        const bool ok = in && (uint32_t)page < (uint32_t)d.n_pages;
+        it[k].page = ok ? page : -1;
+        it[k].row = (int)row & (d.page_rows - 1);
+        if (it[k].wanted && !ok) fault |= kFaultCache;
+    }
+    return fault;
 }
 __device__ __forceinline__ size_t source_of(const Item& it, const int64_t (&s)[4]) {
     return (size_t)(it.l * s[0] + it.b * s[1] + it.g * s[2] + it.r * s[3]);
@@ -69,9 +71,10 @@ __device__ __forceinline__ size_t source_of(const Item& it, const int64_t (&s)[4
 template <typename T>
 __device__ __forceinline__ void read8(const T* p, float (&x)[kElems]) {
     if constexpr (sizeof(T) == 2) {
-        Elem<bf16_t>::unpack(*reinterpret_cast<const u32x4*>(p), x);
+        Elem<bf16_t>::unpack(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)), x);
     } else {
-        const f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
+        const f32x4 lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+        const f32x4 hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] = lo[i];
@@ -101,46 +104,52 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[kElems], uint32_t*
     return finite ? w : 0u;
 }
 
-template <typename T, int D>
+// kItems: rows of keys and of values per lane, their loads together.  Two where that still leaves two workgroups for every CU,
+// else one: one layer of 8 sequences of 8 KV heads x 5,000 .. 8,192 rows of bf16, stored and loaded, took 136 us with one, 124
+// with two and 131 with four, a decode step's rows of 32 such layers 6.9 us with one and 7.9 with two.  The dense side passes the
+// caches by (137 us for the former where nothing does); the pool's side does not, as what is stored is read next (107 us, 5.3
+// TB/s of what has to move, a large copy 4.9; the 124 above are with the pool's reads past the caches as well).
+template <typename T, int D, int kItems>
 __global__ __launch_bounds__(kThreads) void q4_store_kernel(Q4RowArgs a, uint32_t items) {
-    constexpr int kLanes = D / kElems;  // lanes per row
+    constexpr int kLanes = D / kElems, kRows = kThreads / kLanes;  // lanes per row, rows side by side
     const int p = threadIdx.x % kLanes;
-    const uint32_t i = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
-    if (i >= items) return;  // (whole rows of lanes)
-    const Item it = item_of(a, i);
-    bool wanted;
-    uint32_t fault = 0;
-    RowAt at = locate(a, it.b, it.r, &wanted, &fault);
-    if (at.page >= 0) {
-        const int refs = a.cache.refs[at.page];
-        if (refs != 1) {
-            fault |= refs > 1 ? kFaultSharedPage : kFaultCache;
-            at.page = -1;
+    const uint32_t first = blockIdx.x * (kRows * kItems) + threadIdx.x / kLanes;
+    if (first >= items) return;  // (whole rows of lanes)
+    Item it[kItems];
+    uint32_t fault = locate(a, first, kRows, items, it);
+    int refs[kItems];
+    float x[kItems][2][kElems];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        refs[k] = it[k].page >= 0 ? a.cache.refs[it[k].page] : 1;
+        if (!it[k].wanted) continue;
+        read8(static_cast<const T*>(a.k) + source_of(it[k], a.ks) + p * kElems, x[k][0]);
+        read8(static_cast<const T*>(a.v) + source_of(it[k], a.vs) + p * kElems, x[k][1]);
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        if (it[k].wanted && refs[k] != 1) fault |= refs[k] > 1 ? kFaultSharedPage : kFaultCache;
+        if (!it[k].wanted || it[k].page < 0 || refs[k] != 1) continue;
+        uint8_t* rec = a.cache.pool + q4_record(a.dims, a.layer0 + it[k].l, it[k].page, it[k].g);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            uint32_t byte;
+            const uint32_t codes = quantise(x[k][which], &byte);
+            // the row's scale bytes gathered by its lanes, one store for them
+            uint32_t word = byte << 8 * (p / 4);
+            word |= dpp_u<kMirror8>(word);
+            uint8_t* c = rec + (which ? a.dims.vc_off : 0);
+            uint8_t* e = rec + (which ? a.dims.vs_off : a.dims.ks_off);
+            reinterpret_cast<uint32_t*>(c + it[k].row * (D / 2))[p] = codes;
+            if constexpr (D == 128) {
+                word |= dpp_u<kRor8>(word);
+                if (p == 0) reinterpret_cast<uint32_t*>(e)[it[k].row] = word;
+            } else {
+                if (p == 0) reinterpret_cast<uint16_t*>(e)[it[k].row] = (uint16_t)word;
+            }
         }
     }
     if (fault && p == 0) atomicOr(a.faults, fault);
-    if (at.page < 0) return;
-    uint8_t* rec = a.cache.pool + q4_record(a.dims, a.layer0 + it.l, at.page, it.g);
-    float xk[kElems], xv[kElems];
-    read8(static_cast<const T*>(a.k) + source_of(it, a.ks) + p * kElems, xk);
-    read8(static_cast<const T*>(a.v) + source_of(it, a.vs) + p * kElems, xv);
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        uint32_t byte;
-        const uint32_t codes = quantise(which ? xv : xk, &byte);
-        // the row's scale bytes gathered by its lanes, one store for them
-        uint32_t word = byte << 8 * (p / 4);
-        word |= dpp_u<kMirror8>(word);
-        uint8_t* c = rec + (which ? a.dims.vc_off : 0);
-        uint8_t* e = rec + (which ? a.dims.vs_off : a.dims.ks_off);
-        reinterpret_cast<uint32_t*>(c + at.row * (D / 2))[p] = codes;
-        if constexpr (D == 128) {
-            word |= dpp_u<kRor8>(word);
-            if (p == 0) reinterpret_cast<uint32_t*>(e)[at.row] = word;
-        } else {
-            if (p == 0) reinterpret_cast<uint16_t*>(e)[at.row] = (uint16_t)word;
-        }
-    }
 }
 
 // 8 codes and their scale as 8 bf16 (exact)
@@ -154,64 +163,71 @@ __device__ __forceinline__ u32x4 expand(uint32_t codes, uint32_t byte) {
     return r;
 }
 
-template <typename T, int D>
+template <typename T, int D, int kItems>
 __global__ __launch_bounds__(kThreads) void q4_load_kernel(Q4RowArgs a, uint32_t items) {
-    constexpr int kLanes = D / kElems;
+    constexpr int kLanes = D / kElems, kRows = kThreads / kLanes;
     const int p = threadIdx.x % kLanes;
-    const uint32_t i = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
-    if (i >= items) return;
-    const Item it = item_of(a, i);
-    bool wanted;
-    uint32_t fault = 0;
-    const RowAt at = locate(a, it.b, it.r, &wanted, &fault);
+    const uint32_t first = blockIdx.x * (kRows * kItems) + threadIdx.x / kLanes;
+    if (first >= items) return;
+    Item it[kItems];
+    const uint32_t fault = locate(a, first, kRows, items, it);
     if (fault && p == 0) atomicOr(a.faults, fault);
-    if (!wanted) return;
-    uint32_t codes[2] = {0, 0}, byte[2] = {127, 127};  // a row that is not there: zeros
-    if (at.page >= 0) {
-        const uint8_t* rec = a.cache.pool + q4_record(a.dims, a.layer0 + it.l, at.page, it.g);
+    uint32_t codes[kItems][2], byte[kItems][2];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const uint8_t* rec = a.cache.pool + q4_record(a.dims, a.layer0 + it[k].l, max(it[k].page, 0), it[k].g);
+        const int row = it[k].page < 0 ? 0 : it[k].row;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            codes[which] = reinterpret_cast<const uint32_t*>(rec + (which ? a.dims.vc_off : 0) + at.row * (D / 2))[p];
-            byte[which] = rec[(which ? a.dims.vs_off : a.dims.ks_off) + at.row * (D / 32) + p / 4];
+            codes[k][which] = reinterpret_cast<const uint32_t*>(rec + (which ? a.dims.vc_off : 0) + row * (D / 2))[p];
+            byte[k][which] = rec[(which ? a.dims.vs_off : a.dims.ks_off) + row * (D / 32) + p / 4];
         }
     }
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        T* out = static_cast<T*>(which ? a.v_out : a.k_out) + source_of(it, which ? a.vs : a.ks) + p * kElems;
-        const u32x4 x = expand(codes[which], byte[which]);
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<u32x4*>(out) = x;
-        } else {
-            float f[kElems];
-            Elem<bf16_t>::unpack(x, f);
-            reinterpret_cast<f32x4*>(out)[0] = f32x4{f[0], f[1], f[2], f[3]};
-            reinterpret_cast<f32x4*>(out)[1] = f32x4{f[4], f[5], f[6], f[7]};
+    for (int k = 0; k < kItems; ++k) {
+        if (!it[k].wanted) continue;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            T* out = static_cast<T*>(which ? a.v_out : a.k_out) + source_of(it[k], which ? a.vs : a.ks) + p * kElems;
+            // (a row that is not there: zeros)
+            const u32x4 x = it[k].page < 0 ? u32x4{0, 0, 0, 0} : expand(codes[k][which], byte[k][which]);
+            if constexpr (sizeof(T) == 2) {
+                __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(out));
+            } else {
+                float f[kElems];
+                Elem<bf16_t>::unpack(x, f);
+                __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(out));
+                __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(out) + 1);
+            }
         }
     }
+}
+
+template <typename T, int D, int kItems>
+hipError_t launch_rows(const Q4RowArgs& a, uint32_t items, hipStream_t s) {
+    constexpr uint32_t per = kThreads * kElems / D * kItems;
+    const dim3 grid((items + per - 1) / per), block(kThreads);
+    if (a.k_out) hipLaunchKernelGGL((q4_load_kernel<T, D, kItems>), grid, block, 0, s, a, items);
+    else hipLaunchKernelGGL((q4_store_kernel<T, D, kItems>), grid, block, 0, s, a, items);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_by_rows(const Q4RowArgs& a, hipStream_t s) {
+    const uint32_t items = (uint32_t)a.layer_count * a.dims.batch * a.dims.hkv * a.rows;
+    const int cus = device_cus() > 0 ? device_cus() : 256;
+    return items >= (uint32_t)(2 * cus) * (kThreads * kElems / D * 2) ? launch_rows<T, D, 2>(a, items, s)
+                                                                      : launch_rows<T, D, 1>(a, items, s);
+}
+
+hipError_t launch(const Q4RowArgs& a, hipStream_t s) {
+    if (a.dims.bf16) return a.dims.d == 128 ? launch_by_rows<bf16_t, 128>(a, s) : launch_by_rows<bf16_t, 64>(a, s);
+    return a.dims.d == 128 ? launch_by_rows<float, 128>(a, s) : launch_by_rows<float, 64>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_q4_store(const Q4RowArgs& a, hipStream_t s) {
-    const uint32_t items = (uint32_t)a.layer_count * a.dims.batch * a.dims.hkv * a.rows;
-    const uint32_t per = kThreads * kElems / a.dims.d;
-    const dim3 grid((items + per - 1) / per), block(kThreads);
-    if (a.dims.bf16)
-        hipLaunchKernelGGL((a.dims.d == 128 ? q4_store_kernel<bf16_t, 128> : q4_store_kernel<bf16_t, 64>), grid, block, 0, s, a, items);
-    else
-        hipLaunchKernelGGL((a.dims.d == 128 ? q4_store_kernel<float, 128> : q4_store_kernel<float, 64>), grid, block, 0, s, a, items);
-    return hipGetLastError();
-}
-
-hipError_t launch_q4_load(const Q4RowArgs& a, hipStream_t s) {
-    const uint32_t items = (uint32_t)a.layer_count * a.dims.batch * a.dims.hkv * a.rows;
-    const uint32_t per = kThreads * kElems / a.dims.d;
-    const dim3 grid((items + per - 1) / per), block(kThreads);
-    if (a.dims.bf16)
-        hipLaunchKernelGGL((a.dims.d == 128 ? q4_load_kernel<bf16_t, 128> : q4_load_kernel<bf16_t, 64>), grid, block, 0, s, a, items);
-    else
-        hipLaunchKernelGGL((a.dims.d == 128 ? q4_load_kernel<float, 128> : q4_load_kernel<float, 64>), grid, block, 0, s, a, items);
-    return hipGetLastError();
-}
+hipError_t launch_q4_store(const Q4RowArgs& a, hipStream_t s) { return launch(a, s); }
+hipError_t launch_q4_load(const Q4RowArgs& a, hipStream_t s) { return launch(a, s); }
 
 }  // namespace ikv
