@@ -95,7 +95,7 @@ struct Q4PageScratch {
     int32_t* moves;     // [batch] compaction: entries of dst / src
     int32_t* fresh;     // [n_pages] the lowest free pages, ascending
     int32_t* dst;       // [batch][n_max] rows written ...
-    int32_t* src;       // [batch][n_max] ... and the rows that they come from
+    int32_t* src;       // [batch][n_max] ... and the rows that they come from, or -1 - i: the i-th of `from`
     int32_t* from;      // [batch][n_max] kept rows behind the new end, ascending
     int32_t* rank;      // [batch][max_pages] page of dst replaced by the sequence's rank-th fresh page, or -1
     int32_t* old_table; // [batch][max_pages]
