@@ -92,13 +92,15 @@ struct Q4PageScratch {
     int32_t* offset;    // [batch] first of them in `fresh`, or -1: not granted
     int32_t* source;    // [batch] reserve: page to be copied, or -1
     int32_t* rows;      // [batch] reserve: rows added; compaction: rows kept (-1: the sequence is left alone)
-    int32_t* moves;     // [batch] compaction: entries of dst / src
+    int32_t* moves;     // [batch] reserve: rows of `source` in use; compaction: holes
     int32_t* fresh;     // [n_pages] the lowest free pages, ascending
-    int32_t* dst;       // [batch][n_max] rows written ...
-    int32_t* src;       // [batch][n_max] ... and the rows that they come from, or -1 - i: the i-th of `from`
-    int32_t* from;      // [batch][n_max] kept rows behind the new end, ascending
-    int32_t* rank;      // [batch][max_pages] page of dst replaced by the sequence's rank-th fresh page, or -1
+    int32_t* dst;       // [batch][n_max] holes before the new end, ascending, ...
+    int32_t* src;       // [batch][n_max] ... and the kept rows behind it that fill them
+    int32_t* rank;      // [batch][max_pages] a page's number among those replaced (by the sequence's fresh pages), or -1
+    int32_t* replaced;  // [batch][max_pages] the pages replaced
     int32_t* old_table; // [batch][max_pages]
+    uint64_t* mask;     // [batch][ceil(n_max / 64)] a bit for every row that stays
+    int32_t* prefix;    // [batch][ceil(n_max / 64)] kept rows before each word's
 };
 struct Q4PageArgs {
     Q4Dims dims;

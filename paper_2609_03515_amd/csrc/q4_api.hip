@@ -93,8 +93,11 @@ size_t page_layout(const Q4Dims& d, int n_max, void* ws, Q4PageScratch* out) {
     if (n_max > 0) {
         w.dst = take((size_t)d.batch * n_max);
         w.src = take((size_t)d.batch * n_max);
-        w.from = take((size_t)d.batch * n_max);
         w.rank = take((size_t)d.batch * d.max_pages);
+        w.replaced = take((size_t)d.batch * d.max_pages);
+        const size_t words = d.batch * (((size_t)n_max + 63) / 64);
+        w.mask = reinterpret_cast<uint64_t*>(take(2 * words));
+        w.prefix = take(words);
         w.old_table = take((size_t)d.batch * d.max_pages);
     }
     if (out) *out = w;

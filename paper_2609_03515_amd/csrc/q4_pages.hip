@@ -7,6 +7,7 @@
 // A call that allocates runs in launches on the caller's stream: what each sequence needs, the pages for it (one workgroup),
 // and the change itself, spread over sequences and layers.  The last one reads what the others wrote in the scratch, never
 // the table or the lengths that its own workgroups change.
+#include <atomic>
 #include <type_traits>
 
 #include "kv_common.h"
@@ -172,6 +173,7 @@ __global__ __launch_bounds__(kMoveThreads) void q4_reserve_kernel(Q4PageArgs a) 
         __shared__ float prior;
         double x = a.init_mode == 2 ? (double)INFINITY : 0.0;
         if (a.init_mode != 0)
+#pragma unroll 8
             for (int i = threadIdx.x; i < len; i += kMoveThreads) x = a.init_mode == 1 ? x + u[i] : fmin(x, (double)u[i]);
 #pragma unroll
         for (int o = kWave / 2; o >= 1; o >>= 1) {
@@ -232,8 +234,10 @@ __global__ __launch_bounds__(kThreads) void q4_fork_kernel(Q4PageArgs a) {
         if (j < pages) atomicAdd(&a.cache.refs[page], 1);
     }
     if (a.cache.u)
+#pragma unroll 8
         for (int j = threadIdx.x; j < len; j += kThreads) a.cache.u[(size_t)dst * d.cap + j] = a.cache.u[(size_t)src * d.cap + j];
     if (a.cache.pos)
+#pragma unroll 8
         for (int j = threadIdx.x; j < len; j += kThreads) a.cache.pos[(size_t)dst * d.cap + j] = a.cache.pos[(size_t)src * d.cap + j];
     if (threadIdx.x == 0) a.cache.len[dst] = len;
 }
@@ -271,44 +275,26 @@ __global__ __launch_bounds__(kMoveThreads) void q4_free_kernel(Q4PageArgs a) {
 
 // ---- compaction ---------------------------------------------------------------------------------------------
 
-// Eviction order as one number: larger stays.  Larger utility first, then the lower position.
-__device__ __forceinline__ uint64_t rank_key(float u, int pos) { return (uint64_t)float_key(u) << 32 | (uint32_t)~pos; }
-
-// The rows of a thread, `per` consecutive ones, their keys in registers (up to R of them) or read again (R = 0).
-template <int R, int kBlock>
-struct Rows {
+// Eviction order as one number, larger stays: the utility's key, then (the lower position first) the position's complement.
+// The rows of a sequence that a selection looks at: their utilities' keys, in LDS where they fit.
+struct Ranked {
     const float* u;
     const int32_t* pos;
-    int n, per, first;
-    uint64_t key[R > 0 ? R : 1];
-    __device__ __forceinline__ Rows(const float* u_, const int32_t* pos_, int n_)
-        : u(u_), pos(pos_), n(n_), per((n_ + kBlock - 1) / kBlock), first((int)threadIdx.x * per) {
-        if constexpr (R > 0)
-#pragma unroll
-            for (int j = 0; j < R; ++j) key[j] = j < per && first + j < n ? rank_key(u[first + j], pos[first + j]) : 0;
-    }
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {  // f(place, key, exists); every thread makes as many calls
-        if constexpr (R > 0) {
-#pragma unroll
-            for (int j = 0; j < R; ++j)
-                if (j < per) f(j, key[j], first + j < n);
-        } else {
-            for (int j = 0; j < per; ++j) {
-                const int i = first + j;
-                f(j, i < n ? rank_key(u[i], pos[i]) : 0, i < n);
-            }
-        }
-    }
+    const uint32_t* keys;  // nullable
+    int n;
+    __device__ __forceinline__ uint32_t key(int i) const { return keys ? keys[i] : float_key(u[i]); }
+    __device__ __forceinline__ uint64_t full(int i) const { return (uint64_t)key(i) << 32 | (uint32_t)~pos[i]; }
 };
 
-// The smallest key above `last`, over the workgroup.
-template <int R, int kBlock>
-__device__ uint64_t next_key(const Rows<R, kBlock>& rows, uint64_t last, uint64_t* lds /* waves */) {
+// The smallest full key above `last`, over the workgroup.
+template <int kBlock>
+__device__ uint64_t next_key(const Ranked& rows, uint64_t last, uint64_t* lds /* waves */) {
     uint64_t best = ~0ull;
-    rows.each([&](int, uint64_t key, bool exists) __attribute__((always_inline)) {
-        if (exists && key > last && key < best) best = key;
-    });
+#pragma unroll 4
+    for (int i = threadIdx.x; i < rows.n; i += kBlock) {
+        const uint64_t key = rows.full(i);
+        if (key > last && key < best) best = key;
+    }
 #pragma unroll
     for (int o = kWave / 2; o >= 1; o >>= 1) {
         const uint64_t y = __shfl_xor((unsigned long long)best, o, kWave);
@@ -322,29 +308,50 @@ __device__ uint64_t next_key(const Rows<R, kBlock>& rows, uint64_t last, uint64_
     return best;
 }
 
-// The `budget`-th largest key of n > budget >= 1 rows: radix selection from the highest byte, each pass a histogram of the
-// rows that share the bytes chosen so far, until a byte's rows all stay.  Every thread gets it.
-template <int R, int kBlock>
-__device__ uint64_t nth_key(const Rows<R, kBlock>& rows, int budget, int* hist /* 256 */, int* lds) {
-    __shared__ uint64_t chosen;
+// The `budget`-th largest full key of n > budget >= 1 rows, or a lower one with as many rows at least as large: radix
+// selection from the highest byte, each pass a histogram of the rows that share the bytes chosen so far, until a byte's rows
+// all stay.  Positions are looked at only where utilities tie across the border.  Every thread gets it.
+template <int kBlock>
+__device__ uint64_t nth_key(const Ranked& rows, int budget, int* hist /* 256 */, int* lds) {
+    __shared__ uint32_t digit_s;
     __shared__ int left_s, done_s;
-    uint64_t prefix = 0, mask = 0;
+    uint32_t high = 0, low = 0, mask = 0;  // of utility and position: the bytes chosen, and which they are
     int left = budget;
-    for (int shift = 56; shift >= 0; shift -= 8) {
+    for (int pass = 0; pass < 8; ++pass) {
+        const int shift = 24 - pass % 4 * 8;
+        if (pass == 4) mask = 0;
         if (threadIdx.x < 256) hist[threadIdx.x] = 0;
         __syncthreads();
-        rows.each([&](int, uint64_t key, bool exists) __attribute__((always_inline)) {
-            if (!exists || (key & mask) != prefix) return;
-            // utilities share their leading bits: a wave whose rows agree counts once
-            const int digit = (int)(key >> shift) & 255;
-            const int first = __builtin_amdgcn_readfirstlane(digit);
-            const uint64_t live = __ballot(1);
-            if (__ballot(digit == first) == live) {
-                if ((int)(threadIdx.x % kWave) == __ffsll((unsigned long long)live) - 1) atomicAdd(&hist[first], __popcll(live));
-            } else {
-                atomicAdd(&hist[digit], 1);
+        auto digit_of = [&](int i, int* digit) __attribute__((always_inline)) {  // and whether the row is still looked at
+            uint32_t key = rows.key(i);
+            bool in = (key & (pass < 4 ? mask : ~0u)) == high;
+            if (pass >= 4 && in) {
+                key = ~rows.pos[i];
+                in = (key & mask) == low;
             }
-        });
+            *digit = (int)(key >> shift) & 255;
+            return in;
+        };
+        if (pass == 0) {
+            // utilities share their leading bits: the rows of a wave that agree with its first one count once
+            for (int i0 = 0; i0 < rows.n; i0 += kBlock) {
+                const int i = i0 + (int)threadIdx.x;
+                int digit = 0;
+                const bool in = i < rows.n && digit_of(i, &digit);
+                const uint64_t live = __ballot(in);
+                if (!live) continue;
+                const int lead = __ffsll((unsigned long long)live) - 1, first = __builtin_amdgcn_readlane(digit, lead);
+                const uint64_t same = __ballot(in && digit == first);
+                if (in && digit != first) atomicAdd(&hist[digit], 1);
+                if ((int)(threadIdx.x % kWave) == lead) atomicAdd(&hist[first], __popcll(same));
+            }
+        } else {
+#pragma unroll 4
+            for (int i = threadIdx.x; i < rows.n; i += kBlock) {
+                int digit;
+                if (digit_of(i, &digit)) atomicAdd(&hist[digit], 1);
+            }
+        }
         __syncthreads();
         // the byte that holds the left-th row from the top: threads 0 .. 255 hold the digits from 255 down
         const int digit = 255 - (int)threadIdx.x;
@@ -352,46 +359,61 @@ __device__ uint64_t nth_key(const Rows<R, kBlock>& rows, int budget, int* hist /
         int total;
         const int above = block_scan<kBlock / kWave>(c, &total, lds);
         if (threadIdx.x < 256 && above < left && above + c >= left) {
-            chosen = prefix | (uint64_t)digit << shift;
+            digit_s = (uint32_t)digit << shift;
             left_s = left - above;
             done_s = c == left - above;
         }
         __syncthreads();
-        prefix = chosen;
+        if (pass < 4) high |= digit_s;
+        else low |= digit_s;
         left = left_s;
-        mask |= (uint64_t)255 << shift;
+        mask |= 255u << shift;
         if (done_s) break;  // every row that shares these bytes stays
     }
-    return prefix;
+    return (uint64_t)high << 32 | low;
 }
 
-// Workgroup b: what sequence b keeps, the rows that are written (holes, and every kept row of a shared page with a hole),
-// and the pages wanted.  Threads hold consecutive rows, so that one prefix sum of the kept rows, K(i) of them before row i,
-// numbers everything: a dropped row i before the new end is hole i - K(i), a kept row behind it the (K(i) - K(end))-th that moves.
-constexpr int kFewEvicted = 4;  // so few are found one after the other
-template <bool kEvict, int R, int kBlock>
+// Workgroup b: what sequence b keeps, the rows that move, the shared pages that are replaced, and the pages wanted.
+// With K(i) the kept rows before row i, from one mask bit a row and the masks' prefix sums: a dropped row i before the new end
+// is hole i - K(i), a kept row behind it the (K(i) - K(end))-th that moves, and a page has a hole when its rows number more than
+// K grows over it.
+constexpr int kFewEvicted = 4;      // so few are found one after the other
+constexpr int kKeysInLds = 32768, kWordsInLds = 2048;  // rows, and words of 64 of them
+template <bool kEvict, int kBlock>
 __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     constexpr int kWaves = kBlock / kWave;
     __shared__ int lds[kWaves + 1];
     __shared__ uint64_t lds64[kWaves];
     __shared__ int hist[256];
+    extern __shared__ uint64_t dynamic[];  // masks and their prefix sums, then the keys
     const Q4Dims& d = a.dims;
-    const int b = blockIdx.x, n = a.cache.len[b];
+    const int b = blockIdx.x, n = a.cache.len[b], lane = threadIdx.x % kWave;
     const int32_t* table = a.cache.table + (size_t)b * d.max_pages;
     int32_t* rank = a.w.rank + (size_t)b * d.max_pages;
     int32_t* old = a.w.old_table + (size_t)b * d.max_pages;
-    const size_t rows0 = (size_t)b * a.n_max;
+    int32_t* replaced = a.w.replaced + (size_t)b * d.max_pages;
+    const size_t words = ((size_t)a.n_max + 63) / 64;
+    uint64_t* const mask_out = a.w.mask + b * words;
+    const bool masks_in_lds = words <= kWordsInLds;
+    uint64_t* const mask = masks_in_lds ? dynamic : mask_out;
+    int32_t* const prefix = masks_in_lds ? reinterpret_cast<int32_t*>(dynamic + words) : a.w.prefix + b * words;
     const int budget = kEvict ? a.budget[b] : 0;
     int bad = n < 0 || n > a.n_max || budget < 0;
     const int pages = bad ? 0 : pages_of(d, n);
-    const Rows<kEvict ? R : 0, kBlock> rows(a.cache.u + (size_t)b * d.cap, a.cache.pos + (size_t)b * d.cap, bad ? 0 : n);
-    // (rank: -1 for a page of the sequence's own, -2 for a shared one, until the shared ones with a hole are numbered)
+    Ranked rows{a.cache.u + (size_t)b * d.cap, a.cache.pos + (size_t)b * d.cap, nullptr, bad ? 0 : n};
+    const bool select = kEvict && budget > 0 && budget < n;
+    if (select && n - budget > kFewEvicted && a.n_max <= kKeysInLds) {
+        uint32_t* const keys = reinterpret_cast<uint32_t*>(dynamic + words + (words + 1) / 2);
+#pragma unroll 4
+        for (int i = threadIdx.x; i < rows.n; i += kBlock) keys[i] = float_key(rows.u[i]);
+        rows.keys = keys;
+    }
     for (int j = threadIdx.x; j < pages; j += kBlock) {
         const int page = table[j];
         const int refs = in_pool(d, page) ? a.cache.refs[page] : 0;
         bad |= refs < 1;
         old[j] = page;
-        rank[j] = refs > 1 ? -2 : -1;
+        rank[j] = refs > 1 ? -2 : -1;  // (-2: shared, until those that are replaced are numbered)
     }
     bad = __syncthreads_or(bad);
     if (bad) {
@@ -403,104 +425,82 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
         }
         return;
     }
-    // the rows that stay, a bit each (R = 0: asked again)
+    uint64_t least = 0;  // rows with a key of at least this stay
+    if (select) {
+        if (n - budget <= kFewEvicted) {
+            for (int i = 0; i < n - budget; ++i) least = next_key<kBlock>(rows, i ? least : 0, lds64);
+            ++least;
+        } else {
+            least = nth_key<kBlock>(rows, budget, hist, lds);
+        }
+    }
+    // a bit for every row that stays
     const uint8_t* keep = kEvict ? nullptr : a.keep + (size_t)b * d.cap;
-    const int per = rows.per, first = rows.first;
-    uint64_t least = 0;  // evict: rows with a key of at least this stay
-    uint32_t bits = 0;
-    int mine = 0;
-    if constexpr (kEvict) {
-        if (budget > 0 && budget < n) {
-            if (n - budget <= kFewEvicted) {
-                for (int i = 0; i < n - budget; ++i) least = next_key(rows, i ? least : 0, lds64);
-                ++least;
+    for (int i0 = 0; i0 < n; i0 += kBlock) {
+        const int i = i0 + (int)threadIdx.x;
+        bool s = false;
+        if (i < n) {
+            if constexpr (kEvict) {
+                const uint32_t key = select ? rows.key(i) : 0, border = (uint32_t)(least >> 32);
+                s = budget > 0 && (key > border || (key == border && (!(uint32_t)least || (uint32_t)~rows.pos[i] >= (uint32_t)least)));
+                if (a.keep_out) a.keep_out[(size_t)b * d.cap + i] = s;
             } else {
-                least = nth_key(rows, budget, hist, lds);
+                s = keep[i] != 0;
             }
         }
-        rows.each([&](int j, uint64_t key, bool exists) __attribute__((always_inline)) {
-            const bool s = exists && budget > 0 && key >= least;
-            mine += s;
-            if (R > 0) bits |= (uint32_t)s << j;
-            if (a.keep_out && exists) a.keep_out[(size_t)b * d.cap + first + j] = s;
-        });
-    } else {
-        for (int j = 0; j < per && first + j < n; ++j) {
-            const bool s = keep[first + j] != 0;
-            mine += s;
-            if (R > 0) bits |= (uint32_t)s << j;
+        const uint64_t m = __ballot(s);
+        if (lane == 0 && i < n) {
+            mask[i >> 6] = m;
+            if (masks_in_lds) mask_out[i >> 6] = m;
         }
     }
-    auto stays = [&](int i) __attribute__((always_inline)) {
-        if constexpr (R > 0) return (bits >> (i - first) & 1u) != 0;
-        else if constexpr (kEvict) return budget > 0 && rank_key(rows.u[i], rows.pos[i]) >= least;
-        else return keep[i] != 0;
-    };
-    int kept;
-    const int before = block_scan<kWaves>(mine, &kept, lds);
-    const int stop = min(n, first + per), stop_in = min(stop, kept);
-    // kept rows before the new end; shared pages with a hole there
-    int inside = 0, marked = -1;
-    for (int i = first; i < stop_in; ++i) {
-        const bool s = stays(i);
-        inside += s;
-        const int j = i >> d.page_shift;
-        if (!s && j != marked) {
-            marked = j;
-            if (rank[j] != -1) rank[j] = 0;
-        }
-    }
-    int in_place;
-    (void)block_scan<kWaves>(inside, &in_place, lds);
-    // kept rows behind the new end
-    int32_t* from = a.w.from + rows0;
-    if (stop > kept) {
-        int k = before - in_place;
-        for (int i = first; i < stop; ++i) {
-            const bool s = stays(i);
-            if (s && i >= kept) from[k] = i;
-            k += s;
-        }
-    }
-    // the shared pages with a hole numbered, the others left as they are
-    int need = 0;
-    const int end = pages_of(d, kept);
-    for (int j0 = 0; j0 < end; j0 += kBlock) {
-        const int j = j0 + (int)threadIdx.x;
-        const bool copy = j < end && rank[j] == 0;
-        int sum;
-        const int at = block_scan<kWaves>(copy, &sum, lds);
-        if (j < end) rank[j] = copy ? need + at : -1;
-        need += sum;
-    }
-    // the rows written: a hole (-1 - its number, for its one of `from`), a kept row of a replaced page
-    int count = 0, moves, page = -1;
-    bool replaced = false;
-    auto written = [&](int i, bool s) __attribute__((always_inline)) {
-        const int j = i >> d.page_shift;
-        if (need > 0 && j != page) {
-            page = j;
-            replaced = rank[j] >= 0;
-        }
-        return !s || replaced;
-    };
     __syncthreads();
-    for (int i = first; i < stop_in; ++i) count += written(i, stays(i));
-    int at = block_scan<kWaves>(count, &moves, lds);
-    int32_t* dst = a.w.dst + rows0;
-    int32_t* src = a.w.src + rows0;
-    for (int i = first, k = before; i < stop_in; ++i) {
-        const bool s = stays(i);
-        if (written(i, s)) {
-            dst[at] = i;
-            src[at++] = s ? i : -1 - (i - k);
-        }
-        k += s;
+    int kept = 0;
+    for (int w0 = 0; w0 * 64 < n; w0 += kBlock) {
+        const int w = w0 + (int)threadIdx.x;
+        int sum;
+        const int at = block_scan<kWaves>(w * 64 < n ? __popcll(mask[w]) : 0, &sum, lds);
+        if (w * 64 < n) prefix[w] = kept + at;
+        kept += sum;
     }
+    __syncthreads();
+    auto before = [&](int i) __attribute__((always_inline)) {  // K(i), i <= n
+        return i >= n ? kept : prefix[i >> 6] + __popcll(mask[i >> 6] & ((1ull << (i & 63)) - 1));
+    };
+    // shared pages with a hole, numbered
+    const int end = pages_of(d, kept), in_place = before(kept);
+    int need = 0;
+    if (in_place < kept)
+        for (int j0 = 0; j0 < end; j0 += kBlock) {
+            const int j = j0 + (int)threadIdx.x;
+            bool copy = false;
+            if (j < end) {
+                const int from = j << d.page_shift, to = min(kept, from + d.page_rows);
+                copy = rank[j] == -2 && before(to) - before(from) < to - from;
+            }
+            int sum;
+            const int at = block_scan<kWaves>(copy, &sum, lds);
+            if (j < end) rank[j] = copy ? need + at : -1;
+            if (copy) replaced[need + at] = j;
+            need += sum;
+        }
+    else
+        for (int j = threadIdx.x; j < end; j += kBlock) rank[j] = -1;
+    // holes, and the rows that fill them
+    int32_t* dst = a.w.dst + (size_t)b * a.n_max;
+    int32_t* src = a.w.src + (size_t)b * a.n_max;
+    if (in_place < kept)
+#pragma unroll 2
+        for (int i = threadIdx.x; i < n; i += kBlock) {
+            const uint64_t m = mask[i >> 6];
+            const int k = prefix[i >> 6] + __popcll(m & ((1ull << (i & 63)) - 1));
+            const bool s = m >> (i & 63) & 1u;
+            if (i < kept ? !s : s) (i < kept ? dst : src)[i < kept ? i - k : k - in_place] = i;
+        }
     if (threadIdx.x == 0) {
         a.w.need[b] = need;
         a.w.rows[b] = kept;
-        a.w.moves[b] = moves;
+        a.w.moves[b] = kept - in_place;
     }
 }
 
@@ -509,50 +509,67 @@ __global__ __launch_bounds__(kThreads) void q4_grant_kernel(Q4PageArgs a) {
     grant(a, lds);
 }
 
-// Workgroup (part, layer, b): every parts-th kEntries of the sequence's rows, in one layer; the first of a sequence also changes
-// its state.  The rows' places are found once for all KV heads; four copies of a thread are in flight together.
-constexpr int kEntries = 32;
+// Workgroup (part, layer, b): every parts-th kEntries of the sequence's entries, in one layer; the first of a sequence also changes
+// its state.  Entries are the holes, then the rows of the replaced pages (those that are holes, or behind the end, are none).
+// Their places are found once for all KV heads; four copies of a thread are in flight together.
+constexpr int kEntries = 16;
 template <int D>
 __global__ __launch_bounds__(kMoveThreads) void q4_move_kernel(Q4PageArgs a) {
     constexpr int kPieces = D / 32, kTogether = 4;  // 16-byte pieces of a row's codes; copies at a time
     typedef typename std::conditional<D == 128, uint32_t, uint16_t>::type scales_t;  // a row's scales
     __shared__ uint32_t place[2][kEntries];         // page * page_rows + row in the page: from, to
+    __shared__ int entries_s;
     const Q4Dims& d = a.dims;
     const int b = blockIdx.z, layer = blockIdx.y, part = blockIdx.x;
     const int kept = a.w.rows[b], offset = a.w.offset[b];
     if (kept < 0 || offset < 0) return;
-    const int moves = a.w.moves[b];
+    const int moves = a.w.moves[b], all = moves + a.w.need[b] * d.page_rows;
     const int32_t* dst = a.w.dst + (size_t)b * a.n_max;
     const int32_t* src = a.w.src + (size_t)b * a.n_max;
-    const int32_t* holes = a.w.from + (size_t)b * a.n_max;
     const int32_t* rank = a.w.rank + (size_t)b * d.max_pages;
     const int32_t* old = a.w.old_table + (size_t)b * d.max_pages;
-    auto source = [&](int m) __attribute__((always_inline)) {
-        const int r = src[m];
-        return r < 0 ? holes[-1 - r] : r;
-    };
+    const int32_t* replaced = a.w.replaced + (size_t)b * d.max_pages;
+    const uint64_t* mask = a.w.mask + b * (((size_t)a.n_max + 63) / 64);
     const int in = d.page_rows - 1;
     const size_t layer0 = q4_record(d, layer, 0, 0);
-    for (int m0 = part * kEntries; m0 < moves; m0 += gridDim.x * kEntries) {
-        const int entries = min(kEntries, moves - m0);
+    for (int m0 = part * kEntries; m0 < all; m0 += gridDim.x * kEntries) {
         __syncthreads();  // (the places before these are no longer read)
-        if ((int)threadIdx.x < 2 * entries) {
-            const int which = threadIdx.x & 1, m = threadIdx.x >> 1;
-            const int row = which ? dst[m0 + m] : source(m0 + m);
-            int page = old[row >> d.page_shift];
-            if (which) {
-                const int r = rank[row >> d.page_shift];
-                if (r >= 0) page = a.w.fresh[offset + r];
+        if (threadIdx.x < kWave) {
+            const int m = m0 + (int)threadIdx.x;
+            bool is = threadIdx.x < kEntries && m < all;
+            int from = 0, to = 0;
+            if (is && m < moves) {
+                from = src[m];
+                to = dst[m];
+            } else if (is) {
+                from = to = (replaced[(m - moves) >> d.page_shift] << d.page_shift) + ((m - moves) & in);
+                is = to < kept && (mask[to >> 6] >> (to & 63) & 1u);
             }
-            place[which][m] = ((uint32_t)page << d.page_shift) + (row & in);
+            const uint64_t live = __ballot(is);
+            if (is) {
+                const int r = rank[to >> d.page_shift];
+                const int page = r >= 0 ? a.w.fresh[offset + r] : old[to >> d.page_shift];
+                const int e = __popcll(live & ((1ull << threadIdx.x) - 1));
+                place[0][e] = ((uint32_t)old[from >> d.page_shift] << d.page_shift) + (from & in);
+                place[1][e] = ((uint32_t)page << d.page_shift) + (to & in);
+            }
+            if (threadIdx.x == 0) entries_s = __popcll(live);
         }
         __syncthreads();
+        const int entries = entries_s;
         auto record = [&](int which, int m, int g, int* row) __attribute__((always_inline)) {
             const uint32_t p = place[which][m];
             *row = p & in;
             return a.cache.pool + layer0 + ((size_t)(p >> d.page_shift) * d.hkv + g) * d.rec;
         };
-        const int copies = entries * d.hkv * 2 * kPieces;  // pieces fastest, then entries, then heads
+        const int copies = entries * d.hkv * 2 * kPieces, scales = entries * d.hkv * 2;  // pieces fastest, then entries, heads
+        auto scale_of = [&](int i, uint8_t** to) __attribute__((always_inline)) {
+            const int at = i & 1 ? d.vs_off : d.ks_off, e = i >> 1, m = e % entries, g = e / entries;
+            int fr, tr;
+            const uint8_t* s = record(0, m, g, &fr);
+            *to = record(1, m, g, &tr) + at + tr * sizeof(scales_t);
+            return reinterpret_cast<const scales_t*>(s + at)[fr];
+        };
         for (int i0 = threadIdx.x; i0 < copies; i0 += kMoveThreads * kTogether) {
             u32x4 x[kTogether];
             u32x4* to[kTogether];
@@ -567,22 +584,25 @@ __global__ __launch_bounds__(kMoveThreads) void q4_move_kernel(Q4PageArgs a) {
                 x[k] = *reinterpret_cast<const u32x4*>(s + at + fr * (D / 2));
                 to[k] = reinterpret_cast<u32x4*>(t + at + tr * (D / 2));
             }
+            // the scales beside the first pieces (there are no more of them than pieces)
+            const bool scale = i0 < scales;
+            uint8_t* scale_to = nullptr;
+            const scales_t y = scale ? scale_of(i0, &scale_to) : (scales_t)0;
 #pragma unroll
             for (int k = 0; k < kTogether; ++k)
                 if (i0 + k * kMoveThreads < copies) *to[k] = x[k];
+            if (scale) *reinterpret_cast<scales_t*>(scale_to) = y;
         }
-        for (int i = threadIdx.x; i < entries * d.hkv * 2; i += kMoveThreads) {
-            const int at = i & 1 ? d.vs_off : d.ks_off, e = i >> 1, m = e % entries, g = e / entries;
-            int fr, tr;
-            const uint8_t* s = record(0, m, g, &fr);
-            uint8_t* t = record(1, m, g, &tr);
-            reinterpret_cast<scales_t*>(t + at)[tr] = reinterpret_cast<const scales_t*>(s + at)[fr];
+        for (int i = threadIdx.x + kMoveThreads; i < scales; i += kMoveThreads) {
+            if ((i - (int)threadIdx.x) % (kMoveThreads * kTogether) == 0) continue;  // (written above)
+            uint8_t* to;
+            const scales_t y = scale_of(i, &to);
+            *reinterpret_cast<scales_t*>(to) = y;
         }
     }
     if (layer != 0 || part != 0) return;
     for (int m = threadIdx.x; m < moves; m += kMoveThreads) {
-        const int to = dst[m], from = source(m);
-        if (to == from) continue;
+        const int to = dst[m], from = src[m];
         if (a.cache.u) a.cache.u[(size_t)b * d.cap + to] = a.cache.u[(size_t)b * d.cap + from];
         if (a.cache.pos) a.cache.pos[(size_t)b * d.cap + to] = a.cache.pos[(size_t)b * d.cap + from];
     }
@@ -623,21 +643,32 @@ hipError_t launch_q4_free(const Q4PageArgs& a, hipStream_t s) {
 }
 
 namespace {
-template <bool kEvict>
-void launch_plan(const Q4PageArgs& a, hipStream_t s) {
-    // threads, and rows of each in registers, by the longest sequence
-    const auto launch = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, dim3(a.dims.batch), dim3(threads), 0, s, a); };
-    if (a.n_max <= 4 * 256) launch(q4_compact_plan_kernel<kEvict, 4, 256>, 256);
-    else if (a.n_max <= 4 * kThreads) launch(q4_compact_plan_kernel<kEvict, 4, kThreads>, kThreads);
-    else if (a.n_max <= 32 * kThreads) launch(q4_compact_plan_kernel<kEvict, 32, kThreads>, kThreads);
-    else launch(q4_compact_plan_kernel<kEvict, 0, kThreads>, kThreads);
+template <bool kEvict, int kBlock>
+hipError_t launch_plan(const Q4PageArgs& a, hipStream_t s) {
+    auto kern = q4_compact_plan_kernel<kEvict, kBlock>;
+    const size_t words = ((size_t)a.n_max + 63) / 64;
+    size_t lds = words <= (size_t)kWordsInLds ? (words + (words + 1) / 2) * sizeof(uint64_t) : 0;
+    if (kEvict && a.n_max <= kKeysInLds) lds += (size_t)a.n_max * sizeof(uint32_t);
+    if (lds > 60 * 1024) {
+        constexpr int kMost = kKeysInLds * 4 + kWordsInLds * 12;
+        static std::atomic<bool> raised[64];
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
+        if (dev < 0 || !raised[dev].load(std::memory_order_acquire)) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kMost);
+            if (e != hipSuccess) return e;
+            if (dev >= 0) raised[dev].store(true, std::memory_order_release);
+        }
+    }
+    hipLaunchKernelGGL(kern, dim3(a.dims.batch), dim3(kBlock), lds, s, a);
+    return hipGetLastError();
 }
 }  // namespace
 
 hipError_t launch_q4_compact(const Q4PageArgs& a, hipStream_t s) {
-    if (a.budget) launch_plan<true>(a, s);
-    else launch_plan<false>(a, s);
-    hipError_t e = hipGetLastError();
+    // (short sequences: fewer waves to wait for at every step)
+    hipError_t e = a.n_max <= 1024 ? (a.budget ? launch_plan<true, 256>(a, s) : launch_plan<false, 256>(a, s))
+                                   : (a.budget ? launch_plan<true, kThreads>(a, s) : launch_plan<false, kThreads>(a, s));
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(q4_grant_kernel, dim3(1), dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -589,10 +589,11 @@ def test_evict_of_bad_slots():
     t.check(B.KV_FAULT_CACHE)
 
 
-@pytest.mark.parametrize("n,budget", [(5000, 4999), (5000, 500), (3000, 1), (20000, 12345)])
+@pytest.mark.parametrize("n,budget", [(5000, 4999), (5000, 4996), (5000, 500), (3000, 1), (20000, 12345), (33000, 32000), (140000, 70001)])
 def test_evict_of_long_sequences(n, budget):
     """Utilities that share all but their last bits, ties across the border, and infinities among them."""
-    c = B.KvQ4Cache.allocate(B.make_q4_shape(3, 1, 1, 1, 64, 128, 500, 160, "bf16"))
+    pages = -(-n // 128) + 1
+    c = B.KvQ4Cache.allocate(B.make_q4_shape(3, 1, 1, 1, 64, 128, 3 * pages, pages, "bf16"))
     ws = B.q4_workspace(c.shape, n, 1)
     B.kv_q4_reserve(c, i32([n, n, n]), i32([0, 0, 0]), ws)
     u = torch.empty(3, n)
@@ -602,7 +603,7 @@ def test_evict_of_long_sequences(n, budget):
     u[2, 7], u[2, 9], u[2, 11] = float("inf"), float("-inf"), -0.0
     pos = torch.stack([torch.randperm(1 << 20, generator=gen(i))[:n] for i in range(3)]).to(torch.int32)
     c.u[:, :n], c.pos[:, :n] = u.cuda(), pos.cuda()
-    keep = torch.zeros(3, 160 * 128, dtype=torch.uint8, device="cuda")
+    keep = torch.zeros(3, pages * 128, dtype=torch.uint8, device="cuda")
     B.kv_q4_evict(c, n, i32([budget] * 3), ws, keep_out=keep)
     for b in range(3):
         order = np.lexsort((pos[b].numpy(), -u[b].double().numpy()))[:budget]
