@@ -67,7 +67,7 @@ struct Q4AttendArgs {
     float scale2;            // log2(e) / sqrt(d)
     float bias2;             // log2(e) * bias
     int nchunk, chunk_rows, scored;  // Q4AttendPlan
-    int stat_at;             // floats of LDS before the waves' statistics (set by the launch)
+    int stat_at, q_at;       // floats of LDS before the waves' statistics, and before an f32 query's parts (set by the launch)
     float* z;                // scores wanted: base-2 logits [slab][group][n_stride], or [slab][n_stride] parts of the scores
     float2* stat;            // scores wanted: [slab][group] (max, 1 / sum of 2^(z - max)), slab = (layer * batch + b) * hkv + head
     float2* part;            // several chunks: [slab][nchunk][group] (max, sum)

@@ -34,15 +34,6 @@
 namespace ikv {
 namespace {
 
-#ifndef Q4_WAVES
-#define Q4_WAVES 8
-#endif
-#ifndef Q4_WAVES32
-#define Q4_WAVES32 4
-#endif
-#ifndef Q4_PER_CU
-#define Q4_PER_CU 16
-#endif
 constexpr int kTile = 32;             // rows of a wave's tile: two halves of 16, each in one page
 constexpr float kSlack = 8.0f;
 constexpr int kMostRows = 8192;       // rows of a chunk, however many slabs there are: a batch may hold one long sequence
@@ -155,17 +146,15 @@ struct Slab {
 
 constexpr int kZPad = 16;  // floats between the heads' logits in LDS
 
-// Waves of a workgroup: f32 queries take three times the registers.
-template <typename T>
-constexpr int waves_of(bool scored) { return sizeof(T) == 2 ? Q4_WAVES : scored ? 8 : Q4_WAVES32; }
+constexpr int kQ4Waves = 8;
 
 template <typename T, int D, int CP, int NM, bool kScored>
-__global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3) void q4_attend_kernel(Q4AttendArgs a) {
-    constexpr int kWaves = waves_of<T>(kScored), kThreads = kWave * kWaves, kStep = kTile * kWaves;
+__global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendArgs a) {
+    constexpr int kThreads = kWave * kQ4Waves, kStep = kTile * kQ4Waves;
     constexpr int kKey = D / 32, kOut = D / 16;      // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of a query
     constexpr int kStride = D + 4;
-    constexpr int kJoin = kWaves > 4 ? 4 : kWaves;   // waves whose outputs are joined through LDS at once
+    constexpr int kJoin = 4;                         // waves whose outputs are joined through LDS at once
     // [wave] values; in their place [joined wave][column][kStride] outputs; behind both [wave][head] maxima and sums, then (kScored)
     // the heads' own and the slab's logits [head][rows + kZPad]
     extern __shared__ float lds[];
@@ -184,7 +173,7 @@ __global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3
     const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
     const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
     float* const stat = lds + a.stat_at;
-    float* const final = stat + 2 * kWaves * group;  // kScored: [head] maximum, 1 / sum
+    float* const final = stat + 2 * kQ4Waves * group;  // kScored: [head] maximum, 1 / sum
     float* const zs = final + 2 * group;
 
     // grid: KV heads, sequences, then layers and chunks (first chunks first: the later ones, which short sequences lack, spread
@@ -209,26 +198,21 @@ __global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3
     if (first >= len && chunk > 0) return;
     const int end = kScored ? len : min(len, first + a.chunk_rows);
 
-    u32x4 q[kParts][kKey];
+    // the query: bf16 in registers; f32 as three bf16 parts in LDS, [part][product][lane], where all waves read them (48 registers
+    // fewer: four waves per SIMD, as bf16)
+    u32x4 q[kKey];
+    f32x4 qf[sizeof(T) == 2 ? 1 : 2 * kKey];
     {
         const T* qp = static_cast<const T*>(a.q) + ((size_t)lb * d.hq + g * group + head) * D + s * (D / 4);
+        if constexpr (kParts == 1) {
 #pragma unroll
-        for (int j = 0; j < kKey; ++j) {
-            if constexpr (kParts == 1) {
+            for (int j = 0; j < kKey; ++j) {
                 const u32x4 x = reinterpret_cast<const u32x4*>(qp)[j];
-                q[0][j] = column ? x : u32x4{0, 0, 0, 0};
-            } else {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = column ? static_cast<const float*>(static_cast<const void*>(qp))[8 * j + i] : 0.0f;
-#pragma unroll
-                for (int k = 0; k < 3; ++k) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) q[k][j][i] = high2(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]));
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
-                }
+                q[j] = column ? x : u32x4{0, 0, 0, 0};
             }
+        } else if (wave == 0) {
+#pragma unroll
+            for (int j = 0; j < 2 * kKey; ++j) qf[j] = reinterpret_cast<const f32x4*>(qp)[j];
         }
     }
 
@@ -255,6 +239,27 @@ __global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3
         sl.load(keys, now, row);
         sl.load_values(now, value_lds);
     }
+    u32x4* const q_lds = reinterpret_cast<u32x4*>(lds + a.q_at) + lane;
+    if constexpr (kParts == 3) {
+        if (wave == 0) {
+#pragma unroll
+            for (int j = 0; j < kKey; ++j) {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = column ? qf[2 * j + i / 4][i % 4] : 0.0f;
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    u32x4 y;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = high2(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]));
+                    q_lds[(k * kKey + j) * kWave] = y;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
+                }
+            }
+        }
+        __syncthreads();
+    }
     for (; row < end; row += kStep) {
         const bool more = row + kStep < end;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tile's keys, and its values in LDS
@@ -268,7 +273,7 @@ __global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3
             for (int j = 0; j < kKey; ++j) {
                 const u32x4 k = eight(keys.codes[half][j], scale);
 #pragma unroll
-                for (int p = kParts - 1; p >= 0; --p) r = mfma(k, q[p][j], r);
+                for (int p = kParts - 1; p >= 0; --p) r = mfma(k, kParts == 1 ? q[j] : q_lds[(p * kKey + j) * kWave], r);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) z[4 * half + i] = r[i] * a.scale2;
@@ -393,15 +398,15 @@ __global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3
                 *reinterpret_cast<f32x4*>(mine + i * kOut + x) = f32x4{acc[x][i], acc[x + 1][i], acc[x + 2][i], acc[x + 3][i]};
         if (s == 0 && part == 0) {
             stat[wave * group + head] = m;
-            stat[(kWaves + wave) * group + head] = l;
+            stat[(kQ4Waves + wave) * group + head] = l;
         }
     };
-    if constexpr (kWaves > kJoin) {
-        static_assert(kWaves == 2 * kJoin, "one step joins the halves");
+    if constexpr (kQ4Waves > kJoin) {
+        static_assert(kQ4Waves == 2 * kJoin, "one step joins the halves");
         if (wave >= kJoin && column) put();
         __syncthreads();
         if (wave < kJoin && column) {
-            const float m2 = stat[(wave + kJoin) * group + head], l2 = stat[(kWaves + wave + kJoin) * group + head];
+            const float m2 = stat[(wave + kJoin) * group + head], l2 = stat[(kQ4Waves + wave + kJoin) * group + head];
             const float top = fmaxf(m, m2), f = exp2_hw(m - top), f2 = exp2_hw(m2 - top);
             m = top;
             l = l * f + l2 * f2;
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(kWave* waves_of<T>(kScored), sizeof(T) == 2 ? 4 : 3
 #pragma unroll
         for (int w = 0; w < kJoin; ++w) {
             const float f = exp2_hw(stat[w * group + h] - top);
-            sum += f * stat[(kWaves + w) * group + h];
+            sum += f * stat[(kQ4Waves + w) * group + h];
             f32x4 x = *reinterpret_cast<const f32x4*>(lds + (w * columns + h) * kStride + e);
 #pragma unroll
             for (int k = 1; k < CP; ++k) x += *reinterpret_cast<const f32x4*>(lds + (w * columns + k * group + h) * kStride + e);
@@ -512,9 +517,9 @@ __global__ __launch_bounds__(kFewThreads) void q4_join_few_kernel(Q4AttendArgs a
 constexpr int kJoinThreads = 512;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
-    constexpr int kQuads = D / 4, kRows = kJoinThreads / kQuads, kWaves = kJoinThreads / kWave, kTogether = 4;
+    constexpr int kQuads = D / 4, kRows = kJoinThreads / kQuads, kJoinWaves = kJoinThreads / kWave, kTogether = 4;
     __shared__ f32x4 red[kRows][kQuads];
-    __shared__ float mx[kWaves], sm[kWaves];
+    __shared__ float mx[kJoinWaves], sm[kJoinWaves];
     const Q4Dims& d = a.dims;
     const int h = blockIdx.x % d.group, slab = blockIdx.x / d.group, g = slab % d.hkv, lb = slab / d.hkv;
     const int segments = max(1, (attended(a, lb % d.batch) + a.chunk_rows - 1) / a.chunk_rows);
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
     if (threadIdx.x % kWave == 0) mx[threadIdx.x / kWave] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mx[w]);
+    for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, mx[w]);
     float sum = 0.0f;
     for (int i = threadIdx.x; i < segments; i += kJoinThreads) {
         const float2 p = part(i);
@@ -553,7 +558,7 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
     __syncthreads();
     sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += sm[w];
+    for (int w = 0; w < kJoinWaves; ++w) sum += sm[w];
     const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
     if (threadIdx.x == 0 && a.stat) a.stat[(size_t)slab * d.group + h] = make_float2(top, inv);
     if (r != 0) return;
@@ -565,10 +570,10 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
 }
 
 // Scores and their fold: 64 rows of a sequence per workgroup, one a lane.  A wave takes the KV heads slice, slice + per, ... of
-// one layer, kAhead layers at a time (their loads together); the waves' sums of a layer are added in order, and the layers
+// one layer, kAhead layers at a time (their loads together; 1 where the waves side by side cover the call's layers); the waves' sums of a layer are added in order, and the layers
 // folded in order.  kGroups: the scores' parts were summed over each group by the attention.
-constexpr int kScoreWaves = 16, kAhead = 4;
-template <bool kGroups>
+constexpr int kScoreWaves = 16;
+template <bool kGroups, int kAhead>
 __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendArgs a, int per) {
     __shared__ float part[kAhead][kScoreWaves][kWave];
     const Q4Dims& d = a.dims;
@@ -590,7 +595,7 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
             for (int g = wave % per; g < d.hkv; g += per) {
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
-                    const int l = min(l0 + q * together + wave / per, a.layer_count - 1);
+                    const int l = min(l0 + q * together + wave / per, a.layer_count - 1);  // (past the last: not used)
                     const size_t slab = (size_t)(l * d.batch + b) * d.hkv + g;
                     if constexpr (kGroups) {
                         s[q] += a.z[slab * a.n_stride + at];
@@ -627,19 +632,24 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
 
 template <typename T, int D, int CP, int NM, bool kScored>
 hipError_t launch_form(Q4AttendArgs a, hipStream_t s) {
-    constexpr int kWaves = waves_of<T>(kScored), kJoin = kWaves > 4 ? 4 : kWaves;
+    constexpr int kJoin = 4;
     const int slabs = a.layer_count * a.dims.batch * a.dims.hkv;
-    const int joined = kJoin * a.dims.group * CP * (D + 4) * (int)sizeof(float), values = kWaves * kValueBytes<D>;
+    const int joined = kJoin * a.dims.group * CP * (D + 4) * (int)sizeof(float), values = kQ4Waves * kValueBytes<D>;
     a.stat_at = (joined > values ? joined : values) / (int)sizeof(float);
-    size_t lds = (size_t)a.stat_at * sizeof(float) + 2 * (kWaves + 1) * a.dims.group * sizeof(float);
+    size_t lds = (size_t)a.stat_at * sizeof(float) + 2 * (kQ4Waves + 1) * a.dims.group * sizeof(float);
     auto kern = q4_attend_kernel<T, D, CP, NM, kScored>;
-    if (kScored) {
-        lds += (size_t)a.dims.group * (a.n_stride + kZPad) * sizeof(float);
+    if (kScored) lds += (size_t)a.dims.group * (a.n_stride + kZPad) * sizeof(float);
+    if (sizeof(T) == 4) {
+        lds = (lds + 15) / 16 * 16;
+        a.q_at = (int)(lds / sizeof(float));
+        lds += 3 * (D / 32) * kWave * sizeof(u32x4);
+    }
+    if (lds > 64 * 1024) {
         static std::atomic<bool> raised[kMaxDevices];
         const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), raised);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kern, dim3(a.dims.hkv, a.dims.batch, a.layer_count * (kScored ? 1 : a.nchunk)), dim3(kWave * kWaves), lds, s, a);
+    hipLaunchKernelGGL(kern, dim3(a.dims.hkv, a.dims.batch, a.layer_count * (kScored ? 1 : a.nchunk)), dim3(kWave * kQ4Waves), lds, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || kScored || a.nchunk == 1) return e;
     if (a.nchunk <= kFewChunks) hipLaunchKernelGGL((q4_join_few_kernel<T, D>), dim3(slabs), dim3(kFewThreads), 0, s, a);
@@ -665,9 +675,9 @@ hipError_t launch_by_group(const Q4AttendArgs& a, hipStream_t s) {
 Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool scores) {
     Q4AttendPlan p{};
     const int slabs = layer_count * d.batch * d.hkv;
-    const int waves = d.bf16 ? Q4_WAVES : Q4_WAVES32, step = waves * kTile;
+    const int cus = device_cus() > 0 ? device_cus() : 256;
     p.n_stride = (n_max + 63) / 64 * 64;
-    const int want = (256 * Q4_PER_CU / waves + slabs - 1) / slabs, by_rows = (n_max + step - 1) / step;
+    const int step = kQ4Waves * kTile, want = (2 * cus + slabs - 1) / slabs, by_rows = (n_max + step - 1) / step;
     p.most = want < by_rows ? want : by_rows;
     const int least = (n_max + kMostRows - 1) / kMostRows;
     if (least > p.most) p.most = least;
@@ -676,8 +686,9 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     // a workgroup of eight waves with its logits: two of them on a CU
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
     const size_t outputs = 4 * (size_t)d.group * (d.bf16 ? (d.group <= 8 ? 2 : 1) : d.group <= 5 ? 3 : 1) * (d.d + 4) * sizeof(float);
-    const size_t scored = (values > outputs ? values : outputs) + (size_t)d.group * (18 + p.n_stride + kZPad) * sizeof(float);
-    p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 512;
+    const size_t scored = (values > outputs ? values : outputs) + (size_t)d.group * (18 + p.n_stride + kZPad) * sizeof(float) +
+                          (d.bf16 ? 0 : 16 + 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4));
+    p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 2 * cus;
     return p;
 }
 
@@ -689,8 +700,10 @@ hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
     while (per < a.dims.hkv && per < kScoreWaves) per *= 2;
     while (waves < per * a.layer_count && waves < kScoreWaves) waves *= 2;
     const int blocks = (a.n_max + kWave - 1) / kWave;
-    hipLaunchKernelGGL((a.scored ? q4_score_kernel<true> : q4_score_kernel<false>), dim3(a.dims.batch * blocks),
-                       dim3(waves * kWave), 0, s, a, per);
+    const bool one = a.layer_count * per <= waves;
+    auto kern = a.scored ? (one ? q4_score_kernel<true, 1> : q4_score_kernel<true, 4>)
+                         : (one ? q4_score_kernel<false, 1> : q4_score_kernel<false, 4>);
+    hipLaunchKernelGGL(kern, dim3(a.dims.batch * blocks), dim3(waves * kWave), 0, s, a, per);
     return hipGetLastError();
 }
 
