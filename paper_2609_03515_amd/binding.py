@@ -413,6 +413,7 @@ class KvQ4Cache:
         # what every call passes or compares with, taken once (building it took 4 us of a call's 13)
         self._shape, self._buffers = ctypes.byref(shape), ctypes.byref(self.buffers)
         self._device, self._batch, self._rows = dev, shape.batch, shape.batch * cap
+        self._heads, self._dim = shape.n_kv_heads, shape.head_dim
 
     @classmethod
     def allocate(cls, shape: KvQ4Shape, device="cuda") -> "KvQ4Cache":
@@ -428,26 +429,28 @@ class KvQ4Cache:
 
 def _q4_ok(t, dtype, numel, device):
     """Whether a buffer that a kernel indexes without knowing its size is none, or has the type, place, layout and size."""
-    return t is None or (t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() >= numel)
+    return t is None or (t.dtype is dtype and t.numel() >= numel and t.get_device() == device and t.is_contiguous())
 
 
 def _q4_stream(fn, cache, ws, stream):
     """The stream of a call: its workspace has to lie with the cache, and the cache on the current device."""
     dev = cache._device
-    if not _q4_ok(ws, torch.uint8, 0, dev) or (dev >= 0 and dev != (torch.cuda.current_device() if _device is None else _device())):
+    if (ws is not None and (ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous())) or (
+            dev >= 0 and dev != (torch.cuda.current_device() if _device is None else _device())):
         raise KVError(fn, KV_ERR_INVALID_ARG)
     return _stream(stream)
 
 
 def _q4_strides(fn, cache, layer_count, rows, t):
     """Strides of a tensor [layer_count][batch][n_kv_heads][rows][head_dim] whose rows are contiguous."""
-    s, shape, st = cache.shape, t.shape, t.stride()
-    if (shape != (layer_count, cache._batch, s.n_kv_heads, rows, s.head_dim) or st[4] != 1 or t.dtype is not cache.element
-            or t.get_device() != cache._device):
+    batch, heads, d = cache._batch, cache._heads, cache._dim
+    if t.shape != (layer_count, batch, heads, rows, d) or t.dtype is not cache.element or t.get_device() != cache._device:
+        raise KVError(fn, KV_ERR_INVALID_ARG)
+    sl, sb, sh, sr, one = t.stride()
+    if one != 1:
         raise KVError(fn, KV_ERR_INVALID_ARG)
     # (the stride of an extent of 1 is not used, and may be anything)
-    return KvQ4Strides(st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0,
-                       st[3] if shape[3] > 1 else 0)
+    return KvQ4Strides(sl if layer_count > 1 else 0, sb if batch > 1 else 0, sh if heads > 1 else 0, sr if rows > 1 else 0)
 
 
 def kv_q4_reserve(cache: KvQ4Cache, add, new_pos, ws, granted=None, init="mean", stream=None):
@@ -465,7 +468,8 @@ def _q4_rows(fn, cache, layer0, layer_count, rows, k, v, ws, first, count, strea
     n, dev = cache._batch, cache._device
     if not (_q4_ok(first, torch.int32, n, dev) and _q4_ok(count, torch.int32, n, dev)):
         raise KVError(fn, KV_ERR_INVALID_ARG)
-    ks, vs = _q4_strides(fn, cache, layer_count, rows, k), _q4_strides(fn, cache, layer_count, rows, v)
+    ks = _q4_strides(fn, cache, layer_count, rows, k)
+    vs = _q4_strides(fn, cache, layer_count, rows, v)
     st = _q4_stream(fn, cache, ws, stream)
     _check(fn, getattr(load_library(), fn)(cache._shape, cache._buffers, layer0, layer_count, rows, _ptr(first), _ptr(count),
                                            _ptr(k), ks, _ptr(v), vs, _ptr(ws), _ws_bytes(ws), st))
