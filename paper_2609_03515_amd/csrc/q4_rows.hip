@@ -7,7 +7,7 @@
 // element that is not finite gets the scale byte 255 and codes 0, which reads back as NaN.
 //
 // Both directions are bound by memory traffic: a lane takes 8 elements (16 bytes of bf16, 4 bytes of codes), so a row of
-// 128 is 16 lanes and a block's maximum needs two steps inside a quad of lanes.
+// 128 is 16 lanes and a block's maximum needs two or three steps between neighbouring lanes.
 #include "kv_common.h"
 #include "q4.h"
 
@@ -68,13 +68,15 @@ __device__ __forceinline__ size_t source_of(const Item& it, const int64_t (&s)[4
     return (size_t)(it.l * s[0] + it.b * s[1] + it.g * s[2] + it.r * s[3]);
 }
 
-template <typename T>
-__device__ __forceinline__ void read8(const T* p, float (&x)[kElems]) {
+// A lane's 8 elements of a row: bf16 elements 8 p .. 8 p + 7, f32 elements 4 p .. 4 p + 3 of either half of the row, so that the
+// lanes' 16-byte accesses are consecutive.
+template <typename T, int D>
+__device__ __forceinline__ void read8(const T* row, int p, float (&x)[kElems]) {
     if constexpr (sizeof(T) == 2) {
-        Elem<bf16_t>::unpack(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)), x);
+        Elem<bf16_t>::unpack(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row) + p), x);
     } else {
-        const f32x4 lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
-        const f32x4 hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1);
+        const f32x4 lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row) + p);
+        const f32x4 hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row) + D / 8 + p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] = lo[i];
@@ -83,25 +85,77 @@ __device__ __forceinline__ void read8(const T* p, float (&x)[kElems]) {
     }
 }
 
-// A lane's 8 elements and its quad's block of 32: the codes, and the block's scale byte.
-__device__ __forceinline__ uint32_t quantise(const float (&x)[kElems], uint32_t* byte) {
-    uint32_t top = 0;  // |x| as integers: order-preserving, NaN above infinity above every number
-#pragma unroll
-    for (int i = 0; i < kElems; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = max(top, dpp_u<kXor1>(top));
-    top = max(top, dpp_u<kXor2>(top));
-    // the exponent, one higher from 1.75 * 2^k on: the smallest e with max |x| < 7 * 2^e is then two below it
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// A block's scale byte by its largest |x| as an integer (order-preserving, NaN above infinity above every number): the exponent,
+// one higher from 1.75 * 2^k on, less 2 is the smallest e with max |x| < 7 * 2^e.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     const int e = (int)((top + 0x00200000u) >> 23) - 2;
-    const bool finite = top < 0x7f800000u;
-    const uint32_t E = (uint32_t)min(max(e, kQ4MinByte), kQ4MaxByte);
-    const float scale = __uint_as_float(E << 23);
+    return top >= 0x7f800000u ? 255u : (uint32_t)min(max(e, kQ4MinByte), kQ4MaxByte);
+}
+
+// The codes of a lane's elements, and its row's scale bytes together (in every lane).
+template <typename T, int D>
+__device__ __forceinline__ uint32_t quantise(const float (&x)[kElems], int p, uint32_t* scales) {
     uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
-    *byte = finite ? E : 255u;
-    return finite ? w : 0u;
+    if constexpr (sizeof(T) == 2) {  // a block is a quad of lanes
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kElems; ++i) top = max(top, magnitude(x[i]));
+        top = max(top, dpp_u<kXor1>(top));
+        top = max(top, dpp_u<kXor2>(top));
+        const uint32_t byte = scale_byte(top);
+        const float scale = __uint_as_float(byte << 23);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+        if (byte == 255u) w = 0;
+        uint32_t s = byte << 8 * (p / 4);
+        s |= dpp_u<kMirror8>(s);
+        if constexpr (D == 128) s |= dpp_u<kRor8>(s);
+        *scales = s;
+    } else {  // a block is 8 lanes of one half
+        uint32_t top[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            top[h] = max(max(magnitude(x[4 * h]), magnitude(x[4 * h + 1])), max(magnitude(x[4 * h + 2]), magnitude(x[4 * h + 3])));
+            top[h] = max(top[h], dpp_u<kXor1>(top[h]));
+            top[h] = max(top[h], dpp_u<kXor2>(top[h]));
+            top[h] = max(top[h], dpp_u<kMirror8>(top[h]));
+        }
+        const uint32_t b0 = scale_byte(top[0]), b1 = scale_byte(top[1]);
+        const float s0 = __uint_as_float(b0 << 23), s1 = __uint_as_float(b1 << 23);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s0, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s0, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s1, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s1, 3);
+        if (b0 == 255u) w &= 0xffff0000u;
+        if (b1 == 255u) w &= 0x0000ffffu;
+        if constexpr (D == 128) {
+            uint32_t s = (b0 | b1 << 16) << 8 * (p / 8);
+            s |= dpp_u<kRor8>(s);
+            *scales = s;
+        } else {
+            *scales = b0 | b1 << 8;
+        }
+    }
+    return w;
+}
+
+// A lane's codes in a row of codes, and back.
+template <typename T, int D>
+__device__ __forceinline__ void put_codes(uint8_t* row, int p, uint32_t w) {
+    if constexpr (sizeof(T) == 2) {
+        reinterpret_cast<uint32_t*>(row)[p] = w;
+    } else {
+        reinterpret_cast<uint16_t*>(row)[p] = (uint16_t)w;
+        reinterpret_cast<uint16_t*>(row)[D / 8 + p] = (uint16_t)(w >> 16);
+    }
+}
+template <typename T, int D>
+__device__ __forceinline__ uint32_t get_codes(const uint8_t* row, int p) {
+    if constexpr (sizeof(T) == 2) return reinterpret_cast<const uint32_t*>(row)[p];
+    else return reinterpret_cast<const uint16_t*>(row)[p] | (uint32_t)reinterpret_cast<const uint16_t*>(row)[D / 8 + p] << 16;
 }
 
 // kItems: rows of keys and of values per lane, their loads together.  Two where that still leaves two workgroups for every CU,
@@ -123,8 +177,8 @@ __global__ __launch_bounds__(kThreads) void q4_store_kernel(Q4RowArgs a, uint32_
     for (int k = 0; k < kItems; ++k) {
         refs[k] = it[k].page >= 0 ? a.cache.refs[it[k].page] : 1;
         if (!it[k].wanted) continue;
-        read8(static_cast<const T*>(a.k) + source_of(it[k], a.ks) + p * kElems, x[k][0]);
-        read8(static_cast<const T*>(a.v) + source_of(it[k], a.vs) + p * kElems, x[k][1]);
+        read8<T, D>(static_cast<const T*>(a.k) + source_of(it[k], a.ks), p, x[k][0]);
+        read8<T, D>(static_cast<const T*>(a.v) + source_of(it[k], a.vs), p, x[k][1]);
     }
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
@@ -133,33 +187,27 @@ __global__ __launch_bounds__(kThreads) void q4_store_kernel(Q4RowArgs a, uint32_
         uint8_t* rec = a.cache.pool + q4_record(a.dims, a.layer0 + it[k].l, it[k].page, it[k].g);
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            uint32_t byte;
-            const uint32_t codes = quantise(x[k][which], &byte);
-            // the row's scale bytes gathered by its lanes, one store for them
-            uint32_t word = byte << 8 * (p / 4);
-            word |= dpp_u<kMirror8>(word);
-            uint8_t* c = rec + (which ? a.dims.vc_off : 0);
+            uint32_t scales;
+            const uint32_t codes = quantise<T, D>(x[k][which], p, &scales);
+            put_codes<T, D>(rec + (which ? a.dims.vc_off : 0) + it[k].row * (D / 2), p, codes);
             uint8_t* e = rec + (which ? a.dims.vs_off : a.dims.ks_off);
-            reinterpret_cast<uint32_t*>(c + it[k].row * (D / 2))[p] = codes;
-            if constexpr (D == 128) {
-                word |= dpp_u<kRor8>(word);
-                if (p == 0) reinterpret_cast<uint32_t*>(e)[it[k].row] = word;
-            } else {
-                if (p == 0) reinterpret_cast<uint16_t*>(e)[it[k].row] = (uint16_t)word;
+            if (p == 0) {
+                if constexpr (D == 128) reinterpret_cast<uint32_t*>(e)[it[k].row] = scales;
+                else reinterpret_cast<uint16_t*>(e)[it[k].row] = (uint16_t)scales;
             }
         }
     }
     if (fault && p == 0) atomicOr(a.faults, fault);
 }
 
-// 8 codes and their scale as 8 bf16 (exact)
-__device__ __forceinline__ u32x4 expand(uint32_t codes, uint32_t byte) {
-    const float scale = __uint_as_float(byte << 23);
+// 8 codes, the first and the last four of which may have different scales, as 8 bf16 (exact)
+__device__ __forceinline__ u32x4 expand(uint32_t codes, uint32_t first, uint32_t last) {
+    const float s0 = __uint_as_float(first << 23), s1 = __uint_as_float(last << 23);
     u32x4 r;
-    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
-    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
-    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
-    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s0, 0));
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s0, 1));
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s1, 2));
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s1, 3));
     return r;
 }
 
@@ -172,15 +220,18 @@ __global__ __launch_bounds__(kThreads) void q4_load_kernel(Q4RowArgs a, uint32_t
     Item it[kItems];
     const uint32_t fault = locate(a, first, kRows, items, it);
     if (fault && p == 0) atomicOr(a.faults, fault);
-    uint32_t codes[kItems][2], byte[kItems][2];
+    constexpr bool kHalves = sizeof(T) == 4;  // the lane's elements lie in two blocks
+    uint32_t codes[kItems][2], byte[kItems][2][2];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
         const uint8_t* rec = a.cache.pool + q4_record(a.dims, a.layer0 + it[k].l, max(it[k].page, 0), it[k].g);
         const int row = it[k].page < 0 ? 0 : it[k].row;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            codes[k][which] = reinterpret_cast<const uint32_t*>(rec + (which ? a.dims.vc_off : 0) + row * (D / 2))[p];
-            byte[k][which] = rec[(which ? a.dims.vs_off : a.dims.ks_off) + row * (D / 32) + p / 4];
+            const uint8_t* e = rec + (which ? a.dims.vs_off : a.dims.ks_off) + row * (D / 32);
+            codes[k][which] = get_codes<T, D>(rec + (which ? a.dims.vc_off : 0) + row * (D / 2), p);
+            byte[k][which][0] = e[kHalves ? p / 8 : p / 4];
+            byte[k][which][1] = kHalves ? e[D / 64 + p / 8] : byte[k][which][0];
         }
     }
 #pragma unroll
@@ -188,16 +239,16 @@ __global__ __launch_bounds__(kThreads) void q4_load_kernel(Q4RowArgs a, uint32_t
         if (!it[k].wanted) continue;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            T* out = static_cast<T*>(which ? a.v_out : a.k_out) + source_of(it[k], which ? a.vs : a.ks) + p * kElems;
+            T* out = static_cast<T*>(which ? a.v_out : a.k_out) + source_of(it[k], which ? a.vs : a.ks);
             // (a row that is not there: zeros)
-            const u32x4 x = it[k].page < 0 ? u32x4{0, 0, 0, 0} : expand(codes[k][which], byte[k][which]);
-            if constexpr (sizeof(T) == 2) {
-                __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(out));
-            } else {
+            const u32x4 x = it[k].page < 0 ? u32x4{0, 0, 0, 0} : expand(codes[k][which], byte[k][which][0], byte[k][which][1]);
+            if constexpr (kHalves) {
                 float f[kElems];
                 Elem<bf16_t>::unpack(x, f);
-                __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(out));
-                __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(out) + 1);
+                __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(out) + p);
+                __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(out) + D / 8 + p);
+            } else {
+                __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(out) + p);
             }
         }
     }
