@@ -6,8 +6,8 @@
 // A workgroup takes one chunk of rows of one (layer, sequence, KV head) slab for the group's query heads; its waves take
 // tiles of 32 rows in turn, each with a running maximum, sum and output of its own, joined at the end of the chunk.  Both
 // products run on the matrix cores (16x16x32, bf16 in, 32 bits out); lane 16 s + c of a wave:
-//  * keys: row 4 (c % 4) + c / 4 of each half of the tile, elements 32 s ... (d = 64: 16 s ...): 16 consecutive bytes of codes, one scale.
-//    A code with its scale is a bf16 number exactly, and the conversion applies the scale, so the product with a bf16 query is
+//  * keys: row 4 (c % 4) + c / 4 of each half of the tile, elements 32 s ... (d = 64: 16 s ...): 16 (8) consecutive bytes of
+//    codes, one scale.  A code with its scale is a bf16 number exactly, and the conversion applies the scale, so the product with a bf16 query is
 //    exact up to the order of 32-bit sums.  The query's elements lie in the same order.  f32 queries: three bf16 parts whose
 //    sum is the number, a product each.
 //  * logits: the result holds rows s, 4 + s, 8 + s, 12 + s of each half for column c.  A column is a head; where two or three times
@@ -22,6 +22,13 @@
 // The maximum is raised only when a tile exceeds it by 2^8: p stays below 2^8 and the sums in range, and the rescaling of the
 // output is rare.  Rows behind the sequence, and rows of pages that do not exist, get the logit -inf and their values the
 // scale 1 (whatever their bytes are), so that they add 0 * a finite number.
+//
+// What bounds it, measured: all layers of 8 sequences x 3,277 rows x 8 KV heads of 4 (bf16, 913 MB) take 157 us, 5.8 TB/s (a
+// large copy reaches 4.9); with the arithmetic left out of a copy of the kernel the same loads take 141, and 164 when they do not
+// pass the caches by.  One layer of it (28.5 MB) is a matter of latencies: 13 us and 4 for the join, of which an empty kernel is
+// 2.5 and the loads alone 9.  One sequence of 131,072 rows, 143 MB: 27 us + 4.5.
+// On the way (all layers): 190 us with the values in registers and cached loads.  Equal shares of all tiles per workgroup, whatever
+// sequence they belong to, took 226 (the search for the share, and the state that it needs).
 #include <float.h>
 
 #include <atomic>
@@ -144,9 +151,8 @@ struct Slab {
     }
 };
 
-constexpr int kZPad = 16;  // floats between the heads' logits in LDS
-
-constexpr int kQ4Waves = 8;
+constexpr int kZPad = 16;    // floats between the heads' logits in LDS
+constexpr int kQ4Waves = 8;  // (four: one sequence of 131,072 rows 35 us for 34, scored slabs 215 for 190)
 
 template <typename T, int D, int CP, int NM, bool kScored>
 __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendArgs a) {
@@ -304,7 +310,7 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
         }
         if ((kScored || a.z) && c < group) {  // (row 4 i + s of a half at 4 s + i)
             float* zp = kScored ? zs + c * (a.n_stride + kZPad) + row + 4 * s
-                                         : a.z + ((size_t)slab * group + c) * a.n_stride + row + 4 * s;
+                                : a.z + ((size_t)slab * group + c) * a.n_stride + row + 4 * s;
             *reinterpret_cast<f32x4*>(zp) = f32x4{z[0], z[1], z[2], z[3]};
             *reinterpret_cast<f32x4*>(zp + 16) = f32x4{z[4], z[5], z[6], z[7]};
         }
@@ -476,7 +482,7 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
 }
 
 // A few chunks: one workgroup per slab joins their outputs and statistics, four elements of a head per thread and all of its
-// loads at once.
+// loads at once (one layer of 64 slabs in 7 chunks, attention and join: 17.5 -> 16.4 us against a workgroup per head).
 constexpr int kFewChunks = 8, kFewThreads = 256;
 template <typename T, int D>
 __global__ __launch_bounds__(kFewThreads) void q4_join_few_kernel(Q4AttendArgs a) {
@@ -677,13 +683,17 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     const int slabs = layer_count * d.batch * d.hkv;
     const int cus = device_cus() > 0 ? device_cus() : 256;
     p.n_stride = (n_max + 63) / 64 * 64;
+    // Chunks: two workgroups per CU in all, as many as it holds.  More cost more than they balance: 512 slabs of 8,192 rows take
+    // 102 us in one chunk each, 110 in two, 131 in eight, and 512 of 1 .. 8,192 rows 79, 85 and 94.  But no chunk above 8,192
+    // rows: two prompts of up to 16,400 rows among six short samples (512 slabs) 347 -> 312 us with that whole step.
     const int step = kQ4Waves * kTile, want = (2 * cus + slabs - 1) / slabs, by_rows = (n_max + step - 1) / step;
     p.most = want < by_rows ? want : by_rows;
     const int least = (n_max + kMostRows - 1) / kMostRows;
     if (least > p.most) p.most = least;
     p.chunk_rows = ((n_max + p.most - 1) / p.most + step - 1) / step * step;
     p.nchunk = (n_max + p.chunk_rows - 1) / p.chunk_rows;
-    // a workgroup of eight waves with its logits: two of them on a CU
+    // Scored: where a slab's logits fit LDS with two workgroups on a CU, and there is a slab for each: 2,048 slabs of 3,277 rows
+    // with scores 190 us, through memory 241.
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
     const size_t outputs = 4 * (size_t)d.group * (d.bf16 ? (d.group <= 8 ? 2 : 1) : d.group <= 5 ? 3 : 1) * (d.d + 4) * sizeof(float);
     const size_t scored = (values > outputs ? values : outputs) + (size_t)d.group * (18 + p.n_stride + kZPad) * sizeof(float) +

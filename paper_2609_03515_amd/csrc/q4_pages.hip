@@ -7,6 +7,11 @@
 // A call that allocates runs in launches on the caller's stream: what each sequence needs, the pages for it (one workgroup),
 // and the change itself, spread over sequences and layers.  The last one reads what the others wrote in the scratch, never
 // the table or the lengths that its own workgroups change.
+//
+// Small calls are launches and chains of dependent loads (2.5 to 8 us a kernel); measured on six samples of prompts of 12,000 to
+// 16,384 rows in 8 layers of 8 KV heads: fork 11 us, reserve 7 + 9, eviction to 10%: plan 28, pages 5, moves 48 (some 150 MB,
+// 3 TB/s).  The moves took 112 with one workgroup per slab that found every row's place for itself, and the plan 45 with a prefix
+// sum per 1,024 rows (64 with keys in registers: that unrolls into more code than its instruction fetches are worth).
 #include <atomic>
 #include <type_traits>
 

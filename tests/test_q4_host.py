@@ -176,3 +176,15 @@ def test_reference_quantiser():
     assert (err <= top / 3.5).all() and (err[top == 0] == 0).all()  # 2^e <= max |x| / 3.5
     codes, _ = R.quantise(np.array([[0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, 6.0, -0.0] + [0.0] * 22]))
     assert codes[0, :10].tolist() == [0, 2, 2, 4, 4, 6, 6, 8, 7, 8]
+
+
+def test_attention_registers():
+    """Every instance of the 4-bit attention fits four waves per SIMD (128 of 512 registers) without spills to speak of: the
+    loads in flight of fewer waves do not cover the memory's latency."""
+    import test_kernel_resources as K
+
+    objs = K.code_object(open(B.LIB_PATH, "rb").read())
+    seen = {k[".name"]: k for o in objs for k in K.metadata(o)["amdhsa.kernels"] if "q4_attend_kernel" in k[".name"]}
+    assert len(seen) == 16
+    assert max(k[".vgpr_count"] for k in seen.values()) <= 128
+    assert max(k[".vgpr_spill_count"] for k in seen.values()) <= 2
