@@ -576,15 +576,16 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(Q4AttendArgs a) {
 }
 
 // Scores and their fold: 64 rows of a sequence per workgroup, one a lane.  A wave takes the KV heads slice, slice + per, ... of
-// one layer, kAhead layers at a time (their loads together; 1 where the waves side by side cover the call's layers); the waves' sums of a layer are added in order, and the layers
-// folded in order.  kGroups: the scores' parts were summed over each group by the attention.
+// one layer, kAhead layers at a time (their loads together; 1 where the waves side by side cover the call's layers); the waves'
+// sums of a layer are added in order, and the layers folded in order.  kGroups: the scores' parts were summed over each group by
+// the attention.
 constexpr int kScoreWaves = 16;
 template <bool kGroups, int kAhead>
-__global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendArgs a, int per) {
+__global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendArgs a, int per_shift, int together_shift) {
     __shared__ float part[kAhead][kScoreWaves][kWave];
     const Q4Dims& d = a.dims;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int waves = blockDim.x / kWave, together = waves / per;  // layers that the waves take side by side
+    const int waves = blockDim.x / kWave, per = 1 << per_shift, together = 1 << together_shift;  // (layers side by side)
     const int blocks = (a.n_max + kWave - 1) / kWave;
     const int b = blockIdx.x / blocks, row = blockIdx.x % blocks * kWave + lane;
     const int n = attended(a, b);
@@ -598,10 +599,11 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) s[q] = 0.0f;
         if (blockIdx.x % blocks * kWave < n)
-            for (int g = wave % per; g < d.hkv; g += per) {
+#pragma unroll 4
+            for (int g = (wave & (per - 1)); g < d.hkv; g += per) {
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
-                    const int l = min(l0 + q * together + wave / per, a.layer_count - 1);  // (past the last: not used)
+                    const int l = min(l0 + q * together + (wave >> per_shift), a.layer_count - 1);  // (past the last: not used)
                     const size_t slab = (size_t)(l * d.batch + b) * d.hkv + g;
                     if constexpr (kGroups) {
                         s[q] += a.z[slab * a.n_stride + at];
@@ -619,7 +621,7 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
         __syncthreads();
         // (wave, layer) pairs: the layer's sum in place of its first slice's
         for (int i = wave; i < together * kAhead; i += waves) {
-            const int q = i / together, w0 = i % together * per;
+            const int q = i >> together_shift, w0 = (i & (together - 1)) << per_shift;
             float x = part[q][w0][lane];
             for (int w = 1; w < per; ++w) x += part[q][w0 + w][lane];
             x *= inv;
@@ -628,9 +630,10 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
             if (a.s_out && l < a.layer_count && row < a.n_max) a.s_out[((size_t)l * d.batch + b) * a.n_max + row] = live ? x : 0.0f;
         }
         __syncthreads();
-        if (wave == 0)
+        if (wave == 0 && a.u_out)
+#pragma unroll 8
             for (int i = 0; i < together * kAhead && l0 + i < a.layer_count; ++i)
-                u = a.alpha * u + (1.0f - a.alpha) * part[i / together][i % together * per][lane];
+                u = a.alpha * u + (1.0f - a.alpha) * part[i >> together_shift][(i & (together - 1)) << per_shift][lane];
         __syncthreads();
     }
     if (wave == 0 && live && a.u_out) a.u_out[ub] = u;
@@ -705,15 +708,18 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
     hipError_t e = a.dims.d == 128 ? launch_by_group<128>(a, s) : launch_by_group<64>(a, s);
     if (e != hipSuccess || !a.z) return e;
-    // waves: as many as there are KV heads of the call's layers, up to 16, and a power of two of them to a layer
-    int per = 1, waves = 1;
-    while (per < a.dims.hkv && per < kScoreWaves) per *= 2;
-    while (waves < per * a.layer_count && waves < kScoreWaves) waves *= 2;
+    // Waves: as many as the call's layers have KV heads, up to 16; with fewer layers than waves, a power of two of waves to a
+    // layer.  (A wave to a layer leaves one sum to add: 32 layers of 8 KV heads x 8 sequences x 3,277 rows 17 -> 12 us.)
+    int per_shift = 0, waves_shift = 0;
+    while ((1 << per_shift) < a.dims.hkv && a.layer_count << per_shift < kScoreWaves) ++per_shift;
+    while ((1 << waves_shift) < a.layer_count << per_shift && (1 << waves_shift) < kScoreWaves) ++waves_shift;
+    const int waves = 1 << waves_shift;
     const int blocks = (a.n_max + kWave - 1) / kWave;
-    const bool one = a.layer_count * per <= waves;
-    auto kern = a.scored ? (one ? q4_score_kernel<true, 1> : q4_score_kernel<true, 4>)
-                         : (one ? q4_score_kernel<false, 1> : q4_score_kernel<false, 4>);
-    hipLaunchKernelGGL(kern, dim3(a.dims.batch * blocks), dim3(waves * kWave), 0, s, a, per);
+    const int ahead = ((a.layer_count << per_shift) + waves - 1) / waves;
+    auto kern = a.scored ? (ahead == 1 ? q4_score_kernel<true, 1> : ahead == 2 ? q4_score_kernel<true, 2> : q4_score_kernel<true, 4>)
+                         : (ahead == 1 ? q4_score_kernel<false, 1> : q4_score_kernel<false, 4>);
+    hipLaunchKernelGGL(kern, dim3(a.dims.batch * blocks), dim3(waves * kWave), 0, s, a, per_shift,
+                       waves_shift - per_shift);
     return hipGetLastError();
 }
 
