@@ -179,8 +179,8 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
     const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
     const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
     float* const stat = lds + a.stat_at;
-    float* const final = stat + 2 * kQ4Waves * group;  // kScored: [head] maximum, 1 / sum
-    float* const zs = final + 2 * group;
+    float* const heads = stat + 2 * kQ4Waves * group;  // kScored: [head] maximum, 1 / sum
+    float* const zs = heads + 2 * group;
 
     // grid: KV heads, sequences, then layers and chunks (first chunks first: the later ones, which short sequences lack, spread
     // evenly)
@@ -454,8 +454,8 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
             for (int j = 0; j < 4; ++j) Elem<T>::store(op + j, o[j] * inv);
             if (kScored) {
                 if (e == 0) {
-                    final[2 * h] = top;
-                    final[2 * h + 1] = inv;
+                    heads[2 * h] = top;
+                    heads[2 * h + 1] = inv;
                 }
             } else if (e == 0 && a.stat) {
                 a.stat[(size_t)slab * group + h] = make_float2(top, inv);
@@ -469,12 +469,12 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
         // the slab's part of the scores: sum over the group of 2^(z - m) / sum, four rows per thread
         float* rp = a.z + (size_t)slab * a.n_stride;
         __syncthreads();
-        for (int r = threadIdx.x * 4; r < len; r += kThreads * 4) {
+        for (int r = threadIdx.x * 4; r < (len + 15) / 16 * 16; r += kThreads * 4) {  // (whole blocks: their rows lie in another order)
             f32x4 x{0.0f, 0.0f, 0.0f, 0.0f};
             for (int h = 0; h < group; ++h) {
                 const f32x4 z = *reinterpret_cast<const f32x4*>(zs + h * (a.n_stride + kZPad) + r);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = fmaf(exp2_hw(z[i] - final[2 * h]), final[2 * h + 1], x[i]);
+                for (int i = 0; i < 4; ++i) x[i] = fmaf(exp2_hw(z[i] - heads[2 * h]), heads[2 * h + 1], x[i]);
             }
             *reinterpret_cast<f32x4*>(rp + r) = x;
         }

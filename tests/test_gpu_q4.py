@@ -257,6 +257,129 @@ def test_attention_of_a_long_sequence(dtype):
     check_attend(t, q, o, s_out=s)
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(8, 8, 64, "bf16"), (32, 8, 128, "bf16"), (24, 8, 128, "f32"), (56, 8, 64, "f32"),
+                                            (56, 8, 128, "bf16"), (128, 8, 128, "bf16")])
+def test_attention_of_many_slabs(hq, hkv, d, dtype):
+    """As many slabs as two for every CU: with scores their logits stay in the workgroup; without, a workgroup has a whole slab.
+    Lengths end in every place of a tile's order of rows."""
+    lens = [1, 2, 5, 18, 31, 33, 70, 0, 300, 16, 47, 8]
+    t = Cache(lens, layers=6, hq=hq, hkv=hkv, d=d, dtype=dtype).fill()
+    q = torch.randn(6, 12, hq, d, generator=gen(3)).to(DT[dtype]).cuda()
+    cur = i32([t.cap - 1] * 12)
+    o, s = torch.full_like(q, 9.0), torch.full((6, 12, 301), 9.0, device="cuda")
+    out = torch.full_like(t.c.u, 5.0)
+    B.kv_q4_attend(t.c, 0, 6, 301, q, o, t.ws, cur_pos=cur, recency_bias=-0.5, recency_window=100, s_out=s, alpha=0.8,
+                   u_prior=t.c.u, u_out=out)
+    scores = check_attend(t, q, o, cur, -0.5, 100, s)
+    for b, n in enumerate(lens):
+        want = t.c.u[b, :n].double().cpu().numpy()
+        for l in range(6):
+            want = 0.8 * want + 0.2 * scores[l, b, :n]
+        lim = 24 * 2.0 ** -24 * want + 2.0 ** -12 * (scores[:, b, :n].sum(0) * 0.2)
+        assert (np.abs(out[b, :n].double().cpu().numpy() - want) <= lim).all() and (out[b, n:] == 5.0).all()
+    o2 = torch.full_like(q, 9.0)
+    B.kv_q4_attend(t.c, 0, 6, 301, q, o2, t.ws, cur_pos=cur, recency_bias=-0.5, recency_window=100)
+    check_attend(t, q, o2, cur, -0.5, 100)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_in_a_few_chunks(dtype):
+    """A hundred slabs of a thousand rows: each in a few chunks, some of which short sequences lack."""
+    lens = [1000, 255, 256, 257, 513, 999, 1, 0, 770, 1000, 64, 300, 800]
+    t = Cache(lens, layers=2, hq=8, hkv=4, dtype=dtype, page_rows=32).fill()
+    q = torch.randn(2, 13, 8, 128, generator=gen(3)).to(DT[dtype]).cuda()
+    o, s = torch.full_like(q, 9.0), torch.full((2, 13, 1000), 9.0, device="cuda")
+    B.kv_q4_attend(t.c, 0, 2, 1000, q, o, t.ws, s_out=s)
+    check_attend(t, q, o, s_out=s)
+    B.kv_q4_attend(t.c, 0, 2, 1000, q, o.fill_(9.0), t.ws)
+    check_attend(t, q, o)
+
+
+def test_one_long_sequence_among_many():
+    """512 slabs would take a chunk each; no chunk is longer than 8,192 rows."""
+    lens = [9000] + [40] * 63
+    t = Cache(lens, layers=1, hq=8, hkv=8, d=64, page_rows=256, n_pages=120).fill()
+    q = torch.randn(1, 64, 8, 64, generator=gen(3)).bfloat16().cuda()
+    o = torch.full_like(q, 9.0)
+    B.kv_q4_attend(t.c, 0, 1, 9000, q, o, t.ws)
+    check_attend(t, q, o)
+
+
+def test_workspace_serves_smaller_calls():
+    """A workspace for n_max rows and all layers takes every call on fewer of either, whatever way those are divided."""
+    t = Cache([1500, 3], layers=5, hq=4, hkv=2, page_rows=64).fill()
+    ws = B.q4_workspace(t.shape, 1500, 5)
+    q = torch.randn(5, 2, 4, 128, generator=gen(3)).bfloat16().cuda()
+    o = torch.empty_like(q)
+    s = torch.empty(5 * 2 * 1500, device="cuda")
+    ref = torch.empty_like(q)
+    B.kv_q4_attend(t.c, 0, 5, 1500, q, ref, ws)
+    for n in (1500, 1499, 1281, 1280, 1025, 1024, 513, 512, 300, 256, 255, 1):
+        t.c.len.copy_(torch.tensor([min(n, 1500), min(n, 3)]))
+        for layers in (1, 2, 3, 4, 5):
+            B.kv_q4_attend(t.c, 5 - layers, layers, n, q, o, ws, s_out=s)
+    B.kv_q4_evict(t.c, 1, i32([5, 5]), ws)
+    B.kv_q4_reserve(t.c, i32([1, 1]), None, ws)
+    assert B.faults(ws) == 0
+
+
+def test_cache_without_utilities():
+    """u and pos are optional: pages, rows and attention without them."""
+    t = Cache([20, 0, 33], layers=2, d=64)
+    c = B.KvQ4Cache(t.shape, t.c.pool, t.c.table, t.c.len, t.c.refs)
+    t.c = c
+    t.fill()
+    B.kv_q4_fork(c, i32([0]), i32([1]), t.ws)
+    keep = torch.ones(3, t.cap, dtype=torch.uint8)
+    keep[0, 3] = keep[1, 19] = keep[2, ::2] = 0
+    before = [[t.values(l, b) for b in range(3)] for l in range(2)]
+    B.kv_q4_compact(c, t.cap, keep.cuda(), t.ws)
+    assert c.len.tolist() == [19, 19, 16]
+    for l in range(2):
+        for b, n in ((0, 19), (1, 19)):
+            origin = list(range(n))
+            if b == 0:
+                origin[3] = 19
+            for x, y in zip(before[l][b], t.values(l, b)):
+                assert np.array_equal(x[:, origin], y)
+        for x, y in zip(before[l][2], t.values(l, 2)):
+            # rows 1, 3, ... stay: of the places before 16 the even ones are filled with rows 17, 19, ...
+            origin = [i if i % 2 else 17 + i for i in range(16)]
+            assert np.array_equal(x[:, origin], y)
+    B.kv_q4_reserve(c, i32([1, 0, 2]), None, t.ws, init="mean")
+    q = torch.randn(2, 3, 4, 64, generator=gen(3)).bfloat16().cuda()
+    o = torch.empty_like(q)
+    B.kv_q4_attend(c, 0, 2, t.cap, q, o, t.ws)
+    t.lens = c.len.tolist()
+    check_attend(t, q, o)
+
+
+def test_first_calls_inside_a_capture():
+    """Kernels that need more LDS than the default limit, met for the first time while a graph is captured."""
+    t = Cache([2000] * 64, layers=1, hq=40, hkv=8, d=64, dtype="f32", page_rows=256, n_pages=600).fill()
+    q = torch.randn(1, 64, 40, 64, generator=gen(3)).cuda()
+    o, s = torch.empty_like(q), torch.empty(1, 64, 1000, device="cuda")
+    t.c.len.fill_(1000)
+    big = Cache([20000], layers=1, hq=1, hkv=1, d=64, page_rows=256)
+    start = snapshot(big.c)
+    budget = i32([777])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        B.kv_q4_attend(t.c, 0, 1, 1000, q, o, t.ws, s_out=s)
+        B.kv_q4_evict(big.c, 20000, budget, big.ws)
+    for _ in range(3):
+        restore(big.c, start)
+        o.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        o2, s2 = torch.empty_like(q), torch.empty_like(s)
+        B.kv_q4_attend(t.c, 0, 1, 1000, q, o2, t.ws, s_out=s2)
+        assert torch.equal(o, o2) and torch.equal(s, s2) and int(big.c.len[0]) == 777
+    assert t.faults() == 0 and big.faults() == 0
+
+
 def test_recency_bias_and_fold():
     """The bias on recent positions, and the fold of two layers at once and of one layer after the other."""
     t = Cache([70, 33, 0], layers=2, hq=8, hkv=2).fill()
@@ -617,14 +740,17 @@ def test_evict_of_long_sequences(n, budget):
     assert c.len.tolist() == [budget] * 3 and B.faults(ws) == 0
 
 
-def test_any_order_of_page_calls():
-    """A few hundred calls drawn at random, checked after each."""
+@pytest.mark.parametrize("page_rows,steps,kw", [(16, 150, dict(layers=1, hkv=1)), (32, 60, dict(layers=2, hkv=3, d=128, dtype="f32")),
+                                                (256, 40, dict(layers=1, hkv=2))])
+def test_any_order_of_page_calls(page_rows, steps, kw):
+    """Calls drawn at random, checked after each."""
     r = np.random.RandomState(11)
-    t = Twin(batch=6, n_pages=26, max_pages=5, layers=1, hkv=1)
-    for step in range(150):
+    t = Twin(batch=6, n_pages=26, max_pages=5, page_rows=page_rows, **kw)
+    most = 25 * page_rows // 16
+    for step in range(steps):
         kind = r.randint(5)
         if kind == 0:
-            t.append([int(x) for x in r.randint(0, 25, 6) * (r.rand(6) < 0.5)], [1000 * step] * 6, ("mean", "min", "zero")[step % 3])
+            t.append([int(x) for x in r.randint(0, most, 6) * (r.rand(6) < 0.5)], [10000 * step] * 6, ("mean", "min", "zero")[step % 3])
             B.kv_fault_status(t.ws, None, clear=True)
         elif kind == 1:
             src, dst = [int(x) for x in r.randint(0, 6, 2)], [int(x) for x in r.randint(0, 6, 2)]
@@ -637,7 +763,7 @@ def test_any_order_of_page_calls():
             t.m.free(slots)
         else:
             t.set_u(step)
-            budget = [int(x) for x in r.randint(0, 60, 6)]
+            budget = [int(x) for x in r.randint(0, 60 * page_rows // 16, 6)]
             keep = [t.m.best(b, n) for b, n in enumerate(budget)]
             B.kv_q4_evict(t.c, t.cap, i32(budget), t.ws)
             t.m.compact(keep)
