@@ -423,8 +423,8 @@ kv_status kv_q4_free(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t
 kv_status kv_q4_compact(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t n_max, const uint8_t* keep, void* ws,
                         size_t ws_bytes, void* stream);
 
-/* Top-B selection and compaction: every slot keeps the budget[b] >= 0 rows first under (u descending, position ascending),
- * all of them when it has no more.  keep_out (nullable, [batch][capacity]) receives the decision over the slot's rows. */
+/* Top-B selection and compaction: every slot keeps the budget[b] >= 0 rows first under (u descending, position ascending, row
+ * ascending), all of them when it has no more.  keep_out (nullable, [batch][capacity]) receives the decision over the slot's rows. */
 kv_status kv_q4_evict(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t n_max, const int32_t* budget,
                       uint8_t* keep_out, void* ws, size_t ws_bytes, void* stream);
 

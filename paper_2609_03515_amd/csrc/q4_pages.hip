@@ -12,6 +12,8 @@
 // 16,384 rows in 8 layers of 8 KV heads: fork 11 us, reserve 7 + 9, eviction to 10%: plan 28, pages 5, moves 48 (some 150 MB,
 // 3 TB/s).  The moves took 112 with one workgroup per slab that found every row's place for itself, and the plan 45 with a prefix
 // sum per 1,024 rows (64 with keys in registers: that unrolls into more code than its instruction fetches are worth).
+#include <limits.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -280,46 +282,69 @@ __global__ __launch_bounds__(kMoveThreads) void q4_free_kernel(Q4PageArgs a) {
 
 // ---- compaction ---------------------------------------------------------------------------------------------
 
-// Eviction order as one number, larger stays: the utility's key, then (the lower position first) the position's complement.
+// Eviction order as one number, larger stays: the utility's key (0 and -0 alike), then (the lower position first) the position
+// turned round.  Of rows that agree in both, which a caller that sets no positions may have, the lower row stays.
 // The rows of a sequence that a selection looks at: their utilities' keys, in LDS where they fit.
 struct Ranked {
     const float* u;
     const int32_t* pos;
     const uint32_t* keys;  // nullable
     int n;
-    __device__ __forceinline__ uint32_t key(int i) const { return keys ? keys[i] : float_key(u[i]); }
-    __device__ __forceinline__ uint64_t full(int i) const { return (uint64_t)key(i) << 32 | (uint32_t)~pos[i]; }
+    __device__ __forceinline__ uint32_t key_of(int i) const { return float_key(u[i] + 0.0f); }
+    __device__ __forceinline__ uint32_t key(int i) const { return keys ? keys[i] : key_of(i); }
+    __device__ __forceinline__ uint32_t turned(int i) const { return (uint32_t)pos[i] ^ 0x7fffffffu; }
+    __device__ __forceinline__ uint64_t full(int i) const { return (uint64_t)key(i) << 32 | turned(i); }
+};
+// Where a selection ends: rows with a larger full key stay, and of those with this one the rows before `limit`.
+struct Border {
+    uint64_t full;
+    int limit;
 };
 
-// The smallest full key above `last`, over the workgroup.
+// The row that leaves next after those of `last`: the smallest full key, and of equal ones the last row.
 template <int kBlock>
-__device__ uint64_t next_key(const Ranked& rows, uint64_t last, uint64_t* lds /* waves */) {
+__device__ Border next_border(const Ranked& rows, Border last, uint64_t* lds64, int* lds /* waves */) {
     uint64_t best = ~0ull;
+    int row = -1;
 #pragma unroll 4
     for (int i = threadIdx.x; i < rows.n; i += kBlock) {
         const uint64_t key = rows.full(i);
-        if (key > last && key < best) best = key;
+        const bool left = key > last.full || (key == last.full && i < last.limit);
+        if (left && (key < best || (key == best && i > row))) {
+            best = key;
+            row = i;
+        }
     }
+    auto take = [&](uint64_t key, int i) __attribute__((always_inline)) {
+        if (key < best || (key == best && i > row)) {
+            best = key;
+            row = i;
+        }
+    };
 #pragma unroll
     for (int o = kWave / 2; o >= 1; o >>= 1) {
-        const uint64_t y = __shfl_xor((unsigned long long)best, o, kWave);
-        best = y < best ? y : best;
+        const uint64_t key = __shfl_xor((unsigned long long)best, o, kWave);
+        take(key, __shfl_xor(row, o, kWave));
     }
     __syncthreads();
-    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = best;
+    if (threadIdx.x % kWave == 0) {
+        lds64[threadIdx.x / kWave] = best;
+        lds[threadIdx.x / kWave] = row;
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kBlock / kWave; ++w) best = lds[w] < best ? lds[w] : best;
-    return best;
+    for (int w = 0; w < kBlock / kWave; ++w) take(lds64[w], lds[w]);
+    return {best, row};
 }
 
-// The `budget`-th largest full key of n > budget >= 1 rows, or a lower one with as many rows at least as large: radix
-// selection from the highest byte, each pass a histogram of the rows that share the bytes chosen so far, until a byte's rows
-// all stay.  Positions are looked at only where utilities tie across the border.  Every thread gets it.
+// The border of the `budget` best of n > budget >= 1 rows, its full key the budget-th largest or a lower one with as many rows
+// at least as large: radix selection from the highest byte, each pass a histogram of the rows that share the bytes chosen so
+// far, until a byte's rows all stay.  Positions are looked at only where utilities tie across the border, and rows counted only
+// where positions do as well.  Every thread gets it.
 template <int kBlock>
-__device__ uint64_t nth_key(const Ranked& rows, int budget, int* hist /* 256 */, int* lds) {
+__device__ Border nth_border(const Ranked& rows, int budget, int* hist /* 256 */, int* lds) {
     __shared__ uint32_t digit_s;
-    __shared__ int left_s, done_s;
+    __shared__ int left_s, done_s, limit_s;
     uint32_t high = 0, low = 0, mask = 0;  // of utility and position: the bytes chosen, and which they are
     int left = budget;
     for (int pass = 0; pass < 8; ++pass) {
@@ -331,7 +356,7 @@ __device__ uint64_t nth_key(const Ranked& rows, int budget, int* hist /* 256 */,
             uint32_t key = rows.key(i);
             bool in = (key & (pass < 4 ? mask : ~0u)) == high;
             if (pass >= 4 && in) {
-                key = ~rows.pos[i];
+                key = rows.turned(i);
                 in = (key & mask) == low;
             }
             *digit = (int)(key >> shift) & 255;
@@ -373,9 +398,19 @@ __device__ uint64_t nth_key(const Ranked& rows, int budget, int* hist /* 256 */,
         else low |= digit_s;
         left = left_s;
         mask |= 255u << shift;
-        if (done_s) break;  // every row that shares these bytes stays
+        if (done_s) return {(uint64_t)high << 32 | low, INT_MAX};  // every row that shares these bytes stays
     }
-    return (uint64_t)high << 32 | low;
+    const uint64_t full = (uint64_t)high << 32 | low;
+    for (int i0 = 0, seen = 0; seen < left; i0 += kBlock) {  // (more than `left` rows have this key)
+        const int i = i0 + (int)threadIdx.x;
+        const bool in = i < rows.n && rows.full(i) == full;
+        int sum;
+        const int at = seen + block_scan<kBlock / kWave>(in, &sum, lds);
+        if (in && at == left - 1) limit_s = i + 1;
+        seen += sum;
+    }
+    __syncthreads();
+    return {full, limit_s};
 }
 
 // Workgroup b: what sequence b keeps, the rows that move, the shared pages that are replaced, and the pages wanted.
@@ -410,7 +445,7 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     if (select && n - budget > kFewEvicted && a.n_max <= kKeysInLds) {
         uint32_t* const keys = reinterpret_cast<uint32_t*>(dynamic + words + (words + 1) / 2);
 #pragma unroll 4
-        for (int i = threadIdx.x; i < rows.n; i += kBlock) keys[i] = float_key(rows.u[i]);
+        for (int i = threadIdx.x; i < rows.n; i += kBlock) keys[i] = rows.key_of(i);
         rows.keys = keys;
     }
     for (int j = threadIdx.x; j < pages; j += kBlock) {
@@ -430,15 +465,16 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
         }
         return;
     }
-    uint64_t least = 0;  // rows with a key of at least this stay
+    Border least{0, INT_MAX};
     if (select) {
         if (n - budget <= kFewEvicted) {
-            for (int i = 0; i < n - budget; ++i) least = next_key<kBlock>(rows, i ? least : 0, lds64);
-            ++least;
+            for (int i = 0; i < n - budget; ++i) least = next_border<kBlock>(rows, least, lds64, lds);
         } else {
-            least = nth_key<kBlock>(rows, budget, hist, lds);
+            least = nth_border<kBlock>(rows, budget, hist, lds);
         }
     }
+    const uint32_t border = (uint32_t)(least.full >> 32), turned = (uint32_t)least.full;
+    const bool all_equal = turned == 0 && least.limit == INT_MAX;  // (then no position has to be read)
     // a bit for every row that stays
     const uint8_t* keep = kEvict ? nullptr : a.keep + (size_t)b * d.cap;
     for (int i0 = 0; i0 < n; i0 += kBlock) {
@@ -446,8 +482,12 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
         bool s = false;
         if (i < n) {
             if constexpr (kEvict) {
-                const uint32_t key = select ? rows.key(i) : 0, border = (uint32_t)(least >> 32);
-                s = budget > 0 && (key > border || (key == border && (!(uint32_t)least || (uint32_t)~rows.pos[i] >= (uint32_t)least)));
+                const uint32_t key = select ? rows.key(i) : 0;
+                s = budget > 0 && key >= border;
+                if (s && key == border && !all_equal) {
+                    const uint32_t t = rows.turned(i);
+                    s = t > turned || (t == turned && i < least.limit);
+                }
                 if (a.keep_out) a.keep_out[(size_t)b * d.cap + i] = s;
             } else {
                 s = keep[i] != 0;

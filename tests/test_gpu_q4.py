@@ -733,6 +733,28 @@ def test_evict_of_long_sequences(n, budget):
         want = np.zeros(n, dtype=np.uint8)
         want[order] = 1
         assert np.array_equal(keep[b, :n].cpu().numpy(), want), b
+
+
+@pytest.mark.parametrize("n,budget", [(5, 2), (100, 97), (100, 40), (5000, 4996), (5000, 4000), (33000, 9000), (140000, 139999)])
+def test_evict_of_rows_that_tie(n, budget):
+    """Rows alike in utility (0 and -0 are) and position, as where a caller sets no positions: exactly `budget` stay, the lower
+    rows; positions below 0 are lower than others."""
+    pages = -(-n // 128) + 1
+    c = B.KvQ4Cache.allocate(B.make_q4_shape(3, 1, 1, 1, 64, 128, 3 * pages, pages, "bf16"))
+    ws = B.q4_workspace(c.shape, n, 1)
+    B.kv_q4_reserve(c, i32([n, n, n]), None, ws)
+    u = torch.tensor([0.0, -0.0, 0.5])[torch.randint(0, 3, (3, n), generator=gen(7))]
+    pos = torch.tensor([-(1 << 31), -3, 0, 2, (1 << 31) - 1], dtype=torch.int32)[torch.randint(0, 5, (3, n), generator=gen(8))]
+    u[1], pos[1] = 0.25, 0  # (all alike)
+    u[2] = 0.0
+    c.u[:, :n], c.pos[:, :n] = u.cuda(), pos.cuda()
+    keep = torch.zeros(3, pages * 128, dtype=torch.uint8, device="cuda")
+    B.kv_q4_evict(c, n, i32([budget] * 3), ws, keep_out=keep)
+    assert c.len.tolist() == [budget] * 3
+    for b in range(3):
+        want = np.zeros(n, dtype=np.uint8)
+        want[np.lexsort((np.arange(n), pos[b].numpy(), -u[b].double().numpy()))[:budget]] = 1
+        assert np.array_equal(keep[b, :n].cpu().numpy(), want), b
         hole, move = np.nonzero(want[:budget] == 0)[0], budget + np.nonzero(want[budget:])[0]
         origin = np.arange(budget)
         origin[hole] = move
