@@ -340,7 +340,7 @@ typedef struct {
     int32_t batch;      /* slots                                                             1..65535           */
     int32_t layers;     /* 1..256                                                                              */
     int32_t n_q_heads;  /* multiple of n_kv_heads, at most 16 times as many                                    */
-    int32_t n_kv_heads;
+    int32_t n_kv_heads; /* at most 65536                                                                       */
     int32_t head_dim;   /* 64 or 128                                                                           */
     int32_t dtype;      /* kv_dtype of queries, outputs and the rows stored and loaded                         */
     int32_t page_rows;  /* 16, 32, 64, 128 or 256                                                              */
@@ -382,7 +382,8 @@ kv_status kv_q4_reserve(const kv_q4_shape* shape, const kv_q4_cache* cache, cons
 /* Stores rows of layers [layer0, layer0 + layer_count): row r < count[b] of k and v becomes row first[b] + r of slot b.
  * count nullable: `rows` of every slot; first nullable: len[b] - count[b], the newest rows (after kv_q4_reserve, with its
  * granted as count).  Rows r >= count[b] are not read.  Rows outside the slot, and rows in pages that other slots share
- * (KV_FAULT_SHARED_PAGE), are not stored. */
+ * (KV_FAULT_SHARED_PAGE), are not stored.  A call takes at most
+ * 2^28 - 256 rows over its layers, slots and KV heads (KV_ERR_UNSUPPORTED; kv_q4_load likewise). */
 kv_status kv_q4_store(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t rows,
                       const int32_t* first, const int32_t* count, const void* k, const kv_q4_strides* k_strides, const void* v,
                       const kv_q4_strides* v_strides, void* ws, size_t ws_bytes, void* stream);
@@ -399,7 +400,9 @@ kv_status kv_q4_load(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t
  * 0 only).  A slot without rows, or longer than n_max (KV_FAULT_CACHE), gets zeros; rows in pages that do not exist
  * (KV_FAULT_CACHE) take no part.  s_out (nullable, [layer_count][batch][n_max]) receives the pooled scores of Eq. 1, 0
  * behind the slot's rows; u_out (nullable, [batch][capacity], may be u_prior) the fold of Eq. 4 over the call's layers
- * in order, u_out = alpha u + (1 - alpha) s from u_prior, for the slot's rows (others are left as they were). */
+ * in order, u_out = alpha u + (1 - alpha) s from u_prior, for the slot's rows (others are left as they were).
+ * Refused (KV_ERR_UNSUPPORTED: take fewer layers a call): layer_count * ceil(n_max / 8192) above 65535, and, where slots are
+ * worked on in parts, layer_count * batch * n_q_heads from 2^23 on. */
 kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t n_max,
                        const void* q, const int32_t* cur_pos, float recency_bias, int32_t recency_window, void* o,
                        float* s_out, float alpha, const float* u_prior, float* u_out, void* ws, size_t ws_bytes,

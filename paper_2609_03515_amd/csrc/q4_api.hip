@@ -15,6 +15,10 @@ static_assert(kFaultCache == (uint32_t)KV_FAULT_CACHE && kFaultNoPages == (uint3
               "fault bits of the kernels and the ABI");
 
 constexpr size_t kFaultBytes = 256;
+// A launch has fewer than 2^32 threads along each extent of its grid, and at most 65535 workgroups along the second and third.
+constexpr int kMostHeads = 1 << 16;
+constexpr double kMostRowItems = (double)(1 << 28) - 256;  // 16 threads a row of the store and the load, in whole workgroups
+constexpr double kMostJoined = (double)(1 << 23) - 1;      // 512 threads a head of the attention's join
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 kv_status hip_status(hipError_t e) { return e == hipSuccess ? KV_OK : KV_ERR_HIP; }
@@ -29,7 +33,7 @@ kv_status check_shape(const kv_q4_shape* s) {
     if (s->n_q_heads % s->n_kv_heads) return KV_ERR_INVALID_ARG;
     if (s->dtype != KV_F32 && s->dtype != KV_BF16) return KV_ERR_UNSUPPORTED;
     if (s->head_dim != 64 && s->head_dim != 128) return KV_ERR_UNSUPPORTED;
-    if (s->n_q_heads / s->n_kv_heads > kMaxGroup) return KV_ERR_UNSUPPORTED;
+    if (s->n_q_heads / s->n_kv_heads > kMaxGroup || s->n_kv_heads > kMostHeads) return KV_ERR_UNSUPPORTED;
     if (s->page_rows < 16 || s->page_rows > 256 || (s->page_rows & (s->page_rows - 1))) return KV_ERR_UNSUPPORTED;
     // row numbers, items of a row (compaction) and the pages wanted by a batch fit 31 bits, and so does every grid
     const double cap = (double)s->max_pages * s->page_rows;
@@ -134,7 +138,7 @@ kv_status check_rows(const kv_q4_shape& s, int layer0, int layer_count, int rows
                      bool written) {
     if (layer0 < 0 || layer_count < 1 || layer_count > s.layers - layer0 || rows < 1) return KV_ERR_INVALID_ARG;
     if (rows > s.max_pages * s.page_rows || !k || !v || !ks || !vs) return KV_ERR_INVALID_ARG;
-    if ((double)layer_count * s.batch * s.n_kv_heads * rows > 2.0e9) return KV_ERR_UNSUPPORTED;
+    if ((double)layer_count * s.batch * s.n_kv_heads * rows > kMostRowItems) return KV_ERR_UNSUPPORTED;
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(first, 4) || !aligned(count, 4)) return KV_ERR_UNSUPPORTED;
     for (const kv_q4_strides* st : {ks, vs})
         for (int64_t x : {st->layer, st->batch, st->head, st->row})
@@ -268,7 +272,8 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
         return KV_ERR_UNSUPPORTED;
     const bool scores = s_out || u_out;
     const AttendLayout L = attend_layout(d, n_max, layer_count, scores);
-    if ((double)layer_count * L.plan.nchunk > 65535.0) return KV_ERR_UNSUPPORTED;  // (the grid's third extent)
+    if ((double)layer_count * L.plan.nchunk > 65535.0) return KV_ERR_UNSUPPORTED;
+    if (L.plan.nchunk > 1 && (double)layer_count * s.batch * s.n_q_heads > kMostJoined) return KV_ERR_UNSUPPORTED;
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
     Q4AttendArgs a{};
     a.dims = d;

@@ -588,8 +588,7 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
     const Q4Dims& d = a.dims;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int waves = blockDim.x / kWave, per = 1 << per_shift, together = 1 << together_shift;  // (layers side by side)
-    const int blocks = (a.n_max + kWave - 1) / kWave;
-    const int b = blockIdx.x / blocks, row = blockIdx.x % blocks * kWave + lane;
+    const int b = blockIdx.y, row = blockIdx.x * kWave + lane;
     const int n = attended(a, b);
     const bool live = row < n;
     const int at = (row & ~15) | (row & 3) << 2 | (row >> 2 & 3);  // place of a row's logits
@@ -600,7 +599,7 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
         float s[kAhead];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) s[q] = 0.0f;
-        if (blockIdx.x % blocks * kWave < n)
+        if ((int)blockIdx.x * kWave < n)
 #pragma unroll 4
             for (int g = (wave & (per - 1)); g < d.hkv; g += per) {
 #pragma unroll
@@ -720,7 +719,7 @@ hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
     const int ahead = ((a.layer_count << per_shift) + waves - 1) / waves;
     auto kern = a.scored ? (ahead == 1 ? q4_score_kernel<true, 1> : ahead == 2 ? q4_score_kernel<true, 2> : q4_score_kernel<true, 4>)
                          : (ahead == 1 ? q4_score_kernel<false, 1> : q4_score_kernel<false, 4>);
-    hipLaunchKernelGGL(kern, dim3(a.dims.batch * blocks), dim3(waves * kWave), 0, s, a, per_shift,
+    hipLaunchKernelGGL(kern, dim3(blocks, a.dims.batch), dim3(waves * kWave), 0, s, a, per_shift,
                        waves_shift - per_shift);
     return hipGetLastError();
 }

@@ -305,6 +305,25 @@ def test_one_long_sequence_among_many():
     check_attend(t, q, o)
 
 
+def test_scores_with_room_for_many_rows():
+    """A call whose n_max, over all slots, is 2^28 rows, 16 waves for 64 of them: the scores of short slots as with a small n_max."""
+    n_max, lens = 1 << 22, [5 + 3 * b for b in range(64)]
+    small = Cache(lens, hq=16, hkv=16, d=64, page_rows=256, max_pages=1).fill()
+    s = B.make_q4_shape(64, 1, 16, 16, 64, 256, small.shape.n_pages, n_max // 256, "bf16")
+    table = torch.full((64, n_max // 256), -1, dtype=torch.int32, device="cuda")
+    table[:, :1] = small.c.table
+    c = B.KvQ4Cache(s, small.c.pool, table, small.c.len, small.c.refs)
+    q = torch.randn(1, 64, 16, 64, generator=gen(9)).to(torch.bfloat16).cuda()
+    o, want_o = torch.empty_like(q), torch.empty_like(q)
+    scores = torch.full((1, 64, n_max), 7.0, device="cuda")
+    want = torch.empty(1, 64, 256, device="cuda")
+    B.kv_q4_attend(small.c, 0, 1, 256, q, want_o, small.ws, s_out=want)
+    ws = B.q4_workspace(s, n_max, 1)
+    B.kv_q4_attend(c, 0, 1, n_max, q, o, ws, s_out=scores)
+    assert torch.equal(scores[:, :, :256], want) and torch.equal(o, want_o)
+    assert not scores[:, :, 256:].any() and B.faults(ws) == 0
+
+
 def test_workspace_serves_smaller_calls():
     """A workspace for n_max rows and all layers takes every call on fewer of either, whatever way those are divided."""
     t = Cache([1500, 3], layers=5, hq=4, hkv=2, page_rows=64).fill()

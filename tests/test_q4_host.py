@@ -131,6 +131,23 @@ def test_page_refusals():
     assert call("kv_q4_evict", 10, FAKE, None, c=buffers(pos=None)) == INVALID
 
 
+def test_grid_limits():
+    """Calls whose grids a launch cannot have are refused; the largest that it can have get as far as the workspace's check."""
+    for n, status in ((65536, WORKSPACE), (65537, UNSUPPORTED)):
+        assert call("kv_q4_free", 1, FAKE, s=shape(n_q_heads=n, n_kv_heads=n), ws=None) == status
+    long = shape(batch=1, layers=128, n_q_heads=2, max_pages=1 << 15)
+    for name in ("kv_q4_store", "kv_q4_load"):
+        for rows, status in (((1 << 20) - 1, WORKSPACE), (1 << 20, UNSUPPORTED)):
+            assert call(name, 0, 128, rows, None, None, FAKE, STRIDES, FAKE, STRIDES, s=long, ws=None) == status
+    def attend(s, layers, n):
+        return call("kv_q4_attend", 0, layers, n, FAKE, None, 0.0, 0, FAKE, None, 0.0, None, None, s=s, ws=None)
+    very_long = shape(batch=1, layers=256, n_q_heads=2, max_pages=1 << 22)
+    assert attend(very_long, 3, 1 << 27) == WORKSPACE and attend(very_long, 4, 1 << 27) == UNSUPPORTED
+    wide = shape(batch=1 << 13, layers=64, n_q_heads=16, n_kv_heads=16, max_pages=300)
+    assert attend(wide, 63, 8193) == WORKSPACE and attend(wide, 64, 8193) == UNSUPPORTED
+    assert attend(wide, 64, 8192) == WORKSPACE  # (one chunk each: nothing is joined)
+
+
 def host_cache(**kw):
     return B.KvQ4Cache.allocate(shape(**kw), device="cpu")
 
