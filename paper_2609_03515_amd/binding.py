@@ -433,10 +433,10 @@ def _q4_ok(t, dtype, numel, device):
 
 
 def _q4_stream(fn, cache, ws, stream):
-    """The stream of a call: its workspace has to lie with the cache, and the cache on the current device."""
+    """The stream of a call: its workspace has to lie with the cache, and the cache on the current device, a GPU."""
     dev = cache._device
-    if (ws is not None and (ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous())) or (
-            dev >= 0 and dev != (torch.cuda.current_device() if _device is None else _device())):
+    if dev < 0 or (ws is not None and (ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous())) or (
+            dev != (torch.cuda.current_device() if _device is None else _device())):
         raise KVError(fn, KV_ERR_INVALID_ARG)
     return _stream(stream)
 
@@ -458,7 +458,7 @@ def kv_q4_reserve(cache: KvQ4Cache, add, new_pos, ws, granted=None, init="mean",
     n, dev = cache._batch, cache._device
     if not (_q4_ok(add, torch.int32, n, dev) and _q4_ok(new_pos, torch.int32, n, dev) and _q4_ok(granted, torch.int32, n, dev)):
         raise KVError("kv_q4_reserve", KV_ERR_INVALID_ARG)
-    mode = {"mean": KV_INIT_MEAN, "min": KV_INIT_MIN, "zero": KV_INIT_ZERO}[init] if isinstance(init, str) else int(init)
+    mode = {"mean": KV_INIT_MEAN, "min": KV_INIT_MIN, "zero": KV_INIT_ZERO}.get(init, -1) if isinstance(init, str) else int(init)
     st = _q4_stream("kv_q4_reserve", cache, ws, stream)
     _check("kv_q4_reserve", load_library().kv_q4_reserve(cache._shape, cache._buffers, _ptr(add), _ptr(new_pos), mode,
                                                          _ptr(granted), _ptr(ws), _ws_bytes(ws), st))

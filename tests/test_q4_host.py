@@ -180,6 +180,22 @@ def test_binding_checks_its_tensors():
         assert e.value.status == INVALID, i
 
 
+def test_host_memory_is_refused():
+    """A cache, or tensors, in host memory never reach a kernel."""
+    c, ws = host_cache(), torch.zeros(1 << 22, dtype=torch.uint8)
+    n = torch.zeros(3, dtype=torch.int32)
+    kv = torch.zeros(4, 3, 2, 5, 128, dtype=torch.bfloat16)
+    q = torch.zeros(4, 3, 8, 128, dtype=torch.bfloat16)
+    keep = torch.zeros(3, 320, dtype=torch.uint8)
+    for f in (lambda: B.kv_q4_reserve(c, n, n, ws), lambda: B.kv_q4_store(c, 0, 4, 5, kv, kv, ws),
+              lambda: B.kv_q4_load(c, 0, 4, 5, kv, kv, ws), lambda: B.kv_q4_attend(c, 0, 4, 10, q, q, ws),
+              lambda: B.kv_q4_fork(c, n, n, ws), lambda: B.kv_q4_free(c, n, ws), lambda: B.kv_q4_compact(c, 10, keep, ws),
+              lambda: B.kv_q4_evict(c, 10, n, ws)):
+        with pytest.raises(B.KVError) as e:
+            f()
+        assert e.value.status == INVALID
+
+
 def test_reference_quantiser():
     """The reference's two forms agree, and its error is within half the distance of the neighbouring levels."""
     r = np.random.RandomState(3)
