@@ -9,9 +9,10 @@
 // the table or the lengths that its own workgroups change.
 //
 // Small calls are launches and chains of dependent loads (2.5 to 8 us a kernel); measured on six samples of prompts of 12,000 to
-// 16,384 rows in 8 layers of 8 KV heads: fork 11 us, reserve 7 + 9, eviction to 10%: plan 28, pages 5, moves 48 (some 150 MB,
-// 3 TB/s).  The moves took 112 with one workgroup per slab that found every row's place for itself, and the plan 45 with a prefix
-// sum per 1,024 rows (64 with keys in registers: that unrolls into more code than its instruction fetches are worth).
+// 16,384 rows in 8 layers of 8 KV heads: fork 5.4 us, reserve 6.5 + 8.5, eviction to 10%: plan 21.6, pages 5, moves 48 (some
+// 150 MB, 3 TB/s).  The moves took 112 with one workgroup per slab that found every row's place for itself; the plan 45 with a
+// prefix sum per 1,024 rows (64 with keys in registers: that unrolls into more code than its instruction fetches are worth), and 28
+// with one histogram and with pointers that could be LDS or memory; the fork 10.4 copying 4 bytes a thread.
 #include <limits.h>
 
 #include <atomic>
@@ -58,6 +59,8 @@ __device__ __forceinline__ int block_scan(int x, int* total, int* lds /* kWaves 
 
 __device__ __forceinline__ bool in_pool(const Q4Dims& d, int page) { return (uint32_t)page < (uint32_t)d.n_pages; }
 __device__ __forceinline__ int pages_of(const Q4Dims& d, int rows) { return (rows + d.page_rows - 1) >> d.page_shift; }
+
+__device__ __forceinline__ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // The pages for `need`: their places in `fresh` by a prefix sum over the sequences, and `fresh` filled with the lowest free
 // pages.  A sequence whose places lie past the last free page is not granted (offset -1).  One workgroup.
@@ -179,9 +182,18 @@ __global__ __launch_bounds__(kMoveThreads) void q4_reserve_kernel(Q4PageArgs a) 
         __shared__ double part[kMoveThreads / kWave];
         __shared__ float prior;
         double x = a.init_mode == 2 ? (double)INFINITY : 0.0;
-        if (a.init_mode != 0)
+        auto take = [&](float y) __attribute__((always_inline)) { x = a.init_mode == 1 ? x + y : fmin(x, (double)y); };
+        if (a.init_mode != 0) {
+            const int quads = aligned16(u) ? len / 4 : 0;
 #pragma unroll 8
-            for (int i = threadIdx.x; i < len; i += kMoveThreads) x = a.init_mode == 1 ? x + u[i] : fmin(x, (double)u[i]);
+            for (int i = threadIdx.x; i < quads; i += kMoveThreads) {
+                const f32x4 y = reinterpret_cast<const f32x4*>(u)[i];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) take(y[k]);
+            }
+#pragma unroll 4
+            for (int i = quads * 4 + threadIdx.x; i < len; i += kMoveThreads) take(u[i]);
+        }
 #pragma unroll
         for (int o = kWave / 2; o >= 1; o >>= 1) {
             const double y = __shfl_xor(x, o, kWave);
@@ -201,6 +213,23 @@ __global__ __launch_bounds__(kMoveThreads) void q4_reserve_kernel(Q4PageArgs a) 
 }
 
 // ---- fork, free ---------------------------------------------------------------------------------------------
+
+// n words (of a slot's utilities or positions) from one place to another, by the whole workgroup: 16 bytes a thread where they are
+// aligned (slots are then too), four loads of a thread together.
+__device__ __forceinline__ void copy_words(const uint32_t* from, uint32_t* to, int n) {
+    constexpr int kTogether = 4;
+    const int quads = aligned16(from) && aligned16(to) ? n / 4 : 0;
+    for (int j0 = threadIdx.x; j0 < quads; j0 += kThreads * kTogether) {
+        u32x4 x[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) x[k] = reinterpret_cast<const u32x4*>(from)[min(j0 + k * kThreads, quads - 1)];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k)
+            if (j0 + k * kThreads < quads) reinterpret_cast<u32x4*>(to)[j0 + k * kThreads] = x[k];
+    }
+#pragma unroll 4
+    for (int j = quads * 4 + threadIdx.x; j < n; j += kThreads) to[j] = from[j];
+}
 
 // Workgroup i: sequence dst[i] becomes a copy of src[i] that shares its pages.  Refused, and reported: a slot out of range, a
 // destination that is not empty or is named twice (after the first time), a source that is a destination of the call.
@@ -240,12 +269,9 @@ __global__ __launch_bounds__(kThreads) void q4_fork_kernel(Q4PageArgs a) {
         dt[j] = page;
         if (j < pages) atomicAdd(&a.cache.refs[page], 1);
     }
-    if (a.cache.u)
-#pragma unroll 8
-        for (int j = threadIdx.x; j < len; j += kThreads) a.cache.u[(size_t)dst * d.cap + j] = a.cache.u[(size_t)src * d.cap + j];
-    if (a.cache.pos)
-#pragma unroll 8
-        for (int j = threadIdx.x; j < len; j += kThreads) a.cache.pos[(size_t)dst * d.cap + j] = a.cache.pos[(size_t)src * d.cap + j];
+    const size_t from = (size_t)src * d.cap, to = (size_t)dst * d.cap;
+    if (a.cache.u) copy_words(reinterpret_cast<const uint32_t*>(a.cache.u) + from, reinterpret_cast<uint32_t*>(a.cache.u) + to, len);
+    if (a.cache.pos) copy_words(reinterpret_cast<const uint32_t*>(a.cache.pos) + from, reinterpret_cast<uint32_t*>(a.cache.pos) + to, len);
     if (threadIdx.x == 0) a.cache.len[dst] = len;
 }
 
@@ -282,16 +308,23 @@ __global__ __launch_bounds__(kMoveThreads) void q4_free_kernel(Q4PageArgs a) {
 
 // ---- compaction ---------------------------------------------------------------------------------------------
 
+typedef __attribute__((address_space(3))) uint32_t* lds_words;
+typedef __attribute__((address_space(3))) uint64_t* lds_masks;
+
 // Eviction order as one number, larger stays: the utility's key (0 and -0 alike), then (the lower position first) the position
 // turned round.  Of rows that agree in both, which a caller that sets no positions may have, the lower row stays.
-// The rows of a sequence that a selection looks at: their utilities' keys, in LDS where they fit.
+// The rows of a sequence that a selection looks at (kInLds: their utilities' keys are in LDS).
+template <bool kInLds>
 struct Ranked {
     const float* u;
     const int32_t* pos;
-    const uint32_t* keys;  // nullable
+    lds_words keys;
     int n;
     __device__ __forceinline__ uint32_t key_of(int i) const { return float_key(u[i] + 0.0f); }
-    __device__ __forceinline__ uint32_t key(int i) const { return keys ? keys[i] : key_of(i); }
+    __device__ __forceinline__ uint32_t key(int i) const {
+        if constexpr (kInLds) return keys[i];
+        else return key_of(i);
+    }
     __device__ __forceinline__ uint32_t turned(int i) const { return (uint32_t)pos[i] ^ 0x7fffffffu; }
     __device__ __forceinline__ uint64_t full(int i) const { return (uint64_t)key(i) << 32 | turned(i); }
 };
@@ -302,8 +335,8 @@ struct Border {
 };
 
 // The row that leaves next after those of `last`: the smallest full key, and of equal ones the last row.
-template <int kBlock>
-__device__ Border next_border(const Ranked& rows, Border last, uint64_t* lds64, int* lds /* waves */) {
+template <int kBlock, bool kInLds>
+__device__ Border next_border(const Ranked<kInLds>& rows, Border last, uint64_t* lds64, int* lds /* waves */) {
     uint64_t best = ~0ull;
     int row = -1;
 #pragma unroll 4
@@ -340,9 +373,13 @@ __device__ Border next_border(const Ranked& rows, Border last, uint64_t* lds64, 
 // The border of the `budget` best of n > budget >= 1 rows, its full key the budget-th largest or a lower one with as many rows
 // at least as large: radix selection from the highest byte, each pass a histogram of the rows that share the bytes chosen so
 // far, until a byte's rows all stay.  Positions are looked at only where utilities tie across the border, and rows counted only
-// where positions do as well.  Every thread gets it.
+// where positions do as well.  Every thread gets it.  Utilities share their leading bits, and additions to one LDS word go one
+// by one: kHists histograms, by lane.
 template <int kBlock>
-__device__ Border nth_border(const Ranked& rows, int budget, int* hist /* 256 */, int* lds) {
+constexpr int kHistsOf = kBlock / 64;  // (16, or 4 where there are fewer threads to clear and add them)
+template <int kBlock, bool kInLds>
+__device__ Border nth_border(const Ranked<kInLds>& rows, int budget, int* hist /* 256 * kHists */, int* lds) {
+    constexpr int kHists = kHistsOf<kBlock>;
     __shared__ uint32_t digit_s;
     __shared__ int left_s, done_s, limit_s;
     uint32_t high = 0, low = 0, mask = 0;  // of utility and position: the bytes chosen, and which they are
@@ -350,7 +387,7 @@ __device__ Border nth_border(const Ranked& rows, int budget, int* hist /* 256 */
     for (int pass = 0; pass < 8; ++pass) {
         const int shift = 24 - pass % 4 * 8;
         if (pass == 4) mask = 0;
-        if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+        for (int i = threadIdx.x; i < 256 * kHists; i += kBlock) hist[i] = 0;
         __syncthreads();
         auto digit_of = [&](int i, int* digit) __attribute__((always_inline)) {  // and whether the row is still looked at
             uint32_t key = rows.key(i);
@@ -362,30 +399,18 @@ __device__ Border nth_border(const Ranked& rows, int budget, int* hist /* 256 */
             *digit = (int)(key >> shift) & 255;
             return in;
         };
-        if (pass == 0) {
-            // utilities share their leading bits: the rows of a wave that agree with its first one count once
-            for (int i0 = 0; i0 < rows.n; i0 += kBlock) {
-                const int i = i0 + (int)threadIdx.x;
-                int digit = 0;
-                const bool in = i < rows.n && digit_of(i, &digit);
-                const uint64_t live = __ballot(in);
-                if (!live) continue;
-                const int lead = __ffsll((unsigned long long)live) - 1, first = __builtin_amdgcn_readlane(digit, lead);
-                const uint64_t same = __ballot(in && digit == first);
-                if (in && digit != first) atomicAdd(&hist[digit], 1);
-                if ((int)(threadIdx.x % kWave) == lead) atomicAdd(&hist[first], __popcll(same));
-            }
-        } else {
 #pragma unroll 4
-            for (int i = threadIdx.x; i < rows.n; i += kBlock) {
-                int digit;
-                if (digit_of(i, &digit)) atomicAdd(&hist[digit], 1);
-            }
+        for (int i = threadIdx.x; i < rows.n; i += kBlock) {
+            int digit;
+            if (digit_of(i, &digit)) atomicAdd(&hist[digit * kHists + threadIdx.x % kHists], 1);
         }
         __syncthreads();
         // the byte that holds the left-th row from the top: threads 0 .. 255 hold the digits from 255 down
         const int digit = 255 - (int)threadIdx.x;
-        const int c = threadIdx.x < 256 ? hist[digit] : 0;
+        int c = 0;
+        if (threadIdx.x < 256)
+#pragma unroll
+            for (int k = 0; k < kHists; ++k) c += hist[digit * kHists + k];
         int total;
         const int above = block_scan<kBlock / kWave>(c, &total, lds);
         if (threadIdx.x < 256 && above < left && above + c >= left) {
@@ -418,13 +443,13 @@ __device__ Border nth_border(const Ranked& rows, int budget, int* hist /* 256 */
 // is hole i - K(i), a kept row behind it the (K(i) - K(end))-th that moves, and a page has a hole when its rows number more than
 // K grows over it.
 constexpr int kFewEvicted = 4;      // so few are found one after the other
-constexpr int kKeysInLds = 32768, kWordsInLds = 2048;  // rows, and words of 64 of them
-template <bool kEvict, int kBlock>
+constexpr int kRowsInLds = 32768;   // masks, prefix sums and keys of so many rows lie in LDS (kInLds), of more in memory
+template <bool kEvict, int kBlock, bool kInLds>
 __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     constexpr int kWaves = kBlock / kWave;
     __shared__ int lds[kWaves + 1];
     __shared__ uint64_t lds64[kWaves];
-    __shared__ int hist[256];
+    __shared__ int hist[kEvict ? 256 * kHistsOf<kBlock> : 1];
     extern __shared__ uint64_t dynamic[];  // masks and their prefix sums, then the keys
     const Q4Dims& d = a.dims;
     const int b = blockIdx.x, n = a.cache.len[b], lane = threadIdx.x % kWave;
@@ -434,20 +459,23 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     int32_t* replaced = a.w.replaced + (size_t)b * d.max_pages;
     const size_t words = ((size_t)a.n_max + 63) / 64;
     uint64_t* const mask_out = a.w.mask + b * words;
-    const bool masks_in_lds = words <= kWordsInLds;
-    uint64_t* const mask = masks_in_lds ? dynamic : mask_out;
-    int32_t* const prefix = masks_in_lds ? reinterpret_cast<int32_t*>(dynamic + words) : a.w.prefix + b * words;
+    auto* const mask = [&] {
+        if constexpr (kInLds) return (lds_masks)dynamic;
+        else return mask_out;
+    }();
+    auto* const prefix = [&] {
+        if constexpr (kInLds) return (lds_words)(dynamic + words);
+        else return a.w.prefix + b * words;
+    }();
     const int budget = kEvict ? a.budget[b] : 0;
     int bad = n < 0 || n > a.n_max || budget < 0;
     const int pages = bad ? 0 : pages_of(d, n);
-    Ranked rows{a.cache.u + (size_t)b * d.cap, a.cache.pos + (size_t)b * d.cap, nullptr, bad ? 0 : n};
+    const Ranked<kInLds> rows{a.cache.u + (size_t)b * d.cap, a.cache.pos + (size_t)b * d.cap,
+                              (lds_words)(dynamic + words + (words + 1) / 2), bad ? 0 : n};
     const bool select = kEvict && budget > 0 && budget < n;
-    if (select && n - budget > kFewEvicted && a.n_max <= kKeysInLds) {
-        uint32_t* const keys = reinterpret_cast<uint32_t*>(dynamic + words + (words + 1) / 2);
+    if (kInLds && select)
 #pragma unroll 4
-        for (int i = threadIdx.x; i < rows.n; i += kBlock) keys[i] = rows.key_of(i);
-        rows.keys = keys;
-    }
+        for (int i = threadIdx.x; i < rows.n; i += kBlock) rows.keys[i] = rows.key_of(i);
     for (int j = threadIdx.x; j < pages; j += kBlock) {
         const int page = table[j];
         const int refs = in_pool(d, page) ? a.cache.refs[page] : 0;
@@ -468,9 +496,9 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     Border least{0, INT_MAX};
     if (select) {
         if (n - budget <= kFewEvicted) {
-            for (int i = 0; i < n - budget; ++i) least = next_border<kBlock>(rows, least, lds64, lds);
+            for (int i = 0; i < n - budget; ++i) least = next_border<kBlock, kInLds>(rows, least, lds64, lds);
         } else {
-            least = nth_border<kBlock>(rows, budget, hist, lds);
+            least = nth_border<kBlock, kInLds>(rows, budget, hist, lds);
         }
     }
     const uint32_t border = (uint32_t)(least.full >> 32), turned = (uint32_t)least.full;
@@ -496,7 +524,7 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
         const uint64_t m = __ballot(s);
         if (lane == 0 && i < n) {
             mask[i >> 6] = m;
-            if (masks_in_lds) mask_out[i >> 6] = m;
+            if (kInLds) mask_out[i >> 6] = m;
         }
     }
     __syncthreads();
@@ -688,14 +716,14 @@ hipError_t launch_q4_free(const Q4PageArgs& a, hipStream_t s) {
 }
 
 namespace {
-template <bool kEvict, int kBlock>
+template <bool kEvict, int kBlock, bool kInLds>
 hipError_t launch_plan(const Q4PageArgs& a, hipStream_t s) {
-    auto kern = q4_compact_plan_kernel<kEvict, kBlock>;
+    auto kern = q4_compact_plan_kernel<kEvict, kBlock, kInLds>;
     const size_t words = ((size_t)a.n_max + 63) / 64;
-    size_t lds = words <= (size_t)kWordsInLds ? (words + (words + 1) / 2) * sizeof(uint64_t) : 0;
-    if (kEvict && a.n_max <= kKeysInLds) lds += (size_t)a.n_max * sizeof(uint32_t);
-    if (lds > 60 * 1024) {
-        constexpr int kMost = kKeysInLds * 4 + kWordsInLds * 12;
+    size_t lds = kInLds ? (words + (words + 1) / 2) * sizeof(uint64_t) : 0;
+    if (kInLds && kEvict) lds += (size_t)a.n_max * sizeof(uint32_t);
+    if (lds > 40 * 1024) {  // (beside the 16 KB of the histograms)
+        constexpr int kMost = kRowsInLds * 4 + kRowsInLds / 64 * 12;
         static std::atomic<bool> raised[64];
         int dev = 0;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
@@ -708,12 +736,16 @@ hipError_t launch_plan(const Q4PageArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(kern, dim3(a.dims.batch), dim3(kBlock), lds, s, a);
     return hipGetLastError();
 }
+template <bool kEvict>
+hipError_t launch_plan_by_rows(const Q4PageArgs& a, hipStream_t s) {
+    // (short sequences: fewer waves to wait for at every step)
+    if (a.n_max <= 1024) return launch_plan<kEvict, 256, true>(a, s);
+    return a.n_max <= kRowsInLds ? launch_plan<kEvict, kThreads, true>(a, s) : launch_plan<kEvict, kThreads, false>(a, s);
+}
 }  // namespace
 
 hipError_t launch_q4_compact(const Q4PageArgs& a, hipStream_t s) {
-    // (short sequences: fewer waves to wait for at every step)
-    hipError_t e = a.n_max <= 1024 ? (a.budget ? launch_plan<true, 256>(a, s) : launch_plan<false, 256>(a, s))
-                                   : (a.budget ? launch_plan<true, kThreads>(a, s) : launch_plan<false, kThreads>(a, s));
+    hipError_t e = a.budget ? launch_plan_by_rows<true>(a, s) : launch_plan_by_rows<false>(a, s);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(q4_grant_kernel, dim3(1), dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
