@@ -9,8 +9,9 @@
 // the table or the lengths that its own workgroups change.
 //
 // Small calls are launches and chains of dependent loads (2.5 to 8 us a kernel); measured on six samples of prompts of 12,000 to
-// 16,384 rows in 8 layers of 8 KV heads: fork 5.4 us, reserve 6.5 + 8.5, eviction to 10%: plan 21.6, pages 5, moves 48 (some
-// 150 MB, 3 TB/s).  The moves took 112 with one workgroup per slab that found every row's place for itself; the plan 45 with a
+// 16,384 rows in 8 layers of 8 KV heads: fork 5.4 us, reserve 6.5 + 8.5, eviction to 10%: plan 21.6, pages 5, moves 45 (142 MB
+// by the memory's counters, in pieces of 64 and 4 bytes: 3.2 TB/s).  The moves took 112 with one workgroup per slab that found every
+// row's place for itself, and 48 (one row of each of 256 slabs: 14.7, now 11.3) with the places found between the copies; the plan 45 with a
 // prefix sum per 1,024 rows (64 with keys in registers: that unrolls into more code than its instruction fetches are worth), and 28
 // with one histogram and with pointers that could be LDS or memory; the fork 10.4 copying 4 bytes a thread.
 #include <limits.h>
@@ -582,21 +583,70 @@ __global__ __launch_bounds__(kThreads) void q4_grant_kernel(Q4PageArgs a) {
     grant(a, lds);
 }
 
-// Workgroup (part, layer, b): every parts-th kEntries of the sequence's entries, in one layer; the first of a sequence also changes
-// its state.  Entries are the holes, then the rows of the replaced pages (those that are holes, or behind the end, are none).
-// Their places are found once for all KV heads; four copies of a thread are in flight together.
-constexpr int kEntries = 16;
+// What changes in a sequence's state: utilities and positions of the rows that move, table, counts and length.
+__device__ void move_state(const Q4PageArgs& a, int b, int kept, int moves, int offset) {
+    constexpr int kTogether = 4;
+    const Q4Dims& d = a.dims;
+    const int32_t* dst = a.w.dst + (size_t)b * a.n_max;
+    const int32_t* src = a.w.src + (size_t)b * a.n_max;
+    const int32_t* rank = a.w.rank + (size_t)b * d.max_pages;
+    const int32_t* old = a.w.old_table + (size_t)b * d.max_pages;
+    const int threads = (int)blockDim.x;
+    for (int m0 = threadIdx.x; m0 < moves; m0 += threads * kTogether) {
+        int to[kTogether];
+        float u[kTogether];
+        int32_t pos[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const int m = min(m0 + k * threads, moves - 1), from = src[m];
+            to[k] = dst[m];
+            if (a.cache.u) u[k] = a.cache.u[(size_t)b * d.cap + from];
+            if (a.cache.pos) pos[k] = a.cache.pos[(size_t)b * d.cap + from];
+        }
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            if (m0 + k * threads >= moves) break;
+            if (a.cache.u) a.cache.u[(size_t)b * d.cap + to[k]] = u[k];
+            if (a.cache.pos) a.cache.pos[(size_t)b * d.cap + to[k]] = pos[k];
+        }
+    }
+    const int end = pages_of(d, kept), had = pages_of(d, a.cache.len[b]);
+    int32_t* table = a.cache.table + (size_t)b * d.max_pages;
+    uint32_t fault = 0;
+    for (int j = threadIdx.x; j < had; j += threads) {
+        const bool copied = j < end && rank[j] >= 0;
+        if (j < end && !copied) continue;
+        fault |= release(a, old[j]);
+        const int page = copied ? a.w.fresh[offset + rank[j]] : -1;
+        table[j] = page;
+        if (copied) a.cache.refs[page] = 1;
+    }
+    if (fault) atomicOr(a.faults, fault);
+    __syncthreads();  // (every thread has read the length)
+    if (threadIdx.x == 0) a.cache.len[b] = kept;
+}
+
+// Workgroup (part, layer + 1, b): every parts-th kEntries of the sequence's entries, in one layer; (0, 0, b): the sequence's state.
+// Entries are the holes, then the rows of the replaced pages (those that are holes, or behind the end, are none).  Their places,
+// chains of loads, are found once for all KV heads by a wave of its own, one round ahead of the others' copies; four copies of a
+// thread are in flight together.
+constexpr int kEntries = 16, kMoveBlock = kMoveThreads + kWave;
 template <int D>
-__global__ __launch_bounds__(kMoveThreads) void q4_move_kernel(Q4PageArgs a) {
+__global__ __launch_bounds__(kMoveBlock) void q4_move_kernel(Q4PageArgs a) {
     constexpr int kPieces = D / 32, kTogether = 4;  // 16-byte pieces of a row's codes; copies at a time
     typedef typename std::conditional<D == 128, uint32_t, uint16_t>::type scales_t;  // a row's scales
-    __shared__ uint32_t place[2][kEntries];         // page * page_rows + row in the page: from, to
-    __shared__ int entries_s;
+    __shared__ uint32_t place_s[2][2][kEntries];    // of every other round: page * page_rows + row in the page: from, to
+    __shared__ int entries_s[2];
     const Q4Dims& d = a.dims;
-    const int b = blockIdx.z, layer = blockIdx.y, part = blockIdx.x;
+    const int b = blockIdx.z, layer = (int)blockIdx.y - 1, part = blockIdx.x;
+    if (layer < 0 && part > 0) return;
     const int kept = a.w.rows[b], offset = a.w.offset[b];
     if (kept < 0 || offset < 0) return;
     const int moves = a.w.moves[b], all = moves + a.w.need[b] * d.page_rows;
+    if (layer < 0) {
+        move_state(a, b, kept, moves, offset);
+        return;
+    }
     const int32_t* dst = a.w.dst + (size_t)b * a.n_max;
     const int32_t* src = a.w.src + (size_t)b * a.n_max;
     const int32_t* rank = a.w.rank + (size_t)b * d.max_pages;
@@ -605,31 +655,39 @@ __global__ __launch_bounds__(kMoveThreads) void q4_move_kernel(Q4PageArgs a) {
     const uint64_t* mask = a.w.mask + b * (((size_t)a.n_max + 63) / 64);
     const int in = d.page_rows - 1;
     const size_t layer0 = q4_record(d, layer, 0, 0);
-    for (int m0 = part * kEntries; m0 < all; m0 += gridDim.x * kEntries) {
-        __syncthreads();  // (the places before these are no longer read)
-        if (threadIdx.x < kWave) {
-            const int m = m0 + (int)threadIdx.x;
-            bool is = threadIdx.x < kEntries && m < all;
-            int from = 0, to = 0;
-            if (is && m < moves) {
-                from = src[m];
-                to = dst[m];
-            } else if (is) {
-                from = to = (replaced[(m - moves) >> d.page_shift] << d.page_shift) + ((m - moves) & in);
-                is = to < kept && (mask[to >> 6] >> (to & 63) & 1u);
-            }
-            const uint64_t live = __ballot(is);
-            if (is) {
-                const int r = rank[to >> d.page_shift];
-                const int page = r >= 0 ? a.w.fresh[offset + r] : old[to >> d.page_shift];
-                const int e = __popcll(live & ((1ull << threadIdx.x) - 1));
-                place[0][e] = ((uint32_t)old[from >> d.page_shift] << d.page_shift) + (from & in);
-                place[1][e] = ((uint32_t)page << d.page_shift) + (to & in);
-            }
-            if (threadIdx.x == 0) entries_s = __popcll(live);
+    auto find = [&](int m0, int buf) __attribute__((always_inline)) {  // by one wave
+        const int lane = threadIdx.x % kWave, m = m0 + lane;
+        bool is = lane < kEntries && m < all;
+        int from = 0, to = 0;
+        if (is && m < moves) {
+            from = src[m];
+            to = dst[m];
+        } else if (is) {
+            from = to = (replaced[(m - moves) >> d.page_shift] << d.page_shift) + ((m - moves) & in);
+            is = to < kept && (mask[to >> 6] >> (to & 63) & 1u);
         }
+        const uint64_t live = __ballot(is);
+        if (is) {
+            const int r = rank[to >> d.page_shift];
+            const int page = r >= 0 ? a.w.fresh[offset + r] : old[to >> d.page_shift];
+            const int e = __popcll(live & ((1ull << lane) - 1));
+            place_s[buf][0][e] = ((uint32_t)old[from >> d.page_shift] << d.page_shift) + (from & in);
+            place_s[buf][1][e] = ((uint32_t)page << d.page_shift) + (to & in);
+        }
+        if (lane == 0) entries_s[buf] = __popcll(live);
+    };
+    const bool finder = threadIdx.x >= kMoveThreads;
+    const int step = gridDim.x * kEntries;
+    if (finder) find(part * kEntries, 0);
+    int buf = 0;
+    for (int m0 = part * kEntries; m0 < all; m0 += step, buf ^= 1) {
         __syncthreads();
-        const int entries = entries_s;
+        if (finder) {
+            if (m0 + step < all) find(m0 + step, buf ^ 1);
+            continue;
+        }
+        const uint32_t(&place)[2][kEntries] = place_s[buf];
+        const int entries = entries_s[buf];
         auto record = [&](int which, int m, int g, int* row) __attribute__((always_inline)) {
             const uint32_t p = place[which][m];
             *row = p & in;
@@ -673,26 +731,6 @@ __global__ __launch_bounds__(kMoveThreads) void q4_move_kernel(Q4PageArgs a) {
             *reinterpret_cast<scales_t*>(to) = y;
         }
     }
-    if (layer != 0 || part != 0) return;
-    for (int m = threadIdx.x; m < moves; m += kMoveThreads) {
-        const int to = dst[m], from = src[m];
-        if (a.cache.u) a.cache.u[(size_t)b * d.cap + to] = a.cache.u[(size_t)b * d.cap + from];
-        if (a.cache.pos) a.cache.pos[(size_t)b * d.cap + to] = a.cache.pos[(size_t)b * d.cap + from];
-    }
-    const int end = pages_of(d, kept), had = pages_of(d, a.cache.len[b]);
-    int32_t* table = a.cache.table + (size_t)b * d.max_pages;
-    uint32_t fault = 0;
-    for (int j = threadIdx.x; j < had; j += kMoveThreads) {
-        const bool copied = j < end && rank[j] >= 0;
-        if (j < end && !copied) continue;
-        fault |= release(a, old[j]);
-        const int page = copied ? a.w.fresh[offset + rank[j]] : -1;
-        table[j] = page;
-        if (copied) a.cache.refs[page] = 1;
-    }
-    if (fault) atomicOr(a.faults, fault);
-    __syncthreads();  // (every thread has read the length)
-    if (threadIdx.x == 0) a.cache.len[b] = kept;
 }
 
 }  // namespace
@@ -749,12 +787,13 @@ hipError_t launch_q4_compact(const Q4PageArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(q4_grant_kernel, dim3(1), dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    // parts of a sequence's rows: eight workgroups per CU in all, no more than there can be entries for
+    // parts of a sequence's rows: four workgroups per CU in all, no more than there can be entries for (two 52 us, three 46.5, four
+    // 44.8, six 47.6 in the case above)
     const int slabs = a.dims.layers * a.dims.batch, most = (a.n_max + kEntries - 1) / kEntries;
-    const int want = (8 * 256 + slabs - 1) / slabs, parts = want < most ? want : most;
-    const dim3 grid(parts, a.dims.layers, a.dims.batch);
-    if (a.dims.d == 128) hipLaunchKernelGGL(q4_move_kernel<128>, grid, dim3(kMoveThreads), 0, s, a);
-    else hipLaunchKernelGGL(q4_move_kernel<64>, grid, dim3(kMoveThreads), 0, s, a);
+    const int want = (4 * 256 + slabs - 1) / slabs, parts = want < most ? want : most;
+    const dim3 grid(parts, a.dims.layers + 1, a.dims.batch);
+    if (a.dims.d == 128) hipLaunchKernelGGL(q4_move_kernel<128>, grid, dim3(kMoveBlock), 0, s, a);
+    else hipLaunchKernelGGL(q4_move_kernel<64>, grid, dim3(kMoveBlock), 0, s, a);
     return hipGetLastError();
 }
 
