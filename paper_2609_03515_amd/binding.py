@@ -432,25 +432,15 @@ def _q4_ok(t, dtype, numel, device):
     return t is None or (t.dtype is dtype and t.numel() >= numel and t.get_device() == device and t.is_contiguous())
 
 
-def _q4_stream(fn, cache, ws, stream):
-    """The stream of a call: its workspace has to lie with the cache, and the cache on the current device, a GPU."""
+def _q4_tail(fn, cache, ws, stream):
+    """The last arguments of a call, workspace and stream: the workspace has to lie with the cache, and the cache on the current
+    device, a GPU."""
     dev = cache._device
-    if dev < 0 or (ws is not None and (ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous())) or (
-            dev != (torch.cuda.current_device() if _device is None else _device())):
+    if dev < 0 or dev != (torch.cuda.current_device() if _device is None else _device()) or (
+            ws is not None and (ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous())):
         raise KVError(fn, KV_ERR_INVALID_ARG)
-    return _stream(stream)
-
-
-def _q4_strides(fn, cache, layer_count, rows, t):
-    """Strides of a tensor [layer_count][batch][n_kv_heads][rows][head_dim] whose rows are contiguous."""
-    batch, heads, d = cache._batch, cache._heads, cache._dim
-    if t.shape != (layer_count, batch, heads, rows, d) or t.dtype is not cache.element or t.get_device() != cache._device:
-        raise KVError(fn, KV_ERR_INVALID_ARG)
-    sl, sb, sh, sr, one = t.stride()
-    if one != 1:
-        raise KVError(fn, KV_ERR_INVALID_ARG)
-    # (the stride of an extent of 1 is not used, and may be anything)
-    return KvQ4Strides(sl if layer_count > 1 else 0, sb if batch > 1 else 0, sh if heads > 1 else 0, sr if rows > 1 else 0)
+    handle = _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
+    return (None, 0, handle) if ws is None else (ws.data_ptr(), ws.numel(), handle)
 
 
 def kv_q4_reserve(cache: KvQ4Cache, add, new_pos, ws, granted=None, init="mean", stream=None):
@@ -459,20 +449,27 @@ def kv_q4_reserve(cache: KvQ4Cache, add, new_pos, ws, granted=None, init="mean",
     if not (_q4_ok(add, torch.int32, n, dev) and _q4_ok(new_pos, torch.int32, n, dev) and _q4_ok(granted, torch.int32, n, dev)):
         raise KVError("kv_q4_reserve", KV_ERR_INVALID_ARG)
     mode = {"mean": KV_INIT_MEAN, "min": KV_INIT_MIN, "zero": KV_INIT_ZERO}.get(init, -1) if isinstance(init, str) else int(init)
-    st = _q4_stream("kv_q4_reserve", cache, ws, stream)
+    tail = _q4_tail("kv_q4_reserve", cache, ws, stream)
     _check("kv_q4_reserve", load_library().kv_q4_reserve(cache._shape, cache._buffers, _ptr(add), _ptr(new_pos), mode,
-                                                         _ptr(granted), _ptr(ws), _ws_bytes(ws), st))
+                                                         _ptr(granted), *tail))
 
 
 def _q4_rows(fn, cache, layer0, layer_count, rows, k, v, ws, first, count, stream):
-    n, dev = cache._batch, cache._device
-    if not (_q4_ok(first, torch.int32, n, dev) and _q4_ok(count, torch.int32, n, dev)):
+    # (a decode step's rows are bound by the host: 7.3 us a call with a helper per tensor, 6.7 so, of which the kernel is 3.5)
+    n, heads, dev, element = cache._batch, cache._heads, cache._device, cache.element
+    shape = (layer_count, n, heads, rows, cache._dim)
+    ks, vs = k.stride(), v.stride()
+    if not (k.shape == shape and v.shape == shape and k.dtype is element and v.dtype is element and ks[4] == 1 and vs[4] == 1
+            and k.get_device() == dev and v.get_device() == dev
+            and (first is None or _q4_ok(first, torch.int32, n, dev)) and (count is None or _q4_ok(count, torch.int32, n, dev))):
         raise KVError(fn, KV_ERR_INVALID_ARG)
-    ks = _q4_strides(fn, cache, layer_count, rows, k)
-    vs = _q4_strides(fn, cache, layer_count, rows, v)
-    st = _q4_stream(fn, cache, ws, stream)
+    tail = _q4_tail(fn, cache, ws, stream)
+    # (the stride of an extent of 1 is not used, and may be anything)
+    ln, bn, hn, rn = layer_count > 1, n > 1, heads > 1, rows > 1
+    k_strides = KvQ4Strides(ks[0] * ln, ks[1] * bn, ks[2] * hn, ks[3] * rn)
+    v_strides = k_strides if ks == vs else KvQ4Strides(vs[0] * ln, vs[1] * bn, vs[2] * hn, vs[3] * rn)
     _check(fn, getattr(load_library(), fn)(cache._shape, cache._buffers, layer0, layer_count, rows, _ptr(first), _ptr(count),
-                                           _ptr(k), ks, _ptr(v), vs, _ptr(ws), _ws_bytes(ws), st))
+                                           k.data_ptr(), k_strides, v.data_ptr(), v_strides, *tail))
 
 
 def kv_q4_store(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None, count=None, stream=None):
@@ -495,10 +492,10 @@ def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos
             and _q4_ok(s_out, f32, layer_count * n * n_max, dev) and _q4_ok(u_prior, f32, cache._rows, dev)
             and _q4_ok(u_out, f32, cache._rows, dev)):
         raise KVError("kv_q4_attend", KV_ERR_INVALID_ARG)
-    st = _q4_stream("kv_q4_attend", cache, ws, stream)
+    tail = _q4_tail("kv_q4_attend", cache, ws, stream)
     _check("kv_q4_attend", load_library().kv_q4_attend(
         cache._shape, cache._buffers, layer0, layer_count, n_max, _ptr(q), _ptr(cur_pos), recency_bias, recency_window, _ptr(o),
-        _ptr(s_out), alpha, _ptr(u_prior), _ptr(u_out), _ptr(ws), _ws_bytes(ws), st))
+        _ptr(s_out), alpha, _ptr(u_prior), _ptr(u_out), *tail))
 
 
 def kv_q4_fork(cache: KvQ4Cache, src, dst, ws, stream=None):
@@ -506,27 +503,24 @@ def kv_q4_fork(cache: KvQ4Cache, src, dst, ws, stream=None):
     n = src.numel()
     if dst.numel() != n or not (_q4_ok(src, torch.int32, n, cache._device) and _q4_ok(dst, torch.int32, n, cache._device)):
         raise KVError("kv_q4_fork", KV_ERR_INVALID_ARG)
-    st = _q4_stream("kv_q4_fork", cache, ws, stream)
-    _check("kv_q4_fork", load_library().kv_q4_fork(cache._shape, cache._buffers, n, _ptr(src), _ptr(dst), _ptr(ws),
-                                                   _ws_bytes(ws), st))
+    tail = _q4_tail("kv_q4_fork", cache, ws, stream)
+    _check("kv_q4_fork", load_library().kv_q4_fork(cache._shape, cache._buffers, n, _ptr(src), _ptr(dst), *tail))
 
 
 def kv_q4_free(cache: KvQ4Cache, slots, ws, stream=None):
     """slots: int32 tensor of at most batch entries."""
     if not _q4_ok(slots, torch.int32, 0, cache._device):
         raise KVError("kv_q4_free", KV_ERR_INVALID_ARG)
-    st = _q4_stream("kv_q4_free", cache, ws, stream)
-    _check("kv_q4_free", load_library().kv_q4_free(cache._shape, cache._buffers, slots.numel(), _ptr(slots), _ptr(ws),
-                                                   _ws_bytes(ws), st))
+    tail = _q4_tail("kv_q4_free", cache, ws, stream)
+    _check("kv_q4_free", load_library().kv_q4_free(cache._shape, cache._buffers, slots.numel(), _ptr(slots), *tail))
 
 
 def kv_q4_compact(cache: KvQ4Cache, n_max, keep, ws, stream=None):
     """keep: [batch][capacity] uint8."""
     if not _q4_ok(keep, torch.uint8, cache._rows, cache._device):
         raise KVError("kv_q4_compact", KV_ERR_INVALID_ARG)
-    st = _q4_stream("kv_q4_compact", cache, ws, stream)
-    _check("kv_q4_compact", load_library().kv_q4_compact(cache._shape, cache._buffers, n_max, _ptr(keep), _ptr(ws),
-                                                         _ws_bytes(ws), st))
+    tail = _q4_tail("kv_q4_compact", cache, ws, stream)
+    _check("kv_q4_compact", load_library().kv_q4_compact(cache._shape, cache._buffers, n_max, _ptr(keep), *tail))
 
 
 def kv_q4_evict(cache: KvQ4Cache, n_max, budget, ws, keep_out=None, stream=None):
@@ -534,9 +528,9 @@ def kv_q4_evict(cache: KvQ4Cache, n_max, budget, ws, keep_out=None, stream=None)
     dev = cache._device
     if not (_q4_ok(budget, torch.int32, cache._batch, dev) and _q4_ok(keep_out, torch.uint8, cache._rows, dev)):
         raise KVError("kv_q4_evict", KV_ERR_INVALID_ARG)
-    st = _q4_stream("kv_q4_evict", cache, ws, stream)
+    tail = _q4_tail("kv_q4_evict", cache, ws, stream)
     _check("kv_q4_evict", load_library().kv_q4_evict(cache._shape, cache._buffers, n_max, _ptr(budget), _ptr(keep_out),
-                                                     _ptr(ws), _ws_bytes(ws), st))
+                                                     *tail))
 
 
 # --- HIP events for the timing hooks (runtime plumbing, no computation) -------------------------------------
