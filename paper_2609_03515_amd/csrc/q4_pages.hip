@@ -9,8 +9,8 @@
 // the table or the lengths that its own workgroups change.
 //
 // Small calls are launches and chains of dependent loads (2.5 to 8 us a kernel); measured on six samples of prompts of 12,000 to
-// 16,384 rows in 8 layers of 8 KV heads: fork 5.4 us, reserve 6.5 + 8.5, eviction to 10%: plan 21.6, pages 5, moves 45 (142 MB
-// by the memory's counters, in pieces of 64 and 4 bytes: 3.2 TB/s).  The moves took 112 with one workgroup per slab that found every
+// 16,384 rows in 8 layers of 8 KV heads: fork 5.4 us, reserve 6.5 + 8.5, eviction to 10%: plan 21.6, pages 5, moves 45 (81 MB
+// written by the memory's counter and as much read, in pieces of 64 and 4 bytes: 3.6 TB/s).  The moves took 112 with one workgroup per slab that found every
 // row's place for itself, and 48 (one row of each of 256 slabs: 14.7, now 11.3) with the places found between the copies; the plan 45 with a
 // prefix sum per 1,024 rows (64 with keys in registers: that unrolls into more code than its instruction fetches are worth), and 28
 // with one histogram and with pointers that could be LDS or memory; the fork 10.4 copying 4 bytes a thread.
