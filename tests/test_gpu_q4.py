@@ -962,3 +962,54 @@ def test_side_stream_and_two_caches():
         same(a, b, a["len"].tolist(), t.cap)
         assert torch.equal(a["pool"], b["pool"])
         assert all(torch.equal(x, y) for x, y in zip(results[0][1][j], results[1][1][j]))
+
+
+@pytest.mark.parametrize("hq,hkv,d,page_rows,dtype,lens", [
+    (4, 2, 64, 16, "f32", [51, 16, 1, 0, 48]), (7, 1, 128, 32, "bf16", [96, 33, 0, 64, 95]), (32, 2, 128, 16, "f32", [700, 3, 688, 64, 0]),
+    (512, 128, 128, 16, "bf16", [200, 1, 16, 0, 207])])
+def test_guard_bands(hq, hkv, d, page_rows, dtype, lens):
+    """No call writes outside its buffers: each lies between guard bands, the last page of the pool and the last row of a slot
+    in use, the workspace of the size asked for."""
+    from test_gpu_guards import Guarded, check_guards
+
+    Guarded.registry = []
+    layers, batch = 2, len(lens)
+    max_pages = -(-max(lens) // page_rows)
+    cap, used = max_pages * page_rows, sum(-(-n // page_rows) for n in lens)
+    s = B.make_q4_shape(batch, layers, hq, hkv, d, page_rows, used + 2 * max_pages, max_pages, dtype)
+    def buffer(name, dims, t=torch.int32, fill=0):
+        g = Guarded(name, dims, t)
+        g.t.fill_(fill)
+        return g.t
+    pool = buffer("pool", (B.kv_q4_pool_bytes(s),), torch.uint8, 255)
+    c = B.KvQ4Cache(s, pool, buffer("table", (batch, max_pages), fill=-1), buffer("len", (batch,)), buffer("refs", (s.n_pages,)),
+                    buffer("u", (batch, cap), torch.float32), buffer("pos", (batch, cap)))
+    ws = buffer("ws", (B.kv_q4_workspace_bytes(s, cap, layers),), torch.uint8)
+    add, granted, new_pos = buffer("add", (batch,)), buffer("granted", (batch,)), buffer("new_pos", (batch,))
+    add.copy_(i32(lens))
+    q, o = (buffer(n, (layers, batch, hq, d), DT[dtype]) for n in ("q", "o"))
+    q.copy_(torch.randn(q.shape, generator=gen(1)))
+    k, v, k2, v2 = (buffer(n, (layers, batch, hkv, max(lens), d), DT[dtype]) for n in ("k", "v", "k2", "v2"))
+    k.copy_(torch.randn(k.shape, generator=gen(2)))
+    v.copy_(torch.randn(v.shape, generator=gen(3)))
+    scores, u_out = buffer("s", (layers, batch, cap), torch.float32), buffer("u_out", (batch, cap), torch.float32)
+    keep, budget = buffer("keep", (batch, cap), torch.uint8), buffer("budget", (batch,))
+    def run(name, *args, **kw):
+        getattr(B, name)(c, *args, ws, **kw)
+        check_guards(name)
+    run("kv_q4_reserve", add, new_pos, granted=granted)
+    assert granted.tolist() == lens and B.faults(ws) == 0
+    run("kv_q4_store", 0, layers, max(lens), k, v, count=granted)
+    run("kv_q4_load", 0, layers, max(lens), k2, v2, count=granted)
+    for count in (1, layers):
+        run("kv_q4_attend", 0, count, cap, q, o, s_out=scores, alpha=0.5, u_prior=c.u, u_out=u_out)
+    run("kv_q4_attend", 0, layers, cap, q, o)
+    c.u.copy_(torch.rand(c.u.shape, generator=gen(4)))
+    empty = lens.index(0)
+    run("kv_q4_fork", i32([0]), i32([empty]))
+    budget.copy_(i32([n - 1 if b else n // 2 for b, n in enumerate(lens)]).clamp(min=0))
+    budget[empty] = max(lens[0] - 2, 1)
+    run("kv_q4_evict", cap, budget, keep_out=keep)
+    run("kv_q4_compact", cap, keep)
+    run("kv_q4_free", i32(list(range(batch))))
+    assert B.faults(ws) == 0 and not c.refs.any() and not c.len.any()
