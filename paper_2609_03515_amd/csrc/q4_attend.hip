@@ -30,6 +30,7 @@
 // On the way (all layers): 190 us with the values in registers and cached loads.  Equal shares of all tiles per workgroup, whatever
 // sequence they belong to, took 226 (the search for the share, and the state that it needs).
 #include <float.h>
+#include <limits.h>
 
 #include <atomic>
 #include <type_traits>
@@ -602,19 +603,22 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
         if ((int)blockIdx.x * kWave < n)
 #pragma unroll 4
             for (int g = (wave & (per - 1)); g < d.hkv; g += per) {
+                size_t slab[kAhead];
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
                     const int l = min(l0 + q * together + (wave >> per_shift), a.layer_count - 1);  // (past the last: not used)
-                    const size_t slab = (size_t)(l * d.batch + b) * d.hkv + g;
-                    if constexpr (kGroups) {
-                        s[q] += a.z[slab * a.n_stride + at];
-                    } else {
-                        const float* z = a.z + slab * d.group * a.n_stride + at;
-                        const float2* st = a.stat + slab * d.group;
+                    slab[q] = (size_t)(l * d.batch + b) * d.hkv + g;
+                    if constexpr (kGroups) s[q] += a.z[slab[q] * a.n_stride + at];
+                }
+                if constexpr (!kGroups) {
 #pragma unroll 4
-                        for (int h = 0; h < d.group; ++h)
-                            s[q] = fmaf(exp2_hw(z[(size_t)h * a.n_stride] - st[h].x), st[h].y, s[q]);
-                    }
+                    for (int h = 0; h < d.group; ++h)
+#pragma unroll
+                        for (int q = 0; q < kAhead; ++q) {
+                            const size_t head = slab[q] * d.group + h;
+                            const float2 st = a.stat[head];
+                            s[q] = fmaf(exp2_hw(a.z[head * a.n_stride + at] - st.x), st.y, s[q]);
+                        }
                 }
             }
 #pragma unroll
@@ -709,16 +713,32 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
     hipError_t e = a.dims.d == 128 ? launch_by_group<128>(a, s) : launch_by_group<64>(a, s);
     if (e != hipSuccess || !a.z) return e;
-    // Waves: as many as the call's layers have KV heads, up to 16; with fewer layers than waves, a power of two of waves to a
-    // layer.  (A wave to a layer leaves one sum to add: 32 layers of 8 KV heads x 8 sequences x 3,277 rows 17 -> 12 us.)
-    int per_shift = 0, waves_shift = 0;
-    while ((1 << per_shift) < a.dims.hkv && a.layer_count << per_shift < kScoreWaves) ++per_shift;
+    // Waves: as many as the call's layers have KV heads, up to 16, a power of two of them to a layer: the one that leaves a wave the
+    // fewest (layer, KV head) pairs, the lower where they are the same.  (A wave to a layer leaves one sum to add: 32 layers of 8
+    // KV heads x 8 sequences x 3,277 rows 17 -> 12 us.)
+    int per_shift = 0, least = INT_MAX;
+    for (int shift = 0; 1 << shift <= kScoreWaves; ++shift) {
+        const int side = kScoreWaves >> shift, pairs = (a.layer_count + side - 1) / side * ((a.dims.hkv + (1 << shift) - 1) >> shift);
+        if (pairs < least) {
+            least = pairs;
+            per_shift = shift;
+        }
+    }
+    int waves_shift = per_shift;
     while ((1 << waves_shift) < a.layer_count << per_shift && (1 << waves_shift) < kScoreWaves) ++waves_shift;
     const int waves = 1 << waves_shift;
     const int blocks = (a.n_max + kWave - 1) / kWave;
-    const int ahead = ((a.layer_count << per_shift) + waves - 1) / waves;
-    auto kern = a.scored ? (ahead == 1 ? q4_score_kernel<true, 1> : ahead == 2 ? q4_score_kernel<true, 2> : q4_score_kernel<true, 4>)
-                         : (ahead == 1 ? q4_score_kernel<false, 1> : q4_score_kernel<false, 4>);
+    // layers ahead: up to four, the same number in every turn (layers past the last cost as much as others: 6 layers of 21
+    // sequences of 491 .. 2,975 rows 32 us in turns of 16 layers, 18 so)
+    const int rounds = ((a.layer_count << per_shift) + waves - 1) / waves, turns = (rounds + 3) / 4, ahead = (rounds + turns - 1) / turns;
+    auto kern = a.scored ? (ahead == 1   ? q4_score_kernel<true, 1>
+                            : ahead == 2 ? q4_score_kernel<true, 2>
+                            : ahead == 3 ? q4_score_kernel<true, 3>
+                                         : q4_score_kernel<true, 4>)
+                         : (ahead == 1   ? q4_score_kernel<false, 1>
+                            : ahead == 2 ? q4_score_kernel<false, 2>
+                            : ahead == 3 ? q4_score_kernel<false, 3>
+                                         : q4_score_kernel<false, 4>);
     hipLaunchKernelGGL(kern, dim3(blocks, a.dims.batch), dim3(waves * kWave), 0, s, a, per_shift,
                        waves_shift - per_shift);
     return hipGetLastError();

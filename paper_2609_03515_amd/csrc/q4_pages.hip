@@ -439,6 +439,42 @@ __device__ Border nth_border(const Ranked<kInLds>& rows, int budget, int* hist /
     return {full, limit_s};
 }
 
+// The same of at most kFewRows rows: every row counts those before it.
+constexpr int kFewRows = 256;
+template <bool kInLds>
+__device__ Border border_of_few(const Ranked<kInLds>& rows, int budget, uint64_t* full /* kFewRows */) {
+    __shared__ uint32_t key_s;
+    __shared__ int last_s, all_s;
+    const int i = threadIdx.x;
+    const bool in = i < rows.n;
+    uint64_t own = 0;
+    if (in) full[i] = own = (uint64_t)rows.key(i) << 32;
+    __syncthreads();
+    int above = 0, alike = 0;
+    if (in)
+#pragma unroll 8
+        for (int j = 0; j < rows.n; ++j) {
+            above += full[j] > own;
+            alike += full[j] == own;
+        }
+    if (in && above < budget && above + alike >= budget) {  // (rows of one utility)
+        key_s = (uint32_t)(own >> 32);
+        all_s = above + alike == budget;
+    }
+    __syncthreads();
+    if (all_s) return {(uint64_t)key_s << 32, INT_MAX};
+    if (in) full[i] = own = rows.full(i);
+    __syncthreads();
+    if (in) {
+        int before = 0;
+#pragma unroll 8
+        for (int j = 0; j < rows.n; ++j) before += full[j] > own || (full[j] == own && j < i);
+        if (before == budget - 1) last_s = i;
+    }
+    __syncthreads();
+    return {full[last_s], last_s + 1};
+}
+
 // Workgroup b: what sequence b keeps, the rows that move, the shared pages that are replaced, and the pages wanted.
 // With K(i) the kept rows before row i, from one mask bit a row and the masks' prefix sums: a dropped row i before the new end
 // is hole i - K(i), a kept row behind it the (K(i) - K(end))-th that moves, and a page has a hole when its rows number more than
@@ -451,6 +487,7 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     __shared__ int lds[kWaves + 1];
     __shared__ uint64_t lds64[kWaves];
     __shared__ int hist[kEvict ? 256 * kHistsOf<kBlock> : 1];
+    __shared__ uint64_t few[kEvict ? kFewRows : 1];
     extern __shared__ uint64_t dynamic[];  // masks and their prefix sums, then the keys
     const Q4Dims& d = a.dims;
     const int b = blockIdx.x, n = a.cache.len[b], lane = threadIdx.x % kWave;
@@ -496,7 +533,9 @@ __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     }
     Border least{0, INT_MAX};
     if (select) {
-        if (n - budget <= kFewEvicted) {
+        if (n <= kFewRows) {
+            least = border_of_few(rows, budget, few);
+        } else if (n - budget <= kFewEvicted) {
             for (int i = 0; i < n - budget; ++i) least = next_border<kBlock, kInLds>(rows, least, lds64, lds);
         } else {
             least = nth_border<kBlock, kInLds>(rows, budget, hist, lds);
