@@ -754,7 +754,8 @@ def test_evict_of_long_sequences(n, budget):
         assert np.array_equal(keep[b, :n].cpu().numpy(), want), b
 
 
-@pytest.mark.parametrize("n,budget", [(5, 2), (100, 97), (100, 40), (5000, 4996), (5000, 4000), (33000, 9000), (140000, 139999)])
+@pytest.mark.parametrize("n,budget", [(5, 2), (100, 97), (100, 40), (256, 255), (257, 100), (1024, 1000), (1025, 30), (5000, 4996), (5000, 4000), (32768, 12000),
+                                      (33000, 9000), (140000, 139999)])
 def test_evict_of_rows_that_tie(n, budget):
     """Rows alike in utility (0 and -0 are) and position, as where a caller sets no positions: exactly `budget` stay, the lower
     rows; positions below 0 are lower than others."""
