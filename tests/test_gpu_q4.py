@@ -967,7 +967,7 @@ def test_side_stream_and_two_caches():
 
 @pytest.mark.parametrize("hq,hkv,d,page_rows,dtype,lens", [
     (4, 2, 64, 16, "f32", [51, 16, 1, 0, 48]), (7, 1, 128, 32, "bf16", [96, 33, 0, 64, 95]), (32, 2, 128, 16, "f32", [700, 3, 688, 64, 0]),
-    (512, 128, 128, 16, "bf16", [200, 1, 16, 0, 207])])
+    (512, 128, 128, 16, "bf16", [200, 1, 16, 0, 207]), (32, 4, 128, 32, "f32", [3341, 0, 257, 1, 2049])])
 def test_guard_bands(hq, hkv, d, page_rows, dtype, lens):
     """No call writes outside its buffers: each lies between guard bands, the last page of the pool and the last row of a slot
     in use, the workspace of the size asked for."""
