@@ -10,11 +10,11 @@
 //    codes, one scale.  A code with its scale is a bf16 number exactly, and the conversion applies the scale, so the product with a bf16 query is
 //    exact up to the order of 32-bit sums.  The query's elements lie in the same order.  f32 queries: three bf16 parts whose
 //    sum is the number, a product each.
-//  * logits: the result holds rows s, 4 + s, 8 + s, 12 + s of each half for column c.  A column is a head; where two or three times
-//    the group fits 16 columns, the heads are there again, for the parts below.
+//  * logits: the result holds rows s, 4 + s, 8 + s, 12 + s of each half for column c.  A column is a head; where three times the
+//    group fits 16 columns, the heads are there twice more, for the parts below.
 //  * probabilities p = 2^(z - m): as a B operand, the same lane holds the same rows, so nothing moves between lanes.  p is
-//    split into bf16 parts, 8 bits each, that sum up to 16 of its bits (bf16 output: an error of 2^-15, the output's own
-//    rounding is 2^-8) or to all 24 (f32), a column of its own each or a product of its own.
+//    split into three bf16 parts of 8 bits that sum up to all 24 of its bits, a column of its own each or a product of its own
+//    (two parts, 16 bits, are up to 2^-15 low: no slower in columns, in products 72 us for 78 in 4 layers of 32 x 1 .. 8,192 rows).
 //  * values: loaded to LDS as they lie in memory, without registers; the lane takes the same rows' elements 8 c .. 8 c + 7
 //    (d = 64: 4 c ...; the four rows that a read of the wave takes are consecutive, so no two lanes meet in a bank), converted
 //    like the keys; pairs of rows of one element are put together by byte permutes of the lane's own registers.
@@ -155,6 +155,7 @@ struct Slab {
 constexpr int kZPad = 16;    // floats between the heads' logits in LDS
 constexpr int kQ4Waves = 8;  // (four: one sequence of 131,072 rows 35 us for 34, scored slabs 215 for 190)
 
+// CP columns of a head, NM products with its probabilities' parts (3, 1 or 1, 3).
 template <typename T, int D, int CP, int NM, bool kScored>
 __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendArgs a) {
     constexpr int kThreads = kWave * kQ4Waves, kStep = kTile * kQ4Waves;
@@ -174,7 +175,8 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
     const int part = c / group, head = c % group;
     const bool column = part < CP;
     const int columns = CP * group;
-    const uint32_t cut1 = part >= 1 ? 0xffff0000u : 0u, cut2 = part >= 2 ? 0xffff0000u : 0u;
+    // a part is what lies between two cuts of a probability's bits (part 0's lower ones go with the rounding to bf16)
+    const uint32_t cut_low = part == 1 ? 0xffffff00u : ~0u, cut_high = part == 0 ? 0u : part == 1 ? 0xffff0000u : 0xffffff00u;
     // the lane's places in the wave's LDS: codes of elements D / 16 * c ... of row s, and their scale
     uint8_t* const value_lds = reinterpret_cast<uint8_t*>(lds) + wave * kValueBytes<D>;
     const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
@@ -336,12 +338,10 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
             p[j] = exp2_hw(z[j] - m);
             l += p[j];
         }
-        if constexpr (CP >= 2)
+        if constexpr (CP == 3)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] -= __uint_as_float(__float_as_uint(p[j]) & cut1);
-        if constexpr (CP >= 3)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] -= __uint_as_float(__float_as_uint(p[j]) & cut2);
+            for (int j = 0; j < 8; ++j)
+                p[j] = __uint_as_float(__float_as_uint(p[j]) & cut_low) - __uint_as_float(__float_as_uint(p[j]) & cut_high);
         u32x4 pp[NM];
 #pragma unroll
         for (int k = 0; k < NM; ++k) {
@@ -676,12 +676,12 @@ hipError_t launch_attend(const Q4AttendArgs& a, hipStream_t s) {
     return a.scored ? launch_form<T, D, CP, NM, true>(a, s) : launch_form<T, D, CP, NM, false>(a, s);
 }
 
-// Columns of the parts of a probability: as many as fit beside each other.
+// The three parts of a probability: columns beside each other where they fit, products of their own where they do not.
+constexpr int kMostBeside = 5;
 template <int D>
 hipError_t launch_by_group(const Q4AttendArgs& a, hipStream_t s) {
-    const int group = a.dims.group;
-    if (a.dims.bf16) return group <= 8 ? launch_attend<bf16_t, D, 2, 1>(a, s) : launch_attend<bf16_t, D, 1, 2>(a, s);
-    return group <= 5 ? launch_attend<float, D, 3, 1>(a, s) : launch_attend<float, D, 1, 3>(a, s);
+    if (a.dims.group <= kMostBeside) return a.dims.bf16 ? launch_attend<bf16_t, D, 3, 1>(a, s) : launch_attend<float, D, 3, 1>(a, s);
+    return a.dims.bf16 ? launch_attend<bf16_t, D, 1, 3>(a, s) : launch_attend<float, D, 1, 3>(a, s);
 }
 
 }  // namespace
@@ -707,7 +707,7 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     // Scored: where a slab's logits fit LDS with two workgroups on a CU, and there is a slab for each: 2,048 slabs of 3,277 rows
     // with scores 190 us, through memory 241.
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
-    const size_t outputs = 4 * (size_t)d.group * (d.bf16 ? (d.group <= 8 ? 2 : 1) : d.group <= 5 ? 3 : 1) * (d.d + 4) * sizeof(float);
+    const size_t outputs = 4 * (size_t)d.group * (d.group <= kMostBeside ? 3 : 1) * (d.d + 4) * sizeof(float);
     const size_t scored = (values > outputs ? values : outputs) + (size_t)d.group * (18 + p.n_stride + kZPad) * sizeof(float) +
                           (d.bf16 ? 0 : 16 + 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4));
     p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 2 * cus;

@@ -1014,3 +1014,34 @@ def test_guard_bands(hq, hkv, d, page_rows, dtype, lens):
     run("kv_q4_compact", cap, keep)
     run("kv_q4_free", i32(list(range(batch))))
     assert B.faults(ws) == 0 and not c.refs.any() and not c.len.any()
+
+
+# ---- borders of the arguments -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (10, 2), (6, 1), (16, 2), (9, 1), (16, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_probabilities_keep_32_bits(hq, hkv, d):
+    """bf16 outputs are the exact ones rounded once, but for sums and exponentials in 32 bits.
+
+    A query has one element, so a logit is one product, exact but for its scaling: off by 2^-23 of itself in base 2, a
+    probability by ln 2 of both logits' errors and of the subtraction's (2^-24 of it), and the exponential's 2^-23.  Eight rows: as
+    many additions in the products and in the sum (2^-23 each at most), and 8 roundings more.  The output's own rounding: half a
+    step of the exact value."""
+    batch, n = 24, 8
+    t = Cache([n] * batch, hq=hq, hkv=hkv, d=d)
+    levels = torch.tensor([0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    k = torch.zeros(1, batch, hkv, n, d)
+    k[..., 0] = levels[torch.randint(0, 7, (1, batch, hkv, n), generator=gen(1))]
+    v = torch.randn(1, batch, hkv, n, d, generator=gen(2))
+    B.kv_q4_store(t.c, 0, 1, n, k.bfloat16().cuda(), v.bfloat16().cuda(), t.ws)
+    q = torch.zeros(1, batch, hq, d)
+    q[..., 0] = 1.0 + 2.0 * torch.rand(1, batch, hq, generator=gen(3))
+    q = q.bfloat16().cuda()
+    o = torch.empty_like(q)
+    B.kv_q4_attend(t.c, 0, 1, n, q, o, t.ws)
+    for b in range(batch):
+        want, _, size, av = R.attend(q[0, b].double().cpu().numpy(), *t.values(0, b))
+        z = size * 1.4427
+        rel = 2 * (0.6932 * (2 * z * 2.0 ** -23 + z * 2.0 ** -24) + 2.0 ** -23) + (2 * n + 8) * 2.0 ** -23
+        step = 2.0 ** (np.floor(np.log2(np.abs(want) + rel * av)) - 8)
+        assert (np.abs(o[0, b].double().cpu().numpy() - want) <= step + rel * av).all(), b
