@@ -393,27 +393,55 @@ def q4_workspace(shape: KvQ4Shape, n_max: int, layer_count: int, device="cuda") 
     return ws
 
 
+def _q4_buffer(name, needed):
+    """A buffer of a KvQ4Cache: what is assigned is checked and is what the calls see from then on."""
+
+    def get(cache):
+        return cache._tensors[name]
+
+    def put(cache, t):
+        dtype, numel = cache._sizes[name]
+        if (needed if t is None else t.device != cache._place or not _q4_ok(t, dtype, numel, cache._device)):
+            raise KVError("KvQ4Cache." + name, KV_ERR_INVALID_ARG)
+        cache._tensors[name] = t
+        setattr(cache._addresses, name, _ptr(t))
+
+    return property(get, put)
+
+
 class KvQ4Cache:
     """One paged 4-bit cache's device buffers (caller-owned, contiguous torch tensors) for the kv_q4 calls.
 
     pool: uint8, kv_q4_pool_bytes(shape); table: [batch][max_pages] int32; len: [batch] int32; refs: [n_pages] int32;
-    u: [batch][capacity] f32 and pos: [batch][capacity] int32 (nullable: not kept), capacity = max_pages * page_rows."""
+    u: [batch][capacity] f32 and pos: [batch][capacity] int32 (nullable: not kept), capacity = max_pages * page_rows.
+    A buffer may be replaced by assigning another (cache.u = u_out, say); one whose storage is changed under the same tensor
+    (resize_, set_) has to be assigned again.  The shape is a copy of the caller's, and shape and buffers (the addresses) give copies."""
 
     def __init__(self, shape: KvQ4Shape, pool, table, len, refs, u=None, pos=None):
         cap = shape.max_pages * shape.page_rows
-        dev = pool.get_device()
-        if not (_q4_ok(pool, torch.uint8, kv_q4_pool_bytes(shape), dev)
-                and _q4_ok(table, torch.int32, shape.batch * shape.max_pages, dev) and _q4_ok(len, torch.int32, shape.batch, dev)
-                and _q4_ok(refs, torch.int32, shape.n_pages, dev) and _q4_ok(u, torch.float32, shape.batch * cap, dev)
-                and _q4_ok(pos, torch.int32, shape.batch * cap, dev)):
-            raise KVError("KvQ4Cache", KV_ERR_INVALID_ARG)
-        self.shape, self.pool, self.table, self.len, self.refs, self.u, self.pos = shape, pool, table, len, refs, u, pos
-        self.buffers = KvQ4Buffers(*(_ptr(t) for t in (pool, table, len, refs, u, pos)))
+        self._place, self._device = pool.device, pool.get_device()
+        self._own, self._addresses, self._tensors = KvQ4Shape.from_buffer_copy(shape), KvQ4Buffers(), {}
+        i32 = torch.int32
+        self._sizes = {"pool": (torch.uint8, kv_q4_pool_bytes(shape)), "table": (i32, shape.batch * shape.max_pages),
+                       "len": (i32, shape.batch), "refs": (i32, shape.n_pages), "u": (torch.float32, shape.batch * cap),
+                       "pos": (i32, shape.batch * cap)}
+        self.pool, self.table, self.len, self.refs, self.u, self.pos = pool, table, len, refs, u, pos
         self.element = torch.float32 if shape.dtype == KV_F32 else torch.bfloat16
         # what every call passes or compares with, taken once (building it took 4 us of a call's 13)
-        self._shape, self._buffers = ctypes.byref(shape), ctypes.byref(self.buffers)
-        self._device, self._batch, self._rows = dev, shape.batch, shape.batch * cap
+        self._shape, self._buffers = ctypes.byref(self._own), ctypes.byref(self._addresses)
+        self._batch, self._rows = shape.batch, shape.batch * cap
         self._heads, self._dim = shape.n_kv_heads, shape.head_dim
+
+    pool, table, len, refs = (_q4_buffer(name, True) for name in ("pool", "table", "len", "refs"))
+    u, pos = _q4_buffer("u", False), _q4_buffer("pos", False)
+
+    @property
+    def shape(self) -> KvQ4Shape:
+        return KvQ4Shape.from_buffer_copy(self._own)
+
+    @property
+    def buffers(self) -> KvQ4Buffers:
+        return KvQ4Buffers.from_buffer_copy(self._addresses)
 
     @classmethod
     def allocate(cls, shape: KvQ4Shape, device="cuda") -> "KvQ4Cache":
@@ -486,7 +514,7 @@ def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos
                  s_out=None, alpha=0.0, u_prior=None, u_out=None, stream=None):
     """q, o: [layer_count][batch][n_q_heads][head_dim]; cur_pos: [batch] int32; s_out: [layer_count][batch][n_max] f32;
     u_prior, u_out: [batch][capacity] f32."""
-    s, n, dev, f32 = cache.shape, cache._batch, cache._device, torch.float32
+    s, n, dev, f32 = cache._own, cache._batch, cache._device, torch.float32
     size = layer_count * n * s.n_q_heads * s.head_dim
     if not (_q4_ok(q, cache.element, size, dev) and _q4_ok(o, cache.element, size, dev) and _q4_ok(cur_pos, torch.int32, n, dev)
             and _q4_ok(s_out, f32, layer_count * n * n_max, dev) and _q4_ok(u_prior, f32, cache._rows, dev)

@@ -1045,3 +1045,21 @@ def test_probabilities_keep_32_bits(hq, hkv, d):
         rel = 2 * (0.6932 * (2 * z * 2.0 ** -23 + z * 2.0 ** -24) + 2.0 ** -23) + (2 * n + 8) * 2.0 ** -23
         step = 2.0 ** (np.floor(np.log2(np.abs(want) + rel * av)) - 8)
         assert (np.abs(o[0, b].double().cpu().numpy() - want) <= step + rel * av).all(), b
+
+
+def test_utilities_swapped_after_the_fold():
+    """The utilities that a fold wrote elsewhere take the place of the old ones, whose memory goes to something else."""
+    t = Cache([40, 33], hq=4, hkv=2, page_rows=16).fill()
+    q = torch.randn(1, 2, 4, 128, generator=gen(3)).bfloat16().cuda()
+    o, out = torch.empty_like(q), torch.zeros_like(t.c.u)
+    B.kv_q4_attend(t.c, 0, 1, t.cap, q, o, t.ws, alpha=0.5, u_prior=t.c.u, u_out=out)
+    t.c.u.fill_(float("nan"))
+    t.c.u = out
+    u, pos = out.cpu().numpy().astype(np.float64), t.c.pos.cpu().numpy()
+    keep = torch.zeros(2, t.cap, dtype=torch.uint8, device="cuda")
+    B.kv_q4_evict(t.c, t.cap, i32([7, 20]), t.ws, keep_out=keep)
+    for b, (n, m) in enumerate(((40, 7), (33, 20))):
+        want = np.zeros(n, dtype=np.uint8)
+        want[np.lexsort((pos[b, :n], -u[b, :n]))[:m]] = 1
+        assert np.array_equal(keep[b, :n].cpu().numpy(), want)
+    assert t.faults() == 0

@@ -221,3 +221,30 @@ def test_attention_registers():
     assert len(seen) == 16
     assert max(k[".vgpr_count"] for k in seen.values()) <= 128
     assert max(k[".vgpr_spill_count"] for k in seen.values()) <= 2
+
+
+def test_a_cache_follows_its_buffers():
+    """Assigning a buffer of a cache (the utilities that an attention wrote, say) is what the calls see; what does not fit is
+    refused and changes nothing; the shape is the cache's own."""
+    s = shape()
+    c = B.KvQ4Cache.allocate(s, device="cpu")
+    addresses = {name: getattr(c, name).data_ptr() for name in ("pool", "table", "len", "refs", "u", "pos")}
+    assert {name: getattr(c.buffers, name) for name in addresses} == addresses
+    for name, old in addresses.items():
+        new = torch.zeros_like(getattr(c, name))
+        setattr(c, name, new)
+        assert getattr(c, name) is new and getattr(c.buffers, name) == new.data_ptr() != old
+        for wrong in (new.double(), new.flatten()[:-1], torch.zeros(2 * new.numel(), dtype=new.dtype)[::2], new.to("meta")):
+            with pytest.raises(B.KVError) as e:
+                setattr(c, name, wrong)
+            assert e.value.status == INVALID and getattr(c, name) is new and getattr(c.buffers, name) == new.data_ptr()
+    for name in ("pool", "table", "len", "refs"):
+        with pytest.raises(B.KVError):
+            setattr(c, name, None)
+    for name in ("u", "pos"):
+        setattr(c, name, None)
+        assert getattr(c, name) is None and getattr(c.buffers, name) is None
+    s.n_pages = c.shape.max_pages = 1 << 20
+    assert c.shape.n_pages == GOOD["n_pages"] and c.shape.max_pages == GOOD["max_pages"]
+    with pytest.raises(AttributeError):
+        c.shape = s
