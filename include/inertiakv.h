@@ -382,8 +382,9 @@ kv_status kv_q4_reserve(const kv_q4_shape* shape, const kv_q4_cache* cache, cons
 /* Stores rows of layers [layer0, layer0 + layer_count): row r < count[b] of k and v becomes row first[b] + r of slot b.
  * count nullable: `rows` of every slot; first nullable: len[b] - count[b], the newest rows (after kv_q4_reserve, with its
  * granted as count).  Rows r >= count[b] are not read.  Rows outside the slot, and rows in pages that other slots share
- * (KV_FAULT_SHARED_PAGE), are not stored.  A call takes at most
- * 2^28 - 256 rows over its layers, slots and KV heads (KV_ERR_UNSUPPORTED; kv_q4_load likewise). */
+ * (KV_FAULT_SHARED_PAGE), are not stored.  Of a count[b] above `rows` the first `rows` rows are stored (of the newest,
+ * first = len[b] - count[b], the oldest), of one below 0 none (KV_FAULT_CACHE both; kv_q4_load likewise).  A call takes at
+ * most 2^28 - 256 rows over its layers, slots and KV heads (KV_ERR_UNSUPPORTED; kv_q4_load likewise). */
 kv_status kv_q4_store(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t rows,
                       const int32_t* first, const int32_t* count, const void* k, const kv_q4_strides* k_strides, const void* v,
                       const kv_q4_strides* v_strides, void* ws, size_t ws_bytes, void* stream);

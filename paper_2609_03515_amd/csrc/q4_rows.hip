@@ -53,6 +53,7 @@ __device__ __forceinline__ uint32_t locate(const Q4RowArgs& a, uint32_t first, u
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
+        if (it[k].wanted && it[k].r == 0 && (uint32_t)count[k] > (uint32_t)a.rows) fault |= kFaultCache;
         it[k].wanted = it[k].wanted && it[k].r < count[k];
         const int64_t row = (a.first ? (int64_t)from[k] : (int64_t)len[k] - count[k]) + it[k].r;
         const bool in = row >= 0 && row < len[k] && row < d.cap;

@@ -1063,3 +1063,25 @@ def test_utilities_swapped_after_the_fold():
         want[np.lexsort((pos[b, :n], -u[b, :n]))[:m]] = 1
         assert np.array_equal(keep[b, :n].cpu().numpy(), want)
     assert t.faults() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_counts_beyond_the_rows(dtype):
+    """A count above the call's rows, or below 0, is reported; the rows that the call does have are stored and loaded."""
+    t = Cache([40, 20, 33, 7], dtype=dtype)
+    k, v = (torch.randn(1, 4, 2, 4, 128, generator=gen(i)).to(DT[dtype]).cuda() for i in (1, 2))
+    before = t.c.pool.clone()
+    for bad, left in ((i32([6, 0, 4, 3]), 34), (i32([4, -1, 4, 3]), 36)):
+        t.c.pool.copy_(before)
+        B.kv_q4_store(t.c, 0, 1, 4, k, v, t.ws, count=bad)
+        assert t.faults() == B.KV_FAULT_CACHE
+        got, _ = t.values(0, 0)  # rows len - count ...: the first four of them
+        assert np.array_equal(got[:, left : left + 4], R.fast_values(k[0, 0].double().cpu().numpy()))
+        own = t.c.table[1, :2].long()
+        assert torch.equal(t.c.pool.view(t.shape.n_pages, -1)[own], before.view(t.shape.n_pages, -1)[own])
+        y = torch.full_like(k, 7.0)
+        B.kv_q4_load(t.c, 0, 1, 4, y, y.clone(), t.ws, count=bad)
+        assert t.faults() == B.KV_FAULT_CACHE
+        assert np.array_equal(y[0, 0].double().cpu().numpy(), got[:, left : left + 4]) and (y[0, 1] == 7.0).all() and (y[0, 3, :, 3] == 7.0).all()
+    B.kv_q4_store(t.c, 0, 1, 4, k, v, t.ws, count=i32([4, 0, 1, 3]))
+    assert t.faults() == 0
