@@ -235,10 +235,10 @@ __device__ __forceinline__ void copy_words(const uint32_t* from, uint32_t* to, i
 // Workgroup i: sequence dst[i] becomes a copy of src[i] that shares its pages.  Refused, and reported: a slot out of range, a
 // destination that is not empty or is named twice (after the first time), a source that is a destination of the call.
 __global__ __launch_bounds__(kThreads) void q4_fork_kernel(Q4PageArgs a) {
-    __shared__ int bad;
+    __shared__ int bad_call, bad_state;  // (two: a wave may be at the second check while another still reads the first's)
     const Q4Dims& d = a.dims;
     const int i = blockIdx.x, src = a.src_slot[i], dst = a.dst_slot[i];
-    if (threadIdx.x == 0) bad = 0;
+    if (threadIdx.x == 0) bad_call = bad_state = 0;
     __syncthreads();
     const bool range = (uint32_t)src < (uint32_t)d.batch && (uint32_t)dst < (uint32_t)d.batch;
     int mine = !range;
@@ -246,9 +246,9 @@ __global__ __launch_bounds__(kThreads) void q4_fork_kernel(Q4PageArgs a) {
         const int other = a.dst_slot[j];
         mine |= other == src || (j < i && other == dst);
     }
-    if (mine) bad = 1;
+    if (mine) bad_call = 1;
     __syncthreads();
-    if (bad) {  // (before dst's state is read: another workgroup may be writing it)
+    if (bad_call) {  // (before dst's state is read: another workgroup may be writing it)
         if (threadIdx.x == 0) atomicOr(a.faults, kFaultCache);
         return;
     }
@@ -258,9 +258,9 @@ __global__ __launch_bounds__(kThreads) void q4_fork_kernel(Q4PageArgs a) {
     const int32_t* st = a.cache.table + (size_t)src * d.max_pages;
     mine = !fits;
     for (int j = threadIdx.x; j < pages; j += kThreads) mine |= !in_pool(d, st[j]);
-    if (mine) bad = 1;
+    if (mine) bad_state = 1;
     __syncthreads();
-    if (bad) {
+    if (bad_state) {
         if (threadIdx.x == 0) atomicOr(a.faults, kFaultCache);
         return;
     }

@@ -1085,3 +1085,20 @@ def test_counts_beyond_the_rows(dtype):
         assert np.array_equal(y[0, 0].double().cpu().numpy(), got[:, left : left + 4]) and (y[0, 1] == 7.0).all() and (y[0, 3, :, 3] == 7.0).all()
     B.kv_q4_store(t.c, 0, 1, 4, k, v, t.ws, count=i32([4, 0, 1, 3]))
     assert t.faults() == 0
+
+
+def test_fork_refused_by_state_beside_others():
+    """Destinations in use and a source whose table names no page, among forks that are good: each workgroup of the call goes its own
+    way after the second check, whichever of its waves get there first."""
+    t = Cache([1000, 700, 5, 0, 0, 0, 16, 0, 0], layers=1, hq=1, hkv=1, d=64, max_pages=2100, n_pages=130)
+    t.c.table[1, 43] = t.shape.n_pages
+    table, refs = t.c.table.clone(), t.c.refs.clone()
+    for _ in range(3):
+        B.kv_q4_fork(t.c, i32([0, 1, 0, 2, 0, 1]), i32([3, 4, 6, 5, 7, 8]), t.ws)
+        assert t.faults() == B.KV_FAULT_CACHE
+        assert t.c.len.tolist() == [1000, 700, 5, 1000, 0, 5, 16, 1000, 0]
+        for dst, src in ((3, 0), (5, 2), (7, 0)):
+            assert torch.equal(t.c.table[dst], table[src])
+        assert torch.equal(t.c.table[[0, 1, 2, 4, 6, 8]], table[[0, 1, 2, 4, 6, 8]])
+        B.kv_q4_free(t.c, i32([3, 5, 7]), t.ws)
+        assert torch.equal(t.c.refs, refs) and t.faults() == 0
