@@ -154,6 +154,14 @@ struct Slab {
 
 constexpr int kZPad = 16;    // floats between the heads' logits in LDS
 constexpr int kQ4Waves = 8;  // (four: one sequence of 131,072 rows 35 us for 34, scored slabs 215 for 190)
+// Floats of LDS for the waves' and the heads' statistics: whole 16 bytes, since the logits behind them are accessed so.
+__host__ __device__ constexpr int stat_floats(int group) { return (2 * (kQ4Waves + 1) * group + 3) / 4 * 4; }
+constexpr bool logits_aligned() {
+    for (int group = 1; group <= kMaxGroup; ++group)
+        if (stat_floats(group) % 4 || stat_floats(group) < 2 * (kQ4Waves + 1) * group) return false;
+    return kZPad % 4 == 0;  // (a head's logits are n_stride + kZPad floats, n_stride a multiple of 64)
+}
+static_assert(logits_aligned(), "16-byte accesses of the logits in LDS");
 
 // CP columns of a head, NM products with its probabilities' parts (3, 1 or 1, 3).
 template <typename T, int D, int CP, int NM, bool kScored>
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
     const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
     float* const stat = lds + a.stat_at;
     float* const heads = stat + 2 * kQ4Waves * group;  // kScored: [head] maximum, 1 / sum
-    float* const zs = heads + 2 * group;
+    float* const zs = stat + stat_floats(group);
 
     // Grid: KV heads, sequences, then layers and chunks (first chunks first: the later ones, which short sequences lack, spread
     // evenly).  The sequences are turned by one from layer to layer: workgroups a multiple of the CUs apart, which meet on one,
@@ -650,11 +658,11 @@ hipError_t launch_form(Q4AttendArgs a, hipStream_t s) {
     const int slabs = a.layer_count * a.dims.batch * a.dims.hkv;
     const int joined = kJoin * a.dims.group * CP * (D + 4) * (int)sizeof(float), values = kQ4Waves * kValueBytes<D>;
     a.stat_at = (joined > values ? joined : values) / (int)sizeof(float);
-    size_t lds = (size_t)a.stat_at * sizeof(float) + 2 * (kQ4Waves + 1) * a.dims.group * sizeof(float);
+    static_assert(D % 4 == 0 && kValueBytes<D> % 16 == 0, "stat_at is a multiple of 16 bytes");
+    size_t lds = (size_t)(a.stat_at + stat_floats(a.dims.group)) * sizeof(float);
     auto kern = q4_attend_kernel<T, D, CP, NM, kScored>;
     if (kScored) lds += (size_t)a.dims.group * (a.n_stride + kZPad) * sizeof(float);
     if (sizeof(T) == 4) {
-        lds = (lds + 15) / 16 * 16;
         a.q_at = (int)(lds / sizeof(float));
         lds += 3 * (D / 32) * kWave * sizeof(u32x4);
     }
@@ -708,8 +716,8 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     // with scores 190 us, through memory 241.
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
     const size_t outputs = 4 * (size_t)d.group * (d.group <= kMostBeside ? 3 : 1) * (d.d + 4) * sizeof(float);
-    const size_t scored = (values > outputs ? values : outputs) + (size_t)d.group * (18 + p.n_stride + kZPad) * sizeof(float) +
-                          (d.bf16 ? 0 : 16 + 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4));
+    const size_t scored = (values > outputs ? values : outputs) + (stat_floats(d.group) + (size_t)d.group * (p.n_stride + kZPad)) * sizeof(float) +
+                          (d.bf16 ? 0 : 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4));
     p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 2 * cus;
     return p;
 }
