@@ -1,5 +1,6 @@
 // C ABI of the paged 4-bit cache: argument validation, workspace layout and launches.  As in api.hip everything is queued
 // on the caller's stream; nothing is allocated, synchronised or read back.
+#include <float.h>
 #include <math.h>
 
 #include "../../include/inertiakv.h"
@@ -289,7 +290,9 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     a.window = recency_window;
     constexpr double kLog2e = 1.4426950408889634;
     a.scale2 = (float)(kLog2e / sqrt((double)s.head_dim));
-    a.bias2 = (float)(kLog2e * a.bias);
+    // (log2(e) times a bias near the type's border is past it; half of that border still hides every logit, and leaves room above
+    // the running maximum's start for rows that all have it)
+    a.bias2 = (float)fmax(-0.5 * FLT_MAX, fmin(0.5 * FLT_MAX, kLog2e * a.bias));
     a.nchunk = L.plan.nchunk;
     a.chunk_rows = L.plan.chunk_rows;
     a.scored = L.plan.scored;

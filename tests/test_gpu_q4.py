@@ -1102,3 +1102,26 @@ def test_fork_refused_by_state_beside_others():
         assert torch.equal(t.c.table[[0, 1, 2, 4, 6, 8]], table[[0, 1, 2, 4, 6, 8]])
         B.kv_q4_free(t.c, i32([3, 5, 7]), t.ws)
         assert torch.equal(t.c.refs, refs) and t.faults() == 0
+
+
+@pytest.mark.parametrize("bias", [3.0e38, -3.0e38, 2.0e38, float(torch.finfo(torch.float32).max), float(torch.finfo(torch.float32).min)])
+@pytest.mark.parametrize("layers", [1, 32])
+def test_bias_of_the_types_largest(bias, layers):
+    """A finite bias of any size: the rows with it share all weight (or have none where others lack it), alike where it hides the
+    logits; all rows of slot 1 have it, none of slot 2.  32 layers: the logits stay in LDS."""
+    t = Cache([40, 33, 64, 0] * 4, layers=layers, hq=8, hkv=4, d=64, page_rows=16).fill()
+    t.c.pos[:] = torch.arange(t.cap, dtype=torch.int32, device="cuda")
+    q = torch.randn(layers, 16, 8, 64, generator=gen(3)).bfloat16().cuda()
+    cur, window = i32([40, 10, 3000, 0] * 4), 20
+    o, s = torch.full_like(q, 9.0), torch.full((layers, 16, t.cap), 9.0, device="cuda")
+    B.kv_q4_attend(t.c, 0, layers, t.cap, q, o, t.ws, cur_pos=cur, recency_bias=bias, recency_window=window, s_out=s)
+    assert t.faults() == 0
+    for b in range(16):
+        for l in range(0, layers, 5):
+            k, v = t.values(l, b)
+            n = k.shape[1]
+            add = bias * (np.arange(n) >= int(cur[b]) - (window - 1))
+            want, a, _, av = R.attend(q[l, b].double().cpu().numpy(), k, v, add)
+            assert (np.abs(o[l, b].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -12 * av).all(), (b, l)
+            if n:
+                assert np.allclose(s[l, b, :n].double().cpu().numpy(), a.mean(0), rtol=2.0 ** -11, atol=0), (b, l)
