@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
                a.bias2 != 0.0f ? a.cache.pos + (size_t)b * d.cap : nullptr,
                end, last, d.n_pages, d.page_shift, d.page_rows, d.ks_off, d.vc_off,
                (uint32_t)(key_row * (D / 2) + s * (D / 8)), (uint32_t)(D == 128 ? key_row * 4 + s : key_row * 2 + s / 2), 0};
-    const int recent_from = sl.pos ? a.cur_pos[b] - (a.window - 1) : 0;
+    const int recent_from = sl.pos ? (int)max((int64_t)INT_MIN, (int64_t)a.cur_pos[b] - (a.window - 1)) : 0;
     float m = -FLT_MAX, l = 0.0f;
     f32x4 acc[kOut];
 #pragma unroll

@@ -1125,3 +1125,15 @@ def test_bias_of_the_types_largest(bias, layers):
             assert (np.abs(o[l, b].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -12 * av).all(), (b, l)
             if n:
                 assert np.allclose(s[l, b, :n].double().cpu().numpy(), a.mean(0), rtol=2.0 ** -11, atol=0), (b, l)
+
+
+def test_recent_border_below_the_integers():
+    """cur_pos - (window - 1) below every 32-bit number: all rows are recent, those of the largest positions no more than others."""
+    t = Cache([40, 25], hq=4, hkv=2).fill()
+    t.c.pos[:, ::3] = (1 << 31) - 1
+    t.c.pos[:, 1::3] = -(1 << 31)
+    q = torch.randn(1, 2, 4, 128, generator=gen(3)).bfloat16().cuda()
+    o = torch.empty_like(q)
+    cur = i32([-10, -(1 << 31)])
+    B.kv_q4_attend(t.c, 0, 1, t.cap, q, o, t.ws, cur_pos=cur, recency_bias=1.5, recency_window=(1 << 31) - 1)
+    check_attend(t, q, o, cur, 1.5, (1 << 31) - 1)
