@@ -430,7 +430,7 @@ class KvQ4Cache:
         # what every call passes or compares with, taken once (building it took 4 us of a call's 13)
         self._shape, self._buffers = ctypes.byref(self._own), ctypes.byref(self._addresses)
         self._batch, self._rows = shape.batch, shape.batch * cap
-        self._heads, self._dim = shape.n_kv_heads, shape.head_dim
+        self._heads, self._dim, self._query = shape.n_kv_heads, shape.head_dim, (shape.batch, shape.n_q_heads, shape.head_dim)
 
     pool, table, len, refs = (_q4_buffer(name, True) for name in ("pool", "table", "len", "refs"))
     u, pos = _q4_buffer("u", False), _q4_buffer("pos", False)
@@ -458,6 +458,15 @@ class KvQ4Cache:
 def _q4_ok(t, dtype, numel, device):
     """Whether a buffer that a kernel indexes without knowing its size is none, or has the type, place, layout and size."""
     return t is None or (t.dtype is dtype and t.numel() >= numel and t.get_device() == device and t.is_contiguous())
+
+
+def _q4_heads(cache, t, layers):
+    """Whether queries or outputs have the cache's type and place, and the heads of `layers` layers at least, in order."""
+    if t is None:
+        return False
+    s = tuple(t.shape)
+    return (t.dtype is cache.element and t.get_device() == cache._device and t.is_contiguous()
+            and (s == cache._query and layers == 1 or s[1:] == cache._query and s[0] >= layers))
 
 
 def _q4_tail(fn, cache, ws, stream):
@@ -512,11 +521,10 @@ def kv_q4_load(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None
 
 def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos=None, recency_bias=0.0, recency_window=0,
                  s_out=None, alpha=0.0, u_prior=None, u_out=None, stream=None):
-    """q, o: [layer_count][batch][n_q_heads][head_dim]; cur_pos: [batch] int32; s_out: [layer_count][batch][n_max] f32;
-    u_prior, u_out: [batch][capacity] f32."""
-    s, n, dev, f32 = cache._own, cache._batch, cache._device, torch.float32
-    size = layer_count * n * s.n_q_heads * s.head_dim
-    if not (_q4_ok(q, cache.element, size, dev) and _q4_ok(o, cache.element, size, dev) and _q4_ok(cur_pos, torch.int32, n, dev)
+    """q, o: [layer_count][batch][n_q_heads][head_dim] (of more layers: the first ones; of one layer, its dimension may be left
+    out); cur_pos: [batch] int32; s_out: [layer_count][batch][n_max] f32; u_prior, u_out: [batch][capacity] f32."""
+    n, dev, f32 = cache._batch, cache._device, torch.float32
+    if not (_q4_heads(cache, q, layer_count) and _q4_heads(cache, o, layer_count) and _q4_ok(cur_pos, torch.int32, n, dev)
             and _q4_ok(s_out, f32, layer_count * n * n_max, dev) and _q4_ok(u_prior, f32, cache._rows, dev)
             and _q4_ok(u_out, f32, cache._rows, dev)):
         raise KVError("kv_q4_attend", KV_ERR_INVALID_ARG)

@@ -248,3 +248,16 @@ def test_a_cache_follows_its_buffers():
     assert c.shape.n_pages == GOOD["n_pages"] and c.shape.max_pages == GOOD["max_pages"]
     with pytest.raises(AttributeError):
         c.shape = s
+
+
+def test_attend_checks_the_order_of_heads():
+    """Queries and outputs of the right size in another order are refused, as kv_q4_store refuses such rows (host tensors: what
+    passes the check is refused for its place, with the same status, so the check is looked at by itself)."""
+    c = host_cache()  # 4 layers, 3 slots, 8 query heads of 128
+    good = [torch.zeros(4, 3, 8, 128), torch.zeros(2, 3, 8, 128), torch.zeros(1, 3, 8, 128), torch.zeros(3, 8, 128)]
+    fits = lambda t, layers: B._q4_heads(c, t.bfloat16(), layers)
+    assert fits(good[0], 4) and fits(good[0], 1) and fits(good[1], 2) and fits(good[2], 1) and fits(good[3], 1)
+    assert not fits(good[1], 3) and not fits(good[3], 2)
+    for shape_ in ((3, 4, 8, 128), (4, 8, 3, 128), (4, 3, 128, 8), (4 * 3, 8, 128), (4, 3, 8 * 128), (4 * 3 * 8 * 128,), (8, 3, 128), (2, 2, 3, 8, 128)):
+        assert not fits(torch.zeros(*shape_), 4 if len(shape_) == 4 else 1), shape_
+    assert not B._q4_heads(c, None, 1) and not B._q4_heads(c, good[0], 4) and not fits(good[0].transpose(0, 1).reshape(4, 8, 3, 128).transpose(1, 2), 4)
