@@ -1137,3 +1137,93 @@ def test_recent_border_below_the_integers():
     cur = i32([-10, -(1 << 31)])
     B.kv_q4_attend(t.c, 0, 1, t.cap, q, o, t.ws, cur_pos=cur, recency_bias=1.5, recency_window=(1 << 31) - 1)
     check_attend(t, q, o, cur, 1.5, (1 << 31) - 1)
+
+
+# ---- calls of many rounds and many chunks -------------------------------------------------------------------
+
+def origin_of(keep):
+    """The row that ends at each place: the kept rows behind the new end fill the holes before it, both ascending."""
+    k = int(keep.sum())
+    origin = np.arange(k)
+    origin[np.nonzero(keep[:k] == 0)[0]] = k + np.nonzero(keep[k:])[0]
+    return origin
+
+
+@pytest.mark.parametrize("how", ["evict", "compact"])
+@pytest.mark.parametrize("layers,lens,forks,hkv,d,page_rows,dtype", [
+    (8, [4000, 2501, 1000], [0, 0, 1, 1, 2], 4, 128, 64, "bf16"),   # 16 workgroups a sequence and layer: a dozen rounds of 16 rows each
+    (8, [3999, 2048], [0, 1, 0, 1, 0, 1], 16, 64, 32, "f32"),       # more copies a round than the workgroup has in flight
+    (64, [700, 333, 129, 16], [0] * 6 + [1] * 6, 1, 64, 16, "bf16"),  # one workgroup: dozens of rounds
+    (64, [515, 700], [0] * 14, 3, 128, 128, "bf16")])
+def test_moves_of_many_rounds(layers, lens, forks, hkv, d, page_rows, dtype, how):
+    """The keys and values of sequences whose moved rows and replaced pages take many rounds of copies, whole and partial ones."""
+    src = list(range(len(lens), len(lens) + len(forks)))
+    t = Cache(lens + [0] * len(forks), layers=layers, hq=hkv, hkv=hkv, d=d, page_rows=page_rows, dtype=dtype,
+              spare=sum(-(-m // page_rows) for m in lens + [lens[f] for f in forks])).fill()
+    B.kv_q4_fork(t.c, i32(forks), i32(src), t.ws)
+    n = t.c.len.tolist()
+    assert n == lens + [lens[f] for f in forks]
+    rows = max(n)
+    t.c.u.copy_(torch.rand(t.c.u.shape, generator=gen(4)))  # each sample ranks its rows for itself
+    u, pos = t.c.u.cpu().numpy(), t.c.pos.cpu().numpy()
+    old, new = ([torch.zeros(layers, len(n), hkv, rows, d, dtype=DT[dtype], device="cuda") for _ in range(2)] for _ in range(2))
+    B.kv_q4_load(t.c, 0, layers, rows, *old, t.ws, first=i32([0] * len(n)), count=t.c.len)
+    budget = [max(1, int(m * (0.55 - 0.04 * (b % 9)))) | 1 for b, m in enumerate(n)]
+    keep = np.zeros((len(n), t.cap), dtype=np.uint8)
+    for b, m in enumerate(n):
+        keep[b, np.lexsort((pos[b, :m], -u[b, :m].astype(np.float64)))[: budget[b]]] = 1
+    if how == "evict":
+        B.kv_q4_evict(t.c, rows, i32(budget), t.ws)
+    else:
+        B.kv_q4_compact(t.c, rows, torch.from_numpy(keep).cuda(), t.ws)
+    assert t.c.len.tolist() == budget and t.faults() == 0
+    B.kv_q4_load(t.c, 0, layers, max(budget), *(x[:, :, :, : max(budget)] for x in new), t.ws, first=i32([0] * len(n)), count=t.c.len)
+    for b, m in enumerate(n):
+        origin = origin_of(keep[b, :m])
+        at = torch.from_numpy(origin).cuda()
+        for x, y in zip(old, new):
+            assert torch.equal(y[:, b, :, : len(origin)], x[:, b].index_select(2, at)), b
+        assert np.array_equal(t.c.u[b, : len(origin)].cpu().numpy(), u[b, origin])
+        assert np.array_equal(t.c.pos[b, : len(origin)].cpu().numpy(), pos[b, origin])
+    refs = torch.bincount(t.c.table[t.c.table >= 0].flatten().long(), minlength=t.shape.n_pages).to(torch.int32)
+    assert torch.equal(refs, t.c.refs)
+
+
+@pytest.mark.parametrize("n", [20000, 131072])
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "bf16"), (128, "f32"), (64, "f32")])
+def test_attention_in_many_chunks(n, d, dtype):
+    """One slab of so many rows is cut into 79 and 512 chunks of 256 rows.  Values are the same over 128 rows and keys lean
+    towards the queries in some of them, so that each chunk has its own output and maximum, and a chunk left out, or counted
+    twice, shows.  Sums: 32 rows in a product, 8 waves, at most 512 chunks, each addition off by 2^-24."""
+    t = Cache([n], hq=2, hkv=1, d=d, page_rows=256, dtype=dtype)
+    q = torch.randn(1, 1, 2, d, generator=gen(3)).to(DT[dtype])
+    span = torch.arange(n) // 128
+    v = torch.randn(int(span.max()) + 1, d, generator=gen(2))[span]
+    lean = torch.rand(int(span.max()) + 1, generator=gen(4))[span]
+    k = 0.3 * torch.randn(n, d, generator=gen(1)) + 0.15 * lean[:, None] * q[0, 0].float().mean(0)
+    B.kv_q4_store(t.c, 0, 1, n, *(x[None, None, None].to(DT[dtype]).cuda() for x in (k, v)), t.ws)
+    kk, vv = t.values(0, 0)
+    want, a, size, av = R.attend(q[0, 0].double().numpy(), kk, vv)
+    rel = 2 * ((d + 4) * 2.0 ** -24 * size + 2.0 ** -22 * size) + (32 + 8 + 512 + 64) * 2.0 ** -24
+    lim = 2.0 ** -8 * np.abs(want) + (rel + 2.0 ** -15) * av if dtype == "bf16" else (rel + 2.0 ** -23) * av
+    q = q.cuda()
+    for scores in (False, True):
+        o, s = torch.full_like(q, 9.0), torch.full((1, 1, n), 9.0, device="cuda")
+        B.kv_q4_attend(t.c, 0, 1, n, q, o, t.ws, s_out=s if scores else None)
+        assert (np.abs(o[0, 0].double().cpu().numpy() - want) <= lim).all(), scores
+    got = s[0, 0].double().cpu().numpy()
+    assert (np.abs(got - a.mean(0)) <= (rel + 2 * 2.0 ** -24) * a.mean(0)).all() and t.faults() == 0
+
+
+def test_smaller_calls_of_one_workspace():
+    """Every way of dividing fewer rows and layers than the workspace was made for gives what the model gives."""
+    t = Cache([1500, 3], layers=5, hq=4, hkv=2, page_rows=64).fill()
+    t.ws = B.q4_workspace(t.shape, 1500, 5)
+    q = torch.randn(5, 2, 4, 128, generator=gen(3)).bfloat16().cuda()
+    room = torch.empty(5 * 2 * 1500, device="cuda")
+    for n in (1500, 1499, 1281, 1280, 1025, 1024, 513, 512, 300, 256, 255, 1):
+        t.c.len.copy_(torch.tensor([n, min(n, 3)]))
+        for layers in (1, 2, 3, 4, 5):
+            o, s = torch.full_like(q[:layers], 9.0), room[: layers * 2 * n].view(layers, 2, n).fill_(9.0)
+            B.kv_q4_attend(t.c, 5 - layers, layers, n, q[:layers], o, t.ws, s_out=s)
+            check_attend(t, q[:layers], o, s_out=s, layer0=5 - layers)
