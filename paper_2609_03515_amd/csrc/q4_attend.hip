@@ -706,12 +706,12 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     p.most = want < by_rows ? want : by_rows;
     const int least = (n_max + kMostRows - 1) / kMostRows;
     if (least > p.most) p.most = least;
-    // (whole turns of the waves; a few rows more than those do not make a turn, and may make a chunk more: 4,097 rows in 9 chunks of
-    // 512 for 6 of 768, 64 slabs of f32 with scores: 27.8 -> 26.4 us)
-    const int share = (n_max + p.most - 1) / p.most - (p.most > 1 ? step / 16 : 0);
+    // (whole turns of the waves, so there may be fewer: 64 slabs of 4,097 rows in 6 chunks of 768.  One more chunk where a few rows
+    // make the turn, 9 of 512 for these, costs more than it balances, and a kernel with a workgroup per head to join them: bf16
+    // 18.4 -> 19.6 us, f32 19.1 -> 20.7, 2,049 rows 13.4 -> 17.3; 512 slabs of 8,193 rows 107 -> 109.5)
+    const int share = (n_max + p.most - 1) / p.most;
     p.chunk_rows = share > step ? (share + step - 1) / step * step : step;
     p.nchunk = (n_max + p.chunk_rows - 1) / p.chunk_rows;
-    if (p.most > 1) p.most += p.most / 8 + 1;  // (a share is 240 / 256 of itself at least)
     // Scored: where a slab's logits fit LDS with two workgroups on a CU, and there is a slab for each: 2,048 slabs of 3,277 rows
     // with scores 190 us, through memory 241.
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
