@@ -479,8 +479,10 @@ __device__ Border border_of_few(const Ranked<kInLds>& rows, int budget, uint64_t
 // With K(i) the kept rows before row i, from one mask bit a row and the masks' prefix sums: a dropped row i before the new end
 // is hole i - K(i), a kept row behind it the (K(i) - K(end))-th that moves, and a page has a hole when its rows number more than
 // K grows over it.
-constexpr int kFewEvicted = 4;      // so few are found one after the other
-constexpr int kRowsInLds = 32768;   // masks, prefix sums and keys of so many rows lie in LDS (kInLds), of more in memory
+// So few are found one after the other: an eviction of 1, 2, 3, 4 rows of 8 x 3,277 takes 19, 22, 25 and 28 us, by radix passes 32 to
+// 34 for any; they meet at 6 there, at 8 for 1,000 rows, and between 1 and 6 for 16,500 and more, as the utilities' bits have it.
+constexpr int kFewEvicted = 4;
+constexpr int kRowsInLds = 32768;  // masks, prefix sums and keys of so many rows lie in LDS (kInLds), of more in memory
 template <bool kEvict, int kBlock, bool kInLds>
 __global__ __launch_bounds__(kBlock) void q4_compact_plan_kernel(Q4PageArgs a) {
     constexpr int kWaves = kBlock / kWave;
@@ -829,7 +831,8 @@ hipError_t launch_q4_compact(const Q4PageArgs& a, hipStream_t s) {
     // parts of a sequence's rows: four workgroups per CU in all, no more than there can be entries for (two 52 us, three 46.5, four
     // 44.8, six 47.6 in the case above)
     const int slabs = a.dims.layers * a.dims.batch, most = (a.n_max + kEntries - 1) / kEntries;
-    const int want = (4 * 256 + slabs - 1) / slabs, parts = want < most ? want : most;
+    const int cus = device_cus() > 0 ? device_cus() : 256;
+    const int want = (4 * cus + slabs - 1) / slabs, parts = want < most ? want : most;
     const dim3 grid(parts, a.dims.layers + 1, a.dims.batch);
     if (a.dims.d == 128) hipLaunchKernelGGL(q4_move_kernel<128>, grid, dim3(kMoveBlock), 0, s, a);
     else hipLaunchKernelGGL(q4_move_kernel<64>, grid, dim3(kMoveBlock), 0, s, a);
