@@ -10,11 +10,12 @@
 //    codes, one scale.  A code with its scale is a bf16 number exactly, and the conversion applies the scale, so the product with a bf16 query is
 //    exact up to the order of 32-bit sums.  The query's elements lie in the same order.  f32 queries: three bf16 parts whose
 //    sum is the number, a product each.
-//  * logits: the result holds rows s, 4 + s, 8 + s, 12 + s of each half for column c.  A column is a head; where three times the
-//    group fits 16 columns, the heads are there twice more, for the parts below.
+//  * logits: the result holds rows s, 4 + s, 8 + s, 12 + s of each half for column c.  A column is a head; where three or two times
+//    the group fits 16 columns, the heads are there again, for the parts below.
 //  * probabilities p = 2^(z - m): as a B operand, the same lane holds the same rows, so nothing moves between lanes.  p is
 //    split into three bf16 parts of 8 bits that sum up to all 24 of its bits, a column of its own each or a product of its own
-//    (two parts, 16 bits, are up to 2^-15 low: no slower in columns, in products 72 us for 78 in 4 layers of 32 x 1 .. 8,192 rows).
+//    (4 layers of 32 x 1 .. 8,192 rows, 7 heads a KV head: 78 us with three products, 75 with two columns and two products, and 72
+//    with two parts, which are up to 2^-15 low; in three columns the third costs nothing).
 //  * values: loaded to LDS as they lie in memory, without registers; the lane takes the same rows' elements 8 c .. 8 c + 7
 //    (d = 64: 4 c ...; the four rows that a read of the wave takes are consecutive, so no two lanes meet in a bank), converted
 //    like the keys; pairs of rows of one element are put together by byte permutes of the lane's own registers.
@@ -163,9 +164,10 @@ constexpr bool logits_aligned() {
 }
 static_assert(logits_aligned(), "16-byte accesses of the logits in LDS");
 
-// CP columns of a head, NM products with its probabilities' parts (3, 1 or 1, 3).
-template <typename T, int D, int CP, int NM, bool kScored>
-__global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendArgs a) {
+// Columns of a head for the parts of its probabilities (CP): as many as fit 16, three, two or one, with one, two and three products.
+constexpr int columns_of(int group) { return group <= 5 ? 3 : group <= 8 ? 2 : 1; }
+template <typename T, int D, int CP, bool kScored>
+__device__ __forceinline__ void attend(const Q4AttendArgs& a) {
     constexpr int kThreads = kWave * kQ4Waves, kStep = kTile * kQ4Waves;
     constexpr int kKey = D / 32, kOut = D / 16;      // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of a query
@@ -183,8 +185,11 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
     const int part = c / group, head = c % group;
     const bool column = part < CP;
     const int columns = CP * group;
-    // a part is what lies between two cuts of a probability's bits (part 0's lower ones go with the rounding to bf16)
-    const uint32_t cut_low = part == 1 ? 0xffffff00u : ~0u, cut_high = part == 0 ? 0u : part == 1 ? 0xffff0000u : 0xffffff00u;
+    // A part is what lies between two cuts of a probability's bits (the highest part's lower bits go with the rounding to bf16).  Two
+    // columns: the highest and the middle part in one product, the lowest and nothing in the other.
+    const uint32_t cut_low = CP == 3 && part != 1 ? ~0u : 0xffffff00u;
+    const uint32_t cut_high = CP == 3 && part == 2 ? 0xffffff00u : CP > 1 && part == 0 ? 0u : 0xffff0000u;
+    const uint32_t pick_lowest = CP == 2 && part == 1 ? 0x0c0c0c0cu : 0x07060302u;
     // the lane's places in the wave's LDS: codes of elements D / 16 * c ... of row s, and their scale
     uint8_t* const value_lds = reinterpret_cast<uint8_t*>(lds) + wave * kValueBytes<D>;
     const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
@@ -346,18 +351,20 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
             p[j] = exp2_hw(z[j] - m);
             l += p[j];
         }
-        if constexpr (CP == 3)
+        u32x4 pp{}, lowest{}, highest{};
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                p[j] = __uint_as_float(__float_as_uint(p[j]) & cut_low) - __uint_as_float(__float_as_uint(p[j]) & cut_high);
-        u32x4 pp[NM];
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w[2] = {__float_as_uint(p[2 * i]), __float_as_uint(p[2 * i + 1])};
+            float x[2], low[2];
 #pragma unroll
-        for (int k = 0; k < NM; ++k) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pp[k][i] = high2(__float_as_uint(p[2 * i]), __float_as_uint(p[2 * i + 1]));
-            if (k + 1 < NM)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] -= __uint_as_float(__float_as_uint(p[j]) & 0xffff0000u);
+            for (int k = 0; k < 2; ++k) {
+                const float upper = __uint_as_float(w[k] & cut_low);
+                x[k] = upper - __uint_as_float(w[k] & cut_high);
+                low[k] = p[2 * i + k] - upper;
+            }
+            pp[i] = high2(__float_as_uint(x[0]), __float_as_uint(x[1]));
+            if constexpr (CP < 3) lowest[i] = __builtin_amdgcn_perm(__float_as_uint(low[1]), __float_as_uint(low[0]), pick_lowest);
+            if constexpr (CP == 1) highest[i] = high2(w[0], w[1]);
         }
         // output
         float scale[8];
@@ -388,11 +395,13 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
             for (int j = 0; j < 8; ++j) x[j] = pair<kByte>(codes[j], scale[j]);
             const u32x4 even{low2(x[0], x[1]), low2(x[2], x[3]), low2(x[4], x[5]), low2(x[6], x[7])};
             const u32x4 odd{high2(x[0], x[1]), high2(x[2], x[3]), high2(x[4], x[5]), high2(x[6], x[7])};
-#pragma unroll
-            for (int k = NM - 1; k >= 0; --k) {
-                acc[2 * kByte] = mfma(even, pp[k], acc[2 * kByte]);
-                acc[2 * kByte + 1] = mfma(odd, pp[k], acc[2 * kByte + 1]);
-            }
+            auto both = [&](u32x4 q) __attribute__((always_inline)) {
+                acc[2 * kByte] = mfma(even, q, acc[2 * kByte]);
+                acc[2 * kByte + 1] = mfma(odd, q, acc[2 * kByte + 1]);
+            };
+            if constexpr (CP < 3) both(lowest);
+            both(pp);
+            if constexpr (CP == 1) both(highest);
         };
         two_columns(std::integral_constant<int, 0>());
         two_columns(std::integral_constant<int, 1>());
@@ -490,6 +499,15 @@ __global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendA
             *reinterpret_cast<f32x4*>(rp + r) = x;
         }
     }
+}
+
+template <typename T, int D, int CP, bool kScored>
+__global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_kernel(Q4AttendArgs a) {
+    attend<T, D, CP, kScored>(a);
+}
+template <typename T, int D, bool kScored>
+__global__ __launch_bounds__(kWave* kQ4Waves, 4) void q4_attend_pairs_kernel(Q4AttendArgs a) {
+    attend<T, D, 2, kScored>(a);
 }
 
 // A few chunks: one workgroup per slab joins their outputs and statistics, four elements of a head per thread and all of its
@@ -652,15 +670,14 @@ __global__ __launch_bounds__(kScoreWaves* kWave) void q4_score_kernel(Q4AttendAr
     if (wave == 0 && live && a.u_out) a.u_out[ub] = u;
 }
 
-template <typename T, int D, int CP, int NM, bool kScored>
-hipError_t launch_form(Q4AttendArgs a, hipStream_t s) {
+template <typename T, int D, int CP, bool kScored>
+hipError_t launch_form(Q4AttendArgs a, hipStream_t s, void (*kern)(Q4AttendArgs)) {
     constexpr int kJoin = 4;
     const int slabs = a.layer_count * a.dims.batch * a.dims.hkv;
     const int joined = kJoin * a.dims.group * CP * (D + 4) * (int)sizeof(float), values = kQ4Waves * kValueBytes<D>;
     a.stat_at = (joined > values ? joined : values) / (int)sizeof(float);
     static_assert(D % 4 == 0 && kValueBytes<D> % 16 == 0, "stat_at is a multiple of 16 bytes");
     size_t lds = (size_t)(a.stat_at + stat_floats(a.dims.group)) * sizeof(float);
-    auto kern = q4_attend_kernel<T, D, CP, NM, kScored>;
     if (kScored) lds += (size_t)a.dims.group * (a.n_stride + kZPad) * sizeof(float);
     if (sizeof(T) == 4) {
         a.q_at = (int)(lds / sizeof(float));
@@ -679,17 +696,16 @@ hipError_t launch_form(Q4AttendArgs a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <typename T, int D, int CP, int NM>
-hipError_t launch_attend(const Q4AttendArgs& a, hipStream_t s) {
-    return a.scored ? launch_form<T, D, CP, NM, true>(a, s) : launch_form<T, D, CP, NM, false>(a, s);
+template <typename T, int D, bool kScored>
+hipError_t launch_columns(const Q4AttendArgs& a, hipStream_t s) {
+    const int columns = columns_of(a.dims.group);
+    if (columns == 3) return launch_form<T, D, 3, kScored>(a, s, q4_attend_kernel<T, D, 3, kScored>);
+    if (columns == 2) return launch_form<T, D, 2, kScored>(a, s, q4_attend_pairs_kernel<T, D, kScored>);
+    return launch_form<T, D, 1, kScored>(a, s, q4_attend_kernel<T, D, 1, kScored>);
 }
-
-// The three parts of a probability: columns beside each other where they fit, products of their own where they do not.
-constexpr int kMostBeside = 5;
-template <int D>
-hipError_t launch_by_group(const Q4AttendArgs& a, hipStream_t s) {
-    if (a.dims.group <= kMostBeside) return a.dims.bf16 ? launch_attend<bf16_t, D, 3, 1>(a, s) : launch_attend<float, D, 3, 1>(a, s);
-    return a.dims.bf16 ? launch_attend<bf16_t, D, 1, 3>(a, s) : launch_attend<float, D, 1, 3>(a, s);
+template <typename T, int D>
+hipError_t launch_attend(const Q4AttendArgs& a, hipStream_t s) {
+    return a.scored ? launch_columns<T, D, true>(a, s) : launch_columns<T, D, false>(a, s);
 }
 
 }  // namespace
@@ -715,7 +731,7 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     // Scored: where a slab's logits fit LDS with two workgroups on a CU, and there is a slab for each: 2,048 slabs of 3,277 rows
     // with scores 190 us, through memory 241.
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
-    const size_t outputs = 4 * (size_t)d.group * (d.group <= kMostBeside ? 3 : 1) * (d.d + 4) * sizeof(float);
+    const size_t outputs = 4 * (size_t)d.group * columns_of(d.group) * (d.d + 4) * sizeof(float);
     const size_t scored = (values > outputs ? values : outputs) + (stat_floats(d.group) + (size_t)d.group * (p.n_stride + kZPad)) * sizeof(float) +
                           (d.bf16 ? 0 : 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4));
     p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 2 * cus;
@@ -723,7 +739,8 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
 }
 
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s) {
-    hipError_t e = a.dims.d == 128 ? launch_by_group<128>(a, s) : launch_by_group<64>(a, s);
+    hipError_t e = a.dims.bf16 ? (a.dims.d == 128 ? launch_attend<bf16_t, 128>(a, s) : launch_attend<bf16_t, 64>(a, s))
+                                : (a.dims.d == 128 ? launch_attend<float, 128>(a, s) : launch_attend<float, 64>(a, s));
     if (e != hipSuccess || !a.z) return e;
     // Waves: as many as the call's layers have KV heads, up to 16, a power of two of them to a layer: the one that leaves a wave the
     // fewest (layer, KV head) pairs, the lower where they are the same.  (A wave to a layer leaves one sum to add: 32 layers of 8

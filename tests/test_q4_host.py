@@ -261,3 +261,14 @@ def test_attend_checks_the_order_of_heads():
     for shape_ in ((3, 4, 8, 128), (4, 8, 3, 128), (4, 3, 128, 8), (4 * 3, 8, 128), (4, 3, 8 * 128), (4 * 3 * 8 * 128,), (8, 3, 128), (2, 2, 3, 8, 128)):
         assert not fits(torch.zeros(*shape_), 4 if len(shape_) == 4 else 1), shape_
     assert not B._q4_heads(c, None, 1) and not B._q4_heads(c, good[0], 4) and not fits(good[0].transpose(0, 1).reshape(4, 8, 3, 128).transpose(1, 2), 4)
+
+
+def test_attention_pairs_registers():
+    """The attention of 6 to 8 heads a KV head keeps four waves per SIMD as well."""
+    import test_kernel_resources as K
+
+    objs = K.code_object(open(B.LIB_PATH, "rb").read())
+    seen = {k[".name"]: k for o in objs for k in K.metadata(o)["amdhsa.kernels"] if "q4_attend_pairs_kernel" in k[".name"]}
+    assert len(seen) == 8
+    assert max(k[".vgpr_count"] for k in seen.values()) <= 128
+    assert max(k[".vgpr_spill_count"] for k in seen.values()) <= 2
