@@ -319,8 +319,9 @@ kv_status kv_evict_finish(const kv_shape* shape, const kv_params* params, int32_
  * Elements: blocks of 32 consecutive elements of a row hold one scale byte E and 32 codes of 4 bits (sign, two exponent
  * bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6; the OCP microscaling format MXFP4); an element is code * 2^(E - 127).
  * Storing takes the smallest e = E - 127 in [-100, 125] with max |x| < 7 * 2^e and rounds x / 2^e to the nearest code, ties
- * to the even code, saturating at 6: the error is at most half the distance of two neighbouring codes, at most 2^e.  A block
- * with an infinite or NaN element gets E = 255 and reads back as NaN.  A row of d = 128 takes 68 bytes (bf16: 256).
+ * to the even code, saturating at 6: the error is at most half the distance of two neighbouring codes, at most 2^e (where
+ * max |x| >= 7 * 2^125, past the largest e, elements above 6 * 2^125 are stored as that, and are off by less than 2^126).  A
+ * block with an infinite or NaN element gets E = 255 and reads back as NaN.  A row of d = 128 takes 68 bytes (bf16: 256).
  *
  * Pool: [layers][n_pages][n_kv_heads][record], kv_q4_pool_bytes() bytes, no initialisation needed.  A record holds page_rows
  * rows of one KV head: keys' codes [page_rows][d / 2] (element 2 i in the low half of byte i), keys' scales
@@ -399,9 +400,11 @@ kv_status kv_q4_load(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t
  * kv_attend_score: q and o are [layer_count][batch][n_q_heads][d]; recency_bias is added to the logits of rows with
  * pos >= cur_pos[b] - (recency_window - 1) (cur_pos and cache->pos are needed for a bias other than 0 in a window other than
  * 0 only).  A slot without rows, or longer than n_max (KV_FAULT_CACHE), gets zeros; rows in pages that do not exist
- * (KV_FAULT_CACHE) take no part.  s_out (nullable, [layer_count][batch][n_max]) receives the pooled scores of Eq. 1, 0
- * behind the slot's rows; u_out (nullable, [batch][capacity], may be u_prior) the fold of Eq. 4 over the call's layers
- * in order, u_out = alpha u + (1 - alpha) s from u_prior, for the slot's rows (others are left as they were).
+ * (KV_FAULT_CACHE) take no part.  Values are summed with weights of up to 2^8 in 32 bits before the sum is divided by the
+ * weights': outputs are certain to be finite while |v| times the rows is below 2^119.  s_out (nullable,
+ * [layer_count][batch][n_max]) receives the pooled scores of Eq. 1, 0 behind the slot's rows; u_out (nullable,
+ * [batch][capacity], may be u_prior) the fold of Eq. 4 over the call's layers in order, u_out = alpha u + (1 - alpha) s from
+ * u_prior, for the slot's rows (others are left as they were).
  * Refused (KV_ERR_UNSUPPORTED: take fewer layers a call): layer_count * ceil(n_max / 8192) above 65535, and, where slots are
  * worked on in parts, layer_count * batch * n_q_heads from 2^23 on. */
 kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t n_max,

@@ -24,10 +24,10 @@
 // output is rare.  Rows behind the sequence, and rows of pages that do not exist, get the logit -inf and their values the
 // scale 1 (whatever their bytes are), so that they add 0 * a finite number.
 //
-// What bounds it, measured: all layers of 8 sequences x 3,277 rows x 8 KV heads of 4 (bf16, 913 MB) take 157 us, 5.8 TB/s (a
-// large copy reaches 4.9); with the arithmetic left out of a copy of the kernel the same loads take 141, and 164 when they do not
-// pass the caches by.  One layer of it (28.5 MB) is a matter of latencies: 13 us and 4 for the join, of which an empty kernel is
-// 2.5 and the loads alone 9.  One sequence of 131,072 rows, 143 MB: 27 us + 4.5.
+// What bounds it, measured: all layers of 8 sequences x 3,277 rows x 8 KV heads of 4 (bf16, 913 MB) take 160 us, 5.7 TB/s (a
+// large copy reaches 4.9); with the arithmetic left out of a copy of the kernel the same loads take 144, and 164 when they do not
+// pass the caches by.  One layer of it (28.5 MB) is a matter of latencies: 13 us and 4 for the join; without the arithmetic 10 and
+// 4.  One sequence of 131,072 rows, 143 MB: 27 us + 4.5.
 // On the way (all layers): 190 us with the values in registers and cached loads.  Equal shares of all tiles per workgroup, whatever
 // sequence they belong to, took 226 (the search for the share, and the state that it needs).
 #include <float.h>
@@ -200,8 +200,8 @@ __device__ __forceinline__ void attend(const Q4AttendArgs& a) {
 
     // Grid: KV heads, sequences, then layers and chunks (first chunks first: the later ones, which short sequences lack, spread
     // evenly).  The sequences are turned by one from layer to layer: workgroups a multiple of the CUs apart, which meet on one,
-    // would often be of the same sequence (32 sequences of 1 .. 8,192 rows, 16 slabs each: 80 us, turned 73; two prompts of up
-    // to 16,400 rows among six short samples: 218 -> 190 with that whole step).
+    // would often be of the same sequence (32 sequences of 1 .. 8,192 rows, 16 slabs each: 85 us, turned 78; two prompts of up
+    // to 16,400 rows among six short samples: 201 -> 174 with that whole step).
     const int g = blockIdx.x, b = (blockIdx.y + blockIdx.z) % d.batch;
     const int chunk = kScored ? 0 : blockIdx.z / a.layer_count, layer = kScored ? blockIdx.z : blockIdx.z % a.layer_count;
     const int lb = layer * d.batch + b, slab = lb * d.hkv + g;
@@ -729,7 +729,7 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     p.chunk_rows = share > step ? (share + step - 1) / step * step : step;
     p.nchunk = (n_max + p.chunk_rows - 1) / p.chunk_rows;
     // Scored: where a slab's logits fit LDS with two workgroups on a CU, and there is a slab for each: 2,048 slabs of 3,277 rows
-    // with scores 190 us, through memory 241.
+    // with scores 188 us, through memory 232.
     const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
     const size_t outputs = 4 * (size_t)d.group * columns_of(d.group) * (d.d + 4) * sizeof(float);
     const size_t scored = (values > outputs ? values : outputs) + (stat_floats(d.group) + (size_t)d.group * (p.n_stride + kZPad)) * sizeof(float) +
