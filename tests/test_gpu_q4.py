@@ -1227,3 +1227,58 @@ def test_smaller_calls_of_one_workspace():
             o, s = torch.full_like(q[:layers], 9.0), room[: layers * 2 * n].view(layers, 2, n).fill_(9.0)
             B.kv_q4_attend(t.c, 5 - layers, layers, n, q[:layers], o, t.ws, s_out=s)
             check_attend(t, q[:layers], o, s_out=s, layer0=5 - layers)
+
+
+def test_thousands_of_slots():
+    """More slots than a workgroup has threads: pages in the slots' order, copies on write, a call that runs out of pages, and
+    attention, forks and frees of most slots at once."""
+    batch = 2500
+    t = Twin(batch=batch, n_pages=4300, max_pages=3, layers=1, hkv=1)
+    r = np.random.RandomState(5)
+    t.append([int(x) for x in r.randint(1, 20, 1100)] + [0] * (batch - 1100), [3] * batch)
+    t.check()
+    src, dst = list(range(1100)), list(range(1100, 2200))
+    B.kv_q4_fork(t.c, i32(src), i32(dst), t.ws)
+    t.m.fork(src, dst)
+    t.check()
+    t.append([int(x) for x in r.randint(0, 4, batch)], [40] * batch, "mean")
+    t.check()
+    t.set_u(1)
+    budget = [int(x) for x in r.randint(0, 22, batch)]
+    keep = [t.m.best(b, n) for b, n in enumerate(budget)]
+    B.kv_q4_evict(t.c, t.cap, i32(budget), t.ws)
+    t.m.compact(keep)
+    t.check()
+    granted = t.append([48 - n for n in t.m.len], [80] * batch)
+    assert 0 < sum(x > 0 for x in granted) < batch
+    t.check(B.KV_FAULT_NO_PAGES)
+    q = torch.randn(1, batch, 1, 64, generator=gen(3)).bfloat16().cuda()
+    o = torch.full_like(q, 9.0)
+    B.kv_q4_attend(t.c, 0, 1, t.cap, q, o, t.ws)
+    k, v = (torch.zeros(1, batch, 1, t.cap, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.kv_q4_load(t.c, 0, 1, t.cap, k, v, t.ws, first=i32([0] * batch), count=t.c.len)
+    for b in range(0, batch, 7):
+        n = t.m.len[b]
+        want, _, _, av = R.attend(q[0, b].double().cpu().numpy(), k[0, b, :, :n].double().cpu().numpy(), v[0, b, :, :n].double().cpu().numpy())
+        assert (np.abs(o[0, b].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * av).all(), b
+    slots = [int(x) for x in r.permutation(batch)[:2400]]
+    B.kv_q4_free(t.c, i32(slots), t.ws)
+    t.m.free(slots)
+    t.check()
+
+
+@pytest.mark.parametrize("layers,hkv,lens", [(256, 1, [33, 70]), (256, 2, [5]), (37, 3, [100, 1, 0]), (5, 40, [77, 20]), (1, 17, [130, 64]), (17, 5, [65])])
+def test_scores_of_many_layers_and_heads(layers, hkv, lens):
+    """Every way of dividing layers and KV heads among the score's waves, the last turn whole or not."""
+    t = Cache(lens, layers=layers, hq=2 * hkv, hkv=hkv, d=64).fill()
+    q = torch.randn(layers, len(lens), 2 * hkv, 64, generator=gen(3)).bfloat16().cuda()
+    o, s, out = torch.full_like(q, 9.0), torch.full((layers, len(lens), t.cap), 9.0, device="cuda"), torch.full_like(t.c.u, 5.0)
+    B.kv_q4_attend(t.c, 0, layers, t.cap, q, o, t.ws, s_out=s, alpha=0.97, u_prior=t.c.u, u_out=out)
+    scores = check_attend(t, q, o, s_out=s)
+    for b, n in enumerate(lens):
+        want = t.c.u[b, :n].double().cpu().numpy()
+        for l in range(layers):
+            want = 0.97 * want + 0.03 * scores[l, b, :n]
+        # a layer's three roundings and its coefficients' (4 2^-24 of what is left of it: 1 / (1 - 0.97) layers count), and the scores'
+        lim = 4 * 34 * 2.0 ** -24 * want + 2.0 ** -12 * want
+        assert (np.abs(out[b, :n].double().cpu().numpy() - want) <= lim).all() and (out[b, n:] == 5.0).all()
