@@ -66,7 +66,7 @@ struct Q4AttendArgs {
     int window;
     float scale2;            // log2(e) / sqrt(d)
     float bias2;             // log2(e) * bias
-    int nchunk, chunk_rows, scored;  // Q4AttendPlan
+    int nchunk, chunk_rows, scored, columns;  // Q4AttendPlan
     int stat_at, q_at;       // floats of LDS before the waves' statistics, and before an f32 query's parts (set by the launch)
     float* z;                // scores wanted: base-2 logits [slab][group][n_stride], or [slab][n_stride] parts of the scores
     float2* stat;            // scores wanted: [slab][group] (max, 1 / sum of 2^(z - max)), slab = (layer * batch + b) * hkv + head
@@ -79,9 +79,10 @@ struct Q4AttendArgs {
     uint32_t* faults;
 };
 // How a call on layer_count layers and at most n_max rows is divided: chunks of rows per slab, `most` of them at most (which
-// does not fall when n_max grows); or (scored) a slab per workgroup with its logits in LDS.
+// does not fall when n_max grows); or (scored) a slab per workgroup with its logits in LDS.  columns: a head's,
+// for the parts of its probabilities.
 struct Q4AttendPlan {
-    int nchunk, chunk_rows, most, scored, n_stride;
+    int nchunk, chunk_rows, most, scored, n_stride, columns;
 };
 Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool scores);
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);

@@ -296,6 +296,7 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     a.nchunk = L.plan.nchunk;
     a.chunk_rows = L.plan.chunk_rows;
     a.scored = L.plan.scored;
+    a.columns = L.plan.columns;
     char* base = static_cast<char*>(ws);
     a.z = scores ? reinterpret_cast<float*>(base + L.z_off) : nullptr;
     a.stat = scores ? reinterpret_cast<float2*>(base + L.stat_off) : nullptr;

@@ -698,9 +698,8 @@ hipError_t launch_form(Q4AttendArgs a, hipStream_t s, void (*kern)(Q4AttendArgs)
 
 template <typename T, int D, bool kScored>
 hipError_t launch_columns(const Q4AttendArgs& a, hipStream_t s) {
-    const int columns = columns_of(a.dims.group);
-    if (columns == 3) return launch_form<T, D, 3, kScored>(a, s, q4_attend_kernel<T, D, 3, kScored>);
-    if (columns == 2) return launch_form<T, D, 2, kScored>(a, s, q4_attend_pairs_kernel<T, D, kScored>);
+    if (a.columns == 3) return launch_form<T, D, 3, kScored>(a, s, q4_attend_kernel<T, D, 3, kScored>);
+    if (a.columns == 2) return launch_form<T, D, 2, kScored>(a, s, q4_attend_pairs_kernel<T, D, kScored>);
     return launch_form<T, D, 1, kScored>(a, s, q4_attend_kernel<T, D, 1, kScored>);
 }
 template <typename T, int D>
@@ -730,11 +729,20 @@ Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool sc
     p.nchunk = (n_max + p.chunk_rows - 1) / p.chunk_rows;
     // Scored: where a slab's logits fit LDS with two workgroups on a CU, and there is a slab for each: 2,048 slabs of 3,277 rows
     // with scores 188 us, through memory 232.
-    const size_t values = 8 * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
-    const size_t outputs = 4 * (size_t)d.group * columns_of(d.group) * (d.d + 4) * sizeof(float);
-    const size_t scored = (values > outputs ? values : outputs) + (stat_floats(d.group) + (size_t)d.group * (p.n_stride + kZPad)) * sizeof(float) +
-                          (d.bf16 ? 0 : 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4));
-    p.scored = scores && scored <= kLdsPerCu / 2 && slabs >= 2 * cus;
+    const auto fits = [&](int columns) {
+        const size_t values = kQ4Waves * (size_t)(d.d == 128 ? kValueBytes<128> : kValueBytes<64>);
+        const size_t outputs = 4 * (size_t)d.group * columns * (d.d + 4) * sizeof(float);
+        return (values > outputs ? values : outputs) + (stat_floats(d.group) + (size_t)d.group * (p.n_stride + kZPad)) * sizeof(float) +
+                   (d.bf16 ? 0 : 3 * (size_t)d.d / 32 * kWave * sizeof(u32x4)) <= kLdsPerCu / 2;
+    };
+    p.columns = columns_of(d.group);
+    p.scored = scores && slabs >= 2 * cus && fits(p.columns);
+    // (two columns of outputs take less LDS than three, and a product more: 2,048 slabs of 3,520 rows of 4 heads a KV head 202 us,
+    // through memory 240; of 2,900 rows of 5 heads 173 and 224)
+    if (scores && slabs >= 2 * cus && p.columns == 3 && !p.scored && fits(2)) {
+        p.columns = 2;
+        p.scored = 1;
+    }
     return p;
 }
 

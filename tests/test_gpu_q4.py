@@ -1282,3 +1282,21 @@ def test_scores_of_many_layers_and_heads(layers, hkv, lens):
         # a layer's three roundings and its coefficients' (4 2^-24 of what is left of it: 1 / (1 - 0.97) layers count), and the scores'
         lim = 4 * 34 * 2.0 ** -24 * want + 2.0 ** -12 * want
         assert (np.abs(out[b, :n].double().cpu().numpy() - want) <= lim).all() and (out[b, n:] == 5.0).all()
+
+
+@pytest.mark.parametrize("hq,d,dtype,n", [(32, 128, "bf16", 3456), (32, 128, "bf16", 3520), (32, 128, "bf16", 3904), (32, 128, "bf16", 3968),
+                                          (40, 128, "bf16", 2900), (40, 128, "f32", 2600), (24, 64, "bf16", 5000)])
+def test_scores_at_the_border_of_lds(hq, d, dtype, n):
+    """Logits that fill a workgroup's half of the LDS with three columns a head, with two, and that do not fit: one long slot among
+    short ones."""
+    lens = [n] + [33] * 63
+    t = Cache(lens, hq=hq, hkv=8, d=d, dtype=dtype, page_rows=64)
+    for rows, first in ((n, 1), (33, 64)):
+        kv = [torch.randn(1, first, 8, rows, d, generator=gen(i)).to(DT[dtype]) for i in (1, 2)]
+        kv = [x.expand(1, 64, 8, rows, d) if first == 1 else x for x in kv]
+        count = i32([n] + [0] * 63) if first == 1 else i32([0] + [33] * 63)
+        B.kv_q4_store(t.c, 0, 1, rows, *(x.cuda() for x in kv), t.ws, count=count)
+    q = torch.randn(1, 64, hq, d, generator=gen(3)).to(DT[dtype]).cuda()
+    o, s = torch.full_like(q, 9.0), torch.full((1, 64, n), 9.0, device="cuda")
+    B.kv_q4_attend(t.c, 0, 1, n, q, o, t.ws, s_out=s)
+    check_attend(t, q, o, s_out=s)
