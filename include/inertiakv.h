@@ -396,6 +396,30 @@ kv_status kv_q4_load(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t
                      const int32_t* first, const int32_t* count, void* k, const kv_q4_strides* k_strides, void* v,
                      const kv_q4_strides* v_strides, void* ws, size_t ws_bytes, void* stream);
 
+/* Rotary positions.  Pair i < dim / 2 of a row's first dim elements (elements i and i + dim / 2, or with adjacent != 0 elements
+ * 2 i and 2 i + 1) turns by the angle position * inv_freq[i], where position is the row's on axis[i] (images and video: time,
+ * height, width): (x, y) -> scale * (x cos - y sin, x sin + y cos).  Elements from dim on pass unchanged. */
+typedef struct {
+    int32_t dim;         /* a multiple of 16, at most head_dim                                                  */
+    int32_t adjacent;    /* 0 or 1                                                                              */
+    int32_t axes;        /* 1..4 positions of a row                                                             */
+    float scale;         /* finite; 1 for a plain rotation                                                      */
+    float inv_freq[64];  /* finite, dim / 2 of them used                                                        */
+    uint8_t axis[64];    /* below axes, likewise                                                                */
+} kv_rotary;
+
+/* kv_q4_store with keys rotated by their positions (DEVICE [axes][batch][rows] int32, read for rows r < count[b]), and queries
+ * beside them: row r < count[b] of q [layer][batch][query head][row][d] is written rotated to the same row of q_out, in the
+ * shape's type; the other rows of q_out are left as they were.  q and q_out are both null (no queries), or not; q_out may be q
+ * itself, with the same strides.  Angles, rotation and what is quantised are in 64 bits: a stored key is the nearest to the
+ * exact rotated one, a query is rounded once.  Queries are written for every row r < min(count[b], rows), whatever becomes of
+ * its key.  count, first, faults and limits as kv_q4_store, and batch * rows at most 2^25 (KV_ERR_UNSUPPORTED). */
+kv_status kv_q4_store_rotary(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
+                             int32_t rows, const int32_t* first, const int32_t* count, const kv_rotary* rotary,
+                             const int32_t* positions, const void* k, const kv_q4_strides* k_strides, const void* v,
+                             const kv_q4_strides* v_strides, const void* q, const kv_q4_strides* q_strides, void* q_out,
+                             const kv_q4_strides* q_out_strides, void* ws, size_t ws_bytes, void* stream);
+
 /* Decode attention of layers [layer0, layer0 + layer_count) over the len[b] <= n_max rows of every slot, as
  * kv_attend_score: q and o are [layer_count][batch][n_q_heads][d]; recency_bias is added to the logits of rows with
  * pos >= cur_pos[b] - (recency_window - 1) (cur_pos and cache->pos are needed for a bias other than 0 in a window other than

@@ -29,7 +29,7 @@ EXPORTED = ("kv_workspace_bytes", "kv_score_ema", "kv_topk_select", "kv_compact"
             "kv_append", "kv_attend_score", "kv_evict_finish", "kv_rank_trace_state_bytes", "kv_score_merge",
             "kv_score_plan", "kv_fault_status", "kv_set_exchange_wait_limit", "kv_evict_step_static",
             "kv_value_norms", "kv_q4_pool_bytes", "kv_q4_workspace_bytes", "kv_q4_reserve", "kv_q4_store", "kv_q4_load",
-            "kv_q4_attend", "kv_q4_fork", "kv_q4_free", "kv_q4_compact", "kv_q4_evict", "kv_status_string")
+            "kv_q4_store_rotary", "kv_q4_attend", "kv_q4_fork", "kv_q4_free", "kv_q4_compact", "kv_q4_evict", "kv_status_string")
 KV_STATIC_SCRATCH_BYTES = 64 << 20
 KV_TRACE_COUNTS = 10
 
@@ -75,6 +75,11 @@ class KvQ4Buffers(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in ("pool", "table", "len", "refs", "u", "pos")]
 
 
+class KvRotary(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("adjacent", ctypes.c_int32), ("axes", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("inv_freq", ctypes.c_float * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
 class KvQ4Strides(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int64) for name in ("layer", "batch", "head", "row")]
 
@@ -117,6 +122,8 @@ def load_library(path: str = LIB_PATH):
     lib.kv_q4_reserve.argtypes = [qsh, buf, vp, vp, i32, vp, vp, sz, vp]
     lib.kv_q4_store.argtypes = [qsh, buf, i32, i32, i32, vp, vp, vp, std, vp, std, vp, sz, vp]
     lib.kv_q4_load.argtypes = lib.kv_q4_store.argtypes
+    lib.kv_q4_store_rotary.argtypes = [qsh, buf, i32, i32, i32, vp, vp, ctypes.POINTER(KvRotary), vp, vp, std, vp, std, vp, std,
+                                       vp, std, vp, sz, vp]
     lib.kv_q4_attend.argtypes = [qsh, buf, i32, i32, i32, vp, vp, f32, i32, vp, vp, f32, vp, vp, vp, sz, vp]
     lib.kv_q4_fork.argtypes = [qsh, buf, i32, vp, vp, vp, sz, vp]
     lib.kv_q4_free.argtypes = [qsh, buf, i32, vp, vp, sz, vp]
@@ -517,6 +524,48 @@ def kv_q4_store(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=Non
 def kv_q4_load(cache: KvQ4Cache, layer0, layer_count, rows, k, v, ws, first=None, count=None, stream=None):
     """As kv_q4_store, into k and v."""
     _q4_rows("kv_q4_load", cache, layer0, layer_count, rows, k, v, ws, first, count, stream)
+
+
+def make_rotary(inv_freq, axis=None, pairs="halves", scale=1.0, axes=None) -> KvRotary:
+    """inv_freq: the pairs' angles per position, dim / 2 numbers (held as float32); axis: each pair's axis (all 0 without);
+    pairs: "halves" (elements i and i + dim / 2) or "adjacent" (2 i and 2 i + 1); axes: how many there are (the largest + 1)."""
+    inv_freq = [float(x) for x in inv_freq]
+    axis = [0] * len(inv_freq) if axis is None else [int(x) for x in axis]
+    if not 0 < len(inv_freq) <= 64 or len(axis) != len(inv_freq) or not all(0 <= x < 256 for x in axis) or pairs not in ("halves", "adjacent"):
+        raise KVError("make_rotary", KV_ERR_INVALID_ARG)
+    r = KvRotary(2 * len(inv_freq), int(pairs == "adjacent"), max(axis) + 1 if axes is None else int(axes), float(scale))
+    r.inv_freq[: len(inv_freq)] = inv_freq
+    r.axis[: len(axis)] = axis
+    return r
+
+
+def _q4_spread(cache, layer_count, heads, rows, *tensors):
+    """Strides of tensors [layer_count][batch][heads][rows][head_dim] of the cache's type and place, whose rows are contiguous; None
+    where one is not so."""
+    shape, out = (layer_count, cache._batch, heads, rows, cache._dim), []
+    on = (layer_count > 1, cache._batch > 1, heads > 1, rows > 1)  # (the stride of an extent of 1 is not used)
+    for t in tensors:
+        st = t.stride()
+        if t.shape != shape or t.dtype is not cache.element or t.get_device() != cache._device or st[4] != 1:
+            return None
+        out.append(KvQ4Strides(st[0] * on[0], st[1] * on[1], st[2] * on[2], st[3] * on[3]))
+    return out
+
+
+def kv_q4_store_rotary(cache: KvQ4Cache, layer0, layer_count, rows, k, v, rotary: KvRotary, positions, ws, first=None, count=None,
+                       q=None, q_out=None, stream=None):
+    """k, v, first, count as kv_q4_store; positions: [axes][batch][rows] int32, contiguous; q, q_out: [layer_count][batch]
+    [n_q_heads][rows][head_dim] in any strides with contiguous rows (q_out may be q)."""
+    n, dev = cache._batch, cache._device
+    kv = _q4_spread(cache, layer_count, cache._heads, rows, k, v)
+    qs = _q4_spread(cache, layer_count, cache._query[1], rows, q, q_out) if q is not None and q_out is not None else [None, None]
+    if (kv is None or qs is None or (q is None) != (q_out is None) or not _q4_ok(positions, torch.int32, rotary.axes * n * rows, dev)
+            or not (_q4_ok(first, torch.int32, n, dev) and _q4_ok(count, torch.int32, n, dev))):
+        raise KVError("kv_q4_store_rotary", KV_ERR_INVALID_ARG)
+    tail = _q4_tail("kv_q4_store_rotary", cache, ws, stream)
+    _check("kv_q4_store_rotary", load_library().kv_q4_store_rotary(
+        cache._shape, cache._buffers, layer0, layer_count, rows, _ptr(first), _ptr(count), rotary, _ptr(positions), k.data_ptr(), kv[0],
+        v.data_ptr(), kv[1], _ptr(q), qs[0], _ptr(q_out), qs[1], *tail))
 
 
 def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos=None, recency_bias=0.0, recency_window=0,

@@ -1,4 +1,4 @@
-// The paged 4-bit cache: sizes, addresses and launchers (q4_rows.hip, q4_attend.hip, q4_pages.hip).
+// The paged 4-bit cache: sizes, addresses and launchers (q4_rows.hip, q4_rotary.hip, q4_attend.hip, q4_pages.hip).
 //
 // A row's elements are held in blocks of 32: 32 codes of 4 bits (OCP microscaling's e2m1: sign, two exponent bits, one
 // mantissa bit; the first element in the low half of a byte) and one scale byte E, the power of two 2^(E - 127).  gfx950
@@ -53,6 +53,20 @@ struct Q4RowArgs {
 };
 hipError_t launch_q4_store(const Q4RowArgs& a, hipStream_t s);
 hipError_t launch_q4_load(const Q4RowArgs& a, hipStream_t s);
+
+// The store with keys rotated by their positions, and queries beside them.
+struct Q4RotaryArgs {
+    Q4RowArgs rows;
+    const void* q;             // nullable
+    void* q_out;
+    int64_t qs[4], os[4];      // strides in elements: layer, sequence, query head, row
+    const int32_t* positions;  // [axes][batch][rows]
+    int dim, adjacent;         // elements rotated; pairs 2 i, 2 i + 1 instead of i, i + dim / 2
+    float scale;
+    float inv_freq[64];
+    uint8_t axis[64];
+};
+hipError_t launch_q4_store_rotary(const Q4RotaryArgs& a, hipStream_t s);
 
 // Decode attention over rows [0, len[b]) of every sequence.
 struct Q4AttendArgs {

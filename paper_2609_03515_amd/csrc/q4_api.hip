@@ -19,6 +19,7 @@ constexpr size_t kFaultBytes = 256;
 // A launch has fewer than 2^32 threads along each extent of its grid, and at most 65535 workgroups along the second and third.
 constexpr int kMostHeads = 1 << 16;
 constexpr double kMostRowItems = (double)(1 << 28) - 256;  // 16 threads a row of the store and the load, in whole workgroups
+constexpr double kMostTokens = (double)(1 << 25);          // 64 threads a token, 4 or 8 of them a workgroup of 256
 constexpr double kMostJoined = (double)(1 << 23) - 1;      // 512 threads a head of the attention's join
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -151,6 +152,25 @@ kv_status check_rows(const kv_q4_shape& s, int layer0, int layer_count, int rows
     return KV_OK;
 }
 
+// Queries [layer][batch][query head][row][d] read, and rows like them written.
+kv_status check_queries(const kv_q4_shape& s, int layer_count, int rows, const void* q, const kv_q4_strides* qs, const void* out,
+                        const kv_q4_strides* os) {
+    if (!qs || !os) return KV_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16)) return KV_ERR_UNSUPPORTED;
+    for (const kv_q4_strides* st : {qs, os})
+        for (int64_t x : {st->layer, st->batch, st->head, st->row})
+            if (x % (16 / esize(s))) return KV_ERR_UNSUPPORTED;
+    if ((os->layer == 0 && layer_count > 1) || (os->batch == 0 && s.batch > 1) || (os->head == 0 && s.n_q_heads > 1) ||
+        (os->row == 0 && rows > 1))
+        return KV_ERR_INVALID_ARG;
+    return KV_OK;
+}
+
+void set_strides(int64_t (&to)[4], const kv_q4_strides& from) {
+    const int64_t x[4] = {from.layer, from.batch, from.head, from.row};
+    for (int i = 0; i < 4; ++i) to[i] = x[i];
+}
+
 void set_rows(Q4RowArgs* a, const kv_q4_shape& s, const kv_q4_cache& c, int layer0, int layer_count, int rows,
               const int32_t* first, const int32_t* count, const kv_q4_strides& ks, const kv_q4_strides& vs, void* ws) {
     a->dims = dims_of(s);
@@ -160,11 +180,8 @@ void set_rows(Q4RowArgs* a, const kv_q4_shape& s, const kv_q4_cache& c, int laye
     a->rows = rows;
     a->first = first;
     a->count = count;
-    const int64_t k4[4] = {ks.layer, ks.batch, ks.head, ks.row}, v4[4] = {vs.layer, vs.batch, vs.head, vs.row};
-    for (int i = 0; i < 4; ++i) {
-        a->ks[i] = k4[i];
-        a->vs[i] = v4[i];
-    }
+    set_strides(a->ks, ks);
+    set_strides(a->vs, vs);
     a->faults = static_cast<uint32_t*>(ws);
 }
 
@@ -238,6 +255,52 @@ kv_status kv_q4_store(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_
     a.k = k;
     a.v = v;
     return hip_status(launch_q4_store(a, static_cast<hipStream_t>(stream)));
+}
+
+kv_status kv_q4_store_rotary(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
+                             int32_t rows, const int32_t* first, const int32_t* count, const kv_rotary* rotary,
+                             const int32_t* positions, const void* k, const kv_q4_strides* k_strides, const void* v,
+                             const kv_q4_strides* v_strides, const void* q, const kv_q4_strides* q_strides, void* q_out,
+                             const kv_q4_strides* q_out_strides, void* ws, size_t ws_bytes, void* stream) {
+    kv_status rc = check_shape(shape);
+    if (rc == KV_OK) rc = check_cache(cache);
+    if (rc == KV_OK) rc = check_rows(*shape, layer0, layer_count, rows, k, v, k_strides, v_strides, first, count, false);
+    if (rc != KV_OK) return rc;
+    const kv_q4_shape& s = *shape;
+    if (!rotary || !positions || (q != nullptr) != (q_out != nullptr)) return KV_ERR_INVALID_ARG;
+    if (rotary->axes < 1 || rotary->dim < 2 || rotary->dim > s.head_dim || (rotary->adjacent & ~1) || !isfinite(rotary->scale))
+        return KV_ERR_INVALID_ARG;
+    if (rotary->axes > 4 || rotary->dim % 16) return KV_ERR_UNSUPPORTED;
+    for (int i = 0; i < rotary->dim / 2; ++i)
+        if (!isfinite(rotary->inv_freq[i]) || rotary->axis[i] >= rotary->axes) return KV_ERR_INVALID_ARG;
+    if (!aligned(positions, 4) || (double)s.batch * rows > kMostTokens) return KV_ERR_UNSUPPORTED;
+    if (q) {
+        if ((rc = check_queries(s, layer_count, rows, q, q_strides, q_out, q_out_strides)) != KV_OK) return rc;
+        const kv_q4_strides &x = *q_strides, &y = *q_out_strides;
+        if (q == q_out && ((layer_count > 1 && x.layer != y.layer) || (s.batch > 1 && x.batch != y.batch) ||
+                           (s.n_q_heads > 1 && x.head != y.head) || (rows > 1 && x.row != y.row)))
+            return KV_ERR_INVALID_ARG;
+    }
+    if ((rc = check_ws(ws, ws_bytes, kFaultBytes)) != KV_OK) return rc;
+    Q4RotaryArgs a{};
+    set_rows(&a.rows, s, *cache, layer0, layer_count, rows, first, count, *k_strides, *v_strides, ws);
+    a.rows.k = k;
+    a.rows.v = v;
+    a.q = q;
+    a.q_out = q_out;
+    if (q) {
+        set_strides(a.qs, *q_strides);
+        set_strides(a.os, *q_out_strides);
+    }
+    a.positions = positions;
+    a.dim = rotary->dim;
+    a.adjacent = rotary->adjacent;
+    a.scale = rotary->scale;
+    for (int i = 0; i < rotary->dim / 2; ++i) {
+        a.inv_freq[i] = rotary->inv_freq[i];
+        a.axis[i] = rotary->axis[i];
+    }
+    return hip_status(launch_q4_store_rotary(a, static_cast<hipStream_t>(stream)));
 }
 
 kv_status kv_q4_load(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count, int32_t rows,

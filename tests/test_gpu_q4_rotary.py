@@ -1,0 +1,239 @@
+"""Rows rotated into the paged 4-bit cache, against the rotation in numpy's 64 bits and the plain quantiser.
+
+Tolerances.  Both sides rotate in 64 bits, so a stored element is the same code unless the rotated one lies within some 2^-50 of a
+border between two: codes are compared for equality.  A query is the 64-bit value rounded once: off by half a step of its type,
+finfo.eps / 2 of itself, and by the two sides' 64-bit roundings, 2^-50 of the pair's size."""
+import numpy as np
+import pytest
+import torch
+
+import q4_reference as R
+from test_gpu_q4 import DT, Cache, gen, i32, special_rows
+
+pytestmark = pytest.mark.gpu
+
+B = pytest.importorskip("paper_2609_03515_amd.binding")
+
+
+def rotate(x, pos, freq, axis, adjacent, scale):
+    """x [heads][rows][d] float64 by positions pos [axes][rows]; freq float64 values of float32 numbers."""
+    y = x.copy()
+    half = len(freq)
+    for i in range(half):
+        angle = pos[axis[i]].astype(np.float64) * freq[i]
+        c, s = np.cos(angle) * scale, np.sin(angle) * scale
+        a, b = (2 * i, 2 * i + 1) if adjacent else (i, i + half)
+        y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., a] * s + x[..., b] * c
+    return y
+
+
+def pair_size(x, dim, adjacent, scale):
+    """For every element, |x| + |partner|."""
+    z = np.abs(x[..., :dim])
+    other = z.reshape(z.shape[:-1] + (dim // 2, 2))[..., ::-1].reshape(z.shape) if adjacent else np.roll(z, dim // 2, axis=-1)
+    return np.concatenate(((z + other) * max(1.0, abs(scale)), 0 * x[..., dim:]), -1)
+
+
+def rotary(dim, adjacent, axes, scale=1.0, theta=1e4):
+    pairs = dim // 2
+    freq = np.float32(1.0 / theta ** (np.arange(pairs) / pairs))
+    axis = [i * axes // pairs for i in range(pairs)]
+    return B.make_rotary(freq.tolist(), axis, "adjacent" if adjacent else "halves", scale, axes), freq.astype(np.float64), axis
+
+
+def check(t, k, v, q, out, pos, freq, axis, adjacent, scale, counts, layer0=0, first=None, left=9.0):
+    pool = R.Pool(t.shape, t.c.pool.cpu().numpy())
+    pos, dim, eps = pos.cpu().numpy(), 2 * len(freq), torch.finfo(DT[t.dtype]).eps / 2
+    for l in range(k.shape[0]):
+        for b, m in enumerate(counts):
+            n = int(t.c.len[b])
+            at = n - m if first is None else first[b]
+            pages = t.c.table[b].tolist()[: -(-n // t.shape.page_rows)]
+            for x, keys in ((k, True), (v, False)):
+                want = x[l, b, :, :m].double().cpu().numpy()
+                if keys:
+                    want = rotate(want, pos[:, b, :m], freq, axis, adjacent, scale)
+                want = R.fast_values(want)
+                got = pool.sequence(layer0 + l, pages, n, keys)[:, at : at + m]
+                assert np.array_equal(got, want, equal_nan=True), (l, b, keys, np.abs(got - want).max())
+            if q is None:
+                continue
+            x, got = q[l, b].double().cpu().numpy(), out[l, b].double().cpu().numpy()
+            want = rotate(x[:, :m], pos[:, b, :m], freq, axis, adjacent, scale)
+            lim = eps * np.abs(want) + 2.0 ** -50 * pair_size(x[:, :m], dim, adjacent, scale)
+            assert (np.abs(got[:, :m] - want) <= lim).all(), (l, b, np.abs(got[:, :m] - want).max())
+            assert np.array_equal(got[:, :m, dim:], x[:, :m, dim:])
+            assert left is None or (got[:, m:] == left).all()
+
+
+@pytest.mark.parametrize("d,dim,adjacent,axes,dtype", [
+    (128, 128, False, 1, "bf16"), (128, 128, True, 1, "bf16"), (128, 128, False, 3, "bf16"), (128, 64, False, 4, "bf16"), (128, 16, True, 2, "bf16"),
+    (128, 48, False, 3, "bf16"), (64, 64, False, 3, "bf16"), (64, 32, True, 1, "bf16"), (128, 128, False, 3, "f32"), (128, 96, False, 1, "f32"),
+    (128, 112, True, 2, "f32"), (64, 64, False, 1, "f32"), (64, 32, False, 2, "f32"), (64, 16, True, 3, "f32")])
+def test_rows_of_every_form(d, dim, adjacent, axes, dtype):
+    counts, rows = [5, 0, 33, 1], 35
+    t = Cache([9, 3, 40, 1], layers=3, hq=6, hkv=2, d=d, page_rows=16, dtype=dtype)
+    # rows, heads and slots in an order other than the cache's; keys and values in different ones
+    k = special_rows((2, 4, rows, t.hkv, d), 5).to(DT[dtype]).cuda().transpose(2, 3)
+    v = special_rows((4, 2, t.hkv, rows, d), 9).to(DT[dtype]).cuda().transpose(0, 1)
+    if dtype == "f32":  # (products of the largest numbers leave the type)
+        k = k.clamp(-2.0 ** 120, 2.0 ** 120)
+    k = torch.where(k.abs() > 2.0 ** 120, torch.ones_like(k), k)
+    q = torch.randn(2, 4, rows, t.hq, d, generator=gen(7)).to(DT[dtype]).cuda().transpose(2, 3)
+    out = torch.full((4, 2, t.hq, rows, d), 9.0, dtype=DT[dtype], device="cuda").transpose(0, 1)
+    rot, freq, axis = rotary(dim, adjacent, axes, scale=0.75)
+    pos = torch.randint(0, 200_000, (axes, 4, rows), generator=gen(3)).to(torch.int32).cuda()
+    before = t.c.pool.clone()
+    B.kv_q4_store_rotary(t.c, 1, 2, rows, k, v, rot, pos, t.ws, count=i32(counts), q=q, q_out=out)
+    assert t.faults() == 0
+    check(t, k, v, q, out, pos, freq, axis, adjacent, 0.75, counts, layer0=1)
+    assert torch.equal(before.view(3, -1)[0], t.c.pool.view(3, -1)[0])  # a layer that is not the call's
+    # the rows that are not the call's keep their bytes
+    a, c = (R.Pool(t.shape, x.cpu().numpy()) for x in (before, t.c.pool))
+    for b, (n, m) in enumerate(zip(t.lens, counts)):
+        pages = t.c.table[b].tolist()[: -(-n // 16)]
+        for keys in (True, False):
+            assert np.array_equal(a.sequence(1, pages, n, keys)[:, : n - m], c.sequence(1, pages, n, keys)[:, : n - m], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,rows", [(1, 1), (1, 2), (3, 1), (17, 1), (1, 1025), (2, 301)])
+def test_sizes(batch, rows, dtype):
+    """From one token on; without a count every row is stored; without queries only keys and values."""
+    t = Cache([rows] * batch, layers=1, hq=8, hkv=4, d=128, page_rows=64, dtype=dtype)
+    k, v = (torch.randn(1, batch, 4, rows, 128, generator=gen(s)).to(DT[dtype]).cuda() for s in (1, 2))
+    rot, freq, axis = rotary(128, False, 1)
+    pos = (torch.arange(batch * rows, dtype=torch.int32).view(1, batch, rows) * 7).cuda()
+    B.kv_q4_store_rotary(t.c, 0, 1, rows, k, v, rot, pos, t.ws)
+    check(t, k, v, None, None, pos, freq, axis, False, 1.0, [rows] * batch)
+    assert t.faults() == 0
+
+
+def test_far_positions():
+    """The angle is the 64-bit product, for every position that an int32 holds."""
+    t = Cache([6], hq=2, hkv=1)
+    k = torch.randn(1, 1, 1, 6, 128, generator=gen(1)).bfloat16().cuda()
+    q = torch.randn(1, 1, 2, 6, 128, generator=gen(2)).bfloat16().cuda()
+    rot, freq, axis = rotary(128, False, 1)
+    pos = i32([[[0, 2 ** 31 - 1, 2 ** 31 - 2, 16_777_217, -1, -2 ** 31]]])
+    out = torch.full_like(q, 9.0)
+    B.kv_q4_store_rotary(t.c, 0, 1, 6, k, k, rot, pos, t.ws, q=q, q_out=out)
+    check(t, k, k, q, out, pos, freq, axis, False, 1.0, [6])
+    assert torch.equal(out[:, :, :, 0], q[:, :, :, 0])  # an angle of 0
+
+
+def test_in_place_and_in_the_caches_order():
+    """q_out may be q; rows of a projection's output, heads beside each other."""
+    t = Cache([70, 50], hq=4, hkv=2)
+    q = torch.randn(1, 2, 40, 4, 128, generator=gen(2)).bfloat16().cuda().transpose(2, 3)
+    k = torch.randn(1, 2, 40, 2, 128, generator=gen(3)).bfloat16().cuda().transpose(2, 3)
+    rot, freq, axis = rotary(64, False, 2)
+    pos = torch.randint(0, 5000, (2, 2, 40), generator=gen(4)).to(torch.int32).cuda()
+    old = q.clone()
+    B.kv_q4_store_rotary(t.c, 0, 1, 40, k, k, rot, pos, t.ws, first=i32([3, 10]), q=q, q_out=q)
+    check(t, k, k, old, q, pos, freq, axis, False, 1.0, [40, 40], first=[3, 10])
+    # a row's own stride: one position's keys for every row
+    one = k[:, :, :, :1].expand(1, 2, 2, 40, 128)
+    B.kv_q4_store_rotary(t.c, 0, 1, 40, one, one, rot, pos, t.ws, first=i32([0, 0]))
+    check(t, one, one, None, None, pos, freq, axis, False, 1.0, [40, 40], first=[0, 0])
+
+
+def test_rows_that_are_not_stored():
+    """Keys outside the slot, in shared pages and in pages that do not exist are left out; their queries are rotated all the same."""
+    t = Cache([20, 40, 16], hq=4, hkv=2)
+    k = torch.randn(1, 3, 2, 4, 128, generator=gen(1)).bfloat16().cuda()
+    q = torch.randn(1, 3, 4, 4, 128, generator=gen(2)).bfloat16().cuda()
+    out = torch.full_like(q, 9.0)
+    rot, freq, axis = rotary(128, False, 1)
+    pos = torch.arange(12, dtype=torch.int32).view(1, 3, 4).cuda()
+    t.c.refs[t.c.table[2, 0].long()] = 2
+    before, table = t.c.pool.clone(), t.c.table.clone()
+    t.c.table[1, 2] = t.shape.n_pages  # rows 32 .. 39 of slot 1
+    B.kv_q4_store_rotary(t.c, 0, 1, 4, k, k, rot, pos, t.ws, first=i32([18, 30, 3]), q=q, q_out=out)
+    assert t.faults() == B.KV_FAULT_CACHE | B.KV_FAULT_SHARED_PAGE
+    for b in range(3):
+        want = rotate(q[0, b].double().cpu().numpy(), pos[:, b].cpu().numpy(), freq, axis, False, 1.0)
+        assert (np.abs(out[0, b].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 1e-12).all()
+    t.c.table.copy_(table)
+    old, new = (R.Pool(t.shape, x.cpu().numpy()) for x in (before, t.c.pool))
+    want = R.fast_values(rotate(k[0, 0, :, :2].double().cpu().numpy(), pos[:, 0, :2].cpu().numpy(), freq, axis, False, 1.0))
+    for b, (n, at) in enumerate(((20, 18), (40, 30), (16, 16))):
+        a, c = (x.sequence(0, table[b].tolist()[: -(-n // 16)], n, True) for x in (old, new))
+        same = [i for i in range(n) if not at <= i < at + 2]
+        assert np.array_equal(a[:, same], c[:, same], equal_nan=True)
+        if b == 0:
+            assert np.array_equal(c[:, 18:], want)
+
+
+@pytest.mark.parametrize("counts,faults", [([7, 2], 2), ([-3, 4], 2), ([4, 0], 0)])
+def test_counts_out_of_range(counts, faults):
+    """Of a count above the call's rows the first rows are taken, of one below 0 none."""
+    t = Cache([30, 30], hq=2, hkv=1)
+    k = torch.randn(1, 2, 1, 4, 128, generator=gen(1)).bfloat16().cuda()
+    q = torch.randn(1, 2, 2, 4, 128, generator=gen(2)).bfloat16().cuda()
+    out = torch.full_like(q, 9.0)
+    rot, freq, axis = rotary(128, False, 1)
+    pos = torch.arange(8, dtype=torch.int32).view(1, 2, 4).cuda()
+    B.kv_q4_store_rotary(t.c, 0, 1, 4, k, k, rot, pos, t.ws, count=i32(counts), q=q, q_out=out)
+    assert t.faults() == faults
+    taken = [min(max(c, 0), 4) for c in counts]
+    check(t, k, k, q, out, pos, freq, axis, False, 1.0, taken, first=[30 - c for c in counts])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_numbers_that_are_not_finite(dtype):
+    """A block with one reads back as NaN, a query keeps it; other rows and pairs are not touched by it."""
+    t = Cache([3], hq=1, hkv=1, dtype=dtype)
+    x = torch.randn(1, 1, 1, 3, 128, generator=gen(1)).to(DT[dtype])
+    x[0, 0, 0, 1, 5] = float("nan")
+    x[0, 0, 0, 2, 100] = float("inf")
+    x = x.cuda()
+    out = torch.full_like(x, 9.0)
+    rot, freq, axis = rotary(64, False, 1)  # pairs (i, i + 32); elements from 64 on pass
+    B.kv_q4_store_rotary(t.c, 0, 1, 3, x, x, rot, i32([[[1, 2, 3]]]), t.ws, q=x, q_out=out)
+    k, _ = t.values(0, 0)
+    bad = np.isnan(k[0])
+    assert not bad[0].any() and bad[1, :64].all() and not bad[1, 64:].any() and bad[2, 96:].all() and not bad[2, :96].any()
+    o = out[0, 0, 0].cpu()
+    assert torch.isnan(o[1, [5, 37]]).all() and torch.isfinite(o[1]).sum() == 126
+    assert o[2, 100] == float("inf") and torch.isfinite(o[2]).sum() == 127
+
+
+def test_large_pairs():
+    """Pairs whose rotation passes the type's largest number."""
+    t = Cache([2], hq=1, hkv=1, dtype="f32", d=64)
+    x = torch.full((1, 1, 1, 2, 64), 3.3e38).cuda()
+    rot, freq, axis = rotary(64, False, 1)
+    out = torch.empty_like(x)
+    B.kv_q4_store_rotary(t.c, 0, 1, 2, x, x, rot, i32([[[0, 1]]]), t.ws, q=x, q_out=out)
+    k, _ = t.values(0, 0)
+    y = rotate(x[0, 0].double().cpu().numpy(), np.array([[0, 1]]), freq, axis, False, 1.0)
+    assert (np.abs(y) > 3.5e38).any()
+    assert np.array_equal(k, R.fast_values(y)) and np.isfinite(k).all()
+    with np.errstate(over="ignore"):
+        assert np.array_equal(np.isinf(out[0, 0].cpu().numpy()), np.isinf(y.astype(np.float32)))
+
+
+def test_captured_and_replayed():
+    """A captured call replays with other positions, counts and lengths, beside eager calls on another stream."""
+    t = Cache([40, 40], hq=4, hkv=2)
+    k, v = (torch.randn(1, 2, 2, 8, 128, generator=gen(s)).bfloat16().cuda() for s in (1, 2))
+    q = torch.randn(1, 2, 4, 8, 128, generator=gen(3)).bfloat16().cuda()
+    rot, freq, axis = rotary(128, False, 3)
+    pos, count, out = torch.zeros(3, 2, 8, dtype=torch.int32, device="cuda"), i32([8, 8]), torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.kv_q4_store_rotary(t.c, 0, 1, 8, k, v, rot, pos, t.ws, count=count, q=q, q_out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.kv_q4_store_rotary(t.c, 0, 1, 8, k, v, rot, pos, t.ws, count=count, q=q, q_out=out)
+    for i, (c, n) in enumerate((([8, 3], [40, 22]), ([1, 0], [40, 40]), ([8, 8], [8, 17]))):
+        pos.copy_(torch.randint(0, 9999, (3, 2, 8), generator=gen(10 + i)))
+        count.copy_(i32(c))
+        t.c.len.copy_(i32(n))
+        out.fill_(9.0)
+        graph.replay()
+        check(t, k, v, q, out, pos, freq, axis, False, 1.0, c)
+    assert t.faults() == 0
