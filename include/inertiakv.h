@@ -436,6 +436,34 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
                        float* s_out, float alpha, const float* u_prior, float* u_out, void* ws, size_t ws_bytes,
                        void* stream);
 
+/* Attention of layers [layer0, layer0 + layer_count) for the queries of every slot's newest rows, in a sliding window with sinks:
+ * query r < count[b] of slot b belongs to row len[b] - count[b] + r (kv_q4_reserve and kv_q4_store it first) and has that row's
+ * position P; it sees the rows whose position p is at most P and, where window is not 0, above P - window or below sinks.
+ * Positions are cache->pos, or the rows' numbers where that is null.  o = softmax(q . k / sqrt(d)) v over the rows seen, zeros where
+ * there is none.  One query per slot is a decode step, many are a chunk of a prompt.
+ * q and o: [layer][batch][query head][row][d] in the strides given (o not q's memory; no stride of o is 0 where its extent is above
+ * 1).  count nullable: min(rows, len[b]).  Rows r >= count[b] are not read or written.  A slot longer than n_max, or whose count is
+ * below 0, above `rows` or above its length (KV_FAULT_CACHE), gets zeros in all its `rows` outputs; rows in pages that do not
+ * exist (KV_FAULT_CACHE) take no part.  What a masked row holds, NaN included, does not reach an output.  In bf16 calls of more than
+ * one query per slot probabilities may be rounded to bf16 before they weigh the values (to nearest; their sum is of the rounded ones).
+ * Workspace: kv_q4_window_workspace_bytes, for calls of at most n_max rows, `rows` queries and layer_count layers.
+ * Refused (KV_ERR_UNSUPPORTED: take fewer layers or rows a call): 2^23 workgroups or more. */
+kv_status kv_q4_window_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t rows, int32_t layer_count, size_t* bytes);
+kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
+                              int32_t n_max, int32_t rows, const int32_t* count, const void* q, const kv_q4_strides* q_strides,
+                              int32_t window, int32_t sinks, void* o, const kv_q4_strides* o_strides, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* kv_q4_attend (without a bias and scores) for slots that share pages, as the samples of a prompt do after kv_q4_fork: where the
+ * tables of slots of one group name the same page at the same place, it is read and converted once for several of them.  group
+ * [batch]: slots with equal numbers are a group (any numbers: those that share nothing only cost time, and those that share
+ * pages in different groups read them once each).  Pages that an eviction replaced in some samples are read for those.
+ * Workspace: kv_q4_shared_workspace_bytes.  Refused as kv_q4_attend_window. */
+kv_status kv_q4_shared_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t layer_count, size_t* bytes);
+kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
+                              int32_t n_max, const int32_t* group, const void* q, void* o, void* ws, size_t ws_bytes,
+                              void* stream);
+
 /* Slot dst[i] becomes a copy of slot src[i] (rows, utilities, positions) that shares its pages, for i < count <= batch.  A
  * destination has to be empty and named once, and no source may be a destination of the call; what is not so is left out
  * (KV_FAULT_CACHE), of a destination named twice all but the first. */

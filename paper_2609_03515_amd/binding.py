@@ -29,7 +29,8 @@ EXPORTED = ("kv_workspace_bytes", "kv_score_ema", "kv_topk_select", "kv_compact"
             "kv_append", "kv_attend_score", "kv_evict_finish", "kv_rank_trace_state_bytes", "kv_score_merge",
             "kv_score_plan", "kv_fault_status", "kv_set_exchange_wait_limit", "kv_evict_step_static",
             "kv_value_norms", "kv_q4_pool_bytes", "kv_q4_workspace_bytes", "kv_q4_reserve", "kv_q4_store", "kv_q4_load",
-            "kv_q4_store_rotary", "kv_q4_attend", "kv_q4_fork", "kv_q4_free", "kv_q4_compact", "kv_q4_evict", "kv_status_string")
+            "kv_q4_store_rotary", "kv_q4_window_workspace_bytes", "kv_q4_attend_window", "kv_q4_shared_workspace_bytes",
+            "kv_q4_attend_shared", "kv_q4_attend", "kv_q4_fork", "kv_q4_free", "kv_q4_compact", "kv_q4_evict", "kv_status_string")
 KV_STATIC_SCRATCH_BYTES = 64 << 20
 KV_TRACE_COUNTS = 10
 
@@ -125,6 +126,10 @@ def load_library(path: str = LIB_PATH):
     lib.kv_q4_store_rotary.argtypes = [qsh, buf, i32, i32, i32, vp, vp, ctypes.POINTER(KvRotary), vp, vp, std, vp, std, vp, std,
                                        vp, std, vp, sz, vp]
     lib.kv_q4_attend.argtypes = [qsh, buf, i32, i32, i32, vp, vp, f32, i32, vp, vp, f32, vp, vp, vp, sz, vp]
+    lib.kv_q4_window_workspace_bytes.argtypes = [qsh, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.kv_q4_attend_window.argtypes = [qsh, buf, i32, i32, i32, i32, vp, vp, std, i32, i32, vp, std, vp, sz, vp]
+    lib.kv_q4_shared_workspace_bytes.argtypes = [qsh, i32, i32, ctypes.POINTER(sz)]
+    lib.kv_q4_attend_shared.argtypes = [qsh, buf, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.kv_q4_fork.argtypes = [qsh, buf, i32, vp, vp, vp, sz, vp]
     lib.kv_q4_free.argtypes = [qsh, buf, i32, vp, vp, sz, vp]
     lib.kv_q4_compact.argtypes = [qsh, buf, i32, vp, vp, sz, vp]
@@ -581,6 +586,54 @@ def kv_q4_attend(cache: KvQ4Cache, layer0, layer_count, n_max, q, o, ws, cur_pos
     _check("kv_q4_attend", load_library().kv_q4_attend(
         cache._shape, cache._buffers, layer0, layer_count, n_max, _ptr(q), _ptr(cur_pos), recency_bias, recency_window, _ptr(o),
         _ptr(s_out), alpha, _ptr(u_prior), _ptr(u_out), *tail))
+
+
+def kv_q4_window_workspace_bytes(shape: KvQ4Shape, n_max: int, rows: int, layer_count: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kv_q4_window_workspace_bytes", load_library().kv_q4_window_workspace_bytes(
+        ctypes.byref(shape), int(n_max), int(rows), int(layer_count), ctypes.byref(out)))
+    return out.value
+
+
+def kv_q4_shared_workspace_bytes(shape: KvQ4Shape, n_max: int, layer_count: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kv_q4_shared_workspace_bytes", load_library().kv_q4_shared_workspace_bytes(
+        ctypes.byref(shape), int(n_max), int(layer_count), ctypes.byref(out)))
+    return out.value
+
+
+def q4_window_workspace(shape: KvQ4Shape, n_max: int, rows: int, layer_count: int, device="cuda") -> torch.Tensor:
+    """A caller-owned workspace tensor of kv_q4_window_workspace_bytes() bytes, its fault word cleared on the current stream."""
+    ws = torch.empty(kv_q4_window_workspace_bytes(shape, n_max, rows, layer_count), dtype=torch.uint8, device=device)
+    kv_fault_status(ws, None, clear=True)
+    return ws
+
+
+def q4_shared_workspace(shape: KvQ4Shape, n_max: int, layer_count: int, device="cuda") -> torch.Tensor:
+    """As q4_window_workspace, for kv_q4_attend_shared."""
+    ws = torch.empty(kv_q4_shared_workspace_bytes(shape, n_max, layer_count), dtype=torch.uint8, device=device)
+    kv_fault_status(ws, None, clear=True)
+    return ws
+
+
+def kv_q4_attend_window(cache: KvQ4Cache, layer0, layer_count, n_max, rows, q, o, ws, window=0, sinks=0, count=None, stream=None):
+    """q, o: [layer_count][batch][n_q_heads][rows][head_dim] in any strides with contiguous rows; count: [batch] int32."""
+    strides = _q4_spread(cache, layer_count, cache._query[1], rows, q, o)
+    if strides is None or not _q4_ok(count, torch.int32, cache._batch, cache._device):
+        raise KVError("kv_q4_attend_window", KV_ERR_INVALID_ARG)
+    tail = _q4_tail("kv_q4_attend_window", cache, ws, stream)
+    _check("kv_q4_attend_window", load_library().kv_q4_attend_window(
+        cache._shape, cache._buffers, layer0, layer_count, n_max, rows, _ptr(count), q.data_ptr(), strides[0], window, sinks,
+        o.data_ptr(), strides[1], *tail))
+
+
+def kv_q4_attend_shared(cache: KvQ4Cache, layer0, layer_count, n_max, group, q, o, ws, stream=None):
+    """q, o as kv_q4_attend; group: [batch] int32, equal for slots that share pages."""
+    if not (_q4_heads(cache, q, layer_count) and _q4_heads(cache, o, layer_count) and _q4_ok(group, torch.int32, cache._batch, cache._device)):
+        raise KVError("kv_q4_attend_shared", KV_ERR_INVALID_ARG)
+    tail = _q4_tail("kv_q4_attend_shared", cache, ws, stream)
+    _check("kv_q4_attend_shared", load_library().kv_q4_attend_shared(cache._shape, cache._buffers, layer0, layer_count, n_max, _ptr(group),
+                                                                     _ptr(q), _ptr(o), *tail))
 
 
 def kv_q4_fork(cache: KvQ4Cache, src, dst, ws, stream=None):

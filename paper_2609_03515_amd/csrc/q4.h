@@ -1,4 +1,5 @@
-// The paged 4-bit cache: sizes, addresses and launchers (q4_rows.hip, q4_rotary.hip, q4_attend.hip, q4_pages.hip).
+// The paged 4-bit cache: sizes, addresses and launchers (q4_rows.hip, q4_rotary.hip, q4_attend.hip, q4_queries.hip,
+// q4_pages.hip).
 //
 // A row's elements are held in blocks of 32: 32 codes of 4 bits (OCP microscaling's e2m1: sign, two exponent bits, one
 // mantissa bit; the first element in the low half of a byte) and one scale byte E, the power of two 2^(E - 127).  gfx950
@@ -100,6 +101,46 @@ struct Q4AttendPlan {
 };
 Q4AttendPlan q4_attend_plan(const Q4Dims& d, int layer_count, int n_max, bool scores);
 hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);
+
+// Attention of blocks of queries: the newest rows' queries of a slot in a window (kv_q4_attend_window), or one query of each of
+// several slots that share pages (kv_q4_attend_shared).  A block is `vectors` queries; each is `group` columns of a product.
+constexpr int kQ4MostVectors = 32, kQ4MostColumns = 32;  // of a block
+struct Q4QueryPlan {
+    int tiles;    // column tiles of 16 in a block
+    int per;      // queries in a column tile
+    int vectors;  // queries in a block
+    int blocks;   // blocks of a slot (window)
+    int chunks;   // workgroups that divide a block's rows
+};
+struct Q4QueryArgs {
+    Q4Dims dims;
+    Q4Cache cache;
+    Q4QueryPlan plan;
+    int layer0, layer_count, n_max;
+    const void* q;
+    void* o;
+    int64_t qs[4], os[4];    // strides in elements: layer, slot, query head, row
+    float scale2;            // log2(e) / sqrt(d)
+    int stat_at, q_at;       // floats of LDS before the waves' statistics and the queries (set by the launch)
+    float2* part;            // several chunks: [unit][chunk][column] (max, sum); unit: a (layer, slot, block, KV head)
+    float* opart;            // several chunks: [unit][chunk][column][d] unnormalised partial outputs
+    uint32_t* faults;
+    // window
+    int rows, window, sinks;
+    const int32_t* count;    // nullable [batch]
+    uint64_t* visible;       // positions kept: [batch][blocks][words] a bit for every 32 rows of which a block sees any
+    int words;
+    // shared
+    const int32_t* group;    // [batch]
+    int list_pages;          // places of a slot's list
+    int4* items;             // [batch][list_pages] pages (page, rows in use, the block's queries that it is a page of, 0)
+    int32_t* lists;          // [batch] entries of each slot's list
+    int32_t* members;        // [batch][vectors] the slots of the block that begins with a slot, -1 behind the last (first -1: none)
+};
+Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks);
+Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max);
+hipError_t launch_q4_window(const Q4QueryArgs& a, hipStream_t s);
+hipError_t launch_q4_shared(const Q4QueryArgs& a, hipStream_t s);
 
 // Pages.  Scratch of the calls that allocate pages; the lists are the compaction's.
 struct Q4PageScratch {

@@ -20,6 +20,7 @@ constexpr size_t kFaultBytes = 256;
 constexpr int kMostHeads = 1 << 16;
 constexpr double kMostRowItems = (double)(1 << 28) - 256;  // 16 threads a row of the store and the load, in whole workgroups
 constexpr double kMostTokens = (double)(1 << 25);          // 64 threads a token, 4 or 8 of them a workgroup of 256
+constexpr double kMostGroups = (double)(1 << 23) - 1;      // workgroups of 512 threads
 constexpr double kMostJoined = (double)(1 << 23) - 1;      // 512 threads a head of the attention's join
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -135,6 +136,41 @@ AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool sco
     return L;
 }
 
+// The scratch of blocks of queries after the fault word: marks or lists, and the parts of outputs that several workgroups share.
+struct QueryLayout {
+    size_t visible_off, members_off, lists_off, items_off, part_off, opart_off, total;
+};
+QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, size_t parts) {
+    QueryLayout L{};
+    size_t off = kFaultBytes;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align256(off + bytes);
+        return at;
+    };
+    L.visible_off = take(mark_words * sizeof(uint64_t));
+    if (list_pages) {
+        L.members_off = take((size_t)d.batch * kQ4MostVectors * sizeof(int32_t));
+        L.lists_off = take((size_t)d.batch * sizeof(int32_t));
+        L.items_off = take((size_t)d.batch * list_pages * sizeof(int4));
+    }
+    L.part_off = take(parts * sizeof(float2));
+    L.opart_off = take(parts * d.d * sizeof(float));
+    L.total = off;
+    return L;
+}
+size_t mark_words_of(int n_max) { return ((size_t)n_max + 2047) / 2048; }
+// Parts that a call needs, and more than any call of at most these sizes does: chunks are cut where there are fewer than 2 units for a
+// CU (then units * chunks is below twice that, of at most kQ4MostColumns columns each), and have 8 tiles of 32 rows at least.
+size_t parts_of(const Q4Dims& d, int layer_count, int rows, int chunks) {
+    return chunks > 1 ? (size_t)layer_count * d.batch * rows * d.hq * chunks : 0;
+}
+size_t most_parts(const Q4Dims& d, int n_max, int layer_count, int rows) {
+    const size_t cus = device_cus() > 0 ? device_cus() : 256, by_units = 4 * cus * kQ4MostColumns;
+    const size_t by_tiles = (size_t)layer_count * d.batch * rows * d.hq * (((size_t)n_max + 255) / 256);
+    return by_tiles < by_units ? by_tiles : by_units;
+}
+
 kv_status check_rows(const kv_q4_shape& s, int layer0, int layer_count, int rows, const void* k, const void* v,
                      const kv_q4_strides* ks, const kv_q4_strides* vs, const int32_t* first, const int32_t* count,
                      bool written) {
@@ -183,6 +219,19 @@ void set_rows(Q4RowArgs* a, const kv_q4_shape& s, const kv_q4_cache& c, int laye
     set_strides(a->ks, ks);
     set_strides(a->vs, vs);
     a->faults = static_cast<uint32_t*>(ws);
+}
+
+void set_queries(Q4QueryArgs* a, const QueryLayout& L, void* ws) {
+    constexpr double kLog2e = 1.4426950408889634;
+    a->scale2 = (float)(kLog2e / sqrt((double)a->dims.d));
+    char* base = static_cast<char*>(ws);
+    a->visible = reinterpret_cast<uint64_t*>(base + L.visible_off);
+    a->members = reinterpret_cast<int32_t*>(base + L.members_off);
+    a->lists = reinterpret_cast<int32_t*>(base + L.lists_off);
+    a->items = reinterpret_cast<int4*>(base + L.items_off);
+    a->part = reinterpret_cast<float2*>(base + L.part_off);
+    a->opart = reinterpret_cast<float*>(base + L.opart_off);
+    a->faults = reinterpret_cast<uint32_t*>(base);
 }
 
 // Checks and arguments that the page calls share.
@@ -371,6 +420,98 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
     a.alpha = alpha;
     a.faults = reinterpret_cast<uint32_t*>(base);
     return hip_status(launch_q4_attend(a, static_cast<hipStream_t>(stream)));
+}
+
+kv_status kv_q4_window_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t rows, int32_t layer_count, size_t* bytes) {
+    const kv_status rc = check_shape(shape);
+    if (rc != KV_OK) return rc;
+    const Q4Dims d = dims_of(*shape);
+    if (!bytes || n_max < 1 || n_max > d.cap || rows < 1 || rows > d.cap || layer_count < 1 || layer_count > shape->layers)
+        return KV_ERR_INVALID_ARG;
+    const int per = 16 / d.group;
+    *bytes = query_layout(d, (size_t)d.batch * ((rows + per - 1) / per) * mark_words_of(n_max), 0, most_parts(d, n_max, layer_count, rows)).total;
+    return KV_OK;
+}
+
+kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
+                              int32_t n_max, int32_t rows, const int32_t* count, const void* q, const kv_q4_strides* q_strides,
+                              int32_t window, int32_t sinks, void* o, const kv_q4_strides* o_strides, void* ws, size_t ws_bytes,
+                              void* stream) {
+    kv_status rc = check_shape(shape);
+    if (rc == KV_OK) rc = check_cache(cache);
+    if (rc != KV_OK) return rc;
+    const kv_q4_shape& s = *shape;
+    const Q4Dims d = dims_of(s);
+    if (layer0 < 0 || layer_count < 1 || layer_count > s.layers - layer0 || n_max < 1 || n_max > d.cap || rows < 1 || rows > d.cap)
+        return KV_ERR_INVALID_ARG;
+    if (window < 0 || sinks < 0 || !q || !o || q == o) return KV_ERR_INVALID_ARG;
+    if ((rc = check_queries(s, layer_count, rows, q, q_strides, o, o_strides)) != KV_OK) return rc;
+    if (!aligned(count, 4)) return KV_ERR_UNSUPPORTED;
+    Q4QueryArgs a{};
+    a.dims = d;
+    a.cache = cache_of(*cache);
+    a.plan = q4_window_plan(d, layer_count, n_max, rows, window, sinks);
+    a.words = (int)mark_words_of(n_max);
+    const size_t marks = cache->pos ? (size_t)d.batch * a.plan.blocks * a.words : 0;
+    if ((double)layer_count * d.batch * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups || (double)d.batch * a.plan.blocks * ((a.words + 3) / 4) > kMostGroups)
+        return KV_ERR_UNSUPPORTED;
+    const QueryLayout L = query_layout(d, marks, 0, parts_of(d, layer_count, rows, a.plan.chunks));
+    if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
+    a.layer0 = layer0;
+    a.layer_count = layer_count;
+    a.n_max = n_max;
+    a.q = q;
+    a.o = o;
+    set_strides(a.qs, *q_strides);
+    set_strides(a.os, *o_strides);
+    a.rows = rows;
+    a.window = window;
+    a.sinks = sinks;
+    a.count = count;
+    set_queries(&a, L, ws);
+    return hip_status(launch_q4_window(a, static_cast<hipStream_t>(stream)));
+}
+
+kv_status kv_q4_shared_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t layer_count, size_t* bytes) {
+    const kv_status rc = check_shape(shape);
+    if (rc != KV_OK) return rc;
+    const Q4Dims d = dims_of(*shape);
+    if (!bytes || n_max < 1 || n_max > d.cap || layer_count < 1 || layer_count > shape->layers) return KV_ERR_INVALID_ARG;
+    *bytes = query_layout(d, 0, ((size_t)n_max + d.page_rows - 1) / d.page_rows, most_parts(d, n_max, layer_count, 1)).total;
+    return KV_OK;
+}
+
+kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
+                              int32_t n_max, const int32_t* group, const void* q, void* o, void* ws, size_t ws_bytes,
+                              void* stream) {
+    kv_status rc = check_shape(shape);
+    if (rc == KV_OK) rc = check_cache(cache);
+    if (rc != KV_OK) return rc;
+    const kv_q4_shape& s = *shape;
+    const Q4Dims d = dims_of(s);
+    if (layer0 < 0 || layer_count < 1 || layer_count > s.layers - layer0 || n_max < 1 || n_max > d.cap) return KV_ERR_INVALID_ARG;
+    if (!group || !q || !o || q == o) return KV_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(o, 16) || !aligned(group, 4)) return KV_ERR_UNSUPPORTED;
+    Q4QueryArgs a{};
+    a.dims = d;
+    a.cache = cache_of(*cache);
+    a.plan = q4_shared_plan(d, layer_count, n_max);
+    if ((double)layer_count * d.batch * d.hkv * a.plan.chunks > kMostGroups) return KV_ERR_UNSUPPORTED;
+    a.list_pages = (n_max + d.page_rows - 1) / d.page_rows;
+    const QueryLayout L = query_layout(d, 0, a.list_pages, parts_of(d, layer_count, 1, a.plan.chunks));
+    if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
+    a.layer0 = layer0;
+    a.layer_count = layer_count;
+    a.n_max = n_max;
+    a.q = q;
+    a.o = o;
+    a.qs[2] = a.os[2] = d.d;
+    a.qs[1] = a.os[1] = (int64_t)d.hq * d.d;
+    a.qs[0] = a.os[0] = (int64_t)d.batch * d.hq * d.d;
+    a.rows = 1;
+    a.group = group;
+    set_queries(&a, L, ws);
+    return hip_status(launch_q4_shared(a, static_cast<hipStream_t>(stream)));
 }
 
 kv_status kv_q4_fork(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t count, const int32_t* src, const int32_t* dst,

@@ -90,3 +90,81 @@ def test_binding_refuses_host_memory_and_other_layouts():
                dict(q=q.transpose(3, 4), q_out=q)):
         with pytest.raises(B.KVError):
             B.kv_q4_store_rotary(c, 0, 1, 4, k, k, rot, pos, ws, **kw)
+
+
+def window(layer0=0, layers=1, n=10, rows=2, count=None, q=FAKE, qs=STRIDES, win=4, sinks=1, o=FAKE + 4096, os=STRIDES, **kw):
+    return call("kv_q4_attend_window", layer0, layers, n, rows, count, q, qs, win, sinks, o, os, **kw)
+
+
+def shared(layer0=0, layers=1, n=10, group=FAKE, q=FAKE, o=FAKE + 4096, **kw):
+    return call("kv_q4_attend_shared", layer0, layers, n, group, q, o, **kw)
+
+
+@pytest.mark.parametrize("fn", [window, shared])
+def test_attention_refusals(fn):
+    assert fn(ws=None) == WORKSPACE and fn(ws_bytes=255) == WORKSPACE and fn(ws=FAKE + 16) == INVALID
+    assert fn(layer0=-1) == INVALID and fn(layer0=4) == INVALID and fn(layers=0) == INVALID and fn(layer0=2, layers=3) == INVALID
+    assert fn(n=0) == INVALID and fn(n=321) == INVALID and fn(q=None) == INVALID and fn(o=None) == INVALID and fn(o=FAKE) == INVALID
+    assert fn(q=FAKE + 8) == UNSUPPORTED and fn(o=FAKE + 4) == UNSUPPORTED
+    assert fn(s=shape(head_dim=80)) == UNSUPPORTED and fn(s=shape(n_q_heads=7)) == INVALID
+    for field in ("pool", "table", "len", "refs"):
+        assert fn(c=buffers(**{field: None})) == INVALID and fn(c=buffers(**{field: FAKE + 2})) == UNSUPPORTED
+    assert fn(c=buffers(u=None, pos=None), ws=None) == WORKSPACE  # (neither is needed)
+
+
+def test_window_refusals():
+    assert window(rows=0) == INVALID and window(rows=321) == INVALID and window(win=-1) == INVALID and window(sinks=-1) == INVALID
+    assert window(qs=None) == INVALID and window(os=None) == INVALID and window(count=FAKE + 2) == UNSUPPORTED
+    for field in ("layer", "batch", "head", "row"):
+        assert window(qs=strides(**{field: 132})) == UNSUPPORTED and window(os=strides(**{field: 132})) == UNSUPPORTED
+        assert window(os=strides(**{field: 0}), layers=2) == INVALID and window(qs=strides(**{field: 0}), layers=2, ws=None) == WORKSPACE
+    # the largest grid that a launch can have
+    big = shape(batch=1024, layers=16, n_q_heads=512, n_kv_heads=512, max_pages=1)
+    assert window(layers=15, rows=1, s=big, ws=None) == WORKSPACE and window(layers=16, rows=1, s=big, ws=None) == UNSUPPORTED
+    marks = shape(batch=64, layers=1, n_q_heads=1, n_kv_heads=1, head_dim=64, max_pages=1 << 14, dtype="f32")
+    assert window(n=1 << 19, rows=32640, s=marks, ws=None) == WORKSPACE and window(n=1 << 19, rows=32769, s=marks, ws=None) == UNSUPPORTED
+
+
+def test_shared_refusals():
+    assert shared(group=None) == INVALID and shared(group=FAKE + 2) == UNSUPPORTED
+    big = shape(batch=1024, layers=16, n_q_heads=512, n_kv_heads=512, max_pages=1)
+    assert shared(layers=15, s=big, ws=None) == WORKSPACE and shared(layers=16, s=big, ws=None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(head_dim=64, dtype="f32"), dict(n_q_heads=2), dict(n_q_heads=32), dict(page_rows=16)])
+def test_workspaces(kw):
+    """No call needs more than the workspace of a larger one: fewer rows, queries or layers."""
+    s = shape(n_pages=5000, max_pages=4096, **kw)
+    for sizes in ([(n, 3, 4) for n in (1, 100, 3278, 5000, 65536)], [(5000, r, 4) for r in (1, 2, 7, 64, 500)], [(5000, 3, n) for n in (1, 2, 3, 4)]):
+        need = [B.kv_q4_window_workspace_bytes(s, *x) for x in sizes]
+        assert need == sorted(need) and need[0] >= 256
+    by_rows = [B.kv_q4_shared_workspace_bytes(s, n, 4) for n in (1, 100, 3278, 5000, 65536)]
+    by_layers = [B.kv_q4_shared_workspace_bytes(s, 5000, n) for n in (1, 2, 3, 4)]
+    assert by_rows == sorted(by_rows) and by_layers == sorted(by_layers)
+    for n, rows, layers in ((1, 1, 1), (40, 1, 1), (5000, 1, 4), (65536, 2, 1), (65536, 300, 4), (3278, 7, 3)):
+        for win in (0, 4, 4096):
+            # one byte less than the call's own need is refused; what the sizing call gives is enough: the next check refuses
+            assert window(layers=layers, n=n, rows=rows, win=win, s=s, ws=FAKE + 16, ws_bytes=B.kv_q4_window_workspace_bytes(s, 65536, 300, 4)) == INVALID
+            assert window(layers=layers, n=n, rows=rows, win=win, s=s, ws=FAKE + 16, ws_bytes=B.kv_q4_window_workspace_bytes(s, n, rows, layers)) == INVALID
+        assert shared(layers=layers, n=n, s=s, ws=FAKE + 16, ws_bytes=B.kv_q4_shared_workspace_bytes(s, n, layers)) == INVALID
+
+
+@pytest.mark.parametrize("bad", [(0, 1, 1), (321, 1, 1), (10, 0, 1), (10, 321, 1), (10, 1, 0), (10, 1, 5)])
+def test_workspace_refusals(bad):
+    with pytest.raises(B.KVError):
+        B.kv_q4_window_workspace_bytes(shape(), *bad)
+    if bad[1] == 1:
+        with pytest.raises(B.KVError):
+            B.kv_q4_shared_workspace_bytes(shape(), bad[0], bad[2])
+
+
+def test_binding_refuses_attention_of_other_layouts():
+    c, ws = cpu_cache(), torch.zeros(1 << 20, dtype=torch.uint8)
+    q = torch.zeros(1, 3, 8, 2, 128, dtype=torch.bfloat16)
+    flat, group = q[:, :, :, 0].contiguous(), torch.zeros(3, dtype=torch.int32)
+    for x, y, kw in ((q, q, {}), (q, q.float(), {}), (q[..., :64], q, {}), (q, q.transpose(3, 4), {}), (q, q, dict(count=group.long())), (q, q, dict(count=group[:2]))):
+        with pytest.raises(B.KVError):
+            B.kv_q4_attend_window(c, 0, 1, 10, 2, x, y, ws, **kw)
+    for x, y, g in ((flat, flat, group), (flat.float(), flat, group), (flat, q, group), (flat, flat, group[:2]), (flat, flat, group.long()), (flat, flat, None)):
+        with pytest.raises(B.KVError):
+            B.kv_q4_attend_shared(c, 0, 1, 10, g, x, y, ws)
