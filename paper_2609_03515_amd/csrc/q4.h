@@ -104,12 +104,12 @@ hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);
 
 // Attention of blocks of queries: the newest rows' queries of a slot in a window (kv_q4_attend_window), or one query of each of
 // several slots that share pages (kv_q4_attend_shared).  A block is `vectors` queries; each is `group` columns of a product.
-constexpr int kQ4MostVectors = 32, kQ4MostColumns = 32;  // of a block
+constexpr int kQ4MostVectors = 32, kQ4MostColumns = 64;  // of a block
 struct Q4QueryPlan {
     int tiles;    // column tiles of 16 in a block
     int per;      // queries in a column tile
     int vectors;  // queries in a block
-    int blocks;   // blocks of a slot (window)
+    int blocks;   // blocks of a slot (window), or of the batch where its groups fill them (shared)
     int chunks;   // workgroups that divide a block's rows
 };
 struct Q4QueryArgs {
@@ -128,14 +128,15 @@ struct Q4QueryArgs {
     // window
     int rows, window, sinks;
     const int32_t* count;    // nullable [batch]
-    uint64_t* visible;       // positions kept: [batch][blocks][words] a bit for every 32 rows of which a block sees any
+    uint64_t* visible;       // nullable: [batch][blocks][words] a bit for every 32 rows of which a block sees any
     int words;
     // shared
     const int32_t* group;    // [batch]
     int list_pages;          // places of a slot's list
     int4* items;             // [batch][list_pages] pages (page, rows in use, the block's queries that it is a page of, 0)
     int32_t* lists;          // [batch] entries of each slot's list
-    int32_t* members;        // [batch][vectors] the slots of the block that begins with a slot, -1 behind the last (first -1: none)
+    int32_t* heads;          // [batch] whether a block begins with the slot
+    int32_t* members;        // [batch][vectors] the slots of the block that begins with a slot, -1 behind the last
 };
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks);
 Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max);

@@ -138,7 +138,7 @@ AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool sco
 
 // The scratch of blocks of queries after the fault word: marks or lists, and the parts of outputs that several workgroups share.
 struct QueryLayout {
-    size_t visible_off, members_off, lists_off, items_off, part_off, opart_off, total;
+    size_t visible_off, members_off, heads_off, lists_off, items_off, part_off, opart_off, total;
 };
 QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, size_t parts) {
     QueryLayout L{};
@@ -151,6 +151,7 @@ QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, 
     L.visible_off = take(mark_words * sizeof(uint64_t));
     if (list_pages) {
         L.members_off = take((size_t)d.batch * kQ4MostVectors * sizeof(int32_t));
+        L.heads_off = take((size_t)d.batch * sizeof(int32_t));
         L.lists_off = take((size_t)d.batch * sizeof(int32_t));
         L.items_off = take((size_t)d.batch * list_pages * sizeof(int4));
     }
@@ -225,7 +226,7 @@ void set_queries(Q4QueryArgs* a, const QueryLayout& L, void* ws) {
     constexpr double kLog2e = 1.4426950408889634;
     a->scale2 = (float)(kLog2e / sqrt((double)a->dims.d));
     char* base = static_cast<char*>(ws);
-    a->visible = reinterpret_cast<uint64_t*>(base + L.visible_off);
+    a->heads = reinterpret_cast<int32_t*>(base + L.heads_off);
     a->members = reinterpret_cast<int32_t*>(base + L.members_off);
     a->lists = reinterpret_cast<int32_t*>(base + L.lists_off);
     a->items = reinterpret_cast<int4*>(base + L.items_off);
@@ -452,7 +453,8 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.cache = cache_of(*cache);
     a.plan = q4_window_plan(d, layer_count, n_max, rows, window, sinks);
     a.words = (int)mark_words_of(n_max);
-    const size_t marks = cache->pos ? (size_t)d.batch * a.plan.blocks * a.words : 0;
+    // (one block of a slot finds its tiles by itself)
+    const size_t marks = cache->pos && a.plan.blocks > 1 ? (size_t)d.batch * a.plan.blocks * a.words : 0;
     if ((double)layer_count * d.batch * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups || (double)d.batch * a.plan.blocks * ((a.words + 3) / 4) > kMostGroups)
         return KV_ERR_UNSUPPORTED;
     const QueryLayout L = query_layout(d, marks, 0, parts_of(d, layer_count, rows, a.plan.chunks));
@@ -469,6 +471,7 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.sinks = sinks;
     a.count = count;
     set_queries(&a, L, ws);
+    a.visible = marks ? reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + L.visible_off) : nullptr;
     return hip_status(launch_q4_window(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -496,7 +499,7 @@ kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.dims = d;
     a.cache = cache_of(*cache);
     a.plan = q4_shared_plan(d, layer_count, n_max);
-    if ((double)layer_count * d.batch * d.hkv * a.plan.chunks > kMostGroups) return KV_ERR_UNSUPPORTED;
+    if ((double)layer_count * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups) return KV_ERR_UNSUPPORTED;
     a.list_pages = (n_max + d.page_rows - 1) / d.page_rows;
     const QueryLayout L = query_layout(d, 0, a.list_pages, parts_of(d, layer_count, 1, a.plan.chunks));
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;

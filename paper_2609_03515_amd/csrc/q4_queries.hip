@@ -32,7 +32,7 @@
 namespace ikv {
 namespace {
 
-constexpr int kQueryWaves = 8;
+constexpr int kAlone = 768;  // blocks of four column tiles from which a wave takes each for itself
 constexpr int kKeep = 0;  // rows are read again by other workgroups
 constexpr float kNaN = __builtin_nanf("");
 
@@ -70,60 +70,6 @@ __device__ __forceinline__ Slot slot_of(const Q4QueryArgs& a, int b) {
     }
     return s;
 }
-
-// A set of ascending numbers given by bits (or counts), found by rank.  Lane i of the wave holds the i-th word of a run of 64 and the
-// set bits of the words before it in the run; the run moves on as the ranks asked for grow.
-struct Ranks {
-    const uint64_t* words;
-    int total_words, run;  // words in all, the run's first
-    uint64_t word;         // the lane's
-    int before, base, in_run;
-
-    __device__ __forceinline__ void take() {
-        const int i = run + (int)(threadIdx.x % kWave);
-        word = i < total_words ? words[i] : 0;
-        int sum = __popcll(word);
-        const int mine = sum;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int up = __shfl_up(sum, o, kWave);
-            if ((int)(threadIdx.x % kWave) >= o) sum += up;
-        }
-        before = sum - mine;
-        in_run = __builtin_amdgcn_readlane(sum, kWave - 1);
-    }
-    __device__ __forceinline__ void start(const uint64_t* w, int n) {
-        words = w;
-        total_words = n;
-        run = base = 0;
-        take();
-    }
-    // The number with rank k, or -1 past the last.  Ranks do not fall from call to call.
-    __device__ __forceinline__ int at(int k) {
-        while (k >= base + in_run) {
-            if (run + kWave >= total_words) return -1;
-            base += in_run;
-            run += kWave;
-            take();
-        }
-        const int r = k - base, lane = __popcll(__ballot(before <= r)) - 1;
-        // (lanes without bits have the next one's count: the last of those that are not above r holds it)
-        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)word, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(word >> 32), lane);
-        int left = r - __builtin_amdgcn_readlane(before, lane);
-        uint64_t w = (uint64_t)hi << 32 | lo;
-        int bit = 0;
-#pragma unroll
-        for (int half = 32; half >= 1; half >>= 1) {
-            const int low = __popcll(w & ((1ull << half) - 1));
-            if (left >= low) {
-                left -= low;
-                bit += half;
-                w >>= half;
-            }
-        }
-        return (run + lane) * 64 + bit;
-    }
-};
 
 // Tiles that a block sees any row of: one wave to 64 tiles.
 constexpr int kMarkWaves = 4;
@@ -192,7 +138,8 @@ __global__ __launch_bounds__(kListThreads) void q4_list_kernel(Q4QueryArgs a) {
         lens[threadIdx.x] = n < 0 || n > a.n_max ? 0 : n;
         if ((int)threadIdx.x == k && lens[k] != n) atomicOr(a.faults, kFaultCache);
     }
-    if ((int)threadIdx.x < V) a.members[(size_t)b * V + threadIdx.x] = k == 0 && (int)threadIdx.x < count ? members[threadIdx.x] : -1;
+    if (k == 0 && (int)threadIdx.x < V) a.members[(size_t)b * V + threadIdx.x] = (int)threadIdx.x < count ? members[threadIdx.x] : -1;
+    if (threadIdx.x == 0) a.heads[b] = k == 0;
     __syncthreads();
     const int pages = (lens[k] + d.page_rows - 1) >> d.page_shift;
     int done = 0;
@@ -247,44 +194,64 @@ struct KeyTile {
 };
 
 // Column tiles (CT) of 16; parts of a probability (kP): 3 take all of its 24 bits, 1 rounds it to bf16 (8 bits, to nearest; its
-// sum is of the rounded numbers).
-template <typename T, int D, int CT, int kP, bool kShared>
-__global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_kernel(Q4QueryArgs a) {
-    constexpr int kThreads = kWave * kQueryWaves;
+// sum is of the rounded numbers).  kWaves: of a workgroup, which divide a block's tiles and join their outputs; or one.
+template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
+__global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kernel(Q4QueryArgs a) {
+    constexpr int kThreads = kWave * kWaves;
     constexpr int kKey = D / 32, kOut = D / 16;     // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;  // bf16 parts of a query
     constexpr int kStride = D + 4;
-    constexpr int kJoin = kQueryWaves / 2;          // waves whose outputs are joined through LDS at once
-    constexpr bool kQLds = kParts * CT > 1;
+    constexpr int kJoin = (kWaves + 1) / 2;         // waves whose outputs are joined through LDS at once
     // [wave] values; in their place [joined wave][column][kStride] outputs; then [wave][column] maxima and sums; then the queries
     extern __shared__ float lds[];
     const Q4Dims& d = a.dims;
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int c = lane % 16, s = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int group = d.group, per = a.plan.per;
 
     // unit: KV heads fastest (eight of them fall on the eight XCDs), then the blocks, the last (a window's longest) first
     uint32_t x = blockIdx.x;
     const int g = x % (uint32_t)d.hkv;
     x /= (uint32_t)d.hkv;
-    const int block = kShared ? 0 : a.plan.blocks - 1 - x % (uint32_t)a.plan.blocks;
-    if constexpr (!kShared) x /= (uint32_t)a.plan.blocks;
-    const int b = x % (uint32_t)d.batch;
-    x /= (uint32_t)d.batch;
+    const int nth = x % (uint32_t)a.plan.blocks;
+    x /= (uint32_t)a.plan.blocks;
+    int b = 0;
+    if constexpr (!kShared) {
+        b = x % (uint32_t)d.batch;
+        x /= (uint32_t)d.batch;
+    }
     const int layer = x % (uint32_t)a.layer_count, chunk = x / (uint32_t)a.layer_count;
+    const int last = d.cap - 1;
+    const size_t page_bytes = (size_t)d.hkv * d.rec;
+    const int step = a.plan.chunks * kWaves, k0 = chunk * kWaves + wave;
+    uint32_t fault = 0;
 
+  // Shared: a workgroup takes the nth block, and those `blocks` further on, where small groups make more than there are places for.
+  for (int turn = nth;; turn += a.plan.blocks) {
+    int lane = threadIdx.x % kWave;
+    if constexpr (kShared) asm volatile("" : "+v"(lane));  // (nothing of a lane is worked out before the loop and kept over it)
+    const int c = lane % 16, s = lane / 16, part = c / group, head = c - part * group;
+    const uint8_t* const pool = a.cache.pool + q4_record(d, a.layer0 + layer, 0, g);
+    if constexpr (kShared) {
+        // the slot that the block begins with
+        b = -1;
+        int seen = 0;
+        for (int i0 = 0; i0 < d.batch && b < 0; i0 += kWave) {
+            const uint64_t is = __ballot(i0 + lane < d.batch && a.heads[min(i0 + lane, d.batch - 1)]);
+            const uint64_t it = __ballot((is >> lane & 1) && seen + __popcll(is & ((1ull << lane) - 1)) == turn);
+            if (it) b = i0 + __builtin_ctzll(it);
+            seen += __popcll(is);
+        }
+        if (b < 0) break;
+    }
     // the block's queries: the lane's in each column tile, its slot and row (-1: none)
     const int32_t* const members = kShared ? a.members + (size_t)b * a.plan.vectors : nullptr;
+    const int block = kShared ? 0 : a.plan.blocks - 1 - nth, v0 = block * a.plan.vectors;
     Slot slot{0, 0, false};
-    const int v0 = block * a.plan.vectors;
-    if constexpr (kShared) {
-        if (((scalar_ints)(uintptr_t)members)[0] < 0) return;
-    } else {
+    if constexpr (!kShared) {
         slot = slot_of(a, b);
         if (slot.bad && g == 0 && layer == 0 && chunk == 0 && threadIdx.x == 0) atomicOr(a.faults, kFaultCache);
         if (v0 >= slot.count) return;
     }
-    const int part = c / group, head = c - part * group;
     auto slot_row = [&](int ct, int vector_in_tile, int& sl, int& row) __attribute__((always_inline)) {
         const int v = ct * per + vector_in_tile;
         sl = b;
@@ -314,20 +281,22 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
         }
     }
 
-    // queries: bf16 of one column tile in registers, others as bf16 parts in LDS, [part][product][column tile][lane]
-    u32x4 q[kQLds ? 1 : kKey];
+    // queries as bf16 parts in LDS, [part][product][column tile][lane] (in registers one column tile would take 16, and spill as many)
     u32x4* const q_lds = reinterpret_cast<u32x4*>(lds + a.q_at) + lane;
-    for (int ct = kQLds ? wave : 0; ct < CT; ct += kQLds ? kQueryWaves : 1) {
+#pragma unroll
+    for (int i = 0; i < (CT + kWaves - 1) / kWaves; ++i) {
+        const int ct = i * kWaves + wave;
+        if (ct >= CT) break;
         int sl = -1, row = 0;
         if (part < per) slot_row(ct, part, sl, row);
-        const T* qp = static_cast<const T*>(a.q) + layer * a.qs[0] + max(sl, 0) * a.qs[1] + (g * group + head) * a.qs[2] + (sl < 0 ? 0 : row) * a.qs[3] + s * (D / 4);
-        if (sl < 0) qp = static_cast<const T*>(a.q) + s * (D / 4);  // (not used: any row)
+        // (no query: any row, not used)
+        const T* qp = static_cast<const T*>(a.q) + s * (D / 4);
+        if (sl >= 0) qp += layer * a.qs[0] + sl * a.qs[1] + (g * group + head) * a.qs[2] + row * a.qs[3];
         if constexpr (kParts == 1) {
 #pragma unroll
             for (int j = 0; j < kKey; ++j) {
-                const u32x4 w = reinterpret_cast<const u32x4*>(qp)[j], y = sl >= 0 ? w : u32x4{0, 0, 0, 0};
-                if constexpr (kQLds) q_lds[(j * CT + ct) * kWave] = y;
-                else q[j] = y;
+                const u32x4 w = reinterpret_cast<const u32x4*>(qp)[j];
+                q_lds[(j * CT + ct) * kWave] = sl >= 0 ? w : u32x4{0, 0, 0, 0};
             }
         } else {
 #pragma unroll
@@ -352,15 +321,15 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
         }
     }
 
-    // the tiles: `total` of them, found by rank
-    int total = 0, sink_tiles = 0, first_tile = 0, place_top = INT_MIN, place_low = INT_MAX;
-    uint32_t all = 0;                          // shared: every query of the block
-    int list_before = 0, list_slot = 0, items = 0;  // shared: lane i's member, and the pages that those before it list
-    Ranks ranks{};
+    // The wave's tiles are those of numbers k0, k0 + step, ... of `tiles`.  It looks at 64 of them at a time, one a lane: the pages (or
+    // listed pages) of the lane's tile, and a bit for each that takes part.
+    int tiles = 0, top_place = INT_MIN, low_place = INT_MAX;
+    uint32_t all = 0;                              // shared: every query of the block
+    int items = 0;                                 // shared: pages that the block's slots list
+    __shared__ int list_slot[kShared ? kQ4MostVectors : 1], list_before[kShared ? kQ4MostVectors : 1];  // a member, and pages that those before it list
     const int per_page_shift = kShared ? max(0, d.page_shift - 5) : 0;
     if constexpr (kShared) {
         const int m = lane < a.plan.vectors ? members[lane] : -1;
-        list_slot = max(m, 0);
         int sum = m >= 0 ? a.lists[m] : 0;
         const int mine = sum;
 #pragma unroll
@@ -368,11 +337,13 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
             const int up = __shfl_up(sum, o, kWave);
             if (lane >= o) sum += up;
         }
-        list_before = sum - mine;
+        if (wave == 0 && lane < a.plan.vectors) {
+            list_slot[lane] = max(m, 0);
+            list_before[lane] = sum - mine;
+        }
         items = __builtin_amdgcn_readlane(sum, kQ4MostVectors - 1);
-        if (lane >= a.plan.vectors) list_before = INT_MAX;
         all = (uint32_t)__ballot(m >= 0);
-        total = d.page_rows >= kTile ? items << per_page_shift : (items + 1) / 2;
+        tiles = d.page_rows >= kTile ? items << per_page_shift : (items + 1) / 2;
     } else {
         int top = INT_MIN, low = INT_MAX;
 #pragma unroll
@@ -381,63 +352,85 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
                 top = max(top, place[ct]);
                 low = min(low, place[ct]);
             }
-        place_top = __builtin_amdgcn_readfirstlane(wave_max_int(top));
-        place_low = __builtin_amdgcn_readfirstlane(~wave_max_int(~low));
-        if (slot.n > 0) {
-            if (a.cache.pos) {
-                ranks.start(a.visible + ((size_t)b * a.plan.blocks + block) * a.words, (slot.n + 64 * kTile - 1) / (64 * kTile));
-                total = INT_MAX;
+        top_place = __builtin_amdgcn_readfirstlane(wave_max_int(top));
+        low_place = __builtin_amdgcn_readfirstlane(~wave_max_int(~low));
+        tiles = (slot.n + kTile - 1) / kTile;
+    }
+    const int top_from = lower_bound_of(top_place, a.window), low_from = lower_bound_of(low_place, a.window);
+    const int32_t* const table = a.cache.table + (size_t)b * d.max_pages;
+    const int32_t* const pos = kShared || !a.cache.pos ? nullptr : a.cache.pos + (size_t)b * d.cap;
+    int page_of = 0, page_of2 = 0;  // window: pages of the halves; shared: the listed page, its rows in use and its queries (pages of 16
+    uint32_t mask_of = 0;           // rows: lanes 32 .. 63 hold the second halves of lanes 0 .. 31's tiles)
+    uint64_t left = 0;
+    int base = 0;
+    const bool pairs = kShared && d.page_rows < kTile;
+    const int at_once = pairs ? kWave / 2 : kWave;
+    auto look = [&]() __attribute__((always_inline)) {
+        const int k = k0 + (base + (pairs ? lane % (kWave / 2) : lane)) * step;  // (2^27 rows are 2^22 tiles, and 64 steps fewer than 2^25)
+        bool part_of = k < tiles;
+        if constexpr (kShared) {
+            const int i = pairs ? 2 * k + lane / (kWave / 2) : k >> per_page_shift;
+            int before = 0, sl = 0;
+            for (int v = 0; v < a.plan.vectors; ++v) {  // the last member that has as many before it: it lists the page
+                const int y = list_before[v], z = list_slot[v];
+                before = y <= i ? y : before;
+                sl = y <= i ? z : sl;
+            }
+            int4 it = make_int4(0, 0, 0, 0);
+            if (part_of && i < items) it = a.items[(size_t)sl * a.list_pages + (i - before)];
+            page_of = it.x;
+            page_of2 = it.y;
+            mask_of = it.z;
+            if (pairs) part_of = part_of && lane < kWave / 2;
+        } else {
+            const int row = k * kTile;
+            page_of = table[min(row, last) >> d.page_shift];
+            page_of2 = table[min(row + 16, last) >> d.page_shift];
+            if (!pos) {
+                part_of = part_of && row <= top_place && (row + kTile > low_from || row < a.sinks);
+            } else if (a.visible) {
+                part_of = part_of && (a.visible[((size_t)b * a.plan.blocks + block) * a.words + k / 64] >> k % 64 & 1);
             } else {
-                first_tile = max(0, lower_bound_of(place_low, a.window)) / kTile;
-                sink_tiles = a.window ? min(a.sinks / kTile + (a.sinks % kTile != 0), first_tile) : 0;
-                total = sink_tiles + place_top / kTile - first_tile + 1;
+                // two tiles to a load, eight loads together
+                uint64_t bits = 0;
+                constexpr int kTogether = 8;
+                for (int i0 = 0; i0 < kWave && k0 + (base + i0) * step < tiles; i0 += 2 * kTogether) {
+                    int p[kTogether];
+#pragma unroll
+                    for (int i = 0; i < kTogether; ++i) p[i] = pos[min((k0 + (base + i0 + 2 * i + lane / kTile) * step) * kTile + lane % kTile, last)];
+#pragma unroll
+                    for (int i = 0; i < kTogether; ++i) {
+                        const int r = (k0 + (base + i0 + 2 * i + lane / kTile) * step) * kTile + lane % kTile;
+                        const uint64_t any = __ballot(r < slot.n && p[i] <= top_place && (p[i] >= low_from || p[i] < a.sinks));
+                        bits |= (uint64_t)((uint32_t)any != 0) << (i0 + 2 * i) | (uint64_t)((any >> 32) != 0) << (i0 + 2 * i + 1);
+                    }
+                }
+                part_of = bits >> lane & 1;
             }
         }
-    }
-    const int window_from = lower_bound_of(place_top, a.window);
-    const int last = d.cap - 1;
-    const scalar_ints table = (scalar_ints)(uintptr_t)(a.cache.table + (size_t)b * d.max_pages);
-    auto item = [&](int i) __attribute__((always_inline)) {
-        const int m = __popcll(__ballot(list_before <= i)) - 1;  // (of members without pages the last one, which has them)
-        const int sl = __builtin_amdgcn_readlane(list_slot, m), at = i - __builtin_amdgcn_readlane(list_before, m);
-        return ((scalar_int4s)(uintptr_t)a.items)[(size_t)sl * a.list_pages + at];
+        left = __ballot(part_of);
     };
-    auto fetch = [&](int k, Ref& r) __attribute__((always_inline)) {  // whether there is a k-th tile
-        if (k >= total) return false;
+    // the next tile of them that takes part
+    auto fetch = [&](Ref& r) __attribute__((always_inline)) {
+        if (!left) return false;
+        const int i = __builtin_ctzll(left), k = k0 + (base + i) * step;
+        left &= left - 1;
         if constexpr (kShared) {
-            if (d.page_rows >= kTile) {
-                const i32x4 it = item(k >> per_page_shift);
-                r.row = (k & ((1 << per_page_shift) - 1)) * kTile;
+            r.row = (k & ((1 << per_page_shift) - 1)) * kTile;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    r.page[h] = it.x;
-                    r.rows[h] = it.y - r.row - 16 * h;
-                    r.mask[h] = (uint32_t)it.z;
-                }
-            } else {
-                r.row = 0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bool is = 2 * k + h < items;
-                    const i32x4 it = item(min(2 * k + h, items - 1));
-                    r.page[h] = it.x;
-                    r.rows[h] = is ? it.y : 0;
-                    r.mask[h] = is ? (uint32_t)it.z : 0;
-                }
+            for (int h = 0; h < 2; ++h) {
+                const int from_lane = pairs && h ? i + kWave / 2 : i;
+                r.page[h] = __builtin_amdgcn_readlane(page_of, from_lane);
+                r.rows[h] = __builtin_amdgcn_readlane(page_of2, from_lane) - (pairs ? 0 : r.row + 16 * h);
+                r.mask[h] = __builtin_amdgcn_readlane(mask_of, from_lane);
             }
         } else {
-            int t = k < sink_tiles ? k : first_tile + k - sink_tiles;
-            if (a.cache.pos) t = ranks.at(k);
-            if (t < 0) return false;
-            r.row = t * kTile;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) r.page[h] = table[min(r.row + 16 * h, last) >> d.page_shift];
+            r.row = k * kTile;
+            r.page[0] = __builtin_amdgcn_readlane(page_of, i);
+            r.page[1] = __builtin_amdgcn_readlane(page_of2, i);
         }
         return true;
     };
-    uint32_t fault = 0;
-    const uint8_t* const pool = a.cache.pool + q4_record(d, a.layer0 + layer, 0, g);
-    const size_t page_bytes = (size_t)d.hkv * d.rec;
     auto locate = [&](const Ref& r, Half (&h)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -463,7 +456,6 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
     };
     const int key_row = c % 4 * 4 + c / 4;  // row of a half whose keys the lane holds: result rows 4 s + i are rows 4 i + s
     const uint32_t ko = key_row * (D / 2) + s * (D / 8), eo = D == 128 ? key_row * 4 + s : key_row * 2 + s / 2;
-    const int32_t* const pos = kShared || !a.cache.pos ? nullptr : a.cache.pos + (size_t)b * d.cap;
     auto load_keys = [&](KeyTile<D>& t, const Half (&h)[2], int row) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -503,20 +495,20 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
 #pragma unroll
         for (int e = 0; e < kOut; ++e) acc[ct][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    if constexpr (kQLds) __syncthreads();
+    __syncthreads();
 
-    // Loads run one tile ahead, page numbers two.
-    const int step = a.plan.chunks * kQueryWaves;
-    int k = chunk * kQueryWaves + wave;
+    // Loads run one tile ahead (but for the first of 64).
+   for (; k0 + base * step < tiles; base += at_once) {
+    look();
     KeyTile<D> keys;
     Half now[2], next[2];
     Ref ref{}, ahead{};
-    bool have = fetch(k, ref), more = false;
+    bool have = fetch(ref), more = false;
     if (have) {
         locate(ref, now);
         load_keys(keys, now, ref.row);
         load_values(now);
-        more = fetch(k + step, ahead);
+        more = fetch(ahead);
     }
     while (have) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tile's keys, and its values in LDS
@@ -540,9 +532,7 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
                 if (skipped(ct)) continue;
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p) {
-                    u32x4 y;
-                    if constexpr (kQLds) y = q_lds[((p * kKey + j) * CT + ct) * kWave];
-                    else y = q[j];
+                    const u32x4 y = q_lds[((p * kKey + j) * CT + ct) * kWave];
                     z[ct][0] = mfma(k0, y, z[ct][0]);
                     z[ct][1] = mfma(k1, y, z[ct][1]);
                 }
@@ -556,13 +546,13 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
             for (int ct = 0; ct < CT; ++ct) bits[ct] = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int half = j / 4, in = 4 * (j % 4) + s;
-                int p = row + 16 * half + in;
+                const int half = j / 4;
+                int p = row + s + (16 * half + 4 * (j % 4));
                 if constexpr (!kShared)
-                    if (pos) p = __shfl(tile_pos, 16 * half + in, kWave);
+                    if (pos) p = __builtin_amdgcn_ds_bpermute(4 * s + 4 * (16 * half + 4 * (j % 4)), tile_pos);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    uint32_t h = in >= now[half].valid;
+                    uint32_t h = 4 * (j % 4) >= now[half].valid - s;
                     if constexpr (kShared) h |= ~(now[half].mask >> (ct * per + part)) & 1u;
                     else h |= (uint32_t)(p > place[ct]) | ((uint32_t)(p < from[ct]) & (uint32_t)(p >= a.sinks));
                     bits[ct] |= h << j;
@@ -574,7 +564,7 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
             plain = plain && (now[0].mask & now[1].mask) == all;
         } else {
             const int p = pos ? tile_pos : row + lane % kTile;
-            plain = plain && __all(p <= place_low && (p >= window_from || p < a.sinks));
+            plain = plain && __all(p <= low_place && (p >= top_from || p < a.sinks));
         }
         if (!plain) {
             asm volatile("");
@@ -712,12 +702,10 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
             now[0] = next[0];
             now[1] = next[1];
             ref = ahead;
-            k += step;
-            more = fetch(k + step, ahead);
+            more = fetch(ahead);
         }
     }
-    if (fault && lane == 0) atomicOr(a.faults, fault);
-
+   }
     // the waves joined: the upper half into the lower, those through columns of LDS
     constexpr int kColumns = CT * 16;
     float* const stat = lds + a.stat_at;  // [wave][column] maxima, then sums
@@ -735,53 +723,19 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
                     *reinterpret_cast<f32x4*>(mine(ct) + i * kOut + e) = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
             if (s == 0) {
                 stat[wave * kColumns + 16 * ct + c] = m[ct];
-                stat[(kQueryWaves + wave) * kColumns + 16 * ct + c] = l[ct];
+                stat[(kWaves + wave) * kColumns + 16 * ct + c] = l[ct];
             }
         }
     };
-    if (wave >= kJoin) put();
-    __syncthreads();
-    if (wave < kJoin) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const float m2 = stat[(wave + kJoin) * kColumns + 16 * ct + c], l2 = stat[(kQueryWaves + wave + kJoin) * kColumns + 16 * ct + c];
-            const float top = fmaxf(m[ct], m2), f = exp2_hw(m[ct] - top), f2 = exp2_hw(m2 - top);
-            m[ct] = top;
-            l[ct] = l[ct] * f + l2 * f2;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < kOut; e += 4) {
-                    const f32x4 o = *reinterpret_cast<const f32x4*>(mine(ct) + i * kOut + e);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) acc[ct][e + y][i] = acc[ct][e + y][i] * f + o[y] * f2;
-                }
-        }
-    }
-    __syncthreads();
-    if (wave < kJoin) put();
-    __syncthreads();
-    for (int i = threadIdx.x; i < kColumns * (D / 4); i += kThreads) {
-        const int col = i / (D / 4), e = i % (D / 4) * 4;
+    // elements e .. e + 3 of column col: the weights' maximum and sum, and the sum over the rows
+    auto store = [&](int col, int e, float top, float sum, f32x4 o) __attribute__((always_inline)) {
         const int vt = col % 16 / group, h = col % 16 - vt * group;
         int sl = -1, row = 0;
         if (vt < per) slot_row(col / 16, vt, sl, row);
-        if (sl < 0) continue;
-        float top = stat[col];
-#pragma unroll
-        for (int w = 1; w < kJoin; ++w) top = fmaxf(top, stat[w * kColumns + col]);
-        float sum = 0.0f;
-        f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < kJoin; ++w) {
-            const float f = exp2_hw(stat[w * kColumns + col] - top);
-            sum += f * stat[(kQueryWaves + w) * kColumns + col];
-            o += *reinterpret_cast<const f32x4*>(lds + (w * kColumns + col) * kStride + e) * f;
-        }
+        if (sl < 0) return;
         if (a.plan.chunks == 1) {
-            const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+            o *= sum != 0.0f ? 1.0f / sum : 0.0f;
             T* op = static_cast<T*>(a.o) + layer * a.os[0] + sl * a.os[1] + (g * group + h) * a.os[2] + row * a.os[3] + e;
-            o *= inv;
             if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
             else *reinterpret_cast<f32x4*>(op) = o;
         } else {
@@ -790,7 +744,67 @@ __global__ __launch_bounds__(kWave* kQueryWaves, CT == 1 ? 4 : 2) void q4_query_
             if (sum != 0.0f) *reinterpret_cast<f32x4*>(a.opart + at * D + e) = o;
             if (e == 0) a.part[at] = make_float2(top, sum);
         }
+    };
+    if constexpr (kWaves == 1) {
+        // a column tile at a time through LDS, so that a row's elements are written side by side
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            float* const place_of = lds + c * kStride + s * (D / 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < kOut; e += 4)
+                    *reinterpret_cast<f32x4*>(place_of + i * kOut + e) = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
+            __syncthreads();
+            for (int i = lane; i < 16 * (D / 4); i += kWave) {
+                const int col = i / (D / 4), e = i % (D / 4) * 4;
+                store(16 * ct + col, e, __shfl(m[ct], col, kWave), __shfl(l[ct], col, kWave), *reinterpret_cast<const f32x4*>(lds + col * kStride + e));
+            }
+            __syncthreads();
+        }
+    } else {
+        if (wave >= kJoin) put();
+        __syncthreads();
+        if (wave < kJoin) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const float m2 = stat[(wave + kJoin) * kColumns + 16 * ct + c], l2 = stat[(kWaves + wave + kJoin) * kColumns + 16 * ct + c];
+                const float top = fmaxf(m[ct], m2), f = exp2_hw(m[ct] - top), f2 = exp2_hw(m2 - top);
+                m[ct] = top;
+                l[ct] = l[ct] * f + l2 * f2;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < kOut; e += 4) {
+                        const f32x4 o = *reinterpret_cast<const f32x4*>(mine(ct) + i * kOut + e);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) acc[ct][e + y][i] = acc[ct][e + y][i] * f + o[y] * f2;
+                    }
+            }
+        }
+        __syncthreads();
+        if (wave < kJoin) put();
+        __syncthreads();
+        for (int i = threadIdx.x; i < kColumns * (D / 4); i += kThreads) {
+            const int col = i / (D / 4), e = i % (D / 4) * 4;
+            float top = stat[col];
+#pragma unroll
+            for (int w = 1; w < kJoin; ++w) top = fmaxf(top, stat[w * kColumns + col]);
+            float sum = 0.0f;
+            f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kJoin; ++w) {
+                const float f = exp2_hw(stat[w * kColumns + col] - top);
+                sum += f * stat[(kWaves + w) * kColumns + col];
+                o += *reinterpret_cast<const f32x4*>(lds + (w * kColumns + col) * kStride + e) * f;
+            }
+            store(col, e, top, sum, o);
+        }
     }
+    if constexpr (!kShared) break;
+    __syncthreads();  // (the next block's values come to the places of these)
+  }
+    if (fault && threadIdx.x % kWave == 0) atomicOr(a.faults, fault);
 }
 
 // The parts of a query head's output joined: 2^split threads to four elements, each of them every 2^split-th part.
@@ -859,22 +873,23 @@ __global__ __launch_bounds__(kPartThreads) void q4_part_kernel(Q4QueryArgs a, in
     else *reinterpret_cast<f32x4*>(op) = o;
 }
 
-template <typename T, int D, int CT, int kP, bool kShared>
+template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
 hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
-    constexpr int kJoined = kQueryWaves / 2 * CT * 16 * (D + 4) * (int)sizeof(float), kValues = kQueryWaves * kValueBytes<D>;
-    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kStat = 2 * kQueryWaves * CT * 16;
+    constexpr int kJoined = (kWaves + 1) / 2 * (kWaves > 1 ? CT : 1) * 16 * (D + 4) * (int)sizeof(float), kValues = kWaves * kValueBytes<D>;
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kStat = 2 * kWaves * CT * 16;
     static_assert(kJoined % 16 == 0 && kValues % 16 == 0 && kStat % 4 == 0, "queries are read 16 bytes at a time");
+    static_assert(CT * 16 <= kQ4MostColumns, "room for the parts of outputs");
     a.stat_at = (kJoined > kValues ? kJoined : kValues) / (int)sizeof(float);
     a.q_at = a.stat_at + kStat;
-    const size_t lds = (size_t)a.q_at * sizeof(float) + (kParts * CT > 1 ? (size_t)kParts * (D / 32) * CT * kWave * sizeof(u32x4) : 0);
-    auto kern = q4_query_kernel<T, D, CT, kP, kShared>;
+    const size_t lds = (size_t)a.q_at * sizeof(float) + (size_t)kParts * (D / 32) * CT * kWave * sizeof(u32x4);
+    auto kern = q4_query_kernel<T, D, CT, kP, kShared, kWaves>;
     if (lds > 64 * 1024) {
         static std::atomic<bool> raised[kMaxDevices];
         const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), raised);
         if (e != hipSuccess) return e;
     }
-    const uint32_t blocks = kShared ? 1 : a.plan.blocks;
-    hipLaunchKernelGGL(kern, dim3((uint32_t)a.dims.hkv * blocks * a.dims.batch * a.layer_count * a.plan.chunks), dim3(kWave * kQueryWaves), lds, s, a);
+    const uint32_t slots = kShared ? 1 : a.dims.batch;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)a.dims.hkv * a.plan.blocks * slots * a.layer_count * a.plan.chunks), dim3(kWave * kWaves), lds, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.plan.chunks == 1) return e;
     const uint32_t heads = (uint32_t)a.layer_count * a.dims.batch * a.rows * a.dims.hq;
@@ -886,11 +901,16 @@ hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
     return hipGetLastError();
 }
 
+constexpr int kQueryWaves = 8;  // of a workgroup that divides a block's tiles
 template <typename T, int D, bool kShared>
 hipError_t launch_tiles(const Q4QueryArgs& a, hipStream_t s) {
-    if constexpr (sizeof(T) == 2)
-        if (a.plan.tiles == 2) return launch_form<T, D, 2, 1, kShared>(a, s);
-    return launch_form<T, D, 1, 3, kShared>(a, s);
+    if constexpr (sizeof(T) == 2) {
+        if constexpr (!kShared) {
+            if (a.plan.tiles == 4) return launch_form<T, D, 4, 1, kShared, 1>(a, s);
+        }
+        if (a.plan.tiles == 2) return launch_form<T, D, 2, 1, kShared, kQueryWaves>(a, s);
+    }
+    return launch_form<T, D, 1, 3, kShared, kQueryWaves>(a, s);
 }
 template <bool kShared>
 hipError_t launch_queries(const Q4QueryArgs& a, hipStream_t s) {
@@ -898,11 +918,11 @@ hipError_t launch_queries(const Q4QueryArgs& a, hipStream_t s) {
     return a.dims.d == 128 ? launch_tiles<float, 128, kShared>(a, s) : launch_tiles<float, 64, kShared>(a, s);
 }
 
-// Workgroups that divide a block's `tiles` tiles: until there are two for every CU, each with a tile for every wave at least.
-int chunks_of(int64_t units, int tiles) {
-    const int cus = device_cus() > 0 ? device_cus() : 256;
-    const int64_t want = (2 * cus + units - 1) / units, most = (tiles + kQueryWaves - 1) / kQueryWaves;
-    return (int)(want < most ? want : most > 0 ? most : 1);
+int cus_of() { return device_cus() > 0 ? device_cus() : 256; }
+// Workgroups of `waves` waves that divide a block's `tiles` tiles: until there are `want` of them, each with a tile for every wave at least.
+int chunks_of(int64_t units, int64_t tiles, int waves, int want) {
+    const int64_t by_units = (want + units - 1) / units, most = (tiles + waves - 1) / waves;
+    return (int)(by_units < most ? by_units : most > 0 ? most : 1);
 }
 
 }  // namespace
@@ -910,15 +930,19 @@ int chunks_of(int64_t units, int tiles) {
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
-    p.tiles = d.bf16 && rows > p.per ? 2 : 1;
+    const int64_t slabs = (int64_t)layer_count * d.batch * d.hkv;
+    auto blocks = [&](int tiles) { return (rows + tiles * p.per - 1) / (tiles * p.per); };
+    p.tiles = !d.bf16 || rows <= p.per ? 1 : 2;
+    if (d.bf16 && slabs * blocks(4) >= kAlone) p.tiles = 4;
     p.vectors = p.tiles * p.per;
-    p.blocks = (rows + p.vectors - 1) / p.vectors;
+    p.blocks = blocks(p.tiles);
     int64_t tiles = (n_max + kTile - 1) / kTile;
     if (window) {  // (rows in order, in a window that ends inside tiles)
         const int64_t seen = ((int64_t)window + sinks + p.vectors) / kTile + 3;
         tiles = tiles < seen ? tiles : seen;
     }
-    p.chunks = chunks_of((int64_t)layer_count * d.batch * d.hkv * p.blocks, (int)tiles);
+    if (p.tiles == 4) p.chunks = 1;
+    else p.chunks = chunks_of(slabs * p.blocks, tiles, kQueryWaves, 2 * cus_of());
     return p;
 }
 
@@ -928,12 +952,12 @@ Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max) {
     p.tiles = d.bf16 && d.batch > p.per ? 2 : 1;
     p.vectors = p.tiles * p.per;
     p.blocks = (d.batch + p.vectors - 1) / p.vectors;
-    p.chunks = chunks_of((int64_t)layer_count * d.hkv * p.blocks, (n_max + kTile - 1) / kTile);
+    p.chunks = chunks_of((int64_t)layer_count * d.hkv * p.blocks, (n_max + kTile - 1) / kTile, kQueryWaves, 2 * cus_of());
     return p;
 }
 
 hipError_t launch_q4_window(const Q4QueryArgs& a, hipStream_t s) {
-    if (a.cache.pos) {
+    if (a.visible) {
         hipLaunchKernelGGL(q4_mark_kernel, dim3((uint32_t)((a.words + kMarkWaves - 1) / kMarkWaves) * a.plan.blocks * a.dims.batch),
                            dim3(kMarkWaves * kWave), 0, s, a);
         const hipError_t e = hipGetLastError();
