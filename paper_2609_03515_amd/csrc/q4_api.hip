@@ -161,13 +161,13 @@ QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, 
     return L;
 }
 size_t mark_words_of(int n_max) { return ((size_t)n_max + 2047) / 2048; }
-// Parts that a call needs, and more than any call of at most these sizes does: chunks are cut where there are fewer than 2 units for a
-// CU (then units * chunks is below twice that, of at most kQ4MostColumns columns each), and have 8 tiles of 32 rows at least.
+// Parts that a call needs, and more than any call of at most these sizes does: chunks are cut where there are fewer than kQ4Units
+// units for a CU (then units * chunks is below twice that, of at most kQ4MostColumns columns each), and have 8 tiles of 32 rows at least.
 size_t parts_of(const Q4Dims& d, int layer_count, int rows, int chunks) {
     return chunks > 1 ? (size_t)layer_count * d.batch * rows * d.hq * chunks : 0;
 }
 size_t most_parts(const Q4Dims& d, int n_max, int layer_count, int rows) {
-    const size_t cus = device_cus() > 0 ? device_cus() : 256, by_units = 4 * cus * kQ4MostColumns;
+    const size_t cus = device_cus() > 0 ? device_cus() : 256, by_units = 2 * kQ4Units * cus * kQ4MostColumns;
     const size_t by_tiles = (size_t)layer_count * d.batch * rows * d.hq * (((size_t)n_max + 255) / 256);
     return by_tiles < by_units ? by_tiles : by_units;
 }

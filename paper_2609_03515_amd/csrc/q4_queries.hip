@@ -39,6 +39,24 @@ constexpr float kNaN = __builtin_nanf("");
 typedef int __attribute__((ext_vector_type(4))) i32x4;
 typedef const __attribute__((address_space(4))) i32x4* scalar_int4s;
 
+// The kernel's arguments read where they are used, not kept from its beginning on (in spilled scalar registers).
+typedef const __attribute__((address_space(4))) Q4QueryArgs* late_args;
+__device__ __forceinline__ late_args args_again() {
+    late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
+// A lane's offset, widened where it is used: an address is a scalar base and a 32-bit offset then.
+__device__ __forceinline__ uint32_t again(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // (fmaxf first copies operands that might be signalling NaNs)
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // Two numbers rounded to bf16, to nearest even.
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     typedef float __attribute__((ext_vector_type(2))) f32x2;
@@ -220,7 +238,6 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         x /= (uint32_t)d.batch;
     }
     const int layer = x % (uint32_t)a.layer_count, chunk = x / (uint32_t)a.layer_count;
-    const int last = d.cap - 1;
     const size_t page_bytes = (size_t)d.hkv * d.rec;
     const int step = a.plan.chunks * kWaves, k0 = chunk * kWaves + wave;
     uint32_t fault = 0;
@@ -263,22 +280,24 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
             if (row >= slot.count) sl = -1;
         }
     };
-    int place[CT], from[CT];  // window: the query's position, and its window's first
-    bool there[CT];
+    __shared__ int places[kShared ? 1 : CT * 16];  // window: the columns' positions (no query: the lowest)
+    int top_place = INT_MIN, low_place = INT_MAX;
+    if constexpr (!kShared) {
+        int top = INT_MIN, low = INT_MAX;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        int sl = -1, row = 0;
-        if (part < per) slot_row(ct, part, sl, row);
-        there[ct] = sl >= 0;
-        place[ct] = INT_MIN;
-        from[ct] = INT_MAX;
-        if constexpr (!kShared) {
-            if (there[ct] && slot.n > 0) {
+        for (int ct = 0; ct < CT; ++ct) {
+            int sl = -1, row = 0, place = INT_MIN;
+            if (part < per) slot_row(ct, part, sl, row);
+            if (sl >= 0 && slot.n > 0) {
                 const int r = slot.n - slot.count + row;
-                place[ct] = a.cache.pos ? a.cache.pos[(size_t)b * d.cap + r] : r;
-                from[ct] = lower_bound_of(place[ct], a.window);
+                place = a.cache.pos ? a.cache.pos[(size_t)b * d.cap + r] : r;
+                top = max(top, place);
+                low = min(low, place);
             }
+            if (wave == 0 && s == 0) places[16 * ct + c] = place;
         }
+        top_place = __builtin_amdgcn_readfirstlane(wave_max_int(top));
+        low_place = __builtin_amdgcn_readfirstlane(~wave_max_int(~low));
     }
 
     // queries as bf16 parts in LDS, [part][product][column tile][lane] (in registers one column tile would take 16, and spill as many)
@@ -323,7 +342,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
 
     // The wave's tiles are those of numbers k0, k0 + step, ... of `tiles`.  It looks at 64 of them at a time, one a lane: the pages (or
     // listed pages) of the lane's tile, and a bit for each that takes part.
-    int tiles = 0, top_place = INT_MIN, low_place = INT_MAX;
+    int tiles = 0;
     uint32_t all = 0;                              // shared: every query of the block
     int items = 0;                                 // shared: pages that the block's slots list
     __shared__ int list_slot[kShared ? kQ4MostVectors : 1], list_before[kShared ? kQ4MostVectors : 1];  // a member, and pages that those before it list
@@ -345,19 +364,9 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         all = (uint32_t)__ballot(m >= 0);
         tiles = d.page_rows >= kTile ? items << per_page_shift : (items + 1) / 2;
     } else {
-        int top = INT_MIN, low = INT_MAX;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-            if (there[ct]) {
-                top = max(top, place[ct]);
-                low = min(low, place[ct]);
-            }
-        top_place = __builtin_amdgcn_readfirstlane(wave_max_int(top));
-        low_place = __builtin_amdgcn_readfirstlane(~wave_max_int(~low));
         tiles = (slot.n + kTile - 1) / kTile;
     }
     const int top_from = lower_bound_of(top_place, a.window), low_from = lower_bound_of(low_place, a.window);
-    const int32_t* const table = a.cache.table + (size_t)b * d.max_pages;
     const int32_t* const pos = kShared || !a.cache.pos ? nullptr : a.cache.pos + (size_t)b * d.cap;
     int page_of = 0, page_of2 = 0;  // window: pages of the halves; shared: the listed page, its rows in use and its queries (pages of 16
     uint32_t mask_of = 0;           // rows: lanes 32 .. 63 hold the second halves of lanes 0 .. 31's tiles)
@@ -366,30 +375,35 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
     const bool pairs = kShared && d.page_rows < kTile;
     const int at_once = pairs ? kWave / 2 : kWave;
     auto look = [&]() __attribute__((always_inline)) {
+        int lane = threadIdx.x % kWave;
+        asm volatile("" : "+v"(lane));  // (its places are worked out here, not kept over the tiles)
+        const late_args late = args_again();
         const int k = k0 + (base + (pairs ? lane % (kWave / 2) : lane)) * step;  // (2^27 rows are 2^22 tiles, and 64 steps fewer than 2^25)
         bool part_of = k < tiles;
         if constexpr (kShared) {
             const int i = pairs ? 2 * k + lane / (kWave / 2) : k >> per_page_shift;
             int before = 0, sl = 0;
-            for (int v = 0; v < a.plan.vectors; ++v) {  // the last member that has as many before it: it lists the page
+            for (int v = 0; v < late->plan.vectors; ++v) {  // the last member that has as many before it: it lists the page
                 const int y = list_before[v], z = list_slot[v];
                 before = y <= i ? y : before;
                 sl = y <= i ? z : sl;
             }
             int4 it = make_int4(0, 0, 0, 0);
-            if (part_of && i < items) it = a.items[(size_t)sl * a.list_pages + (i - before)];
+            if (part_of && i < items) it = late->items[(size_t)sl * late->list_pages + (i - before)];
             page_of = it.x;
             page_of2 = it.y;
             mask_of = it.z;
             if (pairs) part_of = part_of && lane < kWave / 2;
         } else {
             const int row = k * kTile;
-            page_of = table[min(row, last) >> d.page_shift];
-            page_of2 = table[min(row + 16, last) >> d.page_shift];
+            const int32_t* const table = late->cache.table + (size_t)b * late->dims.max_pages;
+            const int last = late->dims.cap - 1;
+            page_of = table[min(row, last) >> late->dims.page_shift];
+            page_of2 = table[min(row + 16, last) >> late->dims.page_shift];
             if (!pos) {
                 part_of = part_of && row <= top_place && (row + kTile > low_from || row < a.sinks);
-            } else if (a.visible) {
-                part_of = part_of && (a.visible[((size_t)b * a.plan.blocks + block) * a.words + k / 64] >> k % 64 & 1);
+            } else if (late->visible) {
+                part_of = part_of && (late->visible[((size_t)b * late->plan.blocks + block) * late->words + k / 64] >> k % 64 & 1);
             } else {
                 // two tiles to a load, eight loads together
                 uint64_t bits = 0;
@@ -436,12 +450,12 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         for (int i = 0; i < 2; ++i) {
             int page = r.page[i], in;
             if constexpr (kShared) {
-                h[i].valid = min(16, max(0, r.rows[i]));
+                h[i].valid = __builtin_amdgcn_readfirstlane(min(16, max(0, r.rows[i])));
                 h[i].mask = h[i].valid ? r.mask[i] : 0;
                 in = d.page_rows >= kTile ? r.row + 16 * i : 0;
             } else {
                 const int row = r.row + 16 * i;
-                h[i].valid = min(16, max(0, slot.n - row));
+                h[i].valid = __builtin_amdgcn_readfirstlane(min(16, max(0, slot.n - row)));
                 h[i].mask = 0;
                 in = row & (d.page_rows - 1);
                 if ((uint32_t)page >= (uint32_t)d.n_pages) {
@@ -460,25 +474,25 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if constexpr (D == 128) {
-                const u32x4 w = *reinterpret_cast<const u32x4*>(h[i].k + ko);
+                const u32x4 w = *reinterpret_cast<const u32x4*>(h[i].k + again(ko));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) t.codes[i][j] = w[j];
             } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(h[i].k + ko);
+                const u32x2 w = *reinterpret_cast<const u32x2*>(h[i].k + again(ko));
                 t.codes[i][0] = w[0];
                 t.codes[i][1] = w[1];
             }
-            t.scale[i] = h[i].e[eo];
+            t.scale[i] = h[i].e[again(eo)];
         }
-        if (pos) t.pos = pos[min(row + lane % kTile, slot.n - 1)];
+        if (pos) t.pos = *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(pos) + 4 * again(min(row + lane % kTile, slot.n - 1)));
     };
     uint8_t* const value_lds = reinterpret_cast<uint8_t*>(lds) + wave * kValueBytes<D>;
     const uint8_t* const value_codes = value_lds + s * (D / 2) + c * (D / 32);
     const uint8_t* const value_scales = value_lds + kTile * (D / 2) + s * (D / 32) + (D == 128 ? c / 4 : c / 8);
     auto load_values = [&](const Half (&h)[2]) __attribute__((always_inline)) {
         if constexpr (D == 128) {
-            to_lds<16, kKeep>(h[0].k + d.vc_off + lane * 16, value_lds);
-            to_lds<16, kKeep>(h[1].k + d.vc_off + lane * 16, value_lds + 1024);
+            to_lds<16, kKeep>(h[0].k + d.vc_off + again(lane * 16), value_lds);
+            to_lds<16, kKeep>(h[1].k + d.vc_off + again(lane * 16), value_lds + 1024);
             to_lds<4, kKeep>((lane & 16 ? h[1].e : h[0].e) + d.vc_off + lane % 16 * 4, value_lds + 2048);
         } else {
             to_lds<16, kKeep>((lane & 32 ? h[1].k : h[0].k) + d.vc_off + lane % 32 * 16, value_lds);
@@ -524,17 +538,26 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) z[ct][0] = z[ct][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         const float key_scale[2] = {__uint_as_float(keys.scale[0] << 23), __uint_as_float(keys.scale[1] << 23)};
+        // (the next product's queries are read while this one's are used: a wave waits for LDS once, not for each)
+        u32x4 y[2][kParts * CT];
+        auto read_queries = [&](u32x4 (&to)[kParts * CT], int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) to[p * CT + ct] = q_lds[((p * kKey + j) * CT + ct) * kWave];
+        };
+        read_queries(y[0], 0);
 #pragma unroll
         for (int j = 0; j < kKey; ++j) {
+            if (j + 1 < kKey) read_queries(y[(j + 1) & 1], j + 1);
             const u32x4 k0 = eight(keys.codes[0][j], key_scale[0]), k1 = eight(keys.codes[1][j], key_scale[1]);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 if (skipped(ct)) continue;
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p) {
-                    const u32x4 y = q_lds[((p * kKey + j) * CT + ct) * kWave];
-                    z[ct][0] = mfma(k0, y, z[ct][0]);
-                    z[ct][1] = mfma(k1, y, z[ct][1]);
+                    z[ct][0] = mfma(k0, y[j & 1][p * CT + ct], z[ct][0]);
+                    z[ct][1] = mfma(k1, y[j & 1][p * CT + ct], z[ct][1]);
                 }
             }
         }
@@ -544,17 +567,30 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         auto hidden = [&](uint32_t (&bits)[CT]) __attribute__((always_inline)) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) bits[ct] = 0;
+            const int s_of = again(s);
+            int p[8];
+            if constexpr (!kShared) {
+                if (pos) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int half = j / 4;
-                int p = row + s + (16 * half + 4 * (j % 4));
-                if constexpr (!kShared)
-                    if (pos) p = __builtin_amdgcn_ds_bpermute(4 * s + 4 * (16 * half + 4 * (j % 4)), tile_pos);
+                    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_ds_bpermute(4 * s_of + 4 * (16 * (j / 4) + 4 * (j % 4)), tile_pos);
+                } else {
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    uint32_t h = 4 * (j % 4) >= now[half].valid - s;
+                    for (int j = 0; j < 8; ++j) p[j] = row + s_of + 16 * (j / 4) + 4 * (j % 4);
+                }
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                int place = 0, from = 0;
+                if constexpr (!kShared) {
+                    place = places[16 * ct + c];
+                    from = a.window ? __builtin_elementwise_sub_sat(place, a.window - 1) : INT_MIN;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int half = j / 4;
+                    uint32_t h = 4 * (j % 4) >= now[half].valid - s_of;
                     if constexpr (kShared) h |= ~(now[half].mask >> (ct * per + part)) & 1u;
-                    else h |= (uint32_t)(p > place[ct]) | ((uint32_t)(p < from[ct]) & (uint32_t)(p >= a.sinks));
+                    else h |= (uint32_t)(p[j] > place) | ((uint32_t)(p[j] < from) & (uint32_t)(p[j] >= a.sinks));
                     bits[ct] |= h << j;
                 }
             }
@@ -584,10 +620,10 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             if (skipped(ct)) continue;
-            float top = z[ct][0][0];
-#pragma unroll
-            for (int j = 1; j < 8; ++j) top = fmaxf(top, z[ct][j / 4][j % 4]);
-            top *= a.scale2;
+            float top = max3(z[ct][0][0], z[ct][0][1], z[ct][0][2]);
+            top = max3(top, z[ct][0][3], z[ct][1][0]);
+            top = max3(top, z[ct][1][1], z[ct][1][2]);
+            top = max3(top, z[ct][1][3], z[ct][1][3]) * a.scale2;
             if (__any(top > m[ct] + kSlack)) {
                 top = rows_allmax(top);
                 const float raised = top > m[ct] + kSlack ? top : m[ct];
@@ -728,24 +764,26 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         }
     };
     // elements e .. e + 3 of column col: the weights' maximum and sum, and the sum over the rows
+    const late_args late = args_again();
     auto store = [&](int col, int e, float top, float sum, f32x4 o) __attribute__((always_inline)) {
         const int vt = col % 16 / group, h = col % 16 - vt * group;
         int sl = -1, row = 0;
         if (vt < per) slot_row(col / 16, vt, sl, row);
         if (sl < 0) return;
-        if (a.plan.chunks == 1) {
+        if (late->plan.chunks == 1) {
             o *= sum != 0.0f ? 1.0f / sum : 0.0f;
-            T* op = static_cast<T*>(a.o) + layer * a.os[0] + sl * a.os[1] + (g * group + h) * a.os[2] + row * a.os[3] + e;
+            T* op = static_cast<T*>(late->o) + layer * late->os[0] + sl * late->os[1] + (g * group + h) * late->os[2] + row * late->os[3] + e;
             if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
             else *reinterpret_cast<f32x4*>(op) = o;
         } else {
             // (a part without rows for the query is its sum, 0, alone)
-            const size_t at = ((((size_t)layer * d.batch + sl) * a.rows + row) * d.hq + g * group + h) * a.plan.chunks + chunk;
-            if (sum != 0.0f) *reinterpret_cast<f32x4*>(a.opart + at * D + e) = o;
-            if (e == 0) a.part[at] = make_float2(top, sum);
+            const size_t at = ((((size_t)layer * late->dims.batch + sl) * late->rows + row) * late->dims.hq + g * group + h) * late->plan.chunks + chunk;
+            if (sum != 0.0f) *reinterpret_cast<f32x4*>(late->opart + at * D + e) = o;
+            if (e == 0) late->part[at] = make_float2(top, sum);
         }
     };
     if constexpr (kWaves == 1) {
+        // (the barrier above: in the place of its values and queries)
         // a column tile at a time through LDS, so that a row's elements are written side by side
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
@@ -879,9 +917,12 @@ hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kStat = 2 * kWaves * CT * 16;
     static_assert(kJoined % 16 == 0 && kValues % 16 == 0 && kStat % 4 == 0, "queries are read 16 bytes at a time");
     static_assert(CT * 16 <= kQ4MostColumns, "room for the parts of outputs");
+    constexpr int kQueries = kParts * (D / 32) * CT * kWave * (int)sizeof(u32x4);
+    // (a wave by itself has no statistics, and its outputs come to the place of its queries: eight such workgroups fit a CU)
     a.stat_at = (kJoined > kValues ? kJoined : kValues) / (int)sizeof(float);
-    a.q_at = a.stat_at + kStat;
-    const size_t lds = (size_t)a.q_at * sizeof(float) + (size_t)kParts * (D / 32) * CT * kWave * sizeof(u32x4);
+    a.q_at = kWaves == 1 ? kValues / (int)sizeof(float) : a.stat_at + kStat;
+    static_assert(kWaves > 1 || kJoined <= kValues + kQueries, "outputs in the place of values and queries");
+    const size_t lds = (size_t)a.q_at * sizeof(float) + kQueries;
     auto kern = q4_query_kernel<T, D, CT, kP, kShared, kWaves>;
     if (lds > 64 * 1024) {
         static std::atomic<bool> raised[kMaxDevices];
@@ -941,7 +982,7 @@ Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows
         const int64_t seen = ((int64_t)window + sinks + p.vectors) / kTile + 3;
         tiles = tiles < seen ? tiles : seen;
     }
-    if (p.tiles == 4) p.chunks = 1;
+    if (p.tiles == 4) p.chunks = chunks_of(slabs * p.blocks, tiles / 8, 1, kQ4Units * cus_of());
     else p.chunks = chunks_of(slabs * p.blocks, tiles, kQueryWaves, 2 * cus_of());
     return p;
 }
