@@ -110,7 +110,9 @@ struct Q4QueryPlan {
     int tiles;    // column tiles of 16 in a block
     int per;      // queries in a column tile
     int vectors;  // queries in a block
+    int vector_shift;  // shared: the lowest power of two that is no fewer
     int blocks;   // blocks of a slot (window), or of the batch where its groups fill them (shared)
+    int waves;    // of a workgroup
     int chunks;   // workgroups that divide a block's rows
 };
 struct Q4QueryArgs {
@@ -133,11 +135,8 @@ struct Q4QueryArgs {
     int words;
     // shared
     const int32_t* group;    // [batch]
-    int list_pages;          // places of a slot's list
-    int4* items;             // [batch][list_pages] pages (page, rows in use, the block's queries that it is a page of, 0)
-    int32_t* lists;          // [batch] entries of each slot's list
-    int32_t* heads;          // [batch] whether a block begins with the slot
-    int32_t* members;        // [batch][vectors] the slots of the block that begins with a slot, -1 behind the last
+    int32_t* heads;          // nullable (at most 64 slots): [batch] whether a block begins with the slot
+    int32_t* members;        // likewise: [batch][vectors] the slots of the block that begins with a slot, -1 behind the last
 };
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks);
 Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max);

@@ -136,11 +136,11 @@ AttendLayout attend_layout(const Q4Dims& d, int n_max, int layer_count, bool sco
     return L;
 }
 
-// The scratch of blocks of queries after the fault word: marks or lists, and the parts of outputs that several workgroups share.
+// The scratch of blocks of queries after the fault word: marks, or the blocks of more than 64 slots, and the parts of outputs that several workgroups share.
 struct QueryLayout {
-    size_t visible_off, members_off, heads_off, lists_off, items_off, part_off, opart_off, total;
+    size_t visible_off, members_off, heads_off, part_off, opart_off, total;
 };
-QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, size_t parts) {
+QueryLayout query_layout(const Q4Dims& d, size_t mark_words, bool blocks, size_t parts) {
     QueryLayout L{};
     size_t off = kFaultBytes;
     auto take = [&](size_t bytes) {
@@ -149,11 +149,9 @@ QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, 
         return at;
     };
     L.visible_off = take(mark_words * sizeof(uint64_t));
-    if (list_pages) {
+    if (blocks) {
         L.members_off = take((size_t)d.batch * kQ4MostVectors * sizeof(int32_t));
         L.heads_off = take((size_t)d.batch * sizeof(int32_t));
-        L.lists_off = take((size_t)d.batch * sizeof(int32_t));
-        L.items_off = take((size_t)d.batch * list_pages * sizeof(int4));
     }
     L.part_off = take(parts * sizeof(float2));
     L.opart_off = take(parts * d.d * sizeof(float));
@@ -162,13 +160,13 @@ QueryLayout query_layout(const Q4Dims& d, size_t mark_words, size_t list_pages, 
 }
 size_t mark_words_of(int n_max) { return ((size_t)n_max + 2047) / 2048; }
 // Parts that a call needs, and more than any call of at most these sizes does: chunks are cut where there are fewer than kQ4Units
-// units for a CU (then units * chunks is below twice that, of at most kQ4MostColumns columns each), and have 8 tiles of 32 rows at least.
+// units for a CU (then units * chunks is below twice that, of at most kQ4MostColumns columns each), and have 4 tiles of 32 rows at least.
 size_t parts_of(const Q4Dims& d, int layer_count, int rows, int chunks) {
     return chunks > 1 ? (size_t)layer_count * d.batch * rows * d.hq * chunks : 0;
 }
 size_t most_parts(const Q4Dims& d, int n_max, int layer_count, int rows) {
     const size_t cus = device_cus() > 0 ? device_cus() : 256, by_units = 2 * kQ4Units * cus * kQ4MostColumns;
-    const size_t by_tiles = (size_t)layer_count * d.batch * rows * d.hq * (((size_t)n_max + 255) / 256);
+    const size_t by_tiles = (size_t)layer_count * d.batch * rows * d.hq * (((size_t)n_max + 127) / 128);
     return by_tiles < by_units ? by_tiles : by_units;
 }
 
@@ -226,10 +224,6 @@ void set_queries(Q4QueryArgs* a, const QueryLayout& L, void* ws) {
     constexpr double kLog2e = 1.4426950408889634;
     a->scale2 = (float)(kLog2e / sqrt((double)a->dims.d));
     char* base = static_cast<char*>(ws);
-    a->heads = reinterpret_cast<int32_t*>(base + L.heads_off);
-    a->members = reinterpret_cast<int32_t*>(base + L.members_off);
-    a->lists = reinterpret_cast<int32_t*>(base + L.lists_off);
-    a->items = reinterpret_cast<int4*>(base + L.items_off);
     a->part = reinterpret_cast<float2*>(base + L.part_off);
     a->opart = reinterpret_cast<float*>(base + L.opart_off);
     a->faults = reinterpret_cast<uint32_t*>(base);
@@ -430,7 +424,7 @@ kv_status kv_q4_window_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, 
     if (!bytes || n_max < 1 || n_max > d.cap || rows < 1 || rows > d.cap || layer_count < 1 || layer_count > shape->layers)
         return KV_ERR_INVALID_ARG;
     const int per = 16 / d.group;
-    *bytes = query_layout(d, (size_t)d.batch * ((rows + per - 1) / per) * mark_words_of(n_max), 0, most_parts(d, n_max, layer_count, rows)).total;
+    *bytes = query_layout(d, (size_t)d.batch * ((rows + per - 1) / per) * mark_words_of(n_max), false, most_parts(d, n_max, layer_count, rows)).total;
     return KV_OK;
 }
 
@@ -457,7 +451,7 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
     const size_t marks = cache->pos && a.plan.blocks > 1 ? (size_t)d.batch * a.plan.blocks * a.words : 0;
     if ((double)layer_count * d.batch * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups || (double)d.batch * a.plan.blocks * ((a.words + 3) / 4) > kMostGroups)
         return KV_ERR_UNSUPPORTED;
-    const QueryLayout L = query_layout(d, marks, 0, parts_of(d, layer_count, rows, a.plan.chunks));
+    const QueryLayout L = query_layout(d, marks, false, parts_of(d, layer_count, rows, a.plan.chunks));
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
     a.layer0 = layer0;
     a.layer_count = layer_count;
@@ -480,7 +474,7 @@ kv_status kv_q4_shared_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, 
     if (rc != KV_OK) return rc;
     const Q4Dims d = dims_of(*shape);
     if (!bytes || n_max < 1 || n_max > d.cap || layer_count < 1 || layer_count > shape->layers) return KV_ERR_INVALID_ARG;
-    *bytes = query_layout(d, 0, ((size_t)n_max + d.page_rows - 1) / d.page_rows, most_parts(d, n_max, layer_count, 1)).total;
+    *bytes = query_layout(d, 0, d.batch > 64, most_parts(d, n_max, layer_count, 1)).total;
     return KV_OK;
 }
 
@@ -500,8 +494,7 @@ kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.cache = cache_of(*cache);
     a.plan = q4_shared_plan(d, layer_count, n_max);
     if ((double)layer_count * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups) return KV_ERR_UNSUPPORTED;
-    a.list_pages = (n_max + d.page_rows - 1) / d.page_rows;
-    const QueryLayout L = query_layout(d, 0, a.list_pages, parts_of(d, layer_count, 1, a.plan.chunks));
+    const QueryLayout L = query_layout(d, 0, d.batch > 64, parts_of(d, layer_count, 1, a.plan.chunks));
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;
     a.layer0 = layer0;
     a.layer_count = layer_count;
@@ -514,6 +507,10 @@ kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.rows = 1;
     a.group = group;
     set_queries(&a, L, ws);
+    if (d.batch > 64) {
+        a.heads = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + L.heads_off);
+        a.members = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + L.members_off);
+    }
     return hip_status(launch_q4_shared(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -12,8 +12,8 @@
 //
 // Which tiles: without positions the rows are in order, and the tiles of a window are two runs.  With positions (an eviction leaves
 // rows of any position in any place) a kernel before this one marks the tiles of which a block sees any row, a bit each; a wave
-// holds a word per lane and finds its k-th tile by their counts.  Shared: a kernel before this one lists, for every slot of a block,
-// the pages that no slot before it in the block has, with the queries that each is a page of.
+// looks at 64 of its tiles at a time, one a lane.  Shared: a lane looks at a tile of one slot, and at the table entries of the block's
+// other slots there.
 //
 // Masked rows get the logit -inf.  A masked row's values may be NaN (a block stored from infinities); 0 times them would spoil the
 // column, so tiles that hold such blocks take a side path: the blocks are taken as numbers, and a product of two 0/1 matrices finds
@@ -36,16 +36,6 @@ constexpr int kAlone = 768;  // blocks of four column tiles from which a wave ta
 constexpr int kKeep = 0;  // rows are read again by other workgroups
 constexpr float kNaN = __builtin_nanf("");
 
-typedef int __attribute__((ext_vector_type(4))) i32x4;
-typedef const __attribute__((address_space(4))) i32x4* scalar_int4s;
-
-// The kernel's arguments read where they are used, not kept from its beginning on (in spilled scalar registers).
-typedef const __attribute__((address_space(4))) Q4QueryArgs* late_args;
-__device__ __forceinline__ late_args args_again() {
-    late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(p));
-    return p;
-}
 // A lane's offset, widened where it is used: an address is a scalar base and a 32-bit offset then.
 __device__ __forceinline__ uint32_t again(uint32_t x) {
     asm volatile("" : "+v"(x));
@@ -122,87 +112,42 @@ __global__ __launch_bounds__(kMarkWaves* kWave) void q4_mark_kernel(Q4QueryArgs 
     if (lane == 0) a.visible[((size_t)b * a.plan.blocks + block) * a.words + word] = bits;
 }
 
-// Shared: the block that each slot is in, and the slot's list of pages.  One workgroup per slot.
-constexpr int kListThreads = 256;
-__global__ __launch_bounds__(kListThreads) void q4_list_kernel(Q4QueryArgs a) {
-    __shared__ int members[kQ4MostVectors], lens[kQ4MostVectors], info[2];
-    __shared__ int sums[kListThreads / kWave];
+// Shared, more than 64 slots: the slots of a group in ascending order are cut into blocks of `vectors`; whether a slot begins one,
+// and the slots of that.  One wave per slot.
+__global__ __launch_bounds__(kWave) void q4_block_kernel(Q4QueryArgs a) {
+    __shared__ int members[kQ4MostVectors];
     const Q4Dims& d = a.dims;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, b = blockIdx.x, V = a.plan.vectors;
-    const int mine = a.group[b];
-    // The slots of the group in ascending order are cut into blocks of V; `members` holds the block of slot b.
-    if (wave == 0) {
-        int seen = 0, rank = -1;  // slots of the group so far, and those before b
-        for (int i0 = 0; i0 < d.batch; i0 += kWave) {
-            const int i = i0 + lane;
-            const bool same = i < d.batch && a.group[i] == mine;
-            const uint64_t all = __ballot(same);
-            const int r = seen + __popcll(all & ((1ull << lane) - 1));
-            seen += __popcll(all);
-            if (i0 <= b && b < i0 + kWave) rank = __builtin_amdgcn_readlane(r, b - i0);
-            // (before b is found: the last V, which are those that b's block can have)
-            if (same && (rank < 0 ? r >= seen - V : r / V == rank / V)) members[r % V] = i;
-            if (rank >= 0 && seen >= (rank / V + 1) * V) break;
+    const int lane = threadIdx.x, b = blockIdx.x, V = a.plan.vectors, mine = a.group[b];
+    int seen = 0, rank = -1;  // slots of the group so far, and those before b
+    for (int i0 = 0; i0 < d.batch; i0 += kWave) {
+        const int i = i0 + lane;
+        const bool same = i < d.batch && a.group[i] == mine;
+        const uint64_t all = __ballot(same);
+        const int r = seen + __popcll(all & ((1ull << lane) - 1));
+        seen += __popcll(all);
+        if (i0 <= b && b < i0 + kWave) {
+            rank = __builtin_amdgcn_readlane(r, b - i0);
+            if (rank % V) break;
         }
-        if (lane == 0) {
-            info[0] = rank % V;
-            info[1] = min(V, seen - rank / V * V);
-        }
+        if (same && rank >= 0 && r >= rank && r < rank + V) members[r - rank] = i;
+        if (rank >= 0 && seen >= rank + V) break;
     }
+    const bool head = rank % V == 0;
     __syncthreads();
-    const int k = info[0], count = info[1];
-    if ((int)threadIdx.x < count) {
-        const int n = a.cache.len[members[threadIdx.x]];
-        lens[threadIdx.x] = n < 0 || n > a.n_max ? 0 : n;
-        if ((int)threadIdx.x == k && lens[k] != n) atomicOr(a.faults, kFaultCache);
-    }
-    if (k == 0 && (int)threadIdx.x < V) a.members[(size_t)b * V + threadIdx.x] = (int)threadIdx.x < count ? members[threadIdx.x] : -1;
-    if (threadIdx.x == 0) a.heads[b] = k == 0;
-    __syncthreads();
-    const int pages = (lens[k] + d.page_rows - 1) >> d.page_shift;
-    int done = 0;
-    for (int j0 = 0; j0 < pages; j0 += kListThreads) {
-        const int j = j0 + (int)threadIdx.x;
-        uint32_t mask = 0;
-        int page = 0, rows = 0;
-        if (j < pages) {
-            page = a.cache.table[(size_t)b * d.max_pages + j];
-            rows = min(d.page_rows, lens[k] - (j << d.page_shift));
-            if ((uint32_t)page >= (uint32_t)d.n_pages) {
-                atomicOr(a.faults, kFaultCache);
-            } else {
-                for (int m = 0; m < count; ++m) {
-                    const int left = lens[m] - (j << d.page_shift);
-                    if (left > 0 && min(d.page_rows, left) == rows && a.cache.table[(size_t)members[m] * d.max_pages + j] == page) mask |= 1u << m;
-                }
-            }
-        }
-        const bool listed = mask && __builtin_ctz(mask) == k;  // (the first slot that has it lists it)
-        const uint64_t all = __ballot(listed);
-        if (lane == 0) sums[wave] = __popcll(all);
-        __syncthreads();
-        int at = done + __popcll(all & ((1ull << lane) - 1));
-        for (int w = 0; w < kListThreads / kWave; ++w) {
-            if (w < wave) at += sums[w];
-            done += sums[w];
-        }
-        if (listed) a.items[(size_t)b * a.list_pages + at] = make_int4(page, rows, (int)mask, 0);
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) a.lists[b] = done;
+    if (lane == 0) a.heads[b] = head;
+    if (head && lane < V) a.members[(size_t)b * V + lane] = lane < seen - rank ? members[lane] : -1;
 }
 
-// A tile that is to be loaded: its halves' pages and what is known of them before their rows are.
+// A tile that is to be loaded: its first row, how many of its rows there are, its halves' pages, and (shared) the queries of the block
+// that see it.
 struct Ref {
-    int row;  // window: its first row; shared: the first row in the page
-    int page[2], rows[2];
-    uint32_t mask[2];
+    int row, rows, page[2];
+    uint32_t mask;
 };
 struct Half {
     const uint8_t* k;  // the half's first row: keys' codes, ...
     const uint8_t* e;  // ... scales, and the values' of both vc_off bytes on
     int valid;         // rows that take part
-    uint32_t mask;     // shared: queries of the block that it is a half of
 };
 template <int D>
 struct KeyTile {
@@ -214,7 +159,7 @@ struct KeyTile {
 // Column tiles (CT) of 16; parts of a probability (kP): 3 take all of its 24 bits, 1 rounds it to bf16 (8 bits, to nearest; its
 // sum is of the rounded numbers).  kWaves: of a workgroup, which divide a block's tiles and join their outputs; or one.
 template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
-__global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kernel(Q4QueryArgs a) {
+__global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void q4_query_kernel(Q4QueryArgs a) {
     constexpr int kThreads = kWave * kWaves;
     constexpr int kKey = D / 32, kOut = D / 16;     // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;  // bf16 parts of a query
@@ -225,19 +170,26 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
     const Q4Dims& d = a.dims;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int group = d.group, per = a.plan.per;
+    // The arguments that only the later batches of tiles and the end need, in LDS: in scalar registers they would be spilled, and a
+    // scalar load of an argument in the middle of the kernel takes 1.5 us (arguments lie in host memory).
+    constexpr int kArgWords = sizeof(Q4QueryArgs) / 4;
+    __shared__ __align__(16) uint32_t arg_words[kArgWords];
+    static_assert(sizeof(Q4QueryArgs) % 4 == 0, "copied by words");
+    for (int i = threadIdx.x; i < kArgWords; i += kThreads) arg_words[i] = ((const uint32_t*)__builtin_amdgcn_kernarg_segment_ptr())[i];
+    const Q4QueryArgs& late = *reinterpret_cast<const Q4QueryArgs*>(arg_words);
 
-    // unit: KV heads fastest (eight of them fall on the eight XCDs), then the blocks, the last (a window's longest) first
+    // unit: KV heads fastest (eight of them fall on the eight XCDs); then a window's blocks, the last, its longest, first.  Shared: the
+    // blocks slowest, since there may be fewer of them.
     uint32_t x = blockIdx.x;
-    const int g = x % (uint32_t)d.hkv;
-    x /= (uint32_t)d.hkv;
-    const int nth = x % (uint32_t)a.plan.blocks;
-    x /= (uint32_t)a.plan.blocks;
-    int b = 0;
-    if constexpr (!kShared) {
-        b = x % (uint32_t)d.batch;
-        x /= (uint32_t)d.batch;
-    }
-    const int layer = x % (uint32_t)a.layer_count, chunk = x / (uint32_t)a.layer_count;
+    auto take = [&](int n) __attribute__((always_inline)) {
+        const int i = x % (uint32_t)n;
+        x /= (uint32_t)n;
+        return i;
+    };
+    const int g = take(d.hkv);
+    int nth = kShared ? 0 : take(a.plan.blocks), b = kShared ? 0 : take(d.batch);
+    const int layer = take(a.layer_count), chunk = take(a.plan.chunks);
+    if constexpr (kShared) nth = x;
     const size_t page_bytes = (size_t)d.hkv * d.rec;
     const int step = a.plan.chunks * kWaves, k0 = chunk * kWaves + wave;
     uint32_t fault = 0;
@@ -248,21 +200,105 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
     if constexpr (kShared) asm volatile("" : "+v"(lane));  // (nothing of a lane is worked out before the loop and kept over it)
     const int c = lane % 16, s = lane / 16, part = c / group, head = c - part * group;
     const uint8_t* const pool = a.cache.pool + q4_record(d, a.layer0 + layer, 0, g);
+    // shared: the block's slots (-1: none) and their rows
+    __shared__ int member_of[kShared ? kQ4MostVectors : 1], rows_of[kShared ? kQ4MostVectors : 1];
     if constexpr (kShared) {
-        // the slot that the block begins with
-        b = -1;
-        int seen = 0;
-        for (int i0 = 0; i0 < d.batch && b < 0; i0 += kWave) {
-            const uint64_t is = __ballot(i0 + lane < d.batch && a.heads[min(i0 + lane, d.batch - 1)]);
-            const uint64_t it = __ballot((is >> lane & 1) && seen + __popcll(is & ((1ull << lane) - 1)) == turn);
-            if (it) b = i0 + __builtin_ctzll(it);
-            seen += __popcll(is);
+        const int V = a.plan.vectors;
+        if (wave == 0) {
+            int at = lane < V ? lane : -1, it = -1;  // the lane's slot `it` is the block's query `at`
+            if (a.heads) {
+                int seen = 0;
+                b = -1;
+                for (int i0 = 0; i0 < d.batch && b < 0; i0 += kWave) {
+                    const uint64_t is = __ballot(i0 + lane < d.batch && a.heads[min(i0 + lane, d.batch - 1)]);
+                    const uint64_t found = __ballot((is >> lane & 1) && seen + __popcll(is & ((1ull << lane) - 1)) == turn);
+                    if (found) b = i0 + __builtin_ctzll(found);
+                    seen += __popcll(is);
+                }
+                if (b >= 0 && lane < V) it = a.members[(size_t)b * V + lane];
+            } else {
+                // up to 64 slots, one a lane: as q4_block_kernel
+                it = min(lane, d.batch - 1);
+                const int mine = a.group[it];
+                int rank = 0;
+                for (int j = 0; j < d.batch; ++j) rank += (int)(__builtin_amdgcn_readlane(mine, j) == mine) & (int)(j < lane);
+                const bool is = lane < d.batch;
+                const uint64_t heads = __ballot(is && rank % V == 0);
+                const uint64_t found = __ballot((heads >> lane & 1) && __popcll(heads & ((1ull << lane) - 1)) == turn);
+                if (lane < V) member_of[lane] = -1;
+                at = -1;
+                if (found) {
+                    const int begin = __builtin_ctzll(found), r = rank - __builtin_amdgcn_readlane(rank, begin);
+                    if (is && mine == __builtin_amdgcn_readlane(mine, begin) && r >= 0 && r < V) at = r;
+                }
+            }
+            const int raw = it >= 0 ? a.cache.len[it] : 0;
+            if (at >= 0) {
+                const bool bad = raw < 0 || raw > a.n_max;
+                member_of[at] = it;
+                rows_of[at] = bad ? 0 : raw;
+                if (bad && layer == 0 && g == 0 && chunk == 0) atomicOr(a.faults, kFaultCache);
+            }
         }
-        if (b < 0) break;
+        __syncthreads();
+        if (member_of[0] < 0) break;
     }
     // the block's queries: the lane's in each column tile, its slot and row (-1: none)
-    const int32_t* const members = kShared ? a.members + (size_t)b * a.plan.vectors : nullptr;
     const int block = kShared ? 0 : a.plan.blocks - 1 - nth, v0 = block * a.plan.vectors;
+    // The wave's tiles are those of numbers k0, k0 + step, ...  It looks at 64 of them at a time, one a lane: the pages of the lane's tile,
+    // and a bit for each that takes part.
+    // Shared: a lane looks at one tile of one of the block's slots.  Where several name the same pages there, and as many rows, the first
+    // of them has the tile for all.  The later slots' tiles are dealt from other waves on, so that those that only they have (behind a
+    // prompt, say) do not meet in the waves that have the prompt's last tiles.
+    constexpr int kTogether = 8;
+    const int at_once = kShared ? kWave >> a.plan.vector_shift : kWave;
+    const int32_t* const pos = kShared || !a.cache.pos ? nullptr : a.cache.pos + (size_t)b * d.cap;
+    int run = 0;            // shared: tiles of a wave
+    uint32_t all = 0;       // shared: every query of the block
+    if constexpr (kShared) {
+        const int V = a.plan.vectors, sl = lane < V ? member_of[lane] : -1, n = sl >= 0 ? rows_of[min(lane, V - 1)] : 0;
+        all = (uint32_t)__ballot(sl >= 0);
+        run = ((__builtin_amdgcn_readfirstlane(wave_max_int(n)) + kTile - 1) / kTile + step - 1) / step;
+    }
+    // (of a lane's tile: the pages of its halves; shared: its first row and rows, and the queries that see it)
+    int page_of = 0, page_of2 = 0, row_of = 0, rows_in = 0, held[kTogether];
+    uint32_t mask_of = 0;
+    uint64_t left = 0, word = 0;
+    int base = 0;
+    const int how = kShared || !pos ? 0 : a.visible ? 1 : 2;  // window: how tiles are found, by row numbers, marks or positions
+    auto load_entries = [&](const Q4QueryArgs& a, int row, int v0, int (&to)[kTogether]) __attribute__((always_inline)) {  // shared: of the block's slots v0 ... at a row
+        const int entries = a.dims.max_pages, V = a.plan.vectors, at = row >> a.dims.page_shift;
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) to[i] = a.cache.table[(size_t)max(member_of[min(v0 + i, V - 1)], 0) * entries + at];
+    };
+    auto load_look = [&](const Q4QueryArgs& a) __attribute__((always_inline)) {
+        int lane = threadIdx.x % kWave;
+        asm volatile("" : "+v"(lane));  // (its places are worked out here, not kept over the tiles)
+        const int last = a.dims.cap - 1, shift = a.dims.page_shift;
+        if constexpr (kShared) {
+            const int V = a.plan.vectors, own = lane & ((1 << a.plan.vector_shift) - 1), i = lane >> a.plan.vector_shift;
+            const int wave_of = k0 + min(own, V - 1) * max(1, step / V);
+            const int row = min(((wave_of < step ? wave_of : wave_of % step) + (base + i) * step) * kTile, last);
+            row_of = row;
+            rows_in = own < V && base + i < run && member_of[min(own, V - 1)] >= 0 ? min(kTile, rows_of[min(own, V - 1)] - row) : 0;
+            const int32_t* const entry = a.cache.table + (size_t)(own < V ? max(member_of[own], 0) : 0) * a.dims.max_pages;
+            page_of = entry[row >> shift];
+            page_of2 = entry[min(row + 16, last) >> shift];
+            load_entries(a, row, 0, held);
+        } else {
+            const int k = k0 + (base + lane) * step, row = min(k * kTile, last);  // (2^27 rows are 2^22 tiles, and 64 steps fewer than 2^25)
+            const int32_t* const entry = a.cache.table + (size_t)b * a.dims.max_pages;
+            page_of = entry[row >> shift];
+            page_of2 = entry[min(row + 16, last) >> shift];
+            if (how == 1) {
+                word = a.visible[((size_t)b * a.plan.blocks + block) * a.words + min(k / 64, a.words - 1)];
+            } else if (how == 2) {  // two tiles to a load
+#pragma unroll
+                for (int i = 0; i < kTogether; ++i) held[i] = pos[min((k0 + (base + 2 * i + lane / kTile) * step) * kTile + lane % kTile, last)];
+            }
+        }
+    };
+    load_look(a);  // (on their way while the queries are)
     Slot slot{0, 0, false};
     if constexpr (!kShared) {
         slot = slot_of(a, b);
@@ -274,7 +310,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         sl = b;
         row = 0;
         if constexpr (kShared) {
-            sl = members[v];
+            sl = member_of[v];
         } else {
             row = v0 + v;
             if (row >= slot.count) sl = -1;
@@ -309,8 +345,8 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         int sl = -1, row = 0;
         if (part < per) slot_row(ct, part, sl, row);
         // (no query: any row, not used)
-        const T* qp = static_cast<const T*>(a.q) + s * (D / 4);
-        if (sl >= 0) qp += layer * a.qs[0] + sl * a.qs[1] + (g * group + head) * a.qs[2] + row * a.qs[3];
+        const int64_t at = layer * a.qs[0] + max(sl, 0) * a.qs[1] + (g * group + (sl < 0 ? 0 : head)) * a.qs[2] + (sl < 0 ? 0 : row) * a.qs[3];
+        const T* const qp = static_cast<const T*>(a.q) + at + s * (D / 4);
         if constexpr (kParts == 1) {
 #pragma unroll
             for (int j = 0; j < kKey; ++j) {
@@ -340,82 +376,47 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         }
     }
 
-    // The wave's tiles are those of numbers k0, k0 + step, ... of `tiles`.  It looks at 64 of them at a time, one a lane: the pages (or
-    // listed pages) of the lane's tile, and a bit for each that takes part.
-    int tiles = 0;
-    uint32_t all = 0;                              // shared: every query of the block
-    int items = 0;                                 // shared: pages that the block's slots list
-    __shared__ int list_slot[kShared ? kQ4MostVectors : 1], list_before[kShared ? kQ4MostVectors : 1];  // a member, and pages that those before it list
-    const int per_page_shift = kShared ? max(0, d.page_shift - 5) : 0;
-    if constexpr (kShared) {
-        const int m = lane < a.plan.vectors ? members[lane] : -1;
-        int sum = m >= 0 ? a.lists[m] : 0;
-        const int mine = sum;
-#pragma unroll
-        for (int o = 1; o < kQ4MostVectors; o <<= 1) {
-            const int up = __shfl_up(sum, o, kWave);
-            if (lane >= o) sum += up;
-        }
-        if (wave == 0 && lane < a.plan.vectors) {
-            list_slot[lane] = max(m, 0);
-            list_before[lane] = sum - mine;
-        }
-        items = __builtin_amdgcn_readlane(sum, kQ4MostVectors - 1);
-        all = (uint32_t)__ballot(m >= 0);
-        tiles = d.page_rows >= kTile ? items << per_page_shift : (items + 1) / 2;
-    } else {
-        tiles = (slot.n + kTile - 1) / kTile;
-    }
     const int top_from = lower_bound_of(top_place, a.window), low_from = lower_bound_of(low_place, a.window);
-    const int32_t* const pos = kShared || !a.cache.pos ? nullptr : a.cache.pos + (size_t)b * d.cap;
-    int page_of = 0, page_of2 = 0;  // window: pages of the halves; shared: the listed page, its rows in use and its queries (pages of 16
-    uint32_t mask_of = 0;           // rows: lanes 32 .. 63 hold the second halves of lanes 0 .. 31's tiles)
-    uint64_t left = 0;
-    int base = 0;
-    const bool pairs = kShared && d.page_rows < kTile;
-    const int at_once = pairs ? kWave / 2 : kWave;
+    const int tiles = kShared ? 0 : (slot.n + kTile - 1) / kTile;
     auto look = [&]() __attribute__((always_inline)) {
         int lane = threadIdx.x % kWave;
-        asm volatile("" : "+v"(lane));  // (its places are worked out here, not kept over the tiles)
-        const late_args late = args_again();
-        const int k = k0 + (base + (pairs ? lane % (kWave / 2) : lane)) * step;  // (2^27 rows are 2^22 tiles, and 64 steps fewer than 2^25)
-        bool part_of = k < tiles;
+        asm volatile("" : "+v"(lane));
+        bool part_of;
         if constexpr (kShared) {
-            const int i = pairs ? 2 * k + lane / (kWave / 2) : k >> per_page_shift;
-            int before = 0, sl = 0;
-            for (int v = 0; v < late->plan.vectors; ++v) {  // the last member that has as many before it: it lists the page
-                const int y = list_before[v], z = list_slot[v];
-                before = y <= i ? y : before;
-                sl = y <= i ? z : sl;
-            }
-            int4 it = make_int4(0, 0, 0, 0);
-            if (part_of && i < items) it = late->items[(size_t)sl * late->list_pages + (i - before)];
-            page_of = it.x;
-            page_of2 = it.y;
-            mask_of = it.z;
-            if (pairs) part_of = part_of && lane < kWave / 2;
-        } else {
-            const int row = k * kTile;
-            const int32_t* const table = late->cache.table + (size_t)b * late->dims.max_pages;
-            const int last = late->dims.cap - 1;
-            page_of = table[min(row, last) >> late->dims.page_shift];
-            page_of2 = table[min(row + 16, last) >> late->dims.page_shift];
-            if (!pos) {
-                part_of = part_of && row <= top_place && (row + kTile > low_from || row < a.sinks);
-            } else if (late->visible) {
-                part_of = part_of && (late->visible[((size_t)b * late->plan.blocks + block) * late->words + k / 64] >> k % 64 & 1);
-            } else {
-                // two tiles to a load, eight loads together
-                uint64_t bits = 0;
-                constexpr int kTogether = 8;
-                for (int i0 = 0; i0 < kWave && k0 + (base + i0) * step < tiles; i0 += 2 * kTogether) {
-                    int p[kTogether];
+            const int V = late.plan.vectors, own = lane & ((1 << late.plan.vector_shift) - 1);
+            const bool pairs = late.dims.page_rows < kTile;
+            mask_of = 0;
+            for (int v0 = 0; v0 < V; v0 += kTogether) {
+                if (v0) load_entries(late, row_of, v0, held);
+                int second[kTogether];
+                if (pairs) load_entries(late, min(row_of + 16, late.dims.cap - 1), v0, second);
 #pragma unroll
-                    for (int i = 0; i < kTogether; ++i) p[i] = pos[min((k0 + (base + i0 + 2 * i + lane / kTile) * step) * kTile + lane % kTile, last)];
+                for (int i = 0; i < kTogether; ++i) {
+                    const int v = min(v0 + i, V - 1);
+                    const bool same = held[i] == page_of && (!pairs || rows_in <= 16 || second[i] == page_of2) && member_of[v] >= 0 &&
+                                      min(kTile, rows_of[v] - row_of) == rows_in;
+                    mask_of |= (uint32_t)same << v;
+                }
+            }
+            part_of = rows_in > 0 && __builtin_ctz(mask_of) == own;
+        } else {
+            const int k = k0 + (base + lane) * step, row = k * kTile;
+            part_of = k < tiles;
+            if (how == 0) {
+                part_of = part_of && row <= top_place && (row + kTile > low_from || row < a.sinks);
+            } else if (how == 1) {
+                part_of = part_of && (word >> k % 64 & 1);
+            } else {
+                uint64_t bits = 0;
+                for (int i0 = 0; i0 < kWave && k0 + (base + i0) * step < tiles; i0 += 2 * kTogether) {
+                    const int last = late.dims.cap - 1;
+#pragma unroll
+                    for (int i = 0; i < kTogether; ++i)
+                        if (i0) held[i] = pos[min((k0 + (base + i0 + 2 * i + lane / kTile) * step) * kTile + lane % kTile, last)];
 #pragma unroll
                     for (int i = 0; i < kTogether; ++i) {
                         const int r = (k0 + (base + i0 + 2 * i + lane / kTile) * step) * kTile + lane % kTile;
-                        const uint64_t any = __ballot(r < slot.n && p[i] <= top_place && (p[i] >= low_from || p[i] < a.sinks));
+                        const uint64_t any = __ballot(r < slot.n && held[i] <= top_place && (held[i] >= low_from || held[i] < a.sinks));
                         bits |= (uint64_t)((uint32_t)any != 0) << (i0 + 2 * i) | (uint64_t)((any >> 32) != 0) << (i0 + 2 * i + 1);
                     }
                 }
@@ -427,42 +428,30 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
     // the next tile of them that takes part
     auto fetch = [&](Ref& r) __attribute__((always_inline)) {
         if (!left) return false;
-        const int i = __builtin_ctzll(left), k = k0 + (base + i) * step;
+        const int i = __builtin_ctzll(left);
         left &= left - 1;
+        r.page[0] = __builtin_amdgcn_readlane(page_of, i);
+        r.page[1] = __builtin_amdgcn_readlane(page_of2, i);
         if constexpr (kShared) {
-            r.row = (k & ((1 << per_page_shift) - 1)) * kTile;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int from_lane = pairs && h ? i + kWave / 2 : i;
-                r.page[h] = __builtin_amdgcn_readlane(page_of, from_lane);
-                r.rows[h] = __builtin_amdgcn_readlane(page_of2, from_lane) - (pairs ? 0 : r.row + 16 * h);
-                r.mask[h] = __builtin_amdgcn_readlane(mask_of, from_lane);
-            }
+            r.row = __builtin_amdgcn_readlane(row_of, i);
+            r.rows = __builtin_amdgcn_readlane(rows_in, i);
+            r.mask = __builtin_amdgcn_readlane(mask_of, i);
         } else {
-            r.row = k * kTile;
-            r.page[0] = __builtin_amdgcn_readlane(page_of, i);
-            r.page[1] = __builtin_amdgcn_readlane(page_of2, i);
+            r.row = (k0 + (base + i) * step) * kTile;
+            r.rows = slot.n - r.row;
         }
         return true;
     };
     auto locate = [&](const Ref& r, Half (&h)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            int page = r.page[i], in;
-            if constexpr (kShared) {
-                h[i].valid = __builtin_amdgcn_readfirstlane(min(16, max(0, r.rows[i])));
-                h[i].mask = h[i].valid ? r.mask[i] : 0;
-                in = d.page_rows >= kTile ? r.row + 16 * i : 0;
-            } else {
-                const int row = r.row + 16 * i;
-                h[i].valid = __builtin_amdgcn_readfirstlane(min(16, max(0, slot.n - row)));
-                h[i].mask = 0;
-                in = row & (d.page_rows - 1);
-                if ((uint32_t)page >= (uint32_t)d.n_pages) {
-                    if (h[i].valid) fault = kFaultCache;
-                    page = h[i].valid = 0;
-                }
+            int page = r.page[i];
+            h[i].valid = __builtin_amdgcn_readfirstlane(min(16, max(0, r.rows - 16 * i)));
+            if ((uint32_t)page >= (uint32_t)d.n_pages) {
+                if (h[i].valid) fault = kFaultCache;
+                page = h[i].valid = 0;
             }
+            const int in = (r.row + 16 * i) & (d.page_rows - 1);
             const uint8_t* rec = pool + (size_t)(uint32_t)page * page_bytes;
             h[i].k = rec + in * (D / 2);
             h[i].e = rec + d.ks_off + in * (D / 32);
@@ -512,7 +501,8 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
     __syncthreads();
 
     // Loads run one tile ahead (but for the first of 64).
-   for (; k0 + base * step < tiles; base += at_once) {
+   if (kShared ? run > 0 : k0 < tiles)
+   for (;;) {
     look();
     KeyTile<D> keys;
     Half now[2], next[2];
@@ -529,7 +519,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         const int row = ref.row;
         const bool whole = now[0].valid + now[1].valid == kTile;
         uint32_t active = ~0u;  // shared: column tiles with a query that the tile is a tile of
-        if constexpr (kShared && CT > 1) active = now[0].mask | now[1].mask;
+        if constexpr (kShared && CT > 1) active = ref.mask;
         auto skipped = [&](int ct) __attribute__((always_inline)) {
             return kShared && CT > 1 && !(active >> (ct * per) & ((1u << per) - 1));
         };
@@ -589,7 +579,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
                 for (int j = 0; j < 8; ++j) {
                     const int half = j / 4;
                     uint32_t h = 4 * (j % 4) >= now[half].valid - s_of;
-                    if constexpr (kShared) h |= ~(now[half].mask >> (ct * per + part)) & 1u;
+                    if constexpr (kShared) h |= ~(ref.mask >> (ct * per + part)) & 1u;
                     else h |= (uint32_t)(p[j] > place) | ((uint32_t)(p[j] < from) & (uint32_t)(p[j] >= a.sinks));
                     bits[ct] |= h << j;
                 }
@@ -597,7 +587,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         };
         bool plain = whole;  // every column sees every row
         if constexpr (kShared) {
-            plain = plain && (now[0].mask & now[1].mask) == all;
+            plain = plain && ref.mask == all;
         } else {
             const int p = pos ? tile_pos : row + lane % kTile;
             plain = plain && __all(p <= low_place && (p >= top_from || p < a.sinks));
@@ -741,6 +731,9 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
             more = fetch(ahead);
         }
     }
+    base += at_once;
+    if (kShared ? base >= run : k0 + base * step >= tiles) break;
+    load_look(late);
    }
     // the waves joined: the upper half into the lower, those through columns of LDS
     constexpr int kColumns = CT * 16;
@@ -764,41 +757,53 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : 2) void q4_query_kerne
         }
     };
     // elements e .. e + 3 of column col: the weights' maximum and sum, and the sum over the rows
-    const late_args late = args_again();
     auto store = [&](int col, int e, float top, float sum, f32x4 o) __attribute__((always_inline)) {
         const int vt = col % 16 / group, h = col % 16 - vt * group;
         int sl = -1, row = 0;
         if (vt < per) slot_row(col / 16, vt, sl, row);
         if (sl < 0) return;
-        if (late->plan.chunks == 1) {
+        if (late.plan.chunks == 1) {
             o *= sum != 0.0f ? 1.0f / sum : 0.0f;
-            T* op = static_cast<T*>(late->o) + layer * late->os[0] + sl * late->os[1] + (g * group + h) * late->os[2] + row * late->os[3] + e;
+            T* op = static_cast<T*>(late.o) + layer * late.os[0] + sl * late.os[1] + (g * group + h) * late.os[2] + row * late.os[3] + e;
             if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
             else *reinterpret_cast<f32x4*>(op) = o;
         } else {
             // (a part without rows for the query is its sum, 0, alone)
-            const size_t at = ((((size_t)layer * late->dims.batch + sl) * late->rows + row) * late->dims.hq + g * group + h) * late->plan.chunks + chunk;
-            if (sum != 0.0f) *reinterpret_cast<f32x4*>(late->opart + at * D + e) = o;
-            if (e == 0) late->part[at] = make_float2(top, sum);
+            const size_t at = ((((size_t)layer * late.dims.batch + sl) * late.rows + row) * late.dims.hq + g * group + h) * late.plan.chunks + chunk;
+            if (sum != 0.0f) *reinterpret_cast<f32x4*>(late.opart + at * D + e) = o;
+            if (e == 0) late.part[at] = make_float2(top, sum);
         }
     };
     if constexpr (kWaves == 1) {
-        // (the barrier above: in the place of its values and queries)
-        // a column tile at a time through LDS, so that a row's elements are written side by side
+        // a lane has D / 4 consecutive elements of a column
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            float* const place_of = lds + c * kStride + s * (D / 4);
+            int sl = -1, row = 0;
+            if (part < per) slot_row(ct, part, sl, row);
+            if (sl < 0) continue;
+            if (late.plan.chunks == 1) {
+                const float inv = l[ct] != 0.0f ? 1.0f / l[ct] : 0.0f;
+                T* const op = static_cast<T*>(late.o) + layer * late.os[0] + sl * late.os[1] + (g * group + head) * late.os[2] + row * late.os[3] + s * (D / 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < kOut; e += 4)
-                    *reinterpret_cast<f32x4*>(place_of + i * kOut + e) = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
-            __syncthreads();
-            for (int i = lane; i < 16 * (D / 4); i += kWave) {
-                const int col = i / (D / 4), e = i % (D / 4) * 4;
-                store(16 * ct + col, e, __shfl(m[ct], col, kWave), __shfl(l[ct], col, kWave), *reinterpret_cast<const f32x4*>(lds + col * kStride + e));
+                    for (int e = 0; e < kOut; e += 4) {
+                        const f32x4 o = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]} * inv;
+                        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op + i * kOut + e) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
+                        else *reinterpret_cast<f32x4*>(op + i * kOut + e) = o;
+                    }
+            } else {
+                const size_t at = ((((size_t)layer * late.dims.batch + sl) * late.rows + row) * late.dims.hq + g * group + head) * late.plan.chunks + chunk;
+                if (s == 0) late.part[at] = make_float2(m[ct], l[ct]);
+                if (l[ct] != 0.0f) {
+                    float* const op = late.opart + at * D + s * (D / 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < kOut; e += 4)
+                            *reinterpret_cast<f32x4*>(op + i * kOut + e) = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
+                }
             }
-            __syncthreads();
         }
     } else {
         if (wave >= kJoin) put();
@@ -913,15 +918,14 @@ __global__ __launch_bounds__(kPartThreads) void q4_part_kernel(Q4QueryArgs a, in
 
 template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
 hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
-    constexpr int kJoined = (kWaves + 1) / 2 * (kWaves > 1 ? CT : 1) * 16 * (D + 4) * (int)sizeof(float), kValues = kWaves * kValueBytes<D>;
+    constexpr int kJoined = kWaves / 2 * CT * 16 * (D + 4) * (int)sizeof(float), kValues = kWaves * kValueBytes<D>;
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kStat = 2 * kWaves * CT * 16;
     static_assert(kJoined % 16 == 0 && kValues % 16 == 0 && kStat % 4 == 0, "queries are read 16 bytes at a time");
     static_assert(CT * 16 <= kQ4MostColumns, "room for the parts of outputs");
     constexpr int kQueries = kParts * (D / 32) * CT * kWave * (int)sizeof(u32x4);
-    // (a wave by itself has no statistics, and its outputs come to the place of its queries: eight such workgroups fit a CU)
-    a.stat_at = (kJoined > kValues ? kJoined : kValues) / (int)sizeof(float);
-    a.q_at = kWaves == 1 ? kValues / (int)sizeof(float) : a.stat_at + kStat;
-    static_assert(kWaves > 1 || kJoined <= kValues + kQueries, "outputs in the place of values and queries");
+    // (a wave by itself joins nothing: eight such workgroups fit a CU)
+    a.stat_at = (kWaves > 1 && kJoined > kValues ? kJoined : kValues) / (int)sizeof(float);
+    a.q_at = a.stat_at + (kWaves > 1 ? kStat : 0);
     const size_t lds = (size_t)a.q_at * sizeof(float) + kQueries;
     auto kern = q4_query_kernel<T, D, CT, kP, kShared, kWaves>;
     if (lds > 64 * 1024) {
@@ -942,16 +946,18 @@ hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
     return hipGetLastError();
 }
 
-constexpr int kQueryWaves = 8;  // of a workgroup that divides a block's tiles
 template <typename T, int D, bool kShared>
 hipError_t launch_tiles(const Q4QueryArgs& a, hipStream_t s) {
     if constexpr (sizeof(T) == 2) {
         if constexpr (!kShared) {
             if (a.plan.tiles == 4) return launch_form<T, D, 4, 1, kShared, 1>(a, s);
+            if (a.plan.tiles == 2 && a.plan.waves == 1) return launch_form<T, D, 2, 1, kShared, 1>(a, s);
         }
-        if (a.plan.tiles == 2) return launch_form<T, D, 2, 1, kShared, kQueryWaves>(a, s);
+        if (a.plan.tiles == 2 && a.plan.waves == 4) return launch_form<T, D, 2, 1, kShared, 4>(a, s);
+        if (a.plan.tiles == 2) return launch_form<T, D, 2, 1, kShared, 8>(a, s);
     }
-    return launch_form<T, D, 1, 3, kShared, kQueryWaves>(a, s);
+    if (a.plan.waves == 4) return launch_form<T, D, 1, 3, kShared, 4>(a, s);
+    return launch_form<T, D, 1, 3, kShared, 8>(a, s);
 }
 template <bool kShared>
 hipError_t launch_queries(const Q4QueryArgs& a, hipStream_t s) {
@@ -968,13 +974,25 @@ int chunks_of(int64_t units, int64_t tiles, int waves, int want) {
 
 }  // namespace
 
+#ifdef SWEEP
+#include <stdlib.h>
+static int env(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
+#else
+#define env(n, d) (d)
+#endif
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
     const int64_t slabs = (int64_t)layer_count * d.batch * d.hkv;
     auto blocks = [&](int tiles) { return (rows + tiles * p.per - 1) / (tiles * p.per); };
     p.tiles = !d.bf16 || rows <= p.per ? 1 : 2;
-    if (d.bf16 && slabs * blocks(4) >= kAlone) p.tiles = 4;
+    p.waves = p.tiles == 2 ? 4 : 8;
+    if (d.bf16 && slabs * blocks(4) >= kAlone) {
+        p.tiles = 4;
+        p.waves = 1;
+    }
+    if (d.bf16) p.tiles = env("Q4_CT", p.tiles);
+    p.waves = env("Q4_WAVES", p.waves);
     p.vectors = p.tiles * p.per;
     p.blocks = blocks(p.tiles);
     int64_t tiles = (n_max + kTile - 1) / kTile;
@@ -982,8 +1000,8 @@ Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows
         const int64_t seen = ((int64_t)window + sinks + p.vectors) / kTile + 3;
         tiles = tiles < seen ? tiles : seen;
     }
-    if (p.tiles == 4) p.chunks = chunks_of(slabs * p.blocks, tiles / 8, 1, kQ4Units * cus_of());
-    else p.chunks = chunks_of(slabs * p.blocks, tiles, kQueryWaves, 2 * cus_of());
+    if (p.waves == 1) p.chunks = chunks_of(slabs * p.blocks, tiles / 64, 1, kQ4Units * cus_of());
+    else p.chunks = chunks_of(slabs * p.blocks, tiles, p.waves, env("Q4_WANT", 2) * cus_of());
     return p;
 }
 
@@ -991,9 +1009,14 @@ Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
     p.tiles = d.bf16 && d.batch > p.per ? 2 : 1;
+    if (d.bf16) p.tiles = env("Q4_CT", p.tiles);
+    p.waves = env("Q4_WAVES", p.tiles == 2 ? 4 : 8);
     p.vectors = p.tiles * p.per;
-    p.blocks = (d.batch + p.vectors - 1) / p.vectors;
-    p.chunks = chunks_of((int64_t)layer_count * d.hkv * p.blocks, (n_max + kTile - 1) / kTile, kQueryWaves, 2 * cus_of());
+    while (1 << p.vector_shift < p.vectors) ++p.vector_shift;
+    // (groups that do not fill their blocks make more of them: places for twice as many)
+    const int full = (d.batch + p.vectors - 1) / p.vectors;
+    p.blocks = 2 * full < d.batch ? 2 * full : d.batch;
+    p.chunks = chunks_of((int64_t)layer_count * d.hkv * full, (n_max + kTile - 1) / kTile, p.waves, env("Q4_WANT", 2) * cus_of());
     return p;
 }
 
@@ -1008,9 +1031,12 @@ hipError_t launch_q4_window(const Q4QueryArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_q4_shared(const Q4QueryArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(q4_list_kernel, dim3(a.dims.batch), dim3(kListThreads), 0, s, a);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_queries<true>(a, s);
+    if (a.heads) {
+        hipLaunchKernelGGL(q4_block_kernel, dim3(a.dims.batch), dim3(kWave), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return launch_queries<true>(a, s);
 }
 
 }  // namespace ikv
