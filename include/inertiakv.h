@@ -447,7 +447,7 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
  * exist (KV_FAULT_CACHE) take no part.  What a masked row holds, NaN included, does not reach an output.  In bf16 calls of more than
  * one query per slot probabilities may be rounded to bf16 before they weigh the values (to nearest; their sum is of the rounded ones).
  * Workspace: kv_q4_window_workspace_bytes, for calls of at most n_max rows, `rows` queries and layer_count layers.
- * Refused (KV_ERR_UNSUPPORTED: take fewer layers or rows a call): 2^23 workgroups or more. */
+ * Refused (KV_ERR_UNSUPPORTED: take fewer layers or rows a call): rows above 2^27, 2^23 workgroups or more. */
 kv_status kv_q4_window_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t rows, int32_t layer_count, size_t* bytes);
 kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
                               int32_t n_max, int32_t rows, const int32_t* count, const void* q, const kv_q4_strides* q_strides,

@@ -105,7 +105,7 @@ hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);
 // Attention of blocks of queries: the newest rows' queries of a slot in a window (kv_q4_attend_window), or one query of each of
 // several slots that share pages (kv_q4_attend_shared).  A block is `vectors` queries; each is `group` columns of a product.
 constexpr int kQ4MostVectors = 32, kQ4MostColumns = 64;  // of a block
-constexpr int kQ4Units = 8;  // most workgroups for a CU among which blocks are divided
+constexpr int kQ4Units = 4;  // most workgroups for a CU, where blocks are divided
 struct Q4QueryPlan {
     int tiles;    // column tiles of 16 in a block
     int per;      // queries in a column tile
@@ -113,6 +113,7 @@ struct Q4QueryPlan {
     int vector_shift;  // shared: the lowest power of two that is no fewer
     int blocks;   // blocks of a slot (window), or of the batch where its groups fill them (shared)
     int waves;    // of a workgroup
+    int marks;    // window with positions: a kernel marks the tiles of which a block sees any row
     int chunks;   // workgroups that divide a block's rows
 };
 struct Q4QueryArgs {

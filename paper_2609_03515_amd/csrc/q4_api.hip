@@ -20,6 +20,7 @@ constexpr size_t kFaultBytes = 256;
 constexpr int kMostHeads = 1 << 16;
 constexpr double kMostRowItems = (double)(1 << 28) - 256;  // 16 threads a row of the store and the load, in whole workgroups
 constexpr double kMostTokens = (double)(1 << 25);          // 64 threads a token, 4 or 8 of them a workgroup of 256
+constexpr int kMostQueries = 1 << 27;                      // of a slot: as many as it can have rows
 constexpr double kMostGroups = (double)(1 << 23) - 1;      // workgroups of 512 threads
 constexpr double kMostJoined = (double)(1 << 23) - 1;      // 512 threads a head of the attention's join
 
@@ -159,13 +160,13 @@ QueryLayout query_layout(const Q4Dims& d, size_t mark_words, bool blocks, size_t
     return L;
 }
 size_t mark_words_of(int n_max) { return ((size_t)n_max + 2047) / 2048; }
-// Parts that a call needs, and more than any call of at most these sizes does: chunks are cut where there are fewer than kQ4Units
-// units for a CU (then units * chunks is below twice that, of at most kQ4MostColumns columns each), and have 4 tiles of 32 rows at least.
+// Parts that a call needs, and more than any call of at most these sizes does: units * chunks is at most kQ4Units for a CU, of at most
+// kQ4MostColumns columns each, and a chunk has 4 tiles of 32 rows at least.
 size_t parts_of(const Q4Dims& d, int layer_count, int rows, int chunks) {
     return chunks > 1 ? (size_t)layer_count * d.batch * rows * d.hq * chunks : 0;
 }
 size_t most_parts(const Q4Dims& d, int n_max, int layer_count, int rows) {
-    const size_t cus = device_cus() > 0 ? device_cus() : 256, by_units = 2 * kQ4Units * cus * kQ4MostColumns;
+    const size_t cus = device_cus() > 0 ? device_cus() : 256, by_units = kQ4Units * cus * kQ4MostColumns;
     const size_t by_tiles = (size_t)layer_count * d.batch * rows * d.hq * (((size_t)n_max + 127) / 128);
     return by_tiles < by_units ? by_tiles : by_units;
 }
@@ -421,8 +422,9 @@ kv_status kv_q4_window_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, 
     const kv_status rc = check_shape(shape);
     if (rc != KV_OK) return rc;
     const Q4Dims d = dims_of(*shape);
-    if (!bytes || n_max < 1 || n_max > d.cap || rows < 1 || rows > d.cap || layer_count < 1 || layer_count > shape->layers)
+    if (!bytes || n_max < 1 || n_max > d.cap || rows < 1 || layer_count < 1 || layer_count > shape->layers)
         return KV_ERR_INVALID_ARG;
+    if (rows > kMostQueries) return KV_ERR_UNSUPPORTED;
     const int per = 16 / d.group;
     *bytes = query_layout(d, (size_t)d.batch * ((rows + per - 1) / per) * mark_words_of(n_max), false, most_parts(d, n_max, layer_count, rows)).total;
     return KV_OK;
@@ -437,8 +439,9 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
     if (rc != KV_OK) return rc;
     const kv_q4_shape& s = *shape;
     const Q4Dims d = dims_of(s);
-    if (layer0 < 0 || layer_count < 1 || layer_count > s.layers - layer0 || n_max < 1 || n_max > d.cap || rows < 1 || rows > d.cap)
+    if (layer0 < 0 || layer_count < 1 || layer_count > s.layers - layer0 || n_max < 1 || n_max > d.cap || rows < 1)
         return KV_ERR_INVALID_ARG;
+    if (rows > kMostQueries) return KV_ERR_UNSUPPORTED;
     if (window < 0 || sinks < 0 || !q || !o || q == o) return KV_ERR_INVALID_ARG;
     if ((rc = check_queries(s, layer_count, rows, q, q_strides, o, o_strides)) != KV_OK) return rc;
     if (!aligned(count, 4)) return KV_ERR_UNSUPPORTED;
@@ -447,8 +450,7 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.cache = cache_of(*cache);
     a.plan = q4_window_plan(d, layer_count, n_max, rows, window, sinks);
     a.words = (int)mark_words_of(n_max);
-    // (one block of a slot finds its tiles by itself)
-    const size_t marks = cache->pos && a.plan.blocks > 1 ? (size_t)d.batch * a.plan.blocks * a.words : 0;
+    const size_t marks = cache->pos && a.plan.marks ? (size_t)d.batch * a.plan.blocks * a.words : 0;
     if ((double)layer_count * d.batch * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups || (double)d.batch * a.plan.blocks * ((a.words + 3) / 4) > kMostGroups)
         return KV_ERR_UNSUPPORTED;
     const QueryLayout L = query_layout(d, marks, false, parts_of(d, layer_count, rows, a.plan.chunks));

@@ -32,7 +32,6 @@
 namespace ikv {
 namespace {
 
-constexpr int kAlone = 768;  // blocks of four column tiles from which a wave takes each for itself
 constexpr int kKeep = 0;  // rows are read again by other workgroups
 constexpr float kNaN = __builtin_nanf("");
 
@@ -163,9 +162,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
     constexpr int kThreads = kWave * kWaves;
     constexpr int kKey = D / 32, kOut = D / 16;     // products per half, and for the output
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;  // bf16 parts of a query
-    constexpr int kStride = D + 4;
-    constexpr int kJoin = (kWaves + 1) / 2;         // waves whose outputs are joined through LDS at once
-    // [wave] values; in their place [joined wave][column][kStride] outputs; then [wave][column] maxima and sums; then the queries
+    // [wave] values and the queries; in their place the outputs that are joined; then [wave][column] maxima and sums
     extern __shared__ float lds[];
     const Q4Dims& d = a.dims;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -316,24 +313,16 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
             if (row >= slot.count) sl = -1;
         }
     };
-    __shared__ int places[kShared ? 1 : CT * 16];  // window: the columns' positions (no query: the lowest)
-    int top_place = INT_MIN, low_place = INT_MAX;
+    int place[kShared ? 1 : CT];  // window: the positions of the lane's columns (no query: the lowest)
     if constexpr (!kShared) {
-        int top = INT_MIN, low = INT_MAX;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            int sl = -1, row = 0, place = INT_MIN;
+            int sl = -1, row = 0;
             if (part < per) slot_row(ct, part, sl, row);
-            if (sl >= 0 && slot.n > 0) {
-                const int r = slot.n - slot.count + row;
-                place = a.cache.pos ? a.cache.pos[(size_t)b * d.cap + r] : r;
-                top = max(top, place);
-                low = min(low, place);
-            }
-            if (wave == 0 && s == 0) places[16 * ct + c] = place;
+            const int r = max(0, slot.n - slot.count + row);
+            place[ct] = a.cache.pos ? a.cache.pos[(size_t)b * d.cap + min(r, d.cap - 1)] : r;
+            if (sl < 0 || slot.n == 0) place[ct] = INT_MIN;
         }
-        top_place = __builtin_amdgcn_readfirstlane(wave_max_int(top));
-        low_place = __builtin_amdgcn_readfirstlane(~wave_max_int(~low));
     }
 
     // queries as bf16 parts in LDS, [part][product][column tile][lane] (in registers one column tile would take 16, and spill as many)
@@ -376,6 +365,22 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         }
     }
 
+    __shared__ int places[kShared ? 1 : CT * 16];
+    int top_place = INT_MIN, low_place = INT_MAX;
+    if constexpr (!kShared) {
+        int top = INT_MIN, low = INT_MAX;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const bool is = part < per && v0 + ct * per + part < slot.count;
+            if (is) {
+                top = max(top, place[ct]);
+                low = min(low, place[ct]);
+            }
+            if (wave == 0 && s == 0) places[16 * ct + c] = place[ct];
+        }
+        top_place = __builtin_amdgcn_readfirstlane(wave_max_int(top));
+        low_place = __builtin_amdgcn_readfirstlane(~wave_max_int(~low));
+    }
     const int top_from = lower_bound_of(top_place, a.window), low_from = lower_bound_of(low_place, a.window);
     const int tiles = kShared ? 0 : (slot.n + kTile - 1) / kTile;
     auto look = [&]() __attribute__((always_inline)) {
@@ -735,113 +740,77 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
     if (kShared ? base >= run : k0 + base * step >= tiles) break;
     load_look(late);
    }
-    // the waves joined: the upper half into the lower, those through columns of LDS
-    constexpr int kColumns = CT * 16;
+    // The outputs are blocks of 64 lanes' four elements (column c, elements s D / 4 + i kOut + 4 half ...), each joined by one wave: the
+    // others' come through LDS, in the place of values and queries, with every wave's maxima and sums.
+    constexpr int kColumns = CT * 16, kHalves = kOut / 4, kBlocks = CT * 4 * kHalves;
     float* const stat = lds + a.stat_at;  // [wave][column] maxima, then sums
-    __syncthreads();                      // (their values' places are used again)
+    f32x4* const parts = reinterpret_cast<f32x4*>(lds) + lane;
+    __syncthreads();
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) l[ct] = rows_allsum(l[ct]);
-    auto mine = [&](int ct) __attribute__((always_inline)) { return lds + ((wave % kJoin) * kColumns + 16 * ct + c) * kStride + s * (D / 4); };
-    auto put = [&]() __attribute__((always_inline)) {
+    auto block_of = [&](int q) __attribute__((always_inline)) {
+        const int ct = q / (4 * kHalves), i = q / kHalves % 4, e = q % kHalves * 4;
+        return f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
+    };
+    if constexpr (kWaves > 1) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < kOut; e += 4)
-                    *reinterpret_cast<f32x4*>(mine(ct) + i * kOut + e) = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
+        for (int ct = 0; ct < CT; ++ct)
             if (s == 0) {
                 stat[wave * kColumns + 16 * ct + c] = m[ct];
                 stat[(kWaves + wave) * kColumns + 16 * ct + c] = l[ct];
             }
+#pragma unroll
+        for (int q = 0; q < kBlocks; ++q) {
+            const int owner = q % kWaves;
+            if (wave != owner) parts[(q * (kWaves - 1) + (wave > owner ? wave - 1 : wave)) * kWave] = block_of(q);
         }
-    };
-    // elements e .. e + 3 of column col: the weights' maximum and sum, and the sum over the rows
-    auto store = [&](int col, int e, float top, float sum, f32x4 o) __attribute__((always_inline)) {
-        const int vt = col % 16 / group, h = col % 16 - vt * group;
+        __syncthreads();
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
         int sl = -1, row = 0;
-        if (vt < per) slot_row(col / 16, vt, sl, row);
-        if (sl < 0) return;
-        if (late.plan.chunks == 1) {
-            o *= sum != 0.0f ? 1.0f / sum : 0.0f;
-            T* op = static_cast<T*>(late.o) + layer * late.os[0] + sl * late.os[1] + (g * group + h) * late.os[2] + row * late.os[3] + e;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
-            else *reinterpret_cast<f32x4*>(op) = o;
-        } else {
-            // (a part without rows for the query is its sum, 0, alone)
-            const size_t at = ((((size_t)layer * late.dims.batch + sl) * late.rows + row) * late.dims.hq + g * group + h) * late.plan.chunks + chunk;
-            if (sum != 0.0f) *reinterpret_cast<f32x4*>(late.opart + at * D + e) = o;
-            if (e == 0) late.part[at] = make_float2(top, sum);
+        if (part < per) slot_row(ct, part, sl, row);
+        if (sl < 0) continue;
+        float top = m[ct], sum = l[ct], f[kWaves];
+        if constexpr (kWaves > 1) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                f[w] = stat[w * kColumns + 16 * ct + c];
+                top = fmaxf(top, f[w]);
+            }
+            sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                f[w] = exp2_hw(f[w] - top);
+                sum += f[w] * stat[(kWaves + w) * kColumns + 16 * ct + c];
+            }
         }
-    };
-    if constexpr (kWaves == 1) {
-        // a lane has D / 4 consecutive elements of a column
+        const int h = g * group + head, chunks = late.plan.chunks;
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        T* const op = static_cast<T*>(late.o) + layer * late.os[0] + sl * late.os[1] + h * late.os[2] + row * late.os[3] + s * (D / 4);
+        const size_t at = ((((size_t)layer * late.dims.batch + sl) * late.rows + row) * late.dims.hq + h) * chunks + chunk;
+        float* const pp = late.opart + at * D + s * (D / 4);
+        if (chunks > 1 && wave == 0 && s == 0) late.part[at] = make_float2(top, sum);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            int sl = -1, row = 0;
-            if (part < per) slot_row(ct, part, sl, row);
-            if (sl < 0) continue;
-            if (late.plan.chunks == 1) {
-                const float inv = l[ct] != 0.0f ? 1.0f / l[ct] : 0.0f;
-                T* const op = static_cast<T*>(late.o) + layer * late.os[0] + sl * late.os[1] + (g * group + head) * late.os[2] + row * late.os[3] + s * (D / 4);
+        for (int x = 0; x < 4 * kHalves; ++x) {
+            const int q = ct * 4 * kHalves + x;
+            if (wave != q % kWaves) continue;
+            f32x4 o = block_of(q);
+            if constexpr (kWaves > 1) {
+                o *= exp2_hw(m[ct] - top);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < kOut; e += 4) {
-                        const f32x4 o = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]} * inv;
-                        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op + i * kOut + e) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
-                        else *reinterpret_cast<f32x4*>(op + i * kOut + e) = o;
-                    }
+                for (int w = 0; w < kWaves; ++w)
+                    if (w != q % kWaves) o += parts[(q * (kWaves - 1) + (w > q % kWaves ? w - 1 : w)) * kWave] * f[w];
+            }
+            const int e = x / kHalves * kOut + x % kHalves * 4;
+            if (chunks > 1) {
+                // (a part without rows for the query is its sum, 0, alone)
+                if (sum != 0.0f) *reinterpret_cast<f32x4*>(pp + e) = o;
             } else {
-                const size_t at = ((((size_t)layer * late.dims.batch + sl) * late.rows + row) * late.dims.hq + g * group + head) * late.plan.chunks + chunk;
-                if (s == 0) late.part[at] = make_float2(m[ct], l[ct]);
-                if (l[ct] != 0.0f) {
-                    float* const op = late.opart + at * D + s * (D / 4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int e = 0; e < kOut; e += 4)
-                            *reinterpret_cast<f32x4*>(op + i * kOut + e) = f32x4{acc[ct][e][i], acc[ct][e + 1][i], acc[ct][e + 2][i], acc[ct][e + 3][i]};
-                }
+                o *= inv;
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(op + e) = u32x2{pack2(o[0], o[1]), pack2(o[2], o[3])};
+                else *reinterpret_cast<f32x4*>(op + e) = o;
             }
-        }
-    } else {
-        if (wave >= kJoin) put();
-        __syncthreads();
-        if (wave < kJoin) {
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const float m2 = stat[(wave + kJoin) * kColumns + 16 * ct + c], l2 = stat[(kWaves + wave + kJoin) * kColumns + 16 * ct + c];
-                const float top = fmaxf(m[ct], m2), f = exp2_hw(m[ct] - top), f2 = exp2_hw(m2 - top);
-                m[ct] = top;
-                l[ct] = l[ct] * f + l2 * f2;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < kOut; e += 4) {
-                        const f32x4 o = *reinterpret_cast<const f32x4*>(mine(ct) + i * kOut + e);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) acc[ct][e + y][i] = acc[ct][e + y][i] * f + o[y] * f2;
-                    }
-            }
-        }
-        __syncthreads();
-        if (wave < kJoin) put();
-        __syncthreads();
-        for (int i = threadIdx.x; i < kColumns * (D / 4); i += kThreads) {
-            const int col = i / (D / 4), e = i % (D / 4) * 4;
-            float top = stat[col];
-#pragma unroll
-            for (int w = 1; w < kJoin; ++w) top = fmaxf(top, stat[w * kColumns + col]);
-            float sum = 0.0f;
-            f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < kJoin; ++w) {
-                const float f = exp2_hw(stat[w * kColumns + col] - top);
-                sum += f * stat[(kWaves + w) * kColumns + col];
-                o += *reinterpret_cast<const f32x4*>(lds + (w * kColumns + col) * kStride + e) * f;
-            }
-            store(col, e, top, sum, o);
         }
     }
     if constexpr (!kShared) break;
@@ -866,9 +835,10 @@ __global__ __launch_bounds__(kPartThreads) void q4_part_kernel(Q4QueryArgs a, in
     const bool is = i < heads && (kShared || row < slot_of(a, b).count);
     float top = -FLT_MAX, sum = 0.0f;
     f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-    if (is) {
-        const float2* part = a.part + (size_t)i * chunks;
-        const float* from = a.opart + (size_t)i * chunks * D + quad * 4;
+    {
+        // (past the last head, or of a row that is no query: anything that is there)
+        const float2* part = a.part + (size_t)min(i, heads - 1) * chunks;
+        const float* from = a.opart + (size_t)min(i, heads - 1) * chunks * D + quad * 4;
         for (int j0 = k; j0 < chunks; j0 += kTogether << split) {
             float2 p[kTogether];
             f32x4 x[kTogether];
@@ -876,9 +846,13 @@ __global__ __launch_bounds__(kPartThreads) void q4_part_kernel(Q4QueryArgs a, in
             for (int j = 0; j < kTogether; ++j) {
                 const int at = min(j0 + (j << split), chunks - 1);
                 p[j] = part[at];
+                x[j] = *reinterpret_cast<const f32x4*>(from + (size_t)at * D);
+            }
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {  // (a part without rows was not written)
                 if (j0 + (j << split) >= chunks) p[j] = make_float2(-FLT_MAX, 0.0f);
-                x[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (p[j].y != 0.0f) x[j] = *reinterpret_cast<const f32x4*>(from + (size_t)at * D);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[j][e] = p[j].y != 0.0f ? x[j][e] : 0.0f;
             }
             float raised = top;
 #pragma unroll
@@ -918,15 +892,15 @@ __global__ __launch_bounds__(kPartThreads) void q4_part_kernel(Q4QueryArgs a, in
 
 template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
 hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
-    constexpr int kJoined = kWaves / 2 * CT * 16 * (D + 4) * (int)sizeof(float), kValues = kWaves * kValueBytes<D>;
-    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kStat = 2 * kWaves * CT * 16;
-    static_assert(kJoined % 16 == 0 && kValues % 16 == 0 && kStat % 4 == 0, "queries are read 16 bytes at a time");
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+    constexpr int kValues = kWaves * kValueBytes<D>, kQueries = kParts * (D / 32) * CT * kWave * (int)sizeof(u32x4);
+    constexpr int kJoined = CT * (D / 16) * (kWaves - 1) * kWave * (int)sizeof(f32x4), kStat = kWaves > 1 ? 2 * kWaves * CT * 16 * (int)sizeof(float) : 0;
+    static_assert(kJoined % 16 == 0 && kValues % 16 == 0, "queries are read 16 bytes at a time");
     static_assert(CT * 16 <= kQ4MostColumns, "room for the parts of outputs");
-    constexpr int kQueries = kParts * (D / 32) * CT * kWave * (int)sizeof(u32x4);
-    // (a wave by itself joins nothing: eight such workgroups fit a CU)
-    a.stat_at = (kWaves > 1 && kJoined > kValues ? kJoined : kValues) / (int)sizeof(float);
-    a.q_at = a.stat_at + (kWaves > 1 ? kStat : 0);
-    const size_t lds = (size_t)a.q_at * sizeof(float) + kQueries;
+    constexpr int kFirst = kValues + kQueries > kJoined ? kValues + kQueries : kJoined;
+    a.q_at = kValues / (int)sizeof(float);
+    a.stat_at = kFirst / (int)sizeof(float);
+    const size_t lds = kFirst + kStat;
     auto kern = q4_query_kernel<T, D, CT, kP, kShared, kWaves>;
     if (lds > 64 * 1024) {
         static std::atomic<bool> raised[kMaxDevices];
@@ -949,15 +923,13 @@ hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
 template <typename T, int D, bool kShared>
 hipError_t launch_tiles(const Q4QueryArgs& a, hipStream_t s) {
     if constexpr (sizeof(T) == 2) {
-        if constexpr (!kShared) {
-            if (a.plan.tiles == 4) return launch_form<T, D, 4, 1, kShared, 1>(a, s);
-            if (a.plan.tiles == 2 && a.plan.waves == 1) return launch_form<T, D, 2, 1, kShared, 1>(a, s);
-        }
-        if (a.plan.tiles == 2 && a.plan.waves == 4) return launch_form<T, D, 2, 1, kShared, 4>(a, s);
-        if (a.plan.tiles == 2) return launch_form<T, D, 2, 1, kShared, 8>(a, s);
+        if constexpr (!kShared)
+            if (a.plan.tiles == 4) return launch_form<T, D, 4, 1, kShared, 2>(a, s);
+        if constexpr (kShared)
+            if (a.plan.tiles == 2 && a.plan.waves == 8) return launch_form<T, D, 2, 1, kShared, 8>(a, s);
+        if (a.plan.tiles == 2) return launch_form<T, D, 2, 1, kShared, 4>(a, s);
     }
-    if (a.plan.waves == 4) return launch_form<T, D, 1, 3, kShared, 4>(a, s);
-    return launch_form<T, D, 1, 3, kShared, 8>(a, s);
+    return launch_form<T, D, 1, 3, kShared, 4>(a, s);
 }
 template <bool kShared>
 hipError_t launch_queries(const Q4QueryArgs& a, hipStream_t s) {
@@ -966,33 +938,25 @@ hipError_t launch_queries(const Q4QueryArgs& a, hipStream_t s) {
 }
 
 int cus_of() { return device_cus() > 0 ? device_cus() : 256; }
-// Workgroups of `waves` waves that divide a block's `tiles` tiles: until there are `want` of them, each with a tile for every wave at least.
+// Workgroups of `waves` waves that divide a block's `tiles` tiles: no more than `want` in all, and two tiles for a wave at least.
 int chunks_of(int64_t units, int64_t tiles, int waves, int want) {
-    const int64_t by_units = (want + units - 1) / units, most = (tiles + waves - 1) / waves;
-    return (int)(by_units < most ? by_units : most > 0 ? most : 1);
+    const int64_t by_units = want / units, most = (tiles + 2 * waves - 1) / (2 * waves), n = by_units < most ? by_units : most;
+    return n > 1 ? (int)n : 1;
 }
 
 }  // namespace
 
-#ifdef SWEEP
-#include <stdlib.h>
-static int env(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
-#else
-#define env(n, d) (d)
-#endif
+// Forms.  One column tile: four waves, two workgroups for a CU (the 8B layer at its budget 18.0 us; one 20.4, four 18.9; eight waves
+// 19.4).  Two: four waves, as many workgroups as fit a CU, three (128 queries on 32,768 rows 105 us, two 114).  Four, each of two waves,
+// where there are four blocks for a CU, as many as it holds: a chunk of 2,048 queries on 32,768 rows 1,210 us, with two column tiles
+// 1,286; 8 prompts of 1,024 rows 109 and 117; but 64 queries on each of 8 x 4,096 rows 68 and 61.
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
     const int64_t slabs = (int64_t)layer_count * d.batch * d.hkv;
     auto blocks = [&](int tiles) { return (rows + tiles * p.per - 1) / (tiles * p.per); };
-    p.tiles = !d.bf16 || rows <= p.per ? 1 : 2;
-    p.waves = p.tiles == 2 ? 4 : 8;
-    if (d.bf16 && slabs * blocks(4) >= kAlone) {
-        p.tiles = 4;
-        p.waves = 1;
-    }
-    if (d.bf16) p.tiles = env("Q4_CT", p.tiles);
-    p.waves = env("Q4_WAVES", p.waves);
+    p.tiles = !d.bf16 || rows <= p.per ? 1 : slabs * blocks(4) < 4 * cus_of() ? 2 : 4;
+    p.waves = p.tiles == 4 ? 2 : 4;
     p.vectors = p.tiles * p.per;
     p.blocks = blocks(p.tiles);
     int64_t tiles = (n_max + kTile - 1) / kTile;
@@ -1000,23 +964,27 @@ Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows
         const int64_t seen = ((int64_t)window + sinks + p.vectors) / kTile + 3;
         tiles = tiles < seen ? tiles : seen;
     }
-    if (p.waves == 1) p.chunks = chunks_of(slabs * p.blocks, tiles / 64, 1, kQ4Units * cus_of());
-    else p.chunks = chunks_of(slabs * p.blocks, tiles, p.waves, env("Q4_WANT", 2) * cus_of());
+    p.chunks = chunks_of(slabs * p.blocks, tiles, p.waves, (p.tiles == 1 ? 2 : p.tiles == 2 ? 3 : 4) * cus_of());
+    // a wave that looks at more than three times 16 tiles finds them by marks: a kernel before it, 5 us, that all layers and heads share
+    p.marks = p.blocks > 1 && (n_max + kTile - 1) / kTile > 48 * p.chunks * p.waves;
     return p;
 }
 
+// Two column tiles: where there are blocks for every CU, a workgroup of eight waves to each, without a join (32 layers of 8 samples
+// 68 us, four waves in two and three chunks 76 and 71); else four waves, two workgroups for a CU (32 samples of three prompts 53 us, three
+// 58, one 69), since small groups make more blocks than are counted here.
 Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
     p.tiles = d.bf16 && d.batch > p.per ? 2 : 1;
-    if (d.bf16) p.tiles = env("Q4_CT", p.tiles);
-    p.waves = env("Q4_WAVES", p.tiles == 2 ? 4 : 8);
     p.vectors = p.tiles * p.per;
     while (1 << p.vector_shift < p.vectors) ++p.vector_shift;
     // (groups that do not fill their blocks make more of them: places for twice as many)
     const int full = (d.batch + p.vectors - 1) / p.vectors;
     p.blocks = 2 * full < d.batch ? 2 * full : d.batch;
-    p.chunks = chunks_of((int64_t)layer_count * d.hkv * full, (n_max + kTile - 1) / kTile, p.waves, env("Q4_WANT", 2) * cus_of());
+    const int64_t units = (int64_t)layer_count * d.hkv * full;
+    p.waves = p.tiles == 2 && units >= cus_of() ? 8 : 4;
+    p.chunks = p.waves == 8 ? 1 : chunks_of(units, (n_max + kTile - 1) / kTile, p.waves, 2 * cus_of());
     return p;
 }
 

@@ -177,6 +177,15 @@ def test_strides(rows):
     check(t, one, o, rows, None, 16, 2)
 
 
+@pytest.mark.parametrize("places", ["rows", "any"])
+def test_more_queries_than_rows(places):
+    """A call may have room for more queries than a slot can have rows."""
+    t = cache([20, 0, 33], 300, places, hq=4, hkv=2)
+    for counts in (None, [20, 0, 7]):
+        q, o = run(t, 300, counts, 9, 2)
+        check(t, q, o, 300, counts, 9, 2)
+
+
 def test_layers():
     t = cache([100, 7], 5, "rows", layers=4, hq=4, hkv=2)
     q, o = run(t, 5, None, 20, 1, layers=2, layer0=1)

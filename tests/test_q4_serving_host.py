@@ -113,7 +113,7 @@ def test_attention_refusals(fn):
 
 
 def test_window_refusals():
-    assert window(rows=0) == INVALID and window(rows=321) == INVALID and window(win=-1) == INVALID and window(sinks=-1) == INVALID
+    assert window(rows=0) == INVALID and window(rows=321, ws=None) == WORKSPACE and window(rows=(1 << 27) + 1) == UNSUPPORTED and window(win=-1) == INVALID and window(sinks=-1) == INVALID
     assert window(qs=None) == INVALID and window(os=None) == INVALID and window(count=FAKE + 2) == UNSUPPORTED
     for field in ("layer", "batch", "head", "row"):
         assert window(qs=strides(**{field: 132})) == UNSUPPORTED and window(os=strides(**{field: 132})) == UNSUPPORTED
@@ -127,8 +127,8 @@ def test_window_refusals():
 
 def test_shared_refusals():
     assert shared(group=None) == INVALID and shared(group=FAKE + 2) == UNSUPPORTED
-    big = shape(batch=1024, layers=16, n_q_heads=512, n_kv_heads=512, max_pages=1)
-    assert shared(layers=15, s=big, ws=None) == WORKSPACE and shared(layers=16, s=big, ws=None) == UNSUPPORTED
+    big = shape(batch=1024, layers=2, n_q_heads=1 << 16, n_kv_heads=1 << 16, max_pages=1)
+    assert shared(layers=1, s=big, ws=None) == WORKSPACE and shared(layers=2, s=big, ws=None) == UNSUPPORTED
 
 
 @pytest.mark.parametrize("kw", [dict(), dict(head_dim=64, dtype="f32"), dict(n_q_heads=2), dict(n_q_heads=32), dict(page_rows=16)])
@@ -149,7 +149,7 @@ def test_workspaces(kw):
         assert shared(layers=layers, n=n, s=s, ws=FAKE + 16, ws_bytes=B.kv_q4_shared_workspace_bytes(s, n, layers)) == INVALID
 
 
-@pytest.mark.parametrize("bad", [(0, 1, 1), (321, 1, 1), (10, 0, 1), (10, 321, 1), (10, 1, 0), (10, 1, 5)])
+@pytest.mark.parametrize("bad", [(0, 1, 1), (321, 1, 1), (10, 0, 1), (10, (1 << 27) + 1, 1), (10, 1, 0), (10, 1, 5)])
 def test_workspace_refusals(bad):
     with pytest.raises(B.KVError):
         B.kv_q4_window_workspace_bytes(shape(), *bad)
