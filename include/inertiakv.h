@@ -411,8 +411,8 @@ typedef struct {
 /* kv_q4_store with keys rotated by their positions (DEVICE [axes][batch][rows] int32, read for rows r < count[b]), and queries
  * beside them: row r < count[b] of q [layer][batch][query head][row][d] is written rotated to the same row of q_out, in the
  * shape's type; the other rows of q_out are left as they were.  q and q_out are both null (no queries), or not; q_out may be q
- * itself, with the same strides.  Angles, rotation and what is quantised are in 64 bits: a stored key is the nearest to the
- * exact rotated one, a query is rounded once.  Queries are written for every row r < min(count[b], rows), whatever becomes of
+ * itself, with the same strides.  Angles, their cosines and sines and the rotation of keys are in 64 bits: a stored key is the
+ * nearest to the exact rotated one; queries are rotated in 32 bits and rounded to the shape's type.  Queries are written for every row r < min(count[b], rows), whatever becomes of
  * its key.  count, first, faults and limits as kv_q4_store, and batch * rows at most 2^25 (KV_ERR_UNSUPPORTED). */
 kv_status kv_q4_store_rotary(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
                              int32_t rows, const int32_t* first, const int32_t* count, const kv_rotary* rotary,

@@ -544,17 +544,17 @@ def make_rotary(inv_freq, axis=None, pairs="halves", scale=1.0, axes=None) -> Kv
     return r
 
 
-def _q4_spread(cache, layer_count, heads, rows, *tensors):
-    """Strides of tensors [layer_count][batch][heads][rows][head_dim] of the cache's type and place, whose rows are contiguous; None
-    where one is not so."""
-    shape, out = (layer_count, cache._batch, heads, rows, cache._dim), []
-    on = (layer_count > 1, cache._batch > 1, heads > 1, rows > 1)  # (the stride of an extent of 1 is not used)
-    for t in tensors:
-        st = t.stride()
-        if t.shape != shape or t.dtype is not cache.element or t.get_device() != cache._device or st[4] != 1:
-            return None
-        out.append(KvQ4Strides(st[0] * on[0], st[1] * on[1], st[2] * on[2], st[3] * on[3]))
-    return out
+def _q4_spread(cache, layer_count, heads, rows, a, b):
+    """Strides of two tensors [layer_count][batch][heads][rows][head_dim] of the cache's type and place, whose rows are contiguous; None
+    where one is not so.  (The stride of an extent of 1 is not used, and may be anything.)"""
+    shape, dev, element = (layer_count, cache._batch, heads, rows, cache._dim), cache._device, cache.element
+    s, t = a.stride(), b.stride()
+    if not (a.shape == shape and b.shape == shape and a.dtype is element and b.dtype is element and s[4] == 1 and t[4] == 1
+            and a.get_device() == dev and b.get_device() == dev):
+        return None
+    ln, bn, hn, rn = layer_count > 1, cache._batch > 1, heads > 1, rows > 1
+    first = KvQ4Strides(s[0] * ln, s[1] * bn, s[2] * hn, s[3] * rn)
+    return first, first if s == t else KvQ4Strides(t[0] * ln, t[1] * bn, t[2] * hn, t[3] * rn)
 
 
 def kv_q4_store_rotary(cache: KvQ4Cache, layer0, layer_count, rows, k, v, rotary: KvRotary, positions, ws, first=None, count=None,
@@ -563,9 +563,9 @@ def kv_q4_store_rotary(cache: KvQ4Cache, layer0, layer_count, rows, k, v, rotary
     [n_q_heads][rows][head_dim] in any strides with contiguous rows (q_out may be q)."""
     n, dev = cache._batch, cache._device
     kv = _q4_spread(cache, layer_count, cache._heads, rows, k, v)
-    qs = _q4_spread(cache, layer_count, cache._query[1], rows, q, q_out) if q is not None and q_out is not None else [None, None]
+    qs = (None, None) if q is None or q_out is None else _q4_spread(cache, layer_count, cache._query[1], rows, q, q_out)
     if (kv is None or qs is None or (q is None) != (q_out is None) or not _q4_ok(positions, torch.int32, rotary.axes * n * rows, dev)
-            or not (_q4_ok(first, torch.int32, n, dev) and _q4_ok(count, torch.int32, n, dev))):
+            or (first is not None and not _q4_ok(first, torch.int32, n, dev)) or (count is not None and not _q4_ok(count, torch.int32, n, dev))):
         raise KVError("kv_q4_store_rotary", KV_ERR_INVALID_ARG)
     tail = _q4_tail("kv_q4_store_rotary", cache, ws, stream)
     _check("kv_q4_store_rotary", load_library().kv_q4_store_rotary(

@@ -4,14 +4,15 @@
 // x sin + y cos); the other elements pass.  The pairs are elements i and i + dim / 2, or 2 i and 2 i + 1.  Queries are written
 // rotated, keys are quantised from their rotated values, values as they are (q4_rows.hip).
 //
-// Angles, their cosine and sine and the rotation are in 64 bits: a position of 20 bits times a frequency takes 44, and a code is
-// then the nearest to the exact rotated element, where 32 bits would choose a neighbour for one element in millions.  Results
-// are rounded once: to 32 bits with the last bit set where something was cut off (to odd), so that every rounding after it (to
-// bf16, to a code: fewer bits by two at least) sees on which side of a border the 64-bit value lies.
+// Angles, their cosine and sine and the rotation of keys are in 64 bits: a position of 20 bits times a frequency takes 44, and a code
+// is then the nearest to the exact rotated element, where 32 bits would choose a neighbour for one element in millions.  They are
+// rounded once, to 32 bits with the last bit set where something was cut off (to odd), so that the rounding to a code, of fewer bits
+// by far, sees on which side of a border the 64-bit value lies.  Queries, which no border cuts, are turned in 32 bits by cosines
+// and sines rounded from 64 (13,000 tokens of 28/4 heads: 69.5 us with everything in 64 bits, of which the conversions were most).
 //
 // A workgroup takes the rows of 512 / D tokens of one layer, a wave one head of them at a time, a lane 8 elements: the tokens'
-// cosines and sines are made once, in LDS, and stay in a lane's registers over all heads.  The partners are loaded beside the
-// elements (from the same lines: the second load comes from the cache).
+// cosines and sines are made once, in LDS, and stay in a lane's registers over the queries' heads.  The partners are loaded beside
+// the elements (from the same lines: the second load comes from the cache).
 #include "kv_common.h"
 #include "q4.h"
 #include "q4_block.h"
@@ -96,73 +97,93 @@ __global__ __launch_bounds__(kRotaryThreads) void q4_rotary_kernel(Q4RotaryArgs 
     }
     __syncthreads();
 
-    // what the lane's elements are multiplied with, and their partners with
-    double c[2][4], s[2][4];
-    int partner[2];  // first of a run's partners (neighbours: the run itself)
-    bool turned[2];
+    // where the partners of the lane's two runs of four begin (neighbours: the run itself), and what an element and its partner are
+    // multiplied with
+    int partner[2];
+    bool turned[2], low[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int e = run_of<T, D>(p, h);
         turned[h] = e < a.dim;
-        const bool low = a.adjacent || e < pairs;
-        partner[h] = !turned[h] || a.adjacent ? e : low ? e + pairs : e - pairs;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = a.adjacent ? (e + i) / 2 : low ? e + i : e + i - pairs;
-            const double2 x = turn[lane / kLanes][turned[h] ? k : 0];
-            c[h][i] = x.x;
-            s[h][i] = (a.adjacent ? i % 2 == 0 : low) ? -x.y : x.y;
-        }
+        low[h] = a.adjacent || e < pairs;
+        partner[h] = !turned[h] || a.adjacent ? e : low[h] ? e + pairs : e - pairs;
     }
-    // the row at `from`, rotated
-    auto rotated = [&](const T* from, double (&x)[kElems]) __attribute__((always_inline)) {
-        float own[2][4], other[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            read4(from + run_of<T, D>(p, h), own[h]);
-            read4(from + partner[h], other[h]);
-        }
+    auto factors = [&](int h, int i) __attribute__((always_inline)) {
+        const int e = run_of<T, D>(p, h), k = a.adjacent ? (e + i) / 2 : low[h] ? e + i : e + i - pairs;
+        double2 x = turn[lane / kLanes][turned[h] ? k : 0];
+        if (a.adjacent ? i % 2 == 0 : low[h]) x.y = -x.y;
+        return x;
+    };
+    const int first = blockIdx.z * kRotaryWaves + wave, stride = gridDim.z * kRotaryWaves, queries = a.q ? d.hq : 0;
+    // the queries' heads, two at a time: their loads together
+    if (wanted && first < queries) {
+        float c[2][4], s[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float y = a.adjacent ? own[h][i ^ 1] : other[h][i];
-                x[4 * h + i] = turned[h] ? (double)own[h][i] * c[h][i] + (double)y * s[h][i] : (double)own[h][i];
+                const double2 x = factors(h, i);
+                c[h][i] = (float)x.x;
+                s[h][i] = (float)x.y;
             }
-    };
-
-    const int heads = (a.q ? d.hq : 0) + 2 * d.hkv;  // the queries', the keys' and the values'
-    for (int u = blockIdx.z * kRotaryWaves + wave; u < heads; u += gridDim.z * kRotaryWaves) {
-        const int key = u - (a.q ? d.hq : 0);
-        if (key < 0) {
-            if (!wanted) continue;
-            double x[kElems];
-            rotated(static_cast<const T*>(a.q) + layer * a.qs[0] + b * a.qs[1] + u * a.qs[2] + r * a.qs[3], x);
-            T* out = static_cast<T*>(a.q_out) + layer * a.os[0] + b * a.os[1] + u * a.os[2] + r * a.os[3];
-            if constexpr (sizeof(T) == 2) {
-                u32x4 w;
+        const T* const from = static_cast<const T*>(a.q) + layer * a.qs[0] + b * a.qs[1] + r * a.qs[3];
+        T* const to = static_cast<T*>(a.q_out) + layer * a.os[0] + b * a.os[1] + r * a.os[3];
+        for (int u = first; u < queries; u += 2 * stride) {
+            float own[2][2][4], other[2][2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = pack_bf16(to_odd(x[2 * i]), to_odd(x[2 * i + 1]));
-                reinterpret_cast<u32x4*>(out)[p] = w;
-            } else {
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const T* const row = from + min(u + j * stride, queries - 1) * a.qs[2];
+                    read4(row + run_of<T, D>(p, h), own[j][h]);
+                    read4(row + partner[h], other[j][h]);
+                }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (u + j * stride >= queries) break;
+                float x[kElems];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    *reinterpret_cast<f32x4*>(out + run_of<T, D>(p, h)) =
-                        f32x4{(float)x[4 * h], (float)x[4 * h + 1], (float)x[4 * h + 2], (float)x[4 * h + 3]};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = a.adjacent ? own[j][h][i ^ 1] : other[j][h][i];
+                        x[4 * h + i] = turned[h] ? fmaf(y, s[h][i], own[j][h][i] * c[h][i]) : own[j][h][i];
+                    }
+                T* const out = to + (u + j * stride) * a.os[2];
+                if constexpr (sizeof(T) == 2) {
+                    reinterpret_cast<u32x4*>(out)[p] = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        *reinterpret_cast<f32x4*>(out + run_of<T, D>(p, h)) = f32x4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+                }
             }
-            continue;
         }
-        if (!stored) continue;
-        const bool value = key >= d.hkv;
-        const int g = value ? key - d.hkv : key;
+    }
+    // the keys' heads and the values'
+    if (!stored) return;
+    for (int u = first < queries ? first + (queries - first + stride - 1) / stride * stride : first; u < queries + 2 * d.hkv; u += stride) {
+        const bool value = u - queries >= d.hkv;
+        const int g = value ? u - queries - d.hkv : u - queries;
         float x[kElems];
         if (value) {
             read8<T, D>(static_cast<const T*>(a.rows.v) + layer * a.rows.vs[0] + b * a.rows.vs[1] + g * a.rows.vs[2] + r * a.rows.vs[3], p, x);
         } else {
-            double y[kElems];
-            rotated(static_cast<const T*>(a.rows.k) + layer * a.rows.ks[0] + b * a.rows.ks[1] + g * a.rows.ks[2] + r * a.rows.ks[3], y);
+            const T* const row = static_cast<const T*>(a.rows.k) + layer * a.rows.ks[0] + b * a.rows.ks[1] + g * a.rows.ks[2] + r * a.rows.ks[3];
+            float own[2][4], other[2][4];
 #pragma unroll
-            for (int i = 0; i < kElems; ++i) x[i] = to_odd(y[i]);
+            for (int h = 0; h < 2; ++h) {
+                read4(row + run_of<T, D>(p, h), own[h]);
+                read4(row + partner[h], other[h]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double2 f = factors(h, i);
+                    const float y = a.adjacent ? own[h][i ^ 1] : other[h][i];
+                    x[4 * h + i] = turned[h] ? to_odd((double)own[h][i] * f.x + (double)y * f.y) : own[h][i];
+                }
         }
         uint8_t* rec = a.rows.cache.pool + q4_record(d, a.rows.layer0 + layer, page, g);
         uint32_t scales;

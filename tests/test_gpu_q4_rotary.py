@@ -1,8 +1,9 @@
 """Rows rotated into the paged 4-bit cache, against the rotation in numpy's 64 bits and the plain quantiser.
 
 Tolerances.  Both sides rotate in 64 bits, so a stored element is the same code unless the rotated one lies within some 2^-50 of a
-border between two: codes are compared for equality.  A query is the 64-bit value rounded once: off by half a step of its type,
-finfo.eps / 2 of itself, and by the two sides' 64-bit roundings, 2^-50 of the pair's size."""
+border between two: codes are compared for equality.  A query is turned in 32 bits: its cosine or sine, a product and the sum are
+each off by 2^-24, so the result by 3 * 2^-24 of the pair's size |x| + |y| (times the scale); then half a step of its type, finfo.eps / 2
+of itself, of which 2^-24 is the sum's already in float32 and one part in 2^24 more is allowed for what it is half a step of."""
 import numpy as np
 import pytest
 import torch
@@ -60,7 +61,7 @@ def check(t, k, v, q, out, pos, freq, axis, adjacent, scale, counts, layer0=0, f
                 continue
             x, got = q[l, b].double().cpu().numpy(), out[l, b].double().cpu().numpy()
             want = rotate(x[:, :m], pos[:, b, :m], freq, axis, adjacent, scale)
-            lim = eps * np.abs(want) + 2.0 ** -50 * pair_size(x[:, :m], dim, adjacent, scale)
+            lim = eps * np.abs(want) * (1 + 2.0 ** -20) + 3 * 2.0 ** -24 * pair_size(x[:, :m], dim, adjacent, scale)
             assert (np.abs(got[:, :m] - want) <= lim).all(), (l, b, np.abs(got[:, :m] - want).max())
             assert np.array_equal(got[:, :m, dim:], x[:, :m, dim:])
             assert left is None or (got[:, m:] == left).all()
@@ -153,7 +154,8 @@ def test_rows_that_are_not_stored():
     assert t.faults() == B.KV_FAULT_CACHE | B.KV_FAULT_SHARED_PAGE
     for b in range(3):
         want = rotate(q[0, b].double().cpu().numpy(), pos[:, b].cpu().numpy(), freq, axis, False, 1.0)
-        assert (np.abs(out[0, b].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 1e-12).all()
+        size = 3 * 2.0 ** -24 * pair_size(q[0, b].double().cpu().numpy(), 128, False, 1.0)
+        assert (np.abs(out[0, b].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) * (1 + 2.0 ** -20) + size).all()
     t.c.table.copy_(table)
     old, new = (R.Pool(t.shape, x.cpu().numpy()) for x in (before, t.c.pool))
     want = R.fast_values(rotate(k[0, 0, :, :2].double().cpu().numpy(), pos[:, 0, :2].cpu().numpy(), freq, axis, False, 1.0))
