@@ -612,22 +612,34 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         }
         // running maxima, probabilities, their parts
         u32x4 high[CT], mid[kP == 3 ? CT : 1], low[kP == 3 ? CT : 1];
+        // (one branch for all column tiles: a maximum is raised in a few tiles only.  A column tile that is left out has logits 0 here,
+        // and its maximum is not looked at again until it takes part.)
+        float top[CT];
+        bool raise = false;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            if (skipped(ct)) continue;
-            float top = max3(z[ct][0][0], z[ct][0][1], z[ct][0][2]);
-            top = max3(top, z[ct][0][3], z[ct][1][0]);
-            top = max3(top, z[ct][1][1], z[ct][1][2]);
-            top = max3(top, z[ct][1][3], z[ct][1][3]) * a.scale2;
-            if (__any(top > m[ct] + kSlack)) {
-                top = rows_allmax(top);
-                const float raised = top > m[ct] + kSlack ? top : m[ct];
+            top[ct] = max3(z[ct][0][0], z[ct][0][1], z[ct][0][2]);
+            top[ct] = max3(top[ct], z[ct][0][3], z[ct][1][0]);
+            top[ct] = max3(top[ct], z[ct][1][1], z[ct][1][2]);
+            top[ct] = max3(top[ct], z[ct][1][3], z[ct][1][3]) * a.scale2;
+            raise |= top[ct] > m[ct] + kSlack && !skipped(ct);
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if (skipped(ct)) continue;
+                const float all_top = rows_allmax(top[ct]);
+                const float raised = all_top > m[ct] + kSlack ? all_top : m[ct];
                 const float f = exp2_hw(m[ct] - raised);
                 m[ct] = raised;
                 l[ct] *= f;
 #pragma unroll
                 for (int e = 0; e < kOut; ++e) acc[ct][e] *= f;
             }
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            if (skipped(ct)) continue;
             float p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) p[j] = exp2_hw(fmaf(z[ct][j / 4][j % 4], a.scale2, -m[ct]));
