@@ -126,8 +126,8 @@ struct Q4QueryArgs {
     int64_t qs[4], os[4];    // strides in elements: layer, slot, query head, row
     float scale2;            // log2(e) / sqrt(d)
     int stat_at, q_at;       // floats of LDS before the waves' statistics and the queries (set by the launch)
-    float2* part;            // several chunks: [unit][chunk][column] (max, sum); unit: a (layer, slot, block, KV head)
-    float* opart;            // several chunks: [unit][chunk][column][d] unnormalised partial outputs
+    float2* part;            // several chunks: [layer][slot][row][query head][chunk] (max, sum)
+    float* opart;            // several chunks: likewise, and [d]: unnormalised partial outputs (not written where the sum is 0)
     uint32_t* faults;
     // window
     int rows, window, sinks;

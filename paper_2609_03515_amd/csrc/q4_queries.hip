@@ -4,16 +4,25 @@
 // window, p > P - window, or among the first, p < sinks.  Shared: one query of each of several slots; where their tables name the
 // same page it is read and converted once for all of them.
 //
-// A block of queries is one or more column tiles, each `per` queries of the group's heads in 16 columns; the tiles of 32 rows, their
-// products, probabilities and values are those of the decode attention (q4_attend.hip), with each converted tile used by every
-// column tile.  A workgroup takes a block and one KV head; its waves take the block's tiles of rows in turn, each with a running
-// maximum, sum and output of its own, joined at the end.  Where there are few blocks their tiles are divided among workgroups, whose
-// parts a second kernel joins.
+// With z = q . k / sqrt(d) log2(e), a wave keeps for each query m >= max z - kSlack, l = sum 2^(z - m) and acc = sum 2^(z - m) v in
+// 32 bits and passes over its rows once; (m, l, acc) of two sets of rows join as m = max(m1, m2), l = l1 2^(m1 - m) + l2 2^(m2 - m).
 //
-// Which tiles: without positions the rows are in order, and the tiles of a window are two runs.  With positions (an eviction leaves
-// rows of any position in any place) a kernel before this one marks the tiles of which a block sees any row, a bit each; a wave
-// looks at 64 of its tiles at a time, one a lane.  Shared: a lane looks at a tile of one slot, and at the table entries of the block's
-// other slots there.
+// A block of queries is one to four column tiles, each `per` queries of the group's heads in 16 columns (per = 16 / group); the tiles of
+// 32 rows, their products, probabilities and values are those of the decode attention (q4_attend.hip), with each converted tile used
+// by every column tile.  A workgroup takes a block and one KV head; its waves take the block's tiles of rows in turn, each with a running maximum, sum and output of its own, joined
+// in LDS at the end.  Where there are few blocks their tiles are divided among workgroups, whose parts a second kernel joins (4 us).
+//
+// Which tiles: a wave looks at 64 of its tiles at a time, one a lane, and reads the pages of all of them with one load each.  Without
+// positions the rows are in order, and the tiles of a window are found from row numbers.  With positions (an eviction leaves rows of any
+// position in any place) the wave reads the positions of its tiles' rows; where it would have many of them a kernel before this one
+// marks the tiles of which a block sees any row, a bit each, once for all layers and heads.  Shared: a lane looks at a tile of one slot,
+// and at the table entries of the block's other slots there; the first slot with a page has the tile for all that have it.
+//
+// What bounds it.  One query of each of a few slots, and short windows: latency, the dependent loads len -> table -> records (0.6 to
+// 0.8 us each), one tile's 1.1 us, the start of a workgroup, and the join; the 8B layer at its budget takes 13 us and a join of 4.5, its
+// bytes 1.9.  Many shared pages: the bytes of the pages that are read, each once (32 layers of 8 evicted samples: 206 MB, 68 us, 3.0 TB/s
+// with what the join of eight waves takes).  A long chunk: the matrix instructions and what feeds them (2,048 queries on 32,768 rows, 8 KV
+// heads of 4: 1,100 us, 968 TFLOP/s of the 1,195 that a large product reaches).
 //
 // Masked rows get the logit -inf.  A masked row's values may be NaN (a block stored from infinities); 0 times them would spoil the
 // column, so tiles that hold such blocks take a side path: the blocks are taken as numbers, and a product of two 0/1 matrices finds
@@ -156,7 +165,10 @@ struct KeyTile {
 };
 
 // Column tiles (CT) of 16; parts of a probability (kP): 3 take all of its 24 bits, 1 rounds it to bf16 (8 bits, to nearest; its
-// sum is of the rounded numbers).  kWaves: of a workgroup, which divide a block's tiles and join their outputs; or one.
+// sum is of the rounded numbers, so that a row of equal values comes out exact).  Blocks of bf16 queries round: a weight is off by
+// 2^-8 of itself at most, as a bf16 output is, and its error in an average over many rows is less; with 3 parts a chunk of 2,048 queries on
+// 32,768 rows takes 2,391 us, rounded 1,103.  Where one column tile is enough nothing waits for the products, and they are exact (the 8B
+// layer 18.0 us, rounded 16.9).  kWaves: of a workgroup, which divide a block's tiles and join their outputs.
 template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
 __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void q4_query_kernel(Q4QueryArgs a) {
     constexpr int kThreads = kWave * kWaves;
@@ -528,6 +540,9 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         auto skipped = [&](int ct) __attribute__((always_inline)) {
             return kShared && CT > 1 && !(active >> (ct * per) & ((1u << per) - 1));
         };
+        // Two waves meet on a SIMD; one that is past its logits goes first, so that they do not run side by side through the products
+        // and then through the exponentials (a chunk of 2,048 queries on 32,768 rows 1,180 us without, 1,100 so).
+        if constexpr (CT == 4) __builtin_amdgcn_s_setprio(0);
         // logits
         f32x4 z[CT][2];
 #pragma unroll
@@ -556,6 +571,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
                 }
             }
         }
+        if constexpr (CT == 4) __builtin_amdgcn_s_setprio(1);
         const int tile_pos = keys.pos;
         // the lane's rows that its column does not see, a bit each: bit j is row 4 (j % 4) + s of half j / 4.  (Without branches: the
         // compiler, ROCm 7.2's, dropped the first element's store from the same conditions joined by ||.)
@@ -960,7 +976,7 @@ int chunks_of(int64_t units, int64_t tiles, int waves, int want) {
 
 // Forms.  One column tile: four waves, two workgroups for a CU (the 8B layer at its budget 18.0 us; one 20.4, four 18.9; eight waves
 // 19.4).  Two: four waves, as many workgroups as fit a CU, three (128 queries on 32,768 rows 105 us, two 114).  Four, each of two waves,
-// where there are four blocks for a CU, as many as it holds: a chunk of 2,048 queries on 32,768 rows 1,210 us, with two column tiles
+// where there are four blocks for a CU, as many as it holds: a chunk of 2,048 queries on 32,768 rows 1,100 us, with two column tiles
 // 1,286; 8 prompts of 1,024 rows 109 and 117; but 64 queries on each of 8 x 4,096 rows 68 and 61.
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks) {
     Q4QueryPlan p{};
