@@ -412,8 +412,9 @@ typedef struct {
  * beside them: row r < count[b] of q [layer][batch][query head][row][d] is written rotated to the same row of q_out, in the
  * shape's type; the other rows of q_out are left as they were.  q and q_out are both null (no queries), or not; q_out may be q
  * itself, with the same strides.  Angles, their cosines and sines and the rotation of keys are in 64 bits: a stored key is the
- * nearest to the exact rotated one; queries are rotated in 32 bits and rounded to the shape's type.  Queries are written for every row r < min(count[b], rows), whatever becomes of
- * its key.  count, first, faults and limits as kv_q4_store, and batch * rows at most 2^25 (KV_ERR_UNSUPPORTED). */
+ * nearest to the exact rotated one; queries are rotated in 32 bits and rounded to the shape's type.  Queries are written for
+ * every row r < min(count[b], rows), whatever becomes of its key.  count, first, faults and limits as kv_q4_store, and
+ * batch * rows at most 2^25 (KV_ERR_UNSUPPORTED). */
 kv_status kv_q4_store_rotary(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
                              int32_t rows, const int32_t* first, const int32_t* count, const kv_rotary* rotary,
                              const int32_t* positions, const void* k, const kv_q4_strides* k_strides, const void* v,
@@ -457,7 +458,8 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
 /* kv_q4_attend (without a bias and scores) for slots that share pages, as the samples of a prompt do after kv_q4_fork: where the
  * tables of slots of one group name the same page at the same place, it is read and converted once for several of them.  group
  * [batch]: slots with equal numbers are a group (any numbers: those that share nothing only cost time, and those that share
- * pages in different groups read them once each).  Pages that an eviction replaced in some samples are read for those.
+ * pages in different groups read them once each).  Pages that an eviction replaced in some samples are read for those.  Probabilities
+ * of bf16 calls may be rounded as kv_q4_attend_window's.
  * Workspace: kv_q4_shared_workspace_bytes.  Refused as kv_q4_attend_window. */
 kv_status kv_q4_shared_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t layer_count, size_t* bytes);
 kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,
