@@ -13,6 +13,10 @@
 // A workgroup takes the rows of 512 / D tokens of one layer, a wave one head of them at a time, a lane 8 elements: the tokens'
 // cosines and sines are made once, in LDS, and stay in a lane's registers over the queries' heads.  The partners are loaded beside
 // the elements (from the same lines: the second load comes from the cache).
+//
+// What bounds it: with many rows the memory (one layer of some 13,000 tokens of 28 query and 4 KV heads, three axes: 58 us for 223 MB,
+// 3.8 TB/s; queries alone 4.2 TB/s; with nothing written 38 us); with few, one token of 8 slots in 32 layers, latency (7.2 us: the launch
+// and a chain of count and length, page, rows).
 #include "kv_common.h"
 #include "q4.h"
 #include "q4_block.h"

@@ -1,5 +1,7 @@
 """Rotated rows and the attention of windows and shared pages without a GPU: the interface's refusals (every call here is refused
 on the host, so nothing is queued)."""
+import re
+
 import pytest
 import torch
 
@@ -168,3 +170,17 @@ def test_binding_refuses_attention_of_other_layouts():
     for x, y, g in ((flat, flat, group), (flat.float(), flat, group), (flat, q, group), (flat, flat, group[:2]), (flat, flat, group.long()), (flat, flat, None)):
         with pytest.raises(B.KVError):
             B.kv_q4_attend_shared(c, 0, 1, 10, g, x, y, ws)
+
+
+def test_registers():
+    """The kernels keep the waves per SIMD that their plans count on: four with one column tile (128 of 512 registers), three with two,
+    two with four, and spill next to nothing; the rotation holds nothing in memory."""
+    import test_kernel_resources as K
+
+    objs = K.code_object(open(B.LIB_PATH, "rb").read())
+    seen = {k[".name"]: k for o in objs for k in K.metadata(o)["amdhsa.kernels"] if "q4_query_kernel" in k[".name"] or "q4_rotary_kernel" in k[".name"]}
+    forms = {name: int(re.search(r"Li(?:64|128)ELi(\d)E", name).group(1)) for name in seen if "q4_query" in name}
+    assert len(forms) == 16 and len(seen) == 20
+    for name, tiles in forms.items():
+        assert seen[name][".vgpr_count"] <= {1: 128, 2: 168, 4: 256}[tiles] and seen[name][".vgpr_spill_count"] <= 7, name
+    assert all(k[".vgpr_spill_count"] == 0 and k[".vgpr_count"] <= 128 for name, k in seen.items() if name not in forms)
