@@ -159,6 +159,37 @@ def test_two_calls_at_once():
     S.check(t, one, alone[1])
 
 
+def test_graphs_that_share_a_workspace():
+    """A graph of one attention and one of the other in the same workspace, replayed in turn, with a form whose workgroups need more LDS
+    than the default limit met for the first time while capturing."""
+    t = S.samples([130], 12, 2, layers=32, hq=16, hkv=8, d=64, page_rows=32)  # (workgroups of eight waves)
+    batch = t.shape.batch
+    ws = torch.zeros(max(t.sws.numel(), B.kv_q4_window_workspace_bytes(t.shape, t.cap, 70, 32)), dtype=torch.uint8, device="cuda")
+    t.c.pos.copy_(torch.arange(t.cap, dtype=torch.int32).expand(batch, t.cap))
+    t.sws = t.wws = ws
+    q = torch.randn(32, batch, 16, 70, 64, generator=gen(2)).bfloat16().cuda()
+    one, group = q[:, :, :, 3].contiguous(), i32([0] * batch)
+    o, o2 = torch.empty_like(q), torch.empty_like(one)
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graphs[0]):
+        B.kv_q4_attend_shared(t.c, 0, 32, t.cap, group, one, o2, ws)
+    with torch.cuda.graph(graphs[1]):
+        B.kv_q4_attend_window(t.c, 0, 32, t.cap, 70, q, o, ws, window=40, sinks=2)
+    for _ in range(3):
+        o.fill_(9.0)
+        o2.fill_(9.0)
+        for g in graphs:
+            g.replay()
+        _ = (t.c.u * 2).sum().item()
+        e, e2 = torch.full_like(o, 9.0), torch.full_like(o2, 9.0)
+        B.kv_q4_attend_shared(t.c, 0, 32, t.cap, group, one, e2, ws)
+        B.kv_q4_attend_window(t.c, 0, 32, t.cap, 70, q, e, ws, window=40, sinks=2)
+        assert torch.equal(o, e) and torch.equal(o2, e2)
+    S.check(t, one[:3], o2[:3])
+    W.check(t, q[:3], o[:3], 70, None, 40, 2)
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 2^32 bytes: rows stored and attended to in its last pages."""
     layers, pages = 2, 1 << 17
