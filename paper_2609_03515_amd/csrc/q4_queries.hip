@@ -412,6 +412,8 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         if constexpr (kShared) {
             const int V = late.plan.vectors, own = lane & ((1 << late.plan.vector_shift) - 1);
             const bool pairs = late.dims.page_rows < kTile;
+            // The slots' rows, one a lane (-1: no slot), taken from there: from LDS for each one layer of 16 samples took 22.9 us, so 21.8.
+            const int n = lane < V && member_of[min(lane, V - 1)] >= 0 ? rows_of[min(lane, V - 1)] : -1;
             mask_of = 0;
             for (int v0 = 0; v0 < V; v0 += kTogether) {
                 if (v0) load_entries(late, row_of, v0, held);
@@ -419,9 +421,8 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
                 if (pairs) load_entries(late, min(row_of + 16, late.dims.cap - 1), v0, second);
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) {
-                    const int v = min(v0 + i, V - 1);
-                    const bool same = held[i] == page_of && (!pairs || rows_in <= 16 || second[i] == page_of2) && member_of[v] >= 0 &&
-                                      min(kTile, rows_of[v] - row_of) == rows_in;
+                    const int v = min(v0 + i, V - 1), left_of = __builtin_amdgcn_readlane(n, v) - row_of;
+                    const bool same = held[i] == page_of && (!pairs || rows_in <= 16 || second[i] == page_of2) && min(kTile, left_of) == rows_in;
                     mask_of |= (uint32_t)same << v;
                 }
             }
