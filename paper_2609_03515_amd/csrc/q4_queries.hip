@@ -987,22 +987,26 @@ int chunks_of(int64_t units, int64_t tiles, int waves, int want) {
 
 // Forms.  One column tile: four waves, two workgroups for a CU (the 8B layer at its budget 18.0 us; one 20.4, four 18.9; eight waves
 // 19.4).  Two: four waves, as many workgroups as fit a CU, three (128 queries on 32,768 rows 105 us, two 114).  Four, each of two waves,
-// where there are four blocks for a CU, as many as it holds: a chunk of 2,048 queries on 32,768 rows 1,100 us, with two column tiles
-// 1,286; 8 prompts of 1,024 rows 109 and 117; but 64 queries on each of 8 x 4,096 rows 68 and 61.
+// as many as a CU holds, where the blocks have 240 tiles of rows for a CU, of all slots' queries and as many rows as n_max allows (one
+// slot of 32/8 heads, four column tiles and two: 2,048 queries on 32,768 rows 1,095 us and 1,286, 1,024 574 and 689, 256 165 and 186;
+// on 8,192 rows 512 queries 97 and 103, 256 61.4 and 61.7, 128 48 and 37; 2,048 on 2,048 82 and 70; 8 prompts of 1,024 132 and 157).
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
     const int64_t slabs = (int64_t)layer_count * d.batch * d.hkv;
-    auto blocks = [&](int tiles) { return (rows + tiles * p.per - 1) / (tiles * p.per); };
-    p.tiles = !d.bf16 || rows <= p.per ? 1 : slabs * blocks(4) < 4 * cus_of() ? 2 : 4;
+    auto blocks = [&](int rows, int tiles) { return (rows + tiles * p.per - 1) / (tiles * p.per); };
+    // tiles of n rows that a block sees: with a window (of rows in order) those of it, which ends inside tiles
+    auto seen = [&](int n, int vectors) {
+        const int64_t all = (n + kTile - 1) / kTile, some = ((int64_t)window + sinks + vectors) / kTile + 3;
+        return window && some < all ? some : all;
+    };
+    const int most = rows < n_max ? rows : n_max;
+    const bool long_blocks = (double)slabs * blocks(most, 4) * (double)seen(n_max - most / 2, 4 * p.per) >= 240.0 * cus_of();
+    p.tiles = !d.bf16 || rows <= p.per ? 1 : long_blocks ? 4 : 2;
     p.waves = p.tiles == 4 ? 2 : 4;
     p.vectors = p.tiles * p.per;
-    p.blocks = blocks(p.tiles);
-    int64_t tiles = (n_max + kTile - 1) / kTile;
-    if (window) {  // (rows in order, in a window that ends inside tiles)
-        const int64_t seen = ((int64_t)window + sinks + p.vectors) / kTile + 3;
-        tiles = tiles < seen ? tiles : seen;
-    }
+    p.blocks = blocks(rows, p.tiles);
+    const int64_t tiles = seen(n_max, p.vectors);
     p.chunks = chunks_of(slabs * p.blocks, tiles, p.waves, (p.tiles == 1 ? 2 : p.tiles == 2 ? 3 : 4) * cus_of());
     // a wave that looks at more than three times 16 tiles finds them by marks: a kernel before it, 5 us, that all layers and heads share
     p.marks = p.blocks > 1 && (n_max + kTile - 1) / kTile > 48 * p.chunks * p.waves;

@@ -335,3 +335,96 @@ def test_captured_and_replayed():
         check(t, q, o, 20, c, 50, 3)
         side.synchronize()
         check(other, q2, o2, 4, None, 10, 1)
+
+
+# ---- blocks of four column tiles: bf16 calls whose n_max and queries allow for work for the whole GPU --------------------------------
+
+def roomy(lens, rows, places, page_rows=16, **kw):
+    """A cache whose slots could hold 131,072 rows each."""
+    return cache(lens, rows, places, page_rows=page_rows, max_pages=131072 // page_rows, **kw)
+
+
+@pytest.mark.parametrize("hq,hkv,d,page_rows", [(8, 8, 128, 16), (28, 4, 128, 32), (16, 4, 64, 16), (16, 1, 128, 256), (6, 2, 64, 64), (40, 8, 128, 128)])
+@pytest.mark.parametrize("places", ["rows", "ordered", "evicted", "any"])
+def test_long_blocks(hq, hkv, d, page_rows, places):
+    lens = [700, 0, 41, 1, 333]
+    for rows, counts, window, sinks in ((70, None, 0, 0), (70, [70, 0, 41, 1, 7], 90_000, 3000), (130, [130, 0, 3, 0, 129], 0, 0)):
+        t = roomy(lens, rows, places, page_rows, layers=2, hq=hq, hkv=hkv, d=d)
+        q, o = run(t, rows, counts, window, sinks)
+        check(t, q, o, rows, counts, window, sinks)
+
+
+@pytest.mark.parametrize("places", ["rows", "ordered", "any"])
+@pytest.mark.parametrize("window,sinks", [(300, 0), (303, 17), (331, 64)])
+def test_long_blocks_in_windows(window, sinks, places):
+    """Windows that end in several places of a tile, of so many slots and layers that they are worth four column tiles."""
+    lens, rows = [350, 401, 70, 290] * 4, 70
+    t = cache(lens, rows, places, layers=8, hq=32, hkv=8, page_rows=32)
+    q, o = run(t, rows, None, window, sinks)
+    check(t, q[:1], o[:1], rows, None, window, sinks)
+    check(t, q[7:], o[7:], rows, None, window, sinks, layer0=7)
+
+
+def test_long_sequences_in_long_blocks():
+    """Divided among workgroups, many tiles to a wave."""
+    for hq, hkv, layers, rows in ((32, 8, 8, 128), (14, 2, 30, 130)):
+        t = cache([4100], rows, "rows", layers=layers, hq=hq, hkv=hkv, page_rows=64)
+        q, o = run(t, rows, None, 0, 0)
+        check(t, q[:1], o[:1], rows, None, 0, 0)
+        check(t, q[layers - 1 :], o[layers - 1 :], rows, None, 0, 0, layer0=layers - 1)
+
+
+@pytest.mark.parametrize("places", ["rows", "ordered"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_masked_rows_that_are_not_numbers_in_long_blocks(d, places):
+    t = roomy([80, 80], 70, places, hq=16, hkv=4, d=d)
+    k, v = (torch.randn(1, 2, 4, 80, d, generator=gen(s)).bfloat16() for s in (1, 2))
+    k[0, 0, :, 75, 3] = float("inf")
+    v[0, 0, 1, 30, 40] = float("nan")
+    v[0, 1, :, 79, 10] = float("-inf")
+    B.kv_q4_store(t.c, 0, 1, 80, k.cuda(), v.cuda(), t.ws)
+    q, o = run(t, 70, None, 0, 0)
+    o = torch.isnan(o[0].float()).cpu()
+    want = torch.zeros_like(o)
+    want[0, :, 65:] = True           # queries at 75 and behind
+    want[0, 4:8, 20:, 32:64] = True  # KV head 1, queries at 30 and behind
+    want[1, :, 69, :32] = True
+    assert torch.equal(o, want)
+    B.kv_q4_store(t.c, 0, 1, 80, torch.nan_to_num(k, nan=0.0, posinf=0.0).cuda(), torch.nan_to_num(v, nan=0.0, neginf=0.0).cuda(), t.ws)
+    q, o = run(t, 70, None, 0, 0)
+    check(t, q, o, 70, None, 0, 0)
+
+
+def test_slots_that_cannot_be_in_long_blocks():
+    t = roomy([90, 90, 90, 90, 96], 70, "rows", hq=16, hkv=4)
+    t.c.len.copy_(i32([90, 90, 90, t.cap + 1, 96]))
+    t.c.table[4, 1] = t.shape.n_pages + 7  # rows 16 .. 31
+    q, o = run(t, 70, [70, -1, 71, 1, 60], 0, 0)
+    assert (o[:, 1:4] == 0).all() and B.faults(t.wws, clear=True) == B.KV_FAULT_CACHE
+    for b, count, gone in ((0, 70, ()), (4, 60, range(16, 32))):
+        t.c.table[4, 1] = 0
+        k, v = t.values(0, b)
+        n = k.shape[1]
+        seen = seen_of(np.arange(n), n, count, 0, 0)
+        seen[:, list(gone)] = False
+        want, size, av = reference(q[0, b].double().cpu().numpy()[:, :count], k, v, seen)
+        assert (np.abs(o[0, b, :, :count].double().cpu().numpy() - want) <= limits(t, want, size, av, n, 70)).all()
+        assert (o[0, b, :, count:] == 9.0).all()
+
+
+def test_long_blocks_captured_and_replayed():
+    t = roomy([300, 200], 70, "evicted", layers=2, hq=16, hkv=4)
+    q = torch.randn(2, 2, 16, 70, 128, generator=gen(3)).bfloat16().cuda()
+    o, count = torch.full_like(q, 9.0), i32([70, 70])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.kv_q4_attend_window(t.c, 0, 2, t.cap, 70, q, o, t.wws, window=100_000, sinks=3, count=count)
+    for i, (n, c) in enumerate((([300, 200], [70, 1]), ([77, 199], [0, 70]), ([1, 200], [1, 7]))):
+        t.c.len.copy_(i32(n))
+        count.copy_(i32(c))
+        t.c.pos.copy_(torch.stack([torch.randperm(t.cap, generator=gen(20 + i)) for _ in n]).to(torch.int32))
+        o.fill_(9.0)
+        graph.replay()
+        _ = (t.c.u * 2).sum().item()
+        check(t, q, o, 70, c, 100_000, 3)
