@@ -21,9 +21,9 @@
 //
 // What bounds it.  One query of each of a few slots, and short windows: latency, the dependent loads len -> table -> records (0.6 to
 // 0.8 us each), one tile's 1.1 us, the start of a workgroup, and the join; the 8B layer at its budget takes 13 us and a join of 4.5, its
-// bytes 1.9.  Many shared pages: the bytes of the pages that are read, each once (32 layers of 8 evicted samples: 206 MB, 68 us, 3.0 TB/s
-// with what the join of eight waves takes).  A long chunk: the issue of vector instructions (2,048 queries on 32,768 rows, 8 KV heads of 4
-// heads: 1,100 us, 968 TFLOP/s where a product of 8,192 x 8,192 matrices reaches 1,447).  There a tile of 32 rows takes a wave 373 of them
+// bytes 1.9.  Many shared pages: the bytes of the pages that are read, each once (32 layers of 8 evicted samples: 206 MB, 65 us, 3.2 TB/s
+// with each workgroup's start and the join of its eight waves).  A long chunk: the issue of vector instructions (2,048 queries on 32,768 rows, 8 KV heads of 4
+// heads: 1,092 us, 976 TFLOP/s where a product of 8,192 x 8,192 matrices reaches 1,447).  There a tile of 32 rows takes a wave 372 of them
 // for 64 columns, 64 of which are the products: counters show the SIMDs issuing for 63% of the time and the matrix units busy for 40%.
 //
 // Masked rows get the logit -inf.  A masked row's values may be NaN (a block stored from infinities); 0 times them would spoil the
@@ -170,7 +170,7 @@ struct KeyTile {
 // sum is of the rounded numbers, so that a row of equal values comes out exact).  Blocks of bf16 queries round: a weight is off by
 // 2^-8 of itself at most, as a bf16 output is, and its error in an average over many rows is less; with 3 parts a chunk of 2,048 queries on
 // 32,768 rows takes 2,391 us, rounded 1,103.  Where one column tile is enough nothing waits for the products, and they are exact (the 8B
-// layer 18.0 us, rounded 16.9).  (One column tile of 128 elements has 7 registers too few for four waves a SIMD: with three, and none
+// layer 18.0 us, rounded 16.9).  (One column tile of 128 elements has a few registers too few for four waves a SIMD: with three, and none
 // spilled, 2,048 slabs of 3,277 rows take 176 us for 183 seen whole, and 167 for 156 in a masked window.)  kWaves: of a workgroup, which
 // divide a block's tiles and join their outputs.
 template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
