@@ -22,7 +22,7 @@
 // What bounds it.  One query of each of a few slots, and short windows: latency, the dependent loads len -> table -> records (0.6 to
 // 0.8 us each), one tile's 1.1 us, the start of a workgroup, and the join; the 8B layer at its budget takes 13 us and a join of 4.5, its
 // bytes 1.9.  Many shared pages: the bytes of the pages that are read, each once (32 layers of 8 evicted samples: 206 MB, 65 us, 3.2 TB/s
-// with each workgroup's start and the join of its eight waves).  A long chunk: the issue of vector instructions (2,048 queries on 32,768 rows, 8 KV heads of 4
+// with each workgroup's start and the join of its eight waves).  A long chunk: vector instructions beside the products (2,048 queries on 32,768 rows, 8 KV heads of 4
 // heads: 1,092 us, 976 TFLOP/s where a product of 8,192 x 8,192 matrices reaches 1,447).  There a tile of 32 rows takes a wave 372 of them
 // for 64 columns, 64 of which are the products: counters show the SIMDs issuing for 63% of the time and the matrix units busy for 40%.
 //
