@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
     int base = 0;
     const int how = kShared || !pos ? 0 : a.visible ? 1 : 2;  // window: how tiles are found, by row numbers, marks or positions
     auto load_entries = [&](const Q4QueryArgs& a, int row, int v0, int (&to)[kTogether]) __attribute__((always_inline)) {  // shared: of the block's slots v0 ... at a row
-        const int entries = a.dims.max_pages, V = a.plan.vectors, at = row >> a.dims.page_shift;
+        const int entries = a.dims.max_pages, V = a.plan.vectors, at = min(row, a.dims.cap - 1) >> a.dims.page_shift;
 #pragma unroll
         for (int i = 0; i < kTogether; ++i) to[i] = a.cache.table[(size_t)max(member_of[min(v0 + i, V - 1)], 0) * entries + at];
     };
@@ -297,11 +297,12 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         if constexpr (kShared) {
             const int V = a.plan.vectors, own = lane & ((1 << a.plan.vector_shift) - 1), i = lane >> a.plan.vector_shift;
             const int wave_of = k0 + min(own, V - 1) * max(1, step / V);
-            const int row = min(((wave_of < step ? wave_of : wave_of % step) + (base + i) * step) * kTile, last);
+            // (a tile behind a full slot has no rows: only the table's index ends at the capacity)
+            const int row = ((wave_of < step ? wave_of : wave_of % step) + (base + i) * step) * kTile;
             row_of = row;
             rows_in = own < V && base + i < run && member_of[min(own, V - 1)] >= 0 ? min(kTile, rows_of[min(own, V - 1)] - row) : 0;
             const int32_t* const entry = a.cache.table + (size_t)(own < V ? max(member_of[own], 0) : 0) * a.dims.max_pages;
-            page_of = entry[row >> shift];
+            page_of = entry[min(row, last) >> shift];
             page_of2 = entry[min(row + 16, last) >> shift];
             load_entries(a, row, 0, held);
         } else {
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
             for (int v0 = 0; v0 < V; v0 += kTogether) {
                 if (v0) load_entries(late, row_of, v0, held);
                 int second[kTogether];
-                if (pairs) load_entries(late, min(row_of + 16, late.dims.cap - 1), v0, second);
+                if (pairs) load_entries(late, row_of + 16, v0, second);
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) {
                     const int v = min(v0 + i, V - 1), left_of = __builtin_amdgcn_readlane(n, v) - row_of;
