@@ -99,9 +99,10 @@ __global__ __launch_bounds__(kMarkWaves* kWave) void q4_mark_kernel(Q4QueryArgs 
     const int v0 = block * a.plan.vectors;
     if (v0 >= slot.count || word >= a.words) return;
     const int32_t* pos = a.cache.pos + (size_t)b * a.dims.cap;
-    const int first = slot.n - slot.count + v0;
+    // (a slot that cannot be has queries, which get zeros, and no rows)
+    const int first = slot.n - slot.count + v0, queries = slot.bad ? 0 : min(a.plan.vectors, slot.count - v0);
     int top = INT_MIN, low = INT_MAX;
-    for (int i = lane; i < min(a.plan.vectors, slot.count - v0) && first + i < slot.n; i += kWave) {
+    for (int i = lane; i < queries; i += kWave) {
         top = max(top, pos[first + i]);
         low = min(low, pos[first + i]);
     }

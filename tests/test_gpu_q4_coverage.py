@@ -99,3 +99,71 @@ def test_full_tables_of_many_layers():
     shared_call(t, [0] * 8)
     t = filled([256] * 70, layers=8, hq=16, hkv=4, page_rows=64, max_pages=4, d=64)
     shared_call(t, [i % 3 for i in range(70)])
+
+
+# ---- windows, and the marks of the tiles that a block sees any row of ----------------------------------------------------------------
+
+def placed(t, places, rows):
+    """The rows' positions: none kept, in order, with gaps and some out of order under the newest `rows`, or (any) Cache's random order."""
+    if places == "rows":
+        t.c.pos = None
+    elif places == "ordered":
+        t.c.pos.copy_(torch.arange(t.cap, dtype=torch.int32).expand(len(t.lens), t.cap))
+    elif places == "evicted":
+        for b, n in enumerate(t.lens):
+            old = max(0, n - rows)
+            p = 3 * torch.arange(old) + torch.randint(0, 3, (old,), generator=gen(b))
+            swap = torch.randperm(old, generator=gen(b + 50))[: old // 8]
+            p[swap] = p[swap.flip(0)]
+            t.c.pos[b, :old] = p.to(torch.int32)
+            t.c.pos[b, old:n] = torch.arange(3 * old, 3 * old + n - old, dtype=torch.int32)
+    return t
+
+
+def window_call(t, rows, counts, window, sinks, layers=None, vectors=None, n_max=None, faults=0):
+    """vectors: the queries of a block where the call makes marks, which are in the workspace behind its first 256 bytes: 64 tiles to a
+    word, [slot][block][word].  A slot of which counts says None cannot be: zeros."""
+    layers, n_max = layers or t.layers, n_max or t.cap
+    lens = t.c.len.tolist()
+    q = torch.zeros(layers, len(lens), t.hq, rows, t.d, dtype=DT[t.dtype], device="cuda")
+    o = torch.full_like(q, 9.0)
+    ws = B.q4_window_workspace(t.shape, n_max, rows, layers)
+    ws[256:] = 77
+    B.kv_q4_attend_window(t.c, 0, layers, n_max, rows, q, o, ws, window=window, sinks=sinks, count=i32([rows + 1 if m is None else m for m in counts]))
+    blocks, words = -(-rows // (vectors or rows)), -(-n_max // 2048)
+    marks = ws[256 : 256 + 8 * len(lens) * blocks * words].cpu().numpy().view(np.uint64).reshape(len(lens), blocks, words)
+    for b, (n, m) in enumerate(zip(lens, counts)):
+        if m is None:
+            assert (o[:, b] == 0).all() and (not vectors or (marks[b] == 0).all())
+            continue
+        pos = np.arange(n) if t.c.pos is None else t.c.pos[b, :n].cpu().numpy().astype(np.int64)
+        seen = seen_of(pos, n, m, window, sinks)
+        for l in {0, layers - 1}:
+            assert (o[l, b, :, m:] == 9.0).all()
+            same_counts(t, o[l, b, :, :m], t.rows[b][:, :n], seen)
+        for k in range(0, m if vectors else 0, vectors or 1):
+            # (of a block's queries together: up to the last of their positions, from the first one's window on, and the sinks)
+            at = pos[n - m + k : n - m + min(k + vectors, m)]
+            some = (pos <= at.max()) & ((pos > at.min() - window) | (pos < sinks) | (window == 0))
+            bits = np.zeros(words * 64, dtype=bool)
+            bits[: -(-n // 32)] = [some[i : i + 32].any() for i in range(0, n, 32)]
+            assert np.array_equal(marks[b, k // vectors], np.packbits(bits, bitorder="little").view(np.uint64)), (b, k)
+    assert B.faults(ws, clear=True) == faults
+
+
+@pytest.mark.parametrize("dtype,window,vectors", [("bf16", 0, 16), ("bf16", 50, 8), ("f32", 0, 4), ("f32", 50, 4)])
+def test_marks_of_slots_that_cannot_be(dtype, window, vectors):
+    """Bad lengths and counts in every slot, the first among them, of a call that marks tiles."""
+    rows, page_rows = 70, 64
+    t = filled([90, 300, 90, 96, 130], hq=16, hkv=4, d=64, page_rows=page_rows, max_pages=131072 // page_rows, dtype=dtype)
+    # (positions inside a larger buffer)
+    around = torch.zeros(len(t.lens) * t.cap + 2 * 4096, dtype=torch.int32, device="cuda")
+    inner = around[4096 : 4096 + len(t.lens) * t.cap].view(len(t.lens), t.cap)
+    inner.copy_(t.c.pos)
+    t.c.pos = inner
+    good = [70, 70, 1, 50, 70]
+    window_call(t, rows, good, window, 9, vectors=vectors)
+    for bad in ([0], [0, 1, 4], [0, 1, 2, 3, 4]):
+        window_call(t, rows, [None if b in bad else m for b, m in enumerate(good)], window, 9, vectors=vectors, faults=B.KV_FAULT_CACHE)
+    t.c.len[0], t.c.len[3] = -3, t.cap + 1
+    window_call(t, rows, [None, 70, 1, None, 70], window, 9, vectors=vectors, faults=B.KV_FAULT_CACHE)
