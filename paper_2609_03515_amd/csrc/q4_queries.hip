@@ -26,9 +26,10 @@
 // heads: 1,092 us, 976 TFLOP/s where a product of 8,192 x 8,192 matrices reaches 1,447).  There a tile of 32 rows takes a wave 372 of them
 // for 64 columns, 64 of which are the products: counters show the SIMDs issuing for 63% of the time and the matrix units busy for 40%.
 //
-// Masked rows get the logit -inf.  A masked row's values may be NaN (a block stored from infinities); 0 times them would spoil the
-// column, so tiles that hold such blocks take a side path: the blocks are taken as numbers, and a product of two 0/1 matrices finds
-// the outputs whose query sees one.
+// Masked rows get the logit -inf.  A masked row's values may be NaN (a block stored from infinities), or, in rows that were never
+// stored, codes of a scale byte of 253 or 254 that exceed the largest bf16 number; 0 times them would spoil the column, so tiles that
+// hold such blocks take a side path.  NaN blocks are taken as numbers, and a product of two 0/1 matrices finds the outputs whose query
+// sees one; the tile's values are added in quarters, which are bf16 numbers.
 #include <float.h>
 #include <limits.h>
 
@@ -699,7 +700,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         // output
         float scale[8];
         uint32_t codes[8];
-        bool odd = false;  // a block that is NaN
+        bool odd = false;  // a block whose numbers are not all bf16 ones
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int r = 16 * (j / 4) + 4 * (j % 4);  // (and s)
@@ -707,7 +708,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
             else codes[j] = *reinterpret_cast<const uint16_t*>(value_codes + r * (D / 2));
             const uint32_t byte = value_scales[r * (D / 32)];
             scale[j] = __uint_as_float(byte << 23);
-            odd |= byte == 255u;
+            odd |= byte > 252u;
         }
         if (!whole) {
             asm volatile("");
@@ -715,7 +716,8 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
             for (int j = 0; j < 8; ++j)
                 if (4 * (j % 4) >= now[j / 4].valid - s) scale[j] = 1.0f;
         }
-        if (__builtin_expect(__any(odd), 0)) {  // (out of the way: a chunk of 2,048 queries on 32,768 rows 1,104 -> 1,095 us)
+        const bool quarters = __any(odd);
+        if (__builtin_expect(quarters, 0)) {  // (out of the way: a chunk of 2,048 queries on 32,768 rows 1,104 -> 1,095 us)
             asm volatile("");
             u32x4 is;
             uint32_t bits[CT];
@@ -737,6 +739,13 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (__float_as_uint(scale[j]) == 0x7f800000u) scale[j] = 1.0f;
+            // (rows that were stored have scales of 2^-100 and up, of which a quarter is exact)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) scale[j] *= 0.25f;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) acc[ct][e] *= 0.25f;
         }
         if (more) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile's values are out of LDS: the next tile's may come
@@ -768,6 +777,13 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         if constexpr (D == 128) {
             two_columns(std::integral_constant<int, 2>());
             two_columns(std::integral_constant<int, 3>());
+        }
+        if (__builtin_expect(quarters, 0)) {
+            asm volatile("");
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) acc[ct][e] *= 4.0f;
         }
         have = more;
         if (more) {

@@ -167,3 +167,97 @@ def test_marks_of_slots_that_cannot_be(dtype, window, vectors):
         window_call(t, rows, [None if b in bad else m for b, m in enumerate(good)], window, 9, vectors=vectors, faults=B.KV_FAULT_CACHE)
     t.c.len[0], t.c.len[3] = -3, t.cap + 1
     window_call(t, rows, [None, 70, 1, None, 70], window, 9, vectors=vectors, faults=B.KV_FAULT_CACHE)
+
+
+# ---- bytes that no store writes --------------------------------------------------------------------------------------------------
+
+def scribble(t, b, rows, keys=True, seed=5):
+    """Any codes, and scale bytes of every kind, into rows of a slot: values, and keys."""
+    pool = t.c.pool.cpu().view(t.layers, t.shape.n_pages, t.hkv, -1)
+    pr, d, r = t.shape.page_rows, t.d, np.random.RandomState(seed)
+    half = pr * (d // 2 + d // 32)
+    for i in rows:
+        page = int(t.c.table[b, i // pr])
+        for first in ([0, half] if keys else [half]):
+            c, e = first + i % pr * (d // 2), first + pr * (d // 2) + i % pr * (d // 32)
+            shape = (t.layers, t.hkv)
+            pool[:, page, :, c : c + d // 2] = torch.from_numpy(r.randint(0, 256, shape + (d // 2,)).astype(np.uint8))
+            pool[:, page, :, e : e + d // 32] = torch.from_numpy(r.choice([253, 254, 255, 252, 130, 0], shape + (d // 32,)).astype(np.uint8))
+    t.c.pool.copy_(pool.view(-1))
+
+
+FORMS = [("bf16", 128, 1, 0), ("bf16", 128, 20, 0), ("bf16", 64, 20, 0), ("bf16", 128, 70, 1 << 17), ("bf16", 64, 70, 1 << 17), ("f32", 128, 20, 0), ("f32", 64, 1, 0)]
+
+
+@pytest.mark.parametrize("dtype,d,rows,room", FORMS)
+@pytest.mark.parametrize("places", ["rows", "ordered"])
+def test_masked_rows_of_any_bytes(dtype, d, rows, room, places):
+    """Rows before the window and rows that are not stored yet hold anything, and the queries that do not see them are as without."""
+    from test_gpu_q4_window import limits, reference
+
+    n = 200
+    t = placed(Cache([n], hq=8, hkv=2, d=d, dtype=dtype, page_rows=32, max_pages=room // 32 or 8).fill(), places, rows)
+    later = 0 if rows == 1 else rows // 2  # of the newest rows, those that are not stored
+    old = n - rows - 40                    # before the first query's window
+    scribble(t, 0, list(range(n - later, n)) + list(range(old)))
+    q = torch.randn(1, 1, 8, rows, d, generator=gen(2)).to(DT[dtype]).cuda()
+    o = torch.full_like(q, 9.0)
+    ws = B.q4_window_workspace(t.shape, t.cap, rows, 1)
+    B.kv_q4_attend_window(t.c, 0, 1, t.cap, rows, q, o, ws, window=40)
+    m = rows - later
+    pos = np.arange(n)
+    seen = seen_of(pos, n, rows, 40, 0)[:m]
+    assert seen.any(1).all() and not seen[:, :old].any() and not seen[:, n - later :].any()
+    k, v = t.values(0, 0)
+    want, size, av = reference(q[0, 0, :, :m].double().cpu().numpy(), k, v, seen)
+    err, lim = np.abs(o[0, 0, :, :m].double().cpu().numpy() - want), limits(t, want, size, av, n, rows)
+    assert (err <= lim).all(), (np.nanmax(err), np.isnan(err).any())
+
+
+@pytest.mark.parametrize("dtype,d,rows,room", FORMS)
+def test_rows_seen_of_any_bytes(dtype, d, rows, room):
+    """A query that sees one row gives its values, whatever else its tile holds: numbers up to 1.5 2^127, infinities past that (2^128 is
+    neither a bf16 nor an f32 number), NaN for byte 255."""
+    n = 200
+    t = Cache([n], hq=8, hkv=2, d=d, dtype=dtype, page_rows=32, max_pages=room // 32 or 8).fill()
+    t.c.pos = None
+    scribble(t, 0, range(n), keys=False)
+    q = torch.randn(1, 1, 8, rows, d, generator=gen(2)).to(DT[dtype]).cuda()
+    o = torch.full_like(q, 9.0)
+    ws = B.q4_window_workspace(t.shape, t.cap, rows, 1)
+    B.kv_q4_attend_window(t.c, 0, 1, t.cap, rows, q, o, ws, window=1)
+    v = np.repeat(t.values(0, 0)[1][:, n - rows :], 4, axis=0)
+    want = np.where(np.abs(v) >= 2.0 ** 128, np.copysign(np.inf, v), v)
+    got = o[0, 0].double().cpu().numpy()
+    plain = np.isfinite(want)
+    assert np.array_equal(np.where(plain, 0.0, got), np.where(plain, 0.0, want), equal_nan=True)
+    # A weight of the one row is 1 within the logit's error, 2^-22 of it, and a few roundings; codes times scales are bf16 numbers.
+    # Numbers below the smallest normal one, 2^-126, may be 0.  And where the tile holds a byte above 252, its values are added in
+    # quarters and the sum is taken four times: a scale of byte 0 or 1 has no quarter above the smallest scale, 2^-127, so that
+    # x = code 2^-127 or code 2^-126 becomes 4 code 2^-127: off by at most (4 - 1) 6 2^-127 = 2^-122.8.
+    err, size = np.abs(np.where(plain, got, 0.0) - np.where(plain, want, 0.0)), np.abs(np.where(plain, want, 0.0))
+    assert (err <= (2.0 ** -17 if dtype == "f32" else 0.0) * size + 2.0 ** -126 + (size < 6.1 * 2.0 ** -126) * 18 * 2.0 ** -127).all()
+
+
+@pytest.mark.parametrize("dtype,d,fan,layers", [("bf16", 128, 1, 1), ("bf16", 128, 12, 1), ("bf16", 64, 12, 1), ("bf16", 64, 7, 128), ("f32", 128, 5, 1), ("f32", 64, 5, 1)])
+def test_other_samples_rows_of_any_bytes(dtype, d, fan, layers):
+    """Pages that one sample has for itself hold anything; the other samples' outputs are as without."""
+    from test_gpu_q4_window import limits, reference
+
+    n, batch = 96, fan + 1
+    t = Cache([n] + [n] * fan, hq=8, hkv=2, d=d, dtype=dtype, page_rows=32, layers=layers).fill()
+    # the first page of all is the first slot's; slot 1's others hold anything
+    t.c.table[:, 0] = t.c.table[0, 0]
+    scribble(t, 1, range(32, 96))
+    q = torch.randn(layers, batch, 8, d, generator=gen(2)).to(DT[dtype]).cuda()
+    o = torch.full_like(q, 9.0)
+    ws = B.q4_shared_workspace(t.shape, t.cap, layers)
+    B.kv_q4_attend_shared(t.c, 0, layers, t.cap, i32([0] * batch), q, o, ws)
+    for l in {0, layers - 1}:
+        for b in range(batch):
+            if b == 1:
+                continue
+            k, v = t.values(l, b)
+            want, size, av = reference(q[l, b].double().cpu().numpy()[:, None], k, v, np.ones((1, n), dtype=bool))
+            err, lim = np.abs(o[l, b].double().cpu().numpy()[:, None] - want), limits(t, want, size, av, n, 2)
+            assert (err <= lim).all(), (l, b, np.nanmax(err), np.isnan(err).any())
