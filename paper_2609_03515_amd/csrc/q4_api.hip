@@ -451,7 +451,8 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
     a.plan = q4_window_plan(d, layer_count, n_max, rows, window, sinks);
     a.words = (int)mark_words_of(n_max);
     const size_t marks = cache->pos && a.plan.marks ? (size_t)d.batch * a.plan.blocks * a.words : 0;
-    if ((double)layer_count * d.batch * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups || (double)d.batch * a.plan.blocks * ((a.words + 3) / 4) > kMostGroups)
+    if ((double)layer_count * d.batch * a.plan.blocks * d.hkv * a.plan.chunks > kMostGroups ||
+        (marks && (double)d.batch * a.plan.blocks * ((a.words + 3) / 4) > kMostGroups))
         return KV_ERR_UNSUPPORTED;
     const QueryLayout L = query_layout(d, marks, false, parts_of(d, layer_count, rows, a.plan.chunks));
     if ((rc = check_ws(ws, ws_bytes, L.total)) != KV_OK) return rc;

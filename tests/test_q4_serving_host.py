@@ -184,3 +184,12 @@ def test_registers():
     for name, tiles in forms.items():
         assert seen[name][".vgpr_count"] <= {1: 128, 2: 168, 4: 256}[tiles] and seen[name][".vgpr_spill_count"] <= 7, name
     assert all(k[".vgpr_spill_count"] == 0 and k[".vgpr_count"] <= 128 for name, k in seen.items() if name not in forms)
+
+
+def test_window_sizes_without_marks():
+    """The grid of the kernel that marks tiles bounds calls that have it: those of slots that keep positions."""
+    s = shape(batch=64, layers=1, n_q_heads=1, n_kv_heads=1, head_dim=64, max_pages=1 << 14, dtype="f32")
+    assert window(n=1 << 19, rows=32769, s=s, ws=None) == UNSUPPORTED
+    assert window(n=1 << 19, rows=32769, s=s, c=buffers(pos=None), ws=None) == WORKSPACE
+    assert window(n=1 << 19, rows=1 << 21, s=s, c=buffers(pos=None), ws=None) == UNSUPPORTED  # (2^23 blocks)
+    assert window(n=1 << 19, rows=(1 << 21) - 16, s=s, c=buffers(pos=None), ws=None) == WORKSPACE
