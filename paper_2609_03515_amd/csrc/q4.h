@@ -104,7 +104,8 @@ hipError_t launch_q4_attend(const Q4AttendArgs& a, hipStream_t s);
 
 // Attention of blocks of queries: the newest rows' queries of a slot in a window (kv_q4_attend_window), or one query of each of
 // several slots that share pages (kv_q4_attend_shared).  A block is `vectors` queries; each is `group` columns of a product.
-constexpr int kQ4MostVectors = 32, kQ4MostColumns = 64;  // of a block
+constexpr int kQ4MostVectors = 32;  // queries of a shared block (the bits of a tile's mask; a windowed block has up to 64)
+constexpr int kQ4MostColumns = 64;  // columns of a block
 constexpr int kQ4Units = 4;  // most workgroups for a CU, where blocks are divided
 struct Q4QueryPlan {
     int tiles;    // column tiles of 16 in a block

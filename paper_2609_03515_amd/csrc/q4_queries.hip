@@ -954,6 +954,7 @@ hipError_t launch_form(Q4QueryArgs a, hipStream_t s) {
     constexpr int kJoined = CT * (D / 16) * (kWaves - 1) * kWave * (int)sizeof(f32x4), kStat = kWaves > 1 ? 2 * kWaves * CT * 16 * (int)sizeof(float) : 0;
     static_assert(kJoined % 16 == 0 && kValues % 16 == 0, "queries are read 16 bytes at a time");
     static_assert(CT * 16 <= kQ4MostColumns, "room for the parts of outputs");
+    static_assert(!kShared || CT * 16 <= kQ4MostVectors, "a block's slots and their masks (heads of their own: 16 queries a column tile)");
     constexpr int kFirst = kValues + kQueries > kJoined ? kValues + kQueries : kJoined;
     a.q_at = kValues / (int)sizeof(float);
     a.stat_at = kFirst / (int)sizeof(float);
