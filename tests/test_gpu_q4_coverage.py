@@ -2,10 +2,10 @@
 
 With queries of zeros every weight is 1 / (rows seen), and with values of 0 and 1 the sums are whole numbers below 2^24, exact in any
 order: an output is its row count, times the reciprocal of the number seen, rounded.  Tolerance: the reciprocal and the product 2^-24 each
-of the result, the output's rounding 2^-8 (bf16) or 2^-24 (f32) of it; zeros are exact.  In the values' first 32 elements a tile of 32
-rows counts for element `tile % 32`, so that a tile that is lost or weighed twice changes it by at least one in
-(tiles / 32 + 1); each further element belongs to one row of the sequence (the first, the last, others anywhere), so that losing or
-repeating it changes that output by its whole size."""
+of the result, the output's rounding 2^-8 (bf16) or 2^-24 (f32) of it; zeros are exact.  In the values' first d - 16 elements a tile of
+32 rows counts for element `tile % (d - 16)`: of 141,000 rows (d = 64) each has 92 tiles, so that one that is lost or weighed twice moves it
+by 1.08%, which a rounding of 0.39% does not bring back within the tolerance of 0.39%.  Each of the last 16 elements belongs to one
+row of the sequence (the first, the last, others anywhere): losing or repeating it changes that output by its whole size."""
 import numpy as np
 import pytest
 import torch
@@ -22,11 +22,11 @@ def content(n, hkv, d, seed):
     """Values [hkv][n][d] of 0 and 1."""
     x = torch.zeros(hkv, n, d)
     r = torch.arange(n)
-    x[:, r, r // 32 % 32] = 1.0
+    x[:, r, r // 32 % (d - 16)] = 1.0
     for h in range(hkv):
         some = torch.randperm(n, generator=gen(100 * seed + h))
-        some = torch.cat((torch.tensor([0, n - 1] if n > 1 else [0] * n, dtype=torch.int64), some[(some != 0) & (some != n - 1)]))[: d - 32]
-        x[h, some, 32 + torch.arange(len(some))] = 1.0
+        some = torch.cat((torch.tensor([0, n - 1] if n > 1 else [0] * n, dtype=torch.int64), some[(some != 0) & (some != n - 1)]))[:16]
+        x[h, some, d - 16 + torch.arange(len(some))] = 1.0
     return x
 
 
@@ -48,8 +48,8 @@ def filled(lens, seed=3, **kw):
 
 def same_counts(t, got, rows, seen):
     """got [hq][m][d]: outputs of queries of zeros that see seen [m][n] of the rows."""
-    v, s = rows.double().numpy(), seen.astype(np.float64)
-    want = np.repeat(np.matmul(s, v) / np.maximum(s.sum(-1), 1.0)[None, :, None], t.hq // t.hkv, axis=0)
+    sums = np.matmul(seen.astype(np.float32), rows.numpy())  # (whole numbers below 2^24: exact)
+    want = np.repeat(sums.astype(np.float64) / np.maximum(seen.sum(-1), 1)[None, :, None], t.hq // t.hkv, axis=0)
     err = np.abs(got.double().cpu().numpy() - want)
     assert (err <= want * (1.01 * 2.0 ** -8 if t.dtype == "bf16" else 2.0 ** -22)).all(), (err.max(), np.argwhere(err > want * 2.0 ** -7)[:5].tolist())
 
@@ -145,8 +145,7 @@ def window_call(t, rows, counts, window, sinks, layers=None, vectors=None, n_max
             # (of a block's queries together: up to the last of their positions, from the first one's window on, and the sinks)
             at = pos[n - m + k : n - m + min(k + vectors, m)]
             some = (pos <= at.max()) & ((pos > at.min() - window) | (pos < sinks) | (window == 0))
-            bits = np.zeros(words * 64, dtype=bool)
-            bits[: -(-n // 32)] = [some[i : i + 32].any() for i in range(0, n, 32)]
+            bits = np.pad(some, (0, words * 2048 - n)).reshape(-1, 32).any(1)
             assert np.array_equal(marks[b, k // vectors], np.packbits(bits, bitorder="little").view(np.uint64)), (b, k)
     assert B.faults(ws, clear=True) == faults
 
@@ -167,6 +166,97 @@ def test_marks_of_slots_that_cannot_be(dtype, window, vectors):
         window_call(t, rows, [None if b in bad else m for b, m in enumerate(good)], window, 9, vectors=vectors, faults=B.KV_FAULT_CACHE)
     t.c.len[0], t.c.len[3] = -3, t.cap + 1
     window_call(t, rows, [None, 70, 1, None, 70], window, 9, vectors=vectors, faults=B.KV_FAULT_CACHE)
+
+
+DECODE, CHUNK = ((0, 0), (700, 40), (5, 0)), ((0, 0), (1000, 3))
+
+
+@pytest.mark.parametrize("places", ["rows", "ordered", "evicted"])
+@pytest.mark.parametrize("dtype,hq,hkv,d,layers,lens,page_rows,rows,windows", [
+    ("bf16", 4, 1, 128, 1, [9001, 400, 5000], 64, 1, DECODE), ("f32", 4, 1, 64, 1, [9001, 400, 5000], 64, 1, DECODE),
+    ("bf16", 2, 1, 64, 1, [141_000], 256, 1, ((0, 0), (40_000, 100))), ("f32", 4, 1, 64, 1, [9001, 400, 5000], 32, 70, CHUNK),
+    ("bf16", 4, 1, 128, 1, [9001, 400, 5000], 64, 70, CHUNK), ("bf16", 4, 1, 64, 1, [141_000], 256, 24, ((0, 0), (40_000, 100))),
+    ("bf16", 14, 2, 64, 2, [9001, 8999], 16, 130, CHUNK), ("bf16", 32, 8, 64, 1, [32_749], 128, 128, ((0, 0), (30_000, 5))),
+    ("bf16", 32, 8, 128, 8, [4100], 64, 128, ((0, 0),))])
+def test_every_row_once(dtype, hq, hkv, d, layers, lens, page_rows, rows, windows, places):
+    """One, two and four column tiles, blocks divided among workgroups, waves of many runs of 64 tiles."""
+    t = placed(filled(lens, dtype=dtype, hq=hq, hkv=hkv, d=d, layers=layers, page_rows=page_rows), places, rows)
+    for window, sinks in windows:
+        window_call(t, rows, [min(rows, n) for n in lens], window, sinks)
+
+
+@pytest.mark.parametrize("places", ["ordered", "evicted", "any"])
+@pytest.mark.parametrize("dtype,hq,hkv,layers,lens,page_rows,rows,window,vectors", [
+    ("bf16", 16, 4, 2, [9001, 7777, 2049], 64, 130, 40, 8), ("bf16", 16, 4, 2, [9001, 7777, 2049], 64, 260, 0, 16), ("bf16", 16, 4, 2, [9001, 0, 7777], 16, 400, 5000, 16),
+    ("f32", 16, 4, 2, [9001, 4100], 64, 130, 0, 4), ("bf16", 16, 1, 1, [9001, 2048], 256, 1000, 0, 4), ("bf16", 16, 1, 1, [9001, 2048], 256, 300, 0, None),
+    ("bf16", 2, 1, 1, [141_000], 256, 24, 128, 16), ("f32", 2, 1, 1, [141_000], 256, 24, 128, 8), ("bf16", 4, 2, 1, [141_000], 128, 600, 100_000, 32),
+    ("bf16", 2, 2, 1, [141_000], 256, 1100, 100_000, 64)])
+def test_marks(dtype, hq, hkv, layers, lens, page_rows, rows, window, vectors, places):
+    """Marks of many words, past 131,072 rows among them, and every row that a query sees found by them once (vectors None: divided among
+    so many workgroups that the waves look for themselves)."""
+    t = placed(filled(lens, dtype=dtype, hq=hq, hkv=hkv, d=64, layers=layers, page_rows=page_rows), places, rows)
+    counts = [min(rows, n) for n in lens]
+    window_call(t, rows, counts, window, 9, vectors=vectors)
+    window_call(t, rows, [max(0, c - 7 * i - 3) for i, c in enumerate(counts)], window, 9, vectors=vectors)
+
+
+# ---- samples of long prompts ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,fan,hq,hkv,layers", [("bf16", 2, 4, 1, 1), ("bf16", 15, 4, 1, 1), ("bf16", 11, 28, 4, 2), ("f32", 5, 4, 1, 1), ("bf16", 15, 32, 8, 32)])
+@pytest.mark.parametrize("page_rows", [16, 128])
+def test_long_prompts_rows_once(dtype, fan, hq, hkv, layers, page_rows):
+    """Pages that all samples share, and ends of different samples inside them."""
+    n, batch = 9001 if layers < 32 else 2049, fan + 1
+    t = filled([n] + [0] * fan, dtype=dtype, hq=hq, hkv=hkv, d=64, layers=layers, page_rows=page_rows)
+    B.kv_q4_fork(t.c, i32([0] * fan), i32(list(range(1, batch))), t.ws)
+    t.rows = t.rows[:1] * batch
+    shared_call(t, [0] * batch)
+    shared_call(t, [b % 2 for b in range(batch)])
+    t.c.len.copy_(i32([n - (311 * b if b % 3 else b) for b in range(batch)]) if layers < 32 else i32([n - 97 * b for b in range(batch)]))
+    shared_call(t, [0] * batch)
+
+
+# ---- the forms that keep all of a probability -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,rows", [(4, 4, 16), (4, 2, 8), (6, 2, 5), (4, 1, 4), (7, 1, 2), (8, 1, 2)])
+@pytest.mark.parametrize("places", ["rows", "ordered"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_queries_are_exact(hq, hkv, rows, places, d):
+    """bf16 queries that fit one column tile: the bound of a single query, without the rounding of probabilities."""
+    from test_gpu_q4_window import limits, reference
+
+    lens = [33, 700, 150, 16]
+    t = placed(Cache(lens, hq=hq, hkv=hkv, d=d, page_rows=32).fill(), places, rows)
+    q = torch.randn(1, 4, hq, rows, d, generator=gen(7)).bfloat16().cuda()
+    o = torch.full_like(q, 9.0)
+    ws = B.q4_window_workspace(t.shape, t.cap, rows, 1)
+    for window, sinks in ((0, 0), (24, 3)):
+        B.kv_q4_attend_window(t.c, 0, 1, t.cap, rows, q, o, ws, window=window, sinks=sinks)
+        for b, n in enumerate(lens):
+            k, v = t.values(0, b)
+            want, size, av = reference(q[0, b].double().cpu().numpy(), k, v, seen_of(np.arange(n), n, rows, window, sinks))
+            err, lim = np.abs(o[0, b].double().cpu().numpy() - want), limits(t, want, size, av, n, 1)
+            assert (err <= lim).all(), (b, (err / lim).max())
+
+
+@pytest.mark.parametrize("hq,hkv,batch", [(4, 4, 16), (4, 2, 8), (6, 2, 5), (4, 1, 4), (7, 1, 2), (16, 1, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_samples_are_exact(hq, hkv, batch, d):
+    """bf16 samples that fit one column tile, likewise."""
+    from test_gpu_q4_window import limits, reference
+
+    n = 700
+    t = Cache([n] + [0] * (batch - 1), hq=hq, hkv=hkv, d=d, page_rows=32).fill()
+    if batch > 1:
+        B.kv_q4_fork(t.c, i32([0] * (batch - 1)), i32(list(range(1, batch))), t.ws)
+    q = torch.randn(1, batch, hq, d, generator=gen(7)).bfloat16().cuda()
+    o = torch.full_like(q, 9.0)
+    B.kv_q4_attend_shared(t.c, 0, 1, t.cap, i32([0] * batch), q, o, B.q4_shared_workspace(t.shape, t.cap, 1))
+    k, v = t.values(0, 0)
+    for b in range(batch):
+        want, size, av = reference(q[0, b].double().cpu().numpy()[:, None], k, v, np.ones((1, n), dtype=bool))
+        err, lim = np.abs(o[0, b].double().cpu().numpy()[:, None] - want), limits(t, want, size, av, n, 1)
+        assert (err <= lim).all(), (b, (err / lim).max())
 
 
 # ---- bytes that no store writes --------------------------------------------------------------------------------------------------
