@@ -445,9 +445,9 @@ kv_status kv_q4_attend(const kv_q4_shape* shape, const kv_q4_cache* cache, int32
  * q and o: [layer][batch][query head][row][d] in the strides given (o not q's memory; no stride of o is 0 where its extent is above
  * 1).  count nullable: min(rows, len[b]).  Rows r >= count[b] are not read or written.  A slot longer than n_max, or whose count is
  * below 0, above `rows` or above its length (KV_FAULT_CACHE), gets zeros in all its `rows` outputs; rows in pages that do not
- * exist (KV_FAULT_CACHE) take no part.  What a masked row holds, NaN or, where nothing was stored, any
- * bytes, does not reach an output.  In bf16 calls of more than one query per slot probabilities may be rounded to bf16 before they
- * weigh the values (to nearest; their sum is of the rounded ones).
+ * exist (KV_FAULT_CACHE) take no part.  What a masked row holds, NaN or, where nothing was stored, any bytes, does not reach an
+ * output.  bf16 calls whose rows times query heads of a KV head are above 16 may round probabilities to bf16 before they weigh the
+ * values (to nearest, each by 2^-8 of itself at most; their sum is of the rounded ones).  Smaller calls, and f32 calls, keep all bits.
  * Workspace: kv_q4_window_workspace_bytes, for calls of at most n_max rows, `rows` queries and layer_count layers.
  * Refused (KV_ERR_UNSUPPORTED: take fewer layers or rows a call): rows above 2^27, 2^23 workgroups or more. */
 kv_status kv_q4_window_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t rows, int32_t layer_count, size_t* bytes);
@@ -459,8 +459,9 @@ kv_status kv_q4_attend_window(const kv_q4_shape* shape, const kv_q4_cache* cache
 /* kv_q4_attend (without a bias and scores) for slots that share pages, as the samples of a prompt do after kv_q4_fork: where the
  * tables of slots of one group name the same page at the same place, it is read and converted once for several of them.  group
  * [batch]: slots with equal numbers are a group (any numbers: those that share nothing only cost time, and those that share
- * pages in different groups read them once each).  Pages that an eviction replaced in some samples are read for those.  Probabilities
- * of bf16 calls may be rounded as kv_q4_attend_window's.
+ * pages in different groups read them once each).  Pages that an eviction replaced in some samples are read for those.  bf16 calls
+ * whose slots times query heads of a KV head are above 16 may round probabilities as kv_q4_attend_window's; smaller calls, and f32
+ * calls, keep all bits, as kv_q4_attend does.
  * Workspace: kv_q4_shared_workspace_bytes.  Refused as kv_q4_attend_window. */
 kv_status kv_q4_shared_workspace_bytes(const kv_q4_shape* shape, int32_t n_max, int32_t layer_count, size_t* bytes);
 kv_status kv_q4_attend_shared(const kv_q4_shape* shape, const kv_q4_cache* cache, int32_t layer0, int32_t layer_count,

@@ -20,11 +20,13 @@
 // and at the table entries of the block's other slots there; the first slot with a page has the tile for all that have it.
 //
 // What bounds it.  One query of each of a few slots, and short windows: latency, the dependent loads len -> table -> records (0.6 to
-// 0.8 us each), one tile's 1.1 us, the start of a workgroup, and the join; the 8B layer at its budget takes 13 us and a join of 4.5, its
+// 0.8 us each), one tile's 1.1 us, the start of a workgroup, and the join; the 8B layer at its budget takes 13 us and a join of 4, its
 // bytes 1.9.  Many shared pages: the bytes of the pages that are read, each once (32 layers of 8 evicted samples: 206 MB, 65 us, 3.2 TB/s
-// with each workgroup's start and the join of its eight waves).  A long chunk: vector instructions beside the products (2,048 queries on 32,768 rows, 8 KV heads of 4
-// heads: 1,092 us, 976 TFLOP/s where a product of 8,192 x 8,192 matrices reaches 1,447).  There a tile of 32 rows takes a wave 372 of them
-// for 64 columns, 64 of which are the products: counters show the SIMDs issuing for 63% of the time and the matrix units busy for 40%.
+// with each workgroup's start and the join of its eight waves).  A long chunk: vector instructions beside the products (2,048 queries on
+// 32,768 rows, 8 KV heads of 4 heads: 1,085 us, 982 TFLOP/s where a product of 8,192 x 8,192 matrices reaches 1,447).  There a tile of 32
+// rows takes a wave 374 of them for 64 columns, 64 of which are the products: counters show the SIMDs issuing for 65% of the time and the
+// matrix units busy for 40%.  Short ragged chunks (55 us for products of 10) and groups of 7 heads (46 us for bytes of 12): vector
+// instructions as well, 62% and 55% of the time, with the matrix units at 14% and 18%; a wave waits for 40% and 35% of its time.
 //
 // Masked rows get the logit -inf.  A masked row's values may be NaN (a block stored from infinities), or, in rows that were never
 // stored, codes of a scale byte of 253 or 254 that exceed the largest bf16 number; 0 times them would spoil the column, so tiles that
@@ -169,12 +171,14 @@ struct KeyTile {
 };
 
 // Column tiles (CT) of 16; parts of a probability (kP): 3 take all of its 24 bits, 1 rounds it to bf16 (8 bits, to nearest; its
-// sum is of the rounded numbers, so that a row of equal values comes out exact).  Blocks of bf16 queries round: a weight is off by
-// 2^-8 of itself at most, as a bf16 output is, and its error in an average over many rows is less; with 3 parts a chunk of 2,048 queries on
-// 32,768 rows takes 2,391 us, rounded 1,103.  Where one column tile is enough nothing waits for the products, and they are exact (the 8B
-// layer 18.0 us, rounded 16.9).  (One column tile of 128 elements has a few registers too few for four waves a SIMD: with three, and none
-// spilled, 2,048 slabs of 3,277 rows take 176 us for 183 seen whole, and 167 for 156 in a masked window.)  kWaves: of a workgroup, which
-// divide a block's tiles and join their outputs.
+// sum is of the rounded numbers, so that a row of equal values comes out exact).  Blocks of bf16 queries with more than one column tile
+// round: a weight is off by 2^-8 of itself at most, as a bf16 output is, and its error in an average over many rows is less.  With 3 parts
+// those forms spill and wait for the products: a chunk of 2,048 queries on 32,768 rows takes 2.2 times as long, 32 layers of 8 samples 140
+// us for 65, two layers of 32 samples of three prompts 76 for 46, one layer of 16 samples 27 for 21, short ragged chunks 81 for 55.  Where
+// one column tile is enough nothing waits for the products, and all bits are kept (rounded, the 8B layer would take 1 of its 17 us less).
+// (One column tile of 128 elements has a few registers too few for four waves a SIMD: with three, and none spilled, 2,048 slabs of 3,277
+// rows take 176 us for 183 seen whole, and 167 for 156 in a masked window.)  kWaves: of a workgroup, which divide a block's tiles and join
+// their outputs.
 template <typename T, int D, int CT, int kP, bool kShared, int kWaves>
 __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void q4_query_kernel(Q4QueryArgs a) {
     constexpr int kThreads = kWave * kWaves;
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
                 if (it >= 0) raw = a.cache.len[it];
             } else {
                 // up to 64 slots, one a lane: as q4_block_kernel.  (Ranks a group at a time, and lengths beside the groups' numbers: the
-                // 32 layers of 8 samples 70.3 -> 67.4 us, one layer of 16 24.2 -> 23.3.)
+                // 32 layers of 8 samples take 3 us less so, one layer of 16 1 us.)
                 it = min(lane, d.batch - 1);
                 const int mine = a.group[it];
                 raw = a.cache.len[it];
@@ -415,7 +419,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
         if constexpr (kShared) {
             const int V = late.plan.vectors, own = lane & ((1 << late.plan.vector_shift) - 1);
             const bool pairs = late.dims.page_rows < kTile;
-            // The slots' rows, one a lane (-1: no slot), taken from there: from LDS for each one layer of 16 samples took 22.9 us, so 21.8.
+            // The slots' rows, one a lane (-1: no slot), taken from there: from LDS for each, one layer of 16 samples takes 1 us more.
             const int n = lane < V && member_of[min(lane, V - 1)] >= 0 ? rows_of[min(lane, V - 1)] : -1;
             mask_of = 0;
             for (int v0 = 0; v0 < V; v0 += kTogether) {
@@ -555,7 +559,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
             return kShared && CT > 1 && !(active >> (ct * per) & ((1u << per) - 1));
         };
         // Two waves meet on a SIMD; one that is past its logits goes first, so that they do not run side by side through the products
-        // and then through the exponentials (a chunk of 2,048 queries on 32,768 rows 1,180 us without, 1,100 so).
+        // and then through the exponentials (a chunk of 2,048 queries on 32,768 rows takes 80 us more without).
         if constexpr (CT == 4) __builtin_amdgcn_s_setprio(0);
         // logits
         f32x4 z[CT][2];
@@ -717,7 +721,7 @@ __global__ __launch_bounds__(kWave* kWaves, CT == 1 ? 4 : CT == 2 ? 3 : 2) void 
                 if (4 * (j % 4) >= now[j / 4].valid - s) scale[j] = 1.0f;
         }
         const bool quarters = __any(odd);
-        if (__builtin_expect(quarters, 0)) {  // (out of the way: a chunk of 2,048 queries on 32,768 rows 1,104 -> 1,095 us)
+        if (__builtin_expect(quarters, 0)) {  // (out of the way: a chunk of 2,048 queries on 32,768 rows takes 9 us less)
             asm volatile("");
             u32x4 is;
             uint32_t bits[CT];
@@ -1004,11 +1008,12 @@ int chunks_of(int64_t units, int64_t tiles, int waves, int want) {
 
 }  // namespace
 
-// Forms.  One column tile: four waves, two workgroups for a CU (the 8B layer at its budget 18.0 us; one 20.4, four 18.9; eight waves
-// 19.4).  Two: four waves, as many workgroups as fit a CU, three (128 queries on 32,768 rows 105 us, two 114).  Four, each of two waves,
-// as many as a CU holds, where the blocks have 240 tiles of rows for a CU, of all slots' queries and as many rows as n_max allows (one
-// slot of 32/8 heads, four column tiles and two: 2,048 queries on 32,768 rows 1,095 us and 1,286, 1,024 574 and 689, 256 165 and 186;
-// on 8,192 rows 512 queries 97 and 103, 256 61.4 and 61.7, 128 48 and 37; 2,048 on 2,048 82 and 70; 8 prompts of 1,024 132 and 157).
+// Forms; figures of one line were timed side by side.  One column tile: four waves, two workgroups for a CU (the 8B layer at its budget
+// 18.0 us; one 20.4, four 18.9; eight waves 19.4).  Two: four waves, as many workgroups as fit a CU, three (128 queries on 32,768 rows
+// 105 us, two 114).  Four, each of two waves, as many as a CU holds, where the blocks have 240 tiles of rows for a CU, of all slots'
+// queries and as many rows as n_max allows (one slot of 32/8 heads, four column tiles and two: 2,048 queries on 32,768 rows 1,095 us and
+// 1,286, 1,024 574 and 689, 256 165 and 186; on 8,192 rows 512 queries 97 and 103, 256 61.4 and 61.7, 128 48 and 37; 2,048 on 2,048 82 and
+// 70; 8 prompts of 1,024 132 and 157).
 Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows, int window, int sinks) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
@@ -1027,14 +1032,17 @@ Q4QueryPlan q4_window_plan(const Q4Dims& d, int layer_count, int n_max, int rows
     p.blocks = blocks(rows, p.tiles);
     const int64_t tiles = seen(n_max, p.vectors);
     p.chunks = chunks_of(slabs * p.blocks, tiles, p.waves, (p.tiles == 1 ? 2 : p.tiles == 2 ? 3 : 4) * cus_of());
-    // a wave that looks at more than three times 16 tiles finds them by marks: a kernel before it, 5 us, that all layers and heads share
+    // Where a slot has several blocks, a wave that looks at more than three times 16 tiles finds them by marks: a kernel before it, 6 to 8
+    // us, that all layers and heads share.  A single block, a decode step's, looks for itself, by as many waves as its window has tiles
+    // for: with positions a narrow window of a long slot has few of them for all its rows (one query on 131,072 rows, 8 KV heads: a
+    // window of 8,192 17 us, 1,024 22, 128 60; without positions 15).
     p.marks = p.blocks > 1 && (n_max + kTile - 1) / kTile > 48 * p.chunks * p.waves;
     return p;
 }
 
 // Two column tiles: where there are blocks for every CU, a workgroup of eight waves to each, without a join (32 layers of 8 samples
-// 68 us, four waves in two and three chunks 76 and 71); else four waves, two workgroups for a CU (32 samples of three prompts 53 us, three
-// 58, one 69), since small groups make more blocks than are counted here.
+// 65 us, four waves in two and three chunks 8 and 3 more); else four waves, two workgroups for a CU (32 samples of three prompts 46 us,
+// three 5 more, one 16 more), since small groups make more blocks than are counted here.
 Q4QueryPlan q4_shared_plan(const Q4Dims& d, int layer_count, int n_max) {
     Q4QueryPlan p{};
     p.per = 16 / d.group;
