@@ -200,6 +200,18 @@ def test_marks(dtype, hq, hkv, layers, lens, page_rows, rows, window, vectors, p
     window_call(t, rows, [max(0, c - 7 * i - 3) for i, c in enumerate(counts)], window, 9, vectors=vectors)
 
 
+@pytest.mark.parametrize("places", ["rows", "any"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page_rows,pages", [(16, 1), (16, 2), (16, 528), (64, 3), (256, 1), (256, 33)])
+def test_full_tables_in_windows(page_rows, pages, dtype, places):
+    """Slots that fill their tables to the last row, beside an empty and a short one."""
+    n = page_rows * pages
+    t = placed(filled([n, 0, min(n, 9)], hq=4, hkv=1, d=64, page_rows=page_rows, max_pages=pages, dtype=dtype), places, 9)
+    for rows in (1, 9, 70):
+        for window, sinks in ((0, 0), (20, 3)):
+            window_call(t, rows, [min(rows, n), 0, min(rows, n, 9)], window, sinks)
+
+
 # ---- samples of long prompts ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,fan,hq,hkv,layers", [("bf16", 2, 4, 1, 1), ("bf16", 15, 4, 1, 1), ("bf16", 11, 28, 4, 2), ("f32", 5, 4, 1, 1), ("bf16", 15, 32, 8, 32)])
